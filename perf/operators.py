@@ -329,7 +329,7 @@ def _kept(s):
             k["ws"] = ws(B.latent_decode_workspace_bytes(k["spec"], c["B"], c["most"], c["prefix"]))
         elif c["kind"] == "prefill":
             k["kv_total"], k["max_q"] = sum(n for _, n in s["both"]), max(n for n, _ in s["both"])
-            k["ws"] = ws(B.latent_prefill_workspace_bytes(k["spec"], s["qin"].shape[0], k["kv_total"]))
+            k["ws"] = ws(B.latent_prefill_workspace_bytes(k["spec"], c["B"], k["kv_total"]))
         if c["kind"] != "append":
             k["out"] = torch.empty(s["qin"].shape[0], c["H"], c["Dv"], dtype=torch.float16, device="cuda")
     return k
