@@ -17,8 +17,8 @@
  *   memory. `stream` is a hipStream_t passed as void* (NULL means the null stream).
  * - The caller owns every buffer passed in: inputs, outputs and workspaces.
  *   Only the slot-table object and its device table belong to the library.
- * - The hot-path calls (moe_rmsnorm_f16 through moe_topk) only enqueue work
- *   on `stream`. They never allocate, never synchronise the host, and are
+ * - The hot-path calls (moe_rmsnorm_f16 through moe_topk, and the calls of the
+ *   attention block) only enqueue work on `stream`. They never allocate, never synchronise the host, and are
  *   safe to capture in a HIP graph.
  * - Return value: MOE_OK (0) or a negative MOE_E* code. A failed argument
  *   check enqueues nothing.
@@ -51,6 +51,8 @@ extern "C" {
 /* ---- device status bits (OR-ed into *status_dev by the kernels) ---------- */
 #define MOE_STATUS_SLOT_MISS 1u  /* routed expert has no resident slot       */
 #define MOE_STATUS_BAD_INDEX 2u  /* expert id outside [0, E)                  */
+#define MOE_STATUS_BAD_PAGE   8u  /* page id outside [0, n_pages)             */
+#define MOE_STATUS_BAD_LENGTH 16u /* length or position outside its bounds    */
 #define MOE_STATUS_ENGINE_ABORT 4u /* decode engine left a wait on its time limit,
                                       or ran on an unexpected CU/XCD layout     */
 
@@ -305,6 +307,194 @@ int moe_topk(const moe_layer_spec* spec, const float* logits, int T, int32_t* id
  * or NULL. MOE_EINVAL unless spec->routing is MOE_ROUTING_SIGMOID_GROUP. */
 int moe_topk_biased(const moe_layer_spec* spec, const float* logits, const float* bias, int T,
                     int32_t* idx, float* w, void* stream);
+
+/* ---- attention block --------------------------------------------------------
+ * What stands in front of the MoE layer in a decoder layer: the int4
+ * projections with their unmerged adapters, latent attention over a paged
+ * cache, and the pages' bookkeeping. All activations, cache rows and the
+ * latent up-projections are fp16, all sums, norms and softmax statistics fp32.
+ */
+
+/*
+ * One int4 group-64 projection with its adapter, for T rows (Sec. 2,
+ * Quantization; Sec. 3.3, Fig. 1: the adapters of the paper sit on attention
+ * and shared-expert projections):
+ *   y[t] = W x[t] + lora_scale B (A x[t]),  W = s q + z.
+ * The weights are not rounded: per 64-input group the products with the codes
+ * are summed in fp32, and s and z are applied in fp32. `rank` is read where
+ * both lora_a and lora_b are given (1..64), else there is no adapter.
+ * x_f16: device fp16, T rows of in_dim, x_stride halves apart (a multiple of
+ * 8). y: T rows of out_dim, y_stride elements apart, of type y_type:
+ *   MOE_OUT_F32      fp32
+ *   MOE_OUT_F16      fp16, rounded once
+ *   MOE_OUT_F32_ADD  fp32, y += (the residual's form)
+ * y must not overlap x. in_dim: a multiple of 64 up to 32768; out_dim: 1 ..
+ * 2^20; T up to 2^20. The order of a row's sums depends on T, not on the other rows.
+ * workspace: moe_linear_workspace_bytes(out_dim, in_dim, rank, T) (it grows with T
+ * and rank; no initial contents needed). Calls that share one workspace must
+ * be ordered on one stream.
+ */
+#define MOE_OUT_F32     0
+#define MOE_OUT_F16     1
+#define MOE_OUT_F32_ADD 2
+size_t moe_linear_workspace_bytes(int out_dim, int in_dim, int rank, int T);
+int moe_linear_int4_lora(const moe_proj* w, int out_dim, int in_dim, int rank, float lora_scale,
+                         const void* x_f16, int64_t x_stride, int T, void* y, int y_type,
+                         int64_t y_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Latent attention. A cached token is one row (c, k_r): a latent c [d_latent],
+ * from which each head's keys W_uk,h c and values W_uv,h c come, and a rotated
+ * key k_r [d_rope] that all heads share. A query of head h is (q_n, q_r),
+ * d_nope + d_rope long, and the score of a token is
+ *   scale ((q_n, W_uk,h c) + (q_r, k_r)).
+ */
+typedef struct moe_latent_spec {
+  int32_t heads;       /* H: 1..128                                          */
+  int32_t d_latent;    /* 128, 256 or 512                                    */
+  int32_t d_rope;      /* 32 or 64                                           */
+  int32_t d_nope;      /* 64 or 128                                          */
+  int32_t d_v;         /* 64 or 128                                          */
+  int32_t page_tokens; /* tokens of a cache page: a power of two, 16..1024   */
+  float   scale;       /* softmax scale, > 0                                 */
+  int32_t reserved[2]; /* must be zero                                       */
+} moe_latent_spec;
+
+/*
+ * One layer's paged cache. pages: device fp16 [n_pages][page_tokens]
+ * [d_latent + d_rope]. table: device int32, n_seqs rows of max_pages page ids,
+ * table_stride ids apart: token j of sequence b is row j % page_tokens of page
+ * table[b][j / page_tokens]. A table entry is read only where the sequence has
+ * tokens. A page id outside [0, n_pages) sets MOE_STATUS_BAD_PAGE, and its
+ * tokens take no part. Rows past a sequence's last token are never used,
+ * whatever they hold.
+ */
+typedef struct moe_latent_cache {
+  void* pages;
+  const int32_t* table;
+  int64_t table_stride;
+  int32_t n_pages, n_seqs, max_pages;
+  int32_t reserved; /* must be zero */
+} moe_latent_cache;
+
+/* Check a description. Returns MOE_OK or MOE_EINVAL. Host only. */
+int moe_latent_spec_check(const moe_latent_spec* spec);
+
+/*
+ * Write T tokens into the cache, and rotate their queries:
+ *   row = (c / sqrt(mean(c^2) + 1e-6) * gamma, rot(k_r)),  q_out = (q_n, rot(q_r)),
+ * rot by the angles of the token's position: (x, y) -> (x cos - y sin,
+ * x sin + y cos) for the pairs of neighbouring elements.
+ * kv: device fp32 [T][d_latent + d_rope] = (c, k_r). gamma_f16: device fp16
+ * [d_latent]. rope: device fp32 [max_pos][d_rope / 2][2] = (cos, sin). seq,
+ * pos: device int32 [T], the table row and the position of each token (no two
+ * tokens at one place). q_f16, q_out_f16: device fp16 [T][H][d_nope + d_rope],
+ * or both NULL; they may be the same array.
+ * A token with seq < 0 is padding: nothing of it is written. A seq or position
+ * out of range sets MOE_STATUS_BAD_INDEX, a bad page MOE_STATUS_BAD_PAGE;
+ * nothing of that token is written.
+ */
+int moe_latent_append(const moe_latent_spec* spec, const moe_latent_cache* cache, const float* kv,
+                      const void* gamma_f16, const float* rope, int max_pos, const int32_t* seq,
+                      const int32_t* pos, int T, const void* q_f16, void* q_out_f16, uint32_t* status,
+                      void* stream);
+
+/*
+ * One query token per sequence, in the absorbed form: the query is taken into
+ * the latent space (rounded to fp16, the type of the rows it meets), all heads
+ * read each cached row once, and the weighted latents (rounded to fp16) go
+ * through W_uv.
+ * w_kvb_f16: device fp16 [H][d_nope + d_v][d_latent], W_uk,h above W_uv,h.
+ * q_f16: device fp16 [B][H][d_nope + d_rope], rotated. out_f16: [B][H][d_v].
+ * kv_len: device int32 [B], tokens of sequence b = table row b (0: none);
+ * max_len: a bound on them. A length outside [0, max_len] or beyond the table
+ * sets MOE_STATUS_BAD_LENGTH and is taken as the nearest that is not.
+ * A prefix that the whole batch shares: prefix_pages, device int32 ids of its
+ * ceil(prefix_len / page_tokens) pages (NULL with prefix_len 0). Every sequence
+ * attends to the prefix_len tokens of it and to its own kv_len; the prefix is
+ * read once for many sequences. A row that has no token gives zeros.
+ * B up to n_seqs. workspace: moe_latent_decode_workspace_bytes (no initial
+ * contents needed); calls that share one must be ordered on one stream.
+ */
+size_t moe_latent_decode_workspace_bytes(const moe_latent_spec* spec, int B, int max_len, int prefix_len);
+int moe_latent_decode(const moe_latent_spec* spec, const moe_latent_cache* cache, const void* w_kvb_f16,
+                      const void* q_f16, int B, const int32_t* kv_len, int max_len,
+                      const int32_t* prefix_pages, int prefix_len, void* out_f16, uint32_t* status,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Chunks of prompts, in the expanded form (keys and values of the context are
+ * expanded into the workspace once, fp16). A ragged batch: sequence b has the
+ * query rows q_start[b] .. q_start[b + 1] of q, which are the last tokens of
+ * its context of kv_start[b + 1] - kv_start[b] cached tokens (table row b;
+ * already written, the chunk's own among them), and each attends to the
+ * tokens up to its own position.
+ * q_start, kv_start: device int32 [B + 1], ascending from 0 or more. T,
+ * kv_total and max_q: bounds on the last q_start, the last kv_start and the
+ * longest chunk. q_f16: device fp16 [T][H][d_nope + d_rope], rotated; out_f16:
+ * [T][H][d_v]; rows behind the last sequence are left as they were.
+ * Lists that break these rules, a chunk longer than its context or a context
+ * longer than the table set MOE_STATUS_BAD_LENGTH, and what is computed then is
+ * unspecified (no access leaves the arrays; a row before its context's first
+ * token gives zeros).
+ * workspace: moe_latent_prefill_workspace_bytes (no initial contents needed);
+ * calls that share one must be ordered on one stream.
+ */
+size_t moe_latent_prefill_workspace_bytes(const moe_latent_spec* spec, int B, int kv_total);
+int moe_latent_prefill(const moe_latent_spec* spec, const moe_latent_cache* cache, const void* w_kvb_f16,
+                       const void* q_f16, int T, const int32_t* q_start, const int32_t* kv_start, int B,
+                       int kv_total, int max_q, void* out_f16, uint32_t* status, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/*
+ * Pages of a paged cache, on the host: reference counts and the lowest free
+ * ids first. One pool serves all layers (a page id means the same page in
+ * every layer's array). Not thread-safe for concurrent calls on one pool.
+ */
+typedef struct moe_page_pool moe_page_pool;
+int moe_page_pool_create(int n_pages, int page_tokens, moe_page_pool** out);
+int moe_page_pool_destroy(moe_page_pool* p);
+/* Free pages. */
+int moe_page_pool_available(const moe_page_pool* p);
+/* References to `page` (0: free). */
+int moe_page_pool_refs(const moe_page_pool* p, int page);
+/* n pages into pages (host int32 [n]), one reference each. MOE_ENOMEM (the
+ * pool is unchanged) if fewer are free. */
+int moe_page_pool_alloc(moe_page_pool* p, int n, int32_t* pages);
+/*
+ * Fork a sequence of n_tokens tokens in `pages`: its full pages are shared
+ * (one reference more), a last, partly filled one gets a page of its own.
+ * forked: host int32, the fork's pages. Returns 1 with copy = (from, to), the
+ * page to copy (moe_page_copy), or 0. MOE_EINVAL: a page that is not live;
+ * MOE_ENOMEM: no free page; the pool is unchanged then.
+ */
+int moe_page_pool_fork(moe_page_pool* p, const int32_t* pages, int64_t n_tokens, int32_t* forked,
+                       int32_t* copy);
+/* Drop one reference of each of the n pages; a page without any is free. A
+ * page may stand in the list as often as it has references. MOE_EINVAL (the
+ * pool is unchanged) for a page that has none left. */
+int moe_page_pool_free(moe_page_pool* p, const int32_t* pages, int n);
+/*
+ * Close the gaps: the live pages move to the lowest ids. moves: host int32
+ * [n_pages][2], (from, to) of each move; remap: host int32 [n_pages], the id
+ * that each page has now (-1: free). Returns the number of moves. No page is
+ * both a source and a target. The caller moves the pages (moe_page_copy) and
+ * rewrites its tables (moe_page_remap) before the next write to the cache.
+ */
+int moe_page_pool_compact(moe_page_pool* p, int32_t* moves, int32_t* remap);
+/*
+ * Copy n pages in each of n_layers arrays of n_pages pages (page_bytes each, a
+ * multiple of 16), layer_bytes apart. pairs: device int32 [n][2] = (from, to),
+ * 8-byte aligned; no page may be a target twice, or a source and a target. A
+ * pair with an id outside [0, n_pages) sets MOE_STATUS_BAD_PAGE and is skipped.
+ */
+int moe_page_copy(void* pages, int n_layers, int64_t layer_bytes, int64_t page_bytes, int n_pages,
+                  const int32_t* pairs, int n, uint32_t* status, void* stream);
+/* table_out[i] = remap[table_in[i]] for n device int32 entries; negative
+ * entries stay, entries >= n_pages stay and set MOE_STATUS_BAD_PAGE. The
+ * tables may be the same array. */
+int moe_page_remap(const int32_t* table_in, int64_t n, const int32_t* remap, int n_pages,
+                   int32_t* table_out, uint32_t* status, void* stream);
 
 /* ---- decode-chain stand-in for attention ---------------------------------
  * The paper's decoder runs attention before each MoE layer, and the head of

@@ -23,6 +23,7 @@ slots    slot table and the host-tier slot policy.
 stack    40-layer decode chain with prediction-as-routing and the
          residual-mixing stand-in for attention.
 batched  multi-token (prefill / batched decode) layer.
+attention the attention block: one projection, latent attention, cache pages.
 """
 
-from . import quant, routing, expert, slots, stack, batched  # noqa: F401
+from . import quant, routing, expert, slots, stack, batched, attention  # noqa: F401

@@ -15,11 +15,14 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmoe.so")
 
-c_int, c_int32, c_float, c_void_p, c_size_t = (ctypes.c_int, ctypes.c_int32, ctypes.c_float,
-                                               ctypes.c_void_p, ctypes.c_size_t)
+c_int, c_int32, c_int64, c_float, c_void_p, c_size_t = (ctypes.c_int, ctypes.c_int32, ctypes.c_int64,
+                                                        ctypes.c_float, ctypes.c_void_p,
+                                                        ctypes.c_size_t)
 
 MOE_OK, MOE_EINVAL, MOE_EALIGN, MOE_ENOTRESIDENT, MOE_EHIP, MOE_ENOMEM = 0, -1, -2, -3, -4, -5
 MOE_STATUS_SLOT_MISS, MOE_STATUS_BAD_INDEX = 1, 2
+MOE_STATUS_BAD_PAGE, MOE_STATUS_BAD_LENGTH = 8, 16
+MOE_OUT_F32, MOE_OUT_F16, MOE_OUT_F32_ADD = 0, 1, 2
 MOE_ROUTING_SOFTMAX_TOPK, MOE_ROUTING_SIGMOID_GROUP = 0, 1
 
 
@@ -57,6 +60,18 @@ class MoeBundleLayout(ctypes.Structure):
 class MoeStagerStats(ctypes.Structure):
     _fields_ = [("stages", ctypes.c_int64), ("uses", ctypes.c_int64), ("copies", ctypes.c_int64),
                 ("bytes", ctypes.c_int64)]
+
+
+class MoeLatentSpec(ctypes.Structure):
+    _fields_ = [("heads", c_int32), ("d_latent", c_int32), ("d_rope", c_int32), ("d_nope", c_int32),
+                ("d_v", c_int32), ("page_tokens", c_int32), ("scale", c_float),
+                ("reserved", c_int32 * 2)]
+
+
+class MoeLatentCache(ctypes.Structure):
+    _fields_ = [("pages", c_void_p), ("table", c_void_p), ("table_stride", ctypes.c_int64),
+                ("n_pages", c_int32), ("n_seqs", c_int32), ("max_pages", c_int32),
+                ("reserved", c_int32)]
 
 
 class MoeError(RuntimeError):
@@ -127,6 +142,33 @@ SIGNATURES = {
                                 c_void_p]),
     "moe_chain_token_start": (c_int, [c_void_p, c_int, c_void_p, c_void_p]),
     "moe_chain_mix_rmsnorm": (c_int, [c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_void_p]),
+    "moe_linear_workspace_bytes": (c_size_t, [c_int, c_int, c_int, c_int]),
+    "moe_linear_int4_lora": (c_int, [ctypes.POINTER(MoeProj), c_int, c_int, c_int, c_float, c_void_p,
+                                     c_int64, c_int, c_void_p, c_int, c_int64, c_void_p, c_size_t,
+                                     c_void_p]),
+    "moe_latent_spec_check": (c_int, [ctypes.POINTER(MoeLatentSpec)]),
+    "moe_latent_append": (c_int, [ctypes.POINTER(MoeLatentSpec), ctypes.POINTER(MoeLatentCache), c_void_p,
+                                  c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_int, c_void_p,
+                                  c_void_p, c_void_p, c_void_p]),
+    "moe_latent_decode_workspace_bytes": (c_size_t, [ctypes.POINTER(MoeLatentSpec), c_int, c_int, c_int]),
+    "moe_latent_decode": (c_int, [ctypes.POINTER(MoeLatentSpec), ctypes.POINTER(MoeLatentCache), c_void_p,
+                                  c_void_p, c_int, c_void_p, c_int, c_void_p, c_int, c_void_p, c_void_p,
+                                  c_void_p, c_size_t, c_void_p]),
+    "moe_latent_prefill_workspace_bytes": (c_size_t, [ctypes.POINTER(MoeLatentSpec), c_int, c_int]),
+    "moe_latent_prefill": (c_int, [ctypes.POINTER(MoeLatentSpec), ctypes.POINTER(MoeLatentCache), c_void_p,
+                                   c_void_p, c_int, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p,
+                                   c_void_p, c_void_p, c_size_t, c_void_p]),
+    "moe_page_pool_create": (c_int, [c_int, c_int, ctypes.POINTER(c_void_p)]),
+    "moe_page_pool_destroy": (c_int, [c_void_p]),
+    "moe_page_pool_available": (c_int, [c_void_p]),
+    "moe_page_pool_refs": (c_int, [c_void_p, c_int]),
+    "moe_page_pool_alloc": (c_int, [c_void_p, c_int, c_void_p]),
+    "moe_page_pool_fork": (c_int, [c_void_p, c_void_p, c_int64, c_void_p, c_void_p]),
+    "moe_page_pool_free": (c_int, [c_void_p, c_void_p, c_int]),
+    "moe_page_pool_compact": (c_int, [c_void_p, c_void_p, c_void_p]),
+    "moe_page_copy": (c_int, [c_void_p, c_int, c_int64, c_int64, c_int, c_void_p, c_int, c_void_p,
+                              c_void_p]),
+    "moe_page_remap": (c_int, [c_void_p, c_int64, c_void_p, c_int, c_void_p, c_void_p, c_void_p]),
     "moe_engine_supported": (c_int, [ctypes.POINTER(MoeLayerSpec)]),
     "moe_engine_workspace_bytes": (c_size_t, [ctypes.POINTER(MoeLayerSpec), c_int]),
     "moe_engine_layers": (c_int, [ctypes.POINTER(MoeLayerSpec), c_void_p, c_void_p, c_void_p, c_int,
@@ -667,3 +709,219 @@ def engine_chain_mlp(spec, table, layer_arr, head_arr, hidden, n_layers, first_t
                                       _ptr(y_rec), _ptr(status), _ptr(workspace),
                                       workspace.nbytes, _stream(stream)),
            "moe_engine_chain_mlp")
+
+
+# ---- attention block --------------------------------------------------------------
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _dense(what, dtype, *tensors):
+    """Contiguous tensors of one dtype on one GPU: the library sees addresses only."""
+    for t in tensors:
+        if t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError("%s: a contiguous %s tensor on the GPU is needed, got %s %s on %s"
+                             % (what, dtype, t.dtype, tuple(t.stride()), t.device))
+
+
+def linear_workspace_bytes(out_dim, in_dim, rank, T):
+    return int(lib().moe_linear_workspace_bytes(out_dim, in_dim, rank, T))
+
+
+def linear_int4(proj, out_dim, in_dim, rank, lora_scale, x, y, workspace, add=False, stream=None):
+    """moe_linear_int4_lora: ``proj`` a MoeProj of device pointers; ``x`` fp16 ``[T, in]`` and ``y`` fp32 or
+    fp16 ``[T, out]`` with unit column stride; ``add``: into an fp32 ``y``."""
+    import torch
+    T = x.shape[0]
+    f16 = y.dtype == torch.float16
+    _need(x.dtype == torch.float16 and x.dim() == 2 and x.shape[1] == in_dim and (in_dim == 1 or x.stride(1) == 1),
+          "x: fp16 [T, in] with unit column stride")
+    _need((f16 or y.dtype == torch.float32) and tuple(y.shape) == (T, out_dim) and (out_dim == 1 or y.stride(1) == 1),
+          "y: fp32 or fp16 [T, out] with unit column stride")
+    _need(not (add and f16), "add needs an fp32 y")
+    _need(x.is_cuda and x.device == y.device == workspace.device, "x, y and the workspace on one GPU")
+    _check(lib().moe_linear_int4_lora(ctypes.byref(proj), out_dim, in_dim, rank, lora_scale, _ptr(x),
+                                      x.stride(0) if T > 1 else in_dim, T, _ptr(y),
+                                      MOE_OUT_F16 if f16 else MOE_OUT_F32_ADD if add else MOE_OUT_F32,
+                                      y.stride(0) if T > 1 else out_dim, _ptr(workspace), workspace.nbytes,
+                                      _stream(stream)), "moe_linear_int4_lora")
+
+
+def make_latent_spec(heads, d_latent, d_rope, d_nope, d_v, page_tokens, scale):
+    s = MoeLatentSpec()
+    s.heads, s.d_latent, s.d_rope, s.d_nope, s.d_v = heads, d_latent, d_rope, d_nope, d_v
+    s.page_tokens, s.scale = page_tokens, scale
+    return s
+
+
+def latent_spec_check(spec):
+    return lib().moe_latent_spec_check(ctypes.byref(spec))
+
+
+def latent_cache(pages, table):
+    """moe_latent_cache of ``pages`` fp16 ``[n_pages, page_tokens, d_latent + d_rope]`` and ``table`` int32
+    ``[n_seqs, max_pages]`` (rows may be strided). The struct keeps both alive."""
+    import torch
+    _dense("pages", torch.float16, pages)
+    _need(pages.dim() == 3 and table.dim() == 2 and table.dtype == torch.int32
+          and (table.shape[1] == 1 or table.stride(1) == 1) and table.device == pages.device,
+          "pages [n_pages, page_tokens, row] and an int32 table [n_seqs, max_pages] on one GPU")
+    c = MoeLatentCache(pages.data_ptr(), table.data_ptr(),
+                       table.stride(0) if table.shape[0] > 1 else table.shape[1], pages.shape[0], table.shape[0],
+                       table.shape[1], 0)
+    c.keep = (pages, table)
+    return c
+
+
+def _cache_of(spec, cache):
+    pages = cache.keep[0]
+    _need(tuple(pages.shape[1:]) == (spec.page_tokens, spec.d_latent + spec.d_rope),
+          "pages of %d tokens of %d" % (spec.page_tokens, spec.d_latent + spec.d_rope))
+
+
+def latent_append(spec, cache, kv, gamma, rope, seq, pos, status, q=None, q_out=None, stream=None):
+    """moe_latent_append: ``kv`` fp32 ``[T, d_latent + d_rope]``, ``gamma`` fp16, ``rope`` fp32 ``[max_pos,
+    d_rope / 2, 2]``, ``seq`` / ``pos`` int32 ``[T]``, ``q`` / ``q_out`` fp16 ``[T, H, d_nope + d_rope]``."""
+    import torch
+    T = kv.shape[0]
+    _cache_of(spec, cache)
+    _dense("kv, rope", torch.float32, kv, rope)
+    _dense("seq, pos", torch.int32, seq, pos)
+    _dense("gamma", torch.float16, gamma)
+    _need(tuple(kv.shape) == (T, spec.d_latent + spec.d_rope) and tuple(rope.shape[1:]) == (spec.d_rope // 2, 2)
+          and rope.dim() == 3 and gamma.numel() == spec.d_latent and seq.numel() == T and pos.numel() == T,
+          "kv [T, d_latent + d_rope], gamma [d_latent], rope [max_pos, d_rope / 2, 2], seq and pos [T]")
+    _need((q is None) == (q_out is None), "q and q_out: both or none")
+    if q is not None:
+        _dense("q, q_out", torch.float16, q, q_out)
+        _need(tuple(q.shape) == tuple(q_out.shape) == (T, spec.heads, spec.d_nope + spec.d_rope),
+              "q and q_out [T, H, d_nope + d_rope]")
+    _check(lib().moe_latent_append(ctypes.byref(spec), ctypes.byref(cache), _ptr(kv), _ptr(gamma), _ptr(rope),
+                                   rope.shape[0], _ptr(seq), _ptr(pos), T, _ptr(q), _ptr(q_out), _ptr(status),
+                                   _stream(stream)), "moe_latent_append")
+
+
+def latent_decode_workspace_bytes(spec, B, max_len, prefix_len=0):
+    return int(lib().moe_latent_decode_workspace_bytes(ctypes.byref(spec), B, max_len, prefix_len))
+
+
+def _attends(spec, cache, w_kvb, q, out):
+    import torch
+    _cache_of(spec, cache)
+    _dense("w_kvb, q, out", torch.float16, w_kvb, q, out)
+    _need(tuple(w_kvb.shape) == (spec.heads, spec.d_nope + spec.d_v, spec.d_latent)
+          and tuple(q.shape[1:]) == (spec.heads, spec.d_nope + spec.d_rope)
+          and tuple(out.shape) == (q.shape[0], spec.heads, spec.d_v),
+          "w_kvb [H, d_nope + d_v, d_latent], q [T, H, d_nope + d_rope], out [T, H, d_v]")
+
+
+def latent_decode(spec, cache, w_kvb, q, kv_len, max_len, out, status, workspace, prefix=None, prefix_len=0,
+                  stream=None):
+    """moe_latent_decode: ``q`` fp16 ``[B, H, d_nope + d_rope]``, ``kv_len`` int32 ``[B]``; ``prefix``: int32 page
+    ids of ``prefix_len`` tokens that every sequence of the batch begins with."""
+    import torch
+    B = q.shape[0]
+    _attends(spec, cache, w_kvb, q, out)
+    _dense("kv_len", torch.int32, kv_len)
+    _need(kv_len.numel() == B, "kv_len [B]")
+    if prefix_len:
+        _need(prefix is not None and prefix.numel() * spec.page_tokens >= prefix_len, "the prefix's page ids")
+        _dense("prefix", torch.int32, prefix)
+    _check(lib().moe_latent_decode(ctypes.byref(spec), ctypes.byref(cache), _ptr(w_kvb), _ptr(q), B, _ptr(kv_len),
+                                   max_len, _ptr(prefix), prefix_len, _ptr(out), _ptr(status), _ptr(workspace),
+                                   workspace.nbytes, _stream(stream)), "moe_latent_decode")
+
+
+def latent_prefill_workspace_bytes(spec, B, kv_total):
+    return int(lib().moe_latent_prefill_workspace_bytes(ctypes.byref(spec), B, kv_total))
+
+
+def latent_prefill(spec, cache, w_kvb, q, q_start, kv_start, kv_total, max_q, out, status, workspace, stream=None):
+    """moe_latent_prefill: ``q`` fp16 ``[T, H, d_nope + d_rope]``, ``q_start`` / ``kv_start`` int32 ``[B + 1]``."""
+    import torch
+    _attends(spec, cache, w_kvb, q, out)
+    _dense("q_start, kv_start", torch.int32, q_start, kv_start)
+    _need(q_start.numel() == kv_start.numel() >= 1, "q_start and kv_start [B + 1]")
+    _check(lib().moe_latent_prefill(ctypes.byref(spec), ctypes.byref(cache), _ptr(w_kvb), _ptr(q), q.shape[0],
+                                    _ptr(q_start), _ptr(kv_start), q_start.numel() - 1, kv_total, max_q, _ptr(out),
+                                    _ptr(status), _ptr(workspace), workspace.nbytes, _stream(stream)),
+           "moe_latent_prefill")
+
+
+class PagePool:
+    """The library's page bookkeeping (host only): reference counts, forks, compaction."""
+
+    def __init__(self, n_pages, page_tokens):
+        h = c_void_p()
+        _check(lib().moe_page_pool_create(n_pages, page_tokens, ctypes.byref(h)), "moe_page_pool_create")
+        self.handle, self.n_pages, self.page_tokens = h, n_pages, page_tokens
+
+    def available(self):
+        return _check(lib().moe_page_pool_available(self.handle), "moe_page_pool_available")
+
+    def refs(self, page):
+        return _check(lib().moe_page_pool_refs(self.handle, page), "moe_page_pool_refs")
+
+    def alloc(self, n):
+        out = np.zeros(max(n, 1), dtype=np.int32)
+        _check(lib().moe_page_pool_alloc(self.handle, n, out.ctypes.data), "moe_page_pool_alloc")
+        return out[:n].tolist()
+
+    def fork(self, pages, n_tokens):
+        """(pages of the fork, the (from, to) pairs to copy)."""
+        p = _i32(pages)
+        n = -(-n_tokens // self.page_tokens)
+        _need(n <= len(p), "%d tokens need %d pages" % (n_tokens, n))
+        out, copy = np.zeros(max(n, 1), dtype=np.int32), np.zeros(2, dtype=np.int32)
+        k = _check(lib().moe_page_pool_fork(self.handle, p.ctypes.data, n_tokens, out.ctypes.data, copy.ctypes.data),
+                   "moe_page_pool_fork")
+        return out[:n].tolist(), [tuple(copy.tolist())] if k else []
+
+    def free(self, pages):
+        p = _i32(pages)
+        _check(lib().moe_page_pool_free(self.handle, p.ctypes.data, len(p)), "moe_page_pool_free")
+
+    def compact(self):
+        """(int32 [n, 2] moves, int32 [n_pages] remap)."""
+        moves, remap = np.zeros((self.n_pages, 2), dtype=np.int32), np.zeros(self.n_pages, dtype=np.int32)
+        n = _check(lib().moe_page_pool_compact(self.handle, moves.ctypes.data, remap.ctypes.data),
+                   "moe_page_pool_compact")
+        return moves[:n], remap
+
+    def close(self):
+        if self.handle:
+            lib().moe_page_pool_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self, _finalizing=sys.is_finalizing):
+        # no runtime calls while the interpreter shuts down: close() explicitly
+        if _finalizing():
+            return
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def page_copy(pages, pairs, status, stream=None):
+    """moe_page_copy on ``pages [n_layers, n_pages, ...]`` (pages contiguous, layers may be strided); ``pairs``
+    int32 ``[n, 2]`` on the GPU."""
+    import torch
+    _dense("pages of a layer", pages.dtype, pages[0])
+    _dense("pairs", torch.int32, pairs)
+    _need(pages.dim() >= 3 and pairs.dim() == 2 and pairs.shape[1] == 2, "pages [n_layers, n_pages, ...], pairs [n, 2]")
+    size = pages.element_size()
+    _check(lib().moe_page_copy(_ptr(pages), pages.shape[0], pages.stride(0) * size, pages.stride(1) * size,
+                               pages.shape[1], _ptr(pairs), pairs.shape[0], _ptr(status), _stream(stream)),
+           "moe_page_copy")
+
+
+def page_remap(table, remap, table_out, status, stream=None):
+    """moe_page_remap: int32 tensors; ``table_out`` may be ``table``."""
+    import torch
+    _dense("table, remap, table_out", torch.int32, table, remap, table_out)
+    _need(table_out.numel() == table.numel(), "tables of one size")
+    _check(lib().moe_page_remap(_ptr(table), table.numel(), _ptr(remap), remap.numel(), _ptr(table_out), _ptr(status),
+                                _stream(stream)), "moe_page_remap")

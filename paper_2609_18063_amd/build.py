@@ -9,7 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmoe.so")
 SOURCES = ["moe_api.hip", "moe_kernels.hip", "moe_engine.hip", "moe_engine_tokens.hip",
            "moe_engine_pipe.hip",
-           "moe_grouped.hip", "moe_stager.hip", "moe_head.hip", "moe_merge.hip"]
+           "moe_grouped.hip", "moe_stager.hip", "moe_head.hip", "moe_merge.hip",
+           "moe_linear.hip", "moe_latent.hip", "moe_prefill.hip", "moe_pages.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

@@ -1,0 +1,717 @@
+// Latent attention for single tokens, in its absorbed form, and the writes of the
+// paged latent cache. Each cached token is one row (c, k_r): a latent c [Dc], from
+// which every head's keys W_uk,h c and values W_uv,h c come, and one rotated key k_r
+// [Dr] that all heads share. For a query (q_n, q_r) of head h
+//   s_j = scale (q_n . W_uk,h c_j + q_r . k_r,j) = scale ((W_uk,h^T q_n) . c_j + q_r . k_r,j)
+//   o   = sum_j p_j W_uv,h c_j                   = W_uv,h sum_j p_j c_j,   p = softmax(s)
+// so with the query taken into the latent space once, all heads read the same row: the
+// cache is read once for all of them, (Dc + Dr) 2 bytes a token.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "moe_latent.h"
+#include "moe_tile.h"
+
+namespace moe {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr int kCus = 256;
+
+__device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// ---- cache writes -------------------------------------------------------------
+// Block (t, 0) normalizes and rotates token t's row into its page; blocks (t, 1 ..)
+// rotate the query, 8 halves a thread. One pass; bound by the bytes read and written.
+__global__ void __launch_bounds__(256) latent_append_kernel(AppendArgs a) {
+  const LatentArgs& l = a.l;
+  const int t = blockIdx.x, seq = a.seq[t], pos = a.pos[t], row = l.Dc + l.Dr;
+  if (seq < 0) return;                                   // a padding row
+  int32_t page = -1;
+  const bool in = seq < l.n_seqs && pos >= 0 && pos < a.max_pos && pos / l.page < l.max_pages;
+  if (in) page = l.table[seq * l.table_stride + pos / l.page];
+  if (page < 0 || page >= l.n_pages) {
+    if (blockIdx.y == 0 && threadIdx.x == 0 && l.status)
+      atomicOr(l.status, in ? MOE_STATUS_BAD_PAGE : MOE_STATUS_BAD_INDEX);
+    return;
+  }
+  const float2* cs = reinterpret_cast<const float2*>(a.rope) + (size_t)pos * (l.Dr / 2);
+  if (blockIdx.y > 0) {
+    const int hd = l.Dn + l.Dr, e = ((blockIdx.y - 1) * 256 + threadIdx.x) * 8, n = l.H * hd;
+    if (e >= n) return;
+    const int in_head = e % hd;
+    const size_t at = (size_t)t * n + e;
+    h8 v = ld_h8(l.q + at);
+    if (in_head >= l.Dn) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 r = cs[(in_head - l.Dn) / 2 + k];
+        const float x = (float)v[2 * k], y = (float)v[2 * k + 1];
+        v[2 * k] = (_Float16)(x * r.x - y * r.y);
+        v[2 * k + 1] = (_Float16)(x * r.y + y * r.x);
+      }
+    }
+    *reinterpret_cast<h8*>(a.q_out + at) = v;
+    return;
+  }
+  __shared__ float red[4];
+  const float* kv = a.kv + (size_t)t * row;
+  __half* to = a.pages + ((size_t)page * l.page + pos % l.page) * row;
+  float2 v = {0.f, 0.f};                                 // two of Dc <= 512 a thread
+  const int e = 2 * threadIdx.x;
+  if (e < l.Dc) v = *reinterpret_cast<const float2*>(kv + e);
+  const float s = wave_sum(fmaf(v.x, v.x, v.y * v.y));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  const float inv = 1.f / sqrtf((red[0] + red[1] + red[2] + red[3]) / (float)l.Dc + 1e-6f);
+  if (e < l.Dc) {
+    const float2 gm = __half22float2(*reinterpret_cast<const __half2*>(a.gamma + e));
+    *reinterpret_cast<__half2*>(to + e) = __floats2half2_rn(v.x * inv * gm.x, v.y * inv * gm.y);
+  }
+  if (e < l.Dr) {
+    const float2 x = *reinterpret_cast<const float2*>(kv + l.Dc + e), r = cs[threadIdx.x];
+    *reinterpret_cast<__half2*>(to + l.Dc + e) =
+        __floats2half2_rn(x.x * r.x - x.y * r.y, x.x * r.y + x.y * r.x);
+  }
+}
+
+// ---- the decode call's plan -----------------------------------------------------
+__device__ __forceinline__ int own_len(const DecodeArgs& a, int b, bool report) {
+  const int64_t cap = (int64_t)a.l.max_pages * a.l.page;
+  const int most = (int)(cap < a.max_len ? cap : a.max_len), n = a.kv_len[b];
+  if (n >= 0 && n <= most) return n;
+  if (report && a.l.status) atomicOr(a.l.status, MOE_STATUS_BAD_LENGTH);
+  return n < 0 ? 0 : most;
+}
+__device__ __forceinline__ int tiles_of(int len) { return (len + kTile - 1) / kTile; }
+
+struct Item {
+  int index, start, tiles;  // order number, first tile on the line, tiles
+  int row0, rows;           // query rows
+  int tok0, last;           // first token, last token that may be read
+  const int32_t* pages;
+};
+
+__device__ __forceinline__ Item prefix_item(const DecodeArgs& a, int chunk, int rb) {
+  Item it;
+  const int all = tiles_of(a.prefix_len), first = chunk * a.p.chunk_tiles;
+  it.index = chunk * a.p.row_blocks + rb;
+  it.tiles = min(a.p.chunk_tiles, all - first);
+  it.start = first * a.p.row_blocks + rb * it.tiles;
+  it.row0 = rb * a.p.rows;
+  it.rows = min(a.p.rows, a.B * a.l.H - it.row0);
+  it.tok0 = first * kTile;
+  it.last = a.prefix_len - 1;
+  it.pages = a.prefix;
+  return it;
+}
+__device__ __forceinline__ Item own_item(const DecodeArgs& a, int b, int hb, int start, int tiles) {
+  Item it;
+  it.index = a.p.chunks * a.p.row_blocks + b * a.p.head_blocks + hb;
+  it.tiles = tiles;
+  it.start = start + hb * tiles;
+  it.row0 = b * a.l.H + hb * a.p.rows;
+  it.rows = min(a.p.rows, a.l.H - hb * a.p.rows);
+  it.tok0 = 0;
+  it.last = own_len(a, b, false) - 1;
+  it.pages = a.l.table + b * a.l.table_stride;
+  return it;
+}
+// the item that tile t of the line belongs to
+__device__ __forceinline__ Item item_at(const DecodeArgs& a, int t) {
+  if (t < a.p.prefix_tiles) {
+    const int chunk = t / (a.p.chunk_tiles * a.p.row_blocks);
+    const Item first = prefix_item(a, chunk, 0);
+    return prefix_item(a, chunk, (t - first.start) / first.tiles);
+  }
+  int lo = 0, hi = a.B;                                  // starts[lo] <= t < starts[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (a.starts[mid] <= t)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  // (sequences without a tile share their start with the next one: the last of equals
+  // is the one that has the tile)
+  const int tiles = (a.starts[lo + 1] - a.starts[lo]) / a.p.head_blocks;
+  return own_item(a, lo, (t - a.starts[lo]) / tiles, a.starts[lo], tiles);
+}
+
+// ---- q into the latent space ------------------------------------------------------
+// qt_h = W_uk,h^T q_n,h for 64 latent columns of one head and 64 sequences a workgroup;
+// W_uk,h's columns are staged in LDS and read transposed. qt is rounded to fp16, the
+// type of the rows that it meets. The first column block copies q_r beside it; one
+// further block adds up the tiles of the sequences for the plan.
+template <int DN>
+__global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
+  __shared__ __attribute__((aligned(16))) char wt[DN * 128];
+  __shared__ int scan[256];
+  const LatentArgs& l = a.l;
+  const int h = blockIdx.y, b0 = blockIdx.z * 64, b1 = min(b0 + 64, a.B);
+  if ((int)blockIdx.x == l.Dc / 64) {
+    if (blockIdx.y || blockIdx.z) return;
+    int base = a.p.prefix_tiles;
+    for (int c0 = 0; c0 < a.B; c0 += 256) {
+      const int b = c0 + threadIdx.x;
+      const int n = b < a.B ? tiles_of(own_len(a, b, true)) * a.p.head_blocks : 0;
+      scan[threadIdx.x] = n;
+      __syncthreads();
+      for (int o = 1; o < 256; o <<= 1) {
+        const int v = (int)threadIdx.x >= o ? scan[threadIdx.x - o] : 0;
+        __syncthreads();
+        scan[threadIdx.x] += v;
+        __syncthreads();
+      }
+      if (b < a.B) a.starts[b] = base + scan[threadIdx.x] - n;
+      base += scan[255];
+      __syncthreads();
+    }
+    if (threadIdx.x == 0) a.starts[a.B] = base;
+    return;
+  }
+  const int hd = l.Dn + l.Dr, row = l.Dc + l.Dr, c0 = blockIdx.x * 64;
+  const __half* w = l.w + (size_t)h * (l.Dn + l.Dv) * l.Dc + c0;
+  for (int e = threadIdx.x; e < DN * 8; e += 256) {
+    const int n = e >> 3, p = e & 7;
+    *reinterpret_cast<U4*>(wt + n * 128 + 16 * (p ^ tile_key<8>(n))) = ld16(w + (size_t)n * l.Dc + 8 * p);
+  }
+  if (blockIdx.x == 0) {
+    const int pieces = l.Dr / 8;
+    for (int e = threadIdx.x; e < (b1 - b0) * pieces; e += 256) {
+      const size_t r = (size_t)(b0 + e / pieces) * l.H + h;
+      const int p = 8 * (e % pieces);
+      *reinterpret_cast<U4*>(a.ql + r * row + l.Dc + p) = ld16(l.q + r * hd + l.Dn + p);
+    }
+  }
+  __syncthreads();
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  h8 wa[DN / 32];
+#pragma unroll
+  for (int k = 0; k < DN / 32; ++k) {
+    h4 part[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int n = 32 * k + 8 * g + 4 * r + (c >> 2), col = 16 * wave + 4 * (c & 3);
+      part[r] = ld_tr(wt + n * 128 + 16 * ((col >> 3) ^ tile_key<8>(n)) + 2 * (col & 7));
+    }
+    wa[k] = join(part[0], part[1]);
+  }
+  for (int bt = b0; bt < b1; bt += 16) {
+    const size_t r = (size_t)min(bt + c, b1 - 1) * l.H + h;
+    f4 d = {};
+#pragma unroll
+    for (int k = 0; k < DN / 32; ++k) d = mfma16(wa[k], ld_h8(l.q + r * hd + 32 * k + 8 * g), d);
+    if (bt + c < b1) {
+      const h4 v = {(_Float16)d[0], (_Float16)d[1], (_Float16)d[2], (_Float16)d[3]};
+      *reinterpret_cast<h4*>(a.ql + r * row + c0 + 16 * wave + 4 * g) = v;
+    }
+  }
+}
+
+// ---- attention over the cache -------------------------------------------------------
+// A workgroup takes its share of the line of tiles, item by item. Tiles of 64 tokens are
+// copied into LDS one ahead; scores are formed transposed (tokens x query rows), each
+// wave for its own tokens (or, at 64 rows, its tokens and half of the rows), with the
+// query in registers. The waves agree on the rows' new maximum through LDS, put the
+// weights there, and each adds up its quarter of the latent columns from the same tile,
+// read transposed. Three barriers a tile. With few heads HBM bounds it, with many the
+// matrix cores and LDS.
+template <int DC, int DR, int MT>
+struct DecodeShape {
+  static constexpr int M = 16 * MT;
+  static constexpr int WT = MT == 4 ? 2 : 4, WR = 4 / WT;      // waves over tokens and over rows
+  static constexpr int TT = 4 / WT, RT = MT / WR;              // 16-token, 16-row tiles of a wave
+  static constexpr int KS = (DC + DR) / 32, CT = DC / 64;
+  static constexpr int LAT = kTile * DC * 2, BUF = LAT + kTile * DR * 2;
+  static constexpr int LDS = 2 * BUF + M * 128 + 2 * WT * M * 4 + 32;
+};
+
+template <int DC, int DR, int MT>
+__global__ void __launch_bounds__(256, 1) latent_decode_kernel(DecodeArgs a) {
+  using S = DecodeShape<DC, DR, MT>;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  char* pt = lds + 2 * S::BUF;                                  // weights [M][64] halves
+  float* smax = reinterpret_cast<float*>(pt + S::M * 128);      // [WT][M]
+  float* ssum = smax + S::WT * S::M;                            // [WT][M]
+  int* bad = reinterpret_cast<int*>(ssum + S::WT * S::M);       // [2][4]: 16-token groups without a page
+  const LatentArgs& l = a.l;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int c = lane & 15, g = lane >> 4;
+  const int wt = wave % S::WT, wr = wave / S::WT;
+  // neighbours on the line share a chiplet and its L2
+  const int wg = (blockIdx.x % 8) * (a.p.wgs / 8) + blockIdx.x / 8;
+  const int all = a.starts[a.B], per = (all + a.p.wgs - 1) / a.p.wgs;
+  int t = wg * per;
+  const int end = min(all, t + per);
+
+  // rows of 16 tokens of tile `tile` (this wave's group) into buffer `buf`
+  auto copy = [&](const Item& it, int tile, int buf) {
+    const int want = it.tok0 + tile * kTile + 16 * wave;
+    const int base = min(want, it.last & ~15);                  // (past the end: the last group again)
+    const int page = it.pages[base / l.page];
+    const bool ok = page >= 0 && page < l.n_pages;
+    char* lat = lds + buf * S::BUF + 16 * wave * DC * 2;
+    char* rope = lds + buf * S::BUF + S::LAT + 16 * wave * DR * 2;
+    if (lane == 0) bad[4 * buf + wave] = !ok;
+    if (!ok) {
+      if (lane == 0 && l.status) atomicOr(l.status, MOE_STATUS_BAD_PAGE);
+      for (int e = lane; e < 16 * DC / 8; e += kWave) *reinterpret_cast<U4*>(lat + 16 * e) = U4{};
+      for (int e = lane; e < 16 * DR / 8; e += kWave) *reinterpret_cast<U4*>(rope + 16 * e) = U4{};
+      return;
+    }
+    const char* from = reinterpret_cast<const char*>(l.pages) +
+                       ((size_t)page * l.page + base % l.page) * (DC + DR) * 2;
+    const int most = it.last - base;                            // rows past the end repeat the last one
+    constexpr int LP = DC / 8, LR = kWave / LP;                 // pieces of a row, rows of a copy
+#pragma unroll
+    for (int j = 0; j < 16 / LR; ++j) {
+      const int r = j * LR + lane / LP;
+      dma16(from + (size_t)min(r, most) * (DC + DR) * 2 + 16 * ((lane % LP) ^ tile_key<LP>(r)),
+            lat + j * 1024);
+    }
+    constexpr int RP = DR / 8, RR = kWave / RP;
+#pragma unroll
+    for (int j = 0; j < 16 / RR; ++j) {
+      const int r = j * RR + lane / RP;
+      dma16(from + (size_t)min(r, most) * (DC + DR) * 2 + DC * 2 + 16 * ((lane % RP) ^ tile_key<RP>(r)),
+            rope + j * 1024);
+    }
+  };
+
+  while (t < end) {
+    const Item it = item_at(a, t);
+    const int first = t - it.start, n = min(end - t, it.tiles - first);
+    copy(it, first, 0);
+    h8 q[S::RT][S::KS];
+#pragma unroll
+    for (int r = 0; r < S::RT; ++r) {
+      const size_t row = it.row0 + min((wr * S::RT + r) * 16 + c, it.rows - 1);
+#pragma unroll
+      for (int k = 0; k < S::KS; ++k) q[r][k] = ld_h8(a.ql + row * (DC + DR) + 32 * k + 8 * g);
+    }
+    float m[MT], sum[S::RT];
+    f4 o[S::CT][MT] = {};
+#pragma unroll
+    for (int r = 0; r < MT; ++r) m[r] = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < S::RT; ++r) sum[r] = 0.f;
+    const float unit = l.scale * kLog2e;
+    for (int i = 0; i < n; ++i) {
+      const char* buf = lds + (i & 1) * S::BUF;
+      vm_wait<0>();
+      lds_barrier();                                            // tile i is there; tile i - 1 is done with
+      if (i + 1 < n) copy(it, first + i + 1, (i + 1) & 1);
+      f4 s[S::TT][S::RT] = {};
+#pragma unroll
+      for (int k = 0; k < S::KS; ++k) {
+#pragma unroll
+        for (int tt = 0; tt < S::TT; ++tt) {
+          const int tok = (wt * S::TT + tt) * 16 + c;
+          const char* p = k < DC / 32
+                              ? buf + tok * DC * 2 + 16 * ((4 * k + g) ^ tile_key<DC / 8>(tok))
+                              : buf + S::LAT + tok * DR * 2 + 16 * ((4 * (k - DC / 32) + g) ^ tile_key<DR / 8>(tok));
+          const h8 kk = ld_h8(p);
+#pragma unroll
+          for (int r = 0; r < S::RT; ++r) s[tt][r] = mfma16(kk, q[r][k], s[tt][r]);
+        }
+      }
+      const int left = it.last - (it.tok0 + (first + i) * kTile);  // tokens of this tile, less one
+      float top[S::RT];
+#pragma unroll
+      for (int r = 0; r < S::RT; ++r) top[r] = -INFINITY;
+#pragma unroll
+      for (int tt = 0; tt < S::TT; ++tt) {
+        const int grp = wt * S::TT + tt;
+        const bool lost = bad[4 * (i & 1) + grp];
+#pragma unroll
+        for (int r = 0; r < S::RT; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float v = lost || 16 * grp + 4 * g + e > left ? -INFINITY : s[tt][r][e] * unit;
+            s[tt][r][e] = v;
+            top[r] = fmaxf(top[r], v);
+          }
+      }
+#pragma unroll
+      for (int r = 0; r < S::RT; ++r) {
+        const float v = col_max(top[r]);
+        if (g == 0) smax[wt * S::M + (wr * S::RT + r) * 16 + c] = v;
+      }
+      lds_barrier();
+      float keep[MT], mu[MT];
+#pragma unroll
+      for (int r = 0; r < MT; ++r) {
+        float v = m[r];
+#pragma unroll
+        for (int w = 0; w < S::WT; ++w) v = fmaxf(v, smax[w * S::M + 16 * r + c]);
+        mu[r] = v == -INFINITY ? 0.f : v;
+        keep[r] = exp2_fast(m[r] - mu[r]);
+        m[r] = v;
+      }
+#pragma unroll
+      for (int r = 0; r < S::RT; ++r) {
+        const int rr = wr * S::RT + r;                          // (a select below: rr is not a constant)
+        float mr = mu[r], kr = keep[r];
+        if constexpr (S::WR > 1) {
+          mr = wr ? mu[S::RT + r] : mu[r];
+          kr = wr ? keep[S::RT + r] : keep[r];
+        }
+        float add = 0.f;
+#pragma unroll
+        for (int tt = 0; tt < S::TT; ++tt) {
+          h4 p;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float v = exp2_fast(s[tt][r][e] - mr);
+            add += v;
+            p[e] = (_Float16)v;
+          }
+          const int row = rr * 16 + c, tok = (wt * S::TT + tt) * 16 + 4 * g;
+          *reinterpret_cast<h4*>(pt + row * 128 + 16 * ((tok >> 3) ^ tile_key<8>(row)) + 2 * (tok & 7)) = p;
+        }
+        sum[r] = fmaf(sum[r], kr, add);
+      }
+      bool same = true;
+#pragma unroll
+      for (int r = 0; r < MT; ++r) same = same && keep[r] == 1.f;
+      if (!__all(same))
+#pragma unroll
+        for (int r = 0; r < MT; ++r)
+#pragma unroll
+          for (int k = 0; k < S::CT; ++k) o[k][r] *= keep[r];
+      lds_barrier();
+#pragma unroll
+      for (int ks = 0; ks < kTile / 32; ++ks) {
+        h8 p[MT];
+#pragma unroll
+        for (int r = 0; r < MT; ++r) {
+          const int row = 16 * r + c;
+          p[r] = ld_h8(pt + row * 128 + 16 * ((4 * ks + g) ^ tile_key<8>(row)));
+        }
+#pragma unroll
+        for (int k = 0; k < S::CT; ++k) {
+          h4 part[2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const int tok = 32 * ks + 8 * g + 4 * u + (c >> 2), col = wave * (DC / 4) + 16 * k + 4 * (c & 3);
+            part[u] = ld_tr(buf + tok * DC * 2 + 16 * ((col >> 3) ^ tile_key<DC / 8>(tok)) + 2 * (col & 7));
+          }
+          const h8 v = join(part[0], part[1]);
+#pragma unroll
+          for (int r = 0; r < MT; ++r) o[k][r] = mfma16(v, p[r], o[k][r]);
+        }
+      }
+    }
+    // this workgroup's partial result of the item
+    const size_t seg = (size_t)wg + it.index;
+#pragma unroll
+    for (int r = 0; r < S::RT; ++r) {
+      const float v = col_sum(sum[r]);
+      if (g == 0) ssum[wt * S::M + (wr * S::RT + r) * 16 + c] = v;
+    }
+#pragma unroll
+    for (int r = 0; r < MT; ++r)
+#pragma unroll
+      for (int k = 0; k < S::CT; ++k)
+        *reinterpret_cast<f4*>(a.part_o + (seg * S::M + 16 * r + c) * DC + wave * (DC / 4) + 16 * k + 4 * g) = o[k][r];
+    lds_barrier();                                              // (also: the last tile is done with)
+    if (wave == 0 && g == 0)
+#pragma unroll
+      for (int r = 0; r < MT; ++r) {
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < S::WT; ++w) v += ssum[w * S::M + 16 * r + c];
+        *reinterpret_cast<float2*>(a.part_ml + (seg * S::M + 16 * r + c) * 2) = float2{m[r], v};
+      }
+    lds_barrier();
+    t += n;
+  }
+}
+
+// ---- joining the partial results --------------------------------------------------
+// One query row a workgroup, four latent columns a thread: the weights 2^(m - max) of
+// the partial results that the plan says exist, in the plan's order. A row without any
+// (no tokens) gives zeros. The latents are rounded to fp16 for the product with W_uv.
+__global__ void __launch_bounds__(128) latent_join_kernel(DecodeArgs a) {
+  const LatentArgs& l = a.l;
+  const int row = blockIdx.x, b = row / l.H, h = row % l.H, M = a.p.rows;
+  const int all = a.starts[a.B], per = max(1, (all + a.p.wgs - 1) / a.p.wgs);
+  const int col = 4 * threadIdx.x;
+  float top = -INFINITY, sum = 0.f;
+  f4 o = {};
+  auto add = [&](const Item& it, int r) {
+    if (it.tiles <= 0) return;
+    const int w0 = it.start / per, w1 = (it.start + it.tiles - 1) / per;
+    for (int w = w0; w <= w1; ++w) {
+      const size_t seg = (size_t)w + it.index;
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (seg * M + r) * 2);
+      if (ml.x == -INFINITY) continue;                       // (every token of it was lost)
+      f4 v = {};
+      if (col < l.Dc) v = *reinterpret_cast<const f4*>(a.part_o + (seg * M + r) * l.Dc + col);
+      const float m = fmaxf(top, ml.x), x = exp2_fast(top - m), y = exp2_fast(ml.x - m);
+      o = o * x + v * y;
+      sum = sum * x + ml.y * y;
+      top = m;
+    }
+  };
+  for (int k = 0; k < a.p.chunks; ++k) add(prefix_item(a, k, row / M), row % M);
+  add(own_item(a, b, h / M, a.starts[b], (a.starts[b + 1] - a.starts[b]) / a.p.head_blocks), h % M);
+  if (col < l.Dc) {
+    const float inv = sum > 0.f ? 1.f / sum : sum != sum ? sum : 0.f;
+    const h4 v = {(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
+    *reinterpret_cast<h4*>(a.lat + (size_t)row * l.Dc + col) = v;
+  }
+}
+
+// ---- out of the latent space --------------------------------------------------------
+// o_h = W_uv,h lat_h: 16 values of one head a workgroup, whose four waves split the
+// latent columns and keep their weights in registers for all sequences.
+template <int DC>
+__global__ void __launch_bounds__(256) latent_up_kernel(DecodeArgs a) {
+  __shared__ f4 red[4][kWave];
+  const LatentArgs& l = a.l;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const int v0 = blockIdx.x * 16, h = blockIdx.y;
+  const int b0 = blockIdx.z * 128, b1 = min(b0 + 128, a.B);
+  constexpr int KS = DC / 128;
+  h8 w[KS];
+  const __half* wv = l.w + ((size_t)h * (l.Dn + l.Dv) + l.Dn + v0 + c) * DC + wave * (DC / 4) + 8 * g;
+#pragma unroll
+  for (int k = 0; k < KS; ++k) w[k] = ld_h8(wv + 32 * k);
+  for (int bt = b0; bt < b1; bt += 16) {
+    const size_t r = (size_t)min(bt + c, b1 - 1) * l.H + h;
+    f4 d = {};
+#pragma unroll
+    for (int k = 0; k < KS; ++k) d = mfma16(w[k], ld_h8(a.lat + r * DC + wave * (DC / 4) + 32 * k + 8 * g), d);
+    red[wave][lane] = d;
+    __syncthreads();
+    if (wave == 0 && bt + c < b1) {
+      const f4 s = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+      const h4 v = {(_Float16)s[0], (_Float16)s[1], (_Float16)s[2], (_Float16)s[3]};
+      *reinterpret_cast<h4*>(l.out + r * l.Dv + v0 + 4 * g) = v;
+    }
+    __syncthreads();
+  }
+}
+
+int tiles_host(int len) { return (len + kTile - 1) / kTile; }
+size_t round256(size_t v) { return (v + 255) / 256 * 256; }
+
+template <int DC, int DR, int MT>
+hipError_t launch_attention(const DecodeArgs& a, hipStream_t st) {
+  constexpr int lds = DecodeShape<DC, DR, MT>::LDS;
+  static_assert(lds <= 160 * 1024, "LDS of a CU");
+  auto kernel = latent_decode_kernel<DC, DR, MT>;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3(a.p.wgs), dim3(256), lds, st, a);
+  return hipGetLastError();
+}
+template <int DC, int DR>
+hipError_t launch_attention(const DecodeArgs& a, hipStream_t st) {
+  if (a.p.rows == 16) return launch_attention<DC, DR, 1>(a, st);
+  if (a.p.rows == 32) return launch_attention<DC, DR, 2>(a, st);
+  return launch_attention<DC, DR, 4>(a, st);
+}
+template <int DC>
+hipError_t launch_attention(const DecodeArgs& a, hipStream_t st) {
+  return a.l.Dr == 64 ? launch_attention<DC, 64>(a, st) : launch_attention<DC, 32>(a, st);
+}
+
+}  // namespace
+
+DecodePlan decode_plan(int H, int Dc, int Dr, int B, int max_len, int prefix_len) {
+  DecodePlan p{};
+  const int most = prefix_len > 0 ? std::max(H, std::min(B * H, 64)) : H;
+  p.rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
+  p.head_blocks = (H + p.rows - 1) / p.rows;
+  p.row_blocks = prefix_len > 0 ? (B * H + p.rows - 1) / p.rows : 0;
+  const int pt = tiles_host(prefix_len);
+  p.chunks = prefix_len > 0 ? (p.row_blocks >= 8 ? std::min(8, pt) : 1) : 0;
+  p.chunk_tiles = p.chunks ? (pt + p.chunks - 1) / p.chunks : 0;
+  if (p.chunk_tiles) p.chunks = (pt + p.chunk_tiles - 1) / p.chunk_tiles;
+  p.prefix_tiles = pt * p.row_blocks;
+  const long long tiles = p.prefix_tiles + (long long)B * p.head_blocks * tiles_host(max_len);
+  const int wgs = kCus * (Dc <= 128 ? 3 : Dc <= 256 ? 2 : 1);
+  p.wgs = (int)std::min<long long>(wgs, (std::max<long long>(tiles, 1) + 7) / 8 * 8);
+  const size_t rows = (size_t)B * H, parts = (size_t)p.wgs + (size_t)p.chunks * p.row_blocks + (size_t)B * p.head_blocks;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off += round256(bytes);
+    return o;
+  };
+  p.ql = take(rows * (Dc + Dr) * 2);
+  p.lat = take(rows * Dc * 2);
+  p.starts = take(((size_t)B + 1) * 4);
+  p.part_o = take(parts * p.rows * Dc * 4);
+  p.part_ml = take(parts * p.rows * 8);
+  p.total = off;
+  return p;
+}
+
+hipError_t launch_latent_append(const AppendArgs& a, hipStream_t st) {
+  const int n = a.l.q ? a.l.H * (a.l.Dn + a.l.Dr) : 0;
+  hipLaunchKernelGGL(latent_append_kernel, dim3(a.T, 1 + (n + 2047) / 2048), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_latent_decode(const DecodeArgs& a, hipStream_t st) {
+  const LatentArgs& l = a.l;
+  const dim3 ga(l.Dc / 64 + 1, l.H, (a.B + 63) / 64);
+  if (l.Dn == 128)
+    hipLaunchKernelGGL(latent_absorb_kernel<128>, ga, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL(latent_absorb_kernel<64>, ga, dim3(256), 0, st, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  e = l.Dc == 512 ? launch_attention<512>(a, st) : l.Dc == 256 ? launch_attention<256>(a, st) : launch_attention<128>(a, st);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(latent_join_kernel, dim3(a.B * l.H), dim3(128), 0, st, a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const dim3 gu(l.Dv / 16, l.H, (a.B + 127) / 128);
+  if (l.Dc == 512)
+    hipLaunchKernelGGL(latent_up_kernel<512>, gu, dim3(256), 0, st, a);
+  else if (l.Dc == 256)
+    hipLaunchKernelGGL(latent_up_kernel<256>, gu, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL(latent_up_kernel<128>, gu, dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+// ---- arguments of the calls --------------------------------------------------------
+
+int latent_cache_check(const moe_latent_spec* s, const moe_latent_cache* c) {
+  const int rc = moe_latent_spec_check(s);
+  if (rc != MOE_OK) return rc;
+  if (!c || !c->pages || c->n_pages < 1 || c->n_seqs < 1 || !c->table || c->max_pages < 1 ||
+      c->table_stride < c->max_pages || c->reserved != 0 ||
+      (int64_t)c->max_pages * s->page_tokens > (int64_t(1) << 30))
+    return MOE_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(c->pages) & 15) || (reinterpret_cast<uintptr_t>(c->table) & 3)) return MOE_EALIGN;
+  return MOE_OK;
+}
+
+LatentArgs latent_args(const moe_latent_spec* s, const moe_latent_cache* c) {
+  LatentArgs l{};
+  l.H = s->heads;
+  l.Dc = s->d_latent;
+  l.Dr = s->d_rope;
+  l.Dn = s->d_nope;
+  l.Dv = s->d_v;
+  l.page = s->page_tokens;
+  l.scale = s->scale;
+  l.pages = static_cast<const __half*>(c->pages);
+  l.n_pages = c->n_pages;
+  l.n_seqs = c->n_seqs;
+  l.max_pages = c->max_pages;
+  l.table = c->table;
+  l.table_stride = c->table_stride;
+  return l;
+}
+
+}  // namespace moe
+
+// ---- C ABI (contracts in include/moe_api.h) ---------------------------------------
+
+namespace {
+
+bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+
+constexpr int kMaxLen = 1 << 26, kMaxBatch = 1 << 16;
+
+bool decode_shape_ok(const moe_latent_spec* s, int B, int max_len, int prefix_len) {
+  if (moe_latent_spec_check(s) != MOE_OK || B < 0 || B > kMaxBatch || max_len < 0 || max_len > kMaxLen ||
+      prefix_len < 0 || prefix_len > kMaxLen)
+    return false;
+  // tiles on the plan's line, with their row blocks (16 query rows the smallest)
+  const int64_t rows = ((int64_t)B * s->heads + 15) / 16 + B;
+  return rows * (((int64_t)max_len + prefix_len + 63) / 64 + 1) < (int64_t(1) << 30);
+}
+
+}  // namespace
+
+extern "C" {
+
+int moe_latent_spec_check(const moe_latent_spec* s) {
+  if (!s) return MOE_EINVAL;
+  if (s->heads < 1 || s->heads > 128) return MOE_EINVAL;
+  if (s->d_latent != 128 && s->d_latent != 256 && s->d_latent != 512) return MOE_EINVAL;
+  if (s->d_rope != 32 && s->d_rope != 64) return MOE_EINVAL;
+  if ((s->d_nope != 64 && s->d_nope != 128) || (s->d_v != 64 && s->d_v != 128)) return MOE_EINVAL;
+  const int p = s->page_tokens;
+  if (p < 16 || p > 1024 || (p & (p - 1))) return MOE_EINVAL;
+  if (!(s->scale > 0.f) || s->scale > 1e4f) return MOE_EINVAL;
+  return s->reserved[0] == 0 && s->reserved[1] == 0 ? MOE_OK : MOE_EINVAL;
+}
+
+int moe_latent_append(const moe_latent_spec* spec, const moe_latent_cache* cache, const float* kv, const void* gamma_f16,
+                      const float* rope, int max_pos, const int32_t* seq, const int32_t* pos, int T, const void* q_f16,
+                      void* q_out_f16, uint32_t* status, void* stream) {
+  const int rc = moe::latent_cache_check(spec, cache);
+  if (rc != MOE_OK) return rc;
+  if (T < 0 || T > (1 << 22) || max_pos < 1 || (!q_f16) != (!q_out_f16)) return MOE_EINVAL;
+  if (T == 0) return MOE_OK;
+  if (!kv || !gamma_f16 || !rope || !seq || !pos) return MOE_EINVAL;
+  if (misaligned(kv, 16) || misaligned(gamma_f16, 16) || misaligned(rope, 16) || misaligned(seq, 4) ||
+      misaligned(pos, 4) || misaligned(q_f16, 16) || misaligned(q_out_f16, 16) || misaligned(status, 4))
+    return MOE_EALIGN;
+  moe::AppendArgs a{};
+  a.l = moe::latent_args(spec, cache);
+  a.l.q = static_cast<const __half*>(q_f16);
+  a.l.status = status;
+  a.kv = kv;
+  a.gamma = static_cast<const __half*>(gamma_f16);
+  a.rope = rope;
+  a.max_pos = max_pos;
+  a.T = T;
+  a.seq = seq;
+  a.pos = pos;
+  a.pages = static_cast<__half*>(cache->pages);
+  a.q_out = static_cast<__half*>(q_out_f16);
+  return moe::launch_latent_append(a, static_cast<hipStream_t>(stream)) == hipSuccess ? MOE_OK : MOE_EHIP;
+}
+
+size_t moe_latent_decode_workspace_bytes(const moe_latent_spec* s, int B, int max_len, int prefix_len) {
+  if (!decode_shape_ok(s, B, max_len, prefix_len)) return 0;
+  return moe::decode_plan(s->heads, s->d_latent, s->d_rope, B < 1 ? 1 : B, max_len, prefix_len).total;
+}
+
+int moe_latent_decode(const moe_latent_spec* spec, const moe_latent_cache* cache, const void* w_kvb_f16,
+                      const void* q_f16, int B, const int32_t* kv_len, int max_len, const int32_t* prefix_pages,
+                      int prefix_len, void* out_f16, uint32_t* status, void* workspace, size_t workspace_bytes,
+                      void* stream) {
+  const int rc = moe::latent_cache_check(spec, cache);
+  if (rc != MOE_OK) return rc;
+  if (!decode_shape_ok(spec, B, max_len, prefix_len) || B > cache->n_seqs) return MOE_EINVAL;
+  if (B == 0) return MOE_OK;
+  if (!w_kvb_f16 || !q_f16 || !kv_len || !out_f16 || !workspace || (prefix_len > 0 && !prefix_pages)) return MOE_EINVAL;
+  if (misaligned(w_kvb_f16, 16) || misaligned(q_f16, 16) || misaligned(kv_len, 4) || misaligned(prefix_pages, 4) ||
+      misaligned(out_f16, 16) || misaligned(status, 4) || misaligned(workspace, 16))
+    return MOE_EALIGN;
+  moe::DecodeArgs a{};
+  a.l = moe::latent_args(spec, cache);
+  a.l.w = static_cast<const __half*>(w_kvb_f16);
+  a.l.q = static_cast<const __half*>(q_f16);
+  a.l.out = static_cast<__half*>(out_f16);
+  a.l.status = status;
+  a.B = B;
+  a.max_len = max_len;
+  a.prefix_len = prefix_len;
+  a.kv_len = kv_len;
+  a.prefix = prefix_len > 0 ? prefix_pages : nullptr;
+  a.p = moe::decode_plan(a.l.H, a.l.Dc, a.l.Dr, B, max_len, prefix_len);
+  if (workspace_bytes < a.p.total) return MOE_ENOMEM;
+  char* ws = static_cast<char*>(workspace);
+  a.ql = reinterpret_cast<__half*>(ws + a.p.ql);
+  a.lat = reinterpret_cast<__half*>(ws + a.p.lat);
+  a.starts = reinterpret_cast<int32_t*>(ws + a.p.starts);
+  a.part_o = reinterpret_cast<float*>(ws + a.p.part_o);
+  a.part_ml = reinterpret_cast<float*>(ws + a.p.part_ml);
+  return moe::launch_latent_decode(a, static_cast<hipStream_t>(stream)) == hipSuccess ? MOE_OK : MOE_EHIP;
+}
+
+}  // extern "C"
