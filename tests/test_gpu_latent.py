@@ -71,7 +71,7 @@ class Cache:
                              prefix=self.prefix_ids if prefix else None, prefix_len=prefix)
         return out.cpu().numpy()
 
-    def prefill(self, q, counts, rows=None, spare_q=0, spare_kv=0, max_q=None):
+    def prefill(self, q, counts, spare_q=0, spare_kv=0, max_q=None):
         torch = self.torch
         qs = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
         ks = np.concatenate([[0], np.cumsum(self.lens)]).astype(np.int32)
@@ -217,7 +217,7 @@ def test_prefill_broken_lists(torch_cuda):
     from paper_2609_18063_amd import binding as B
     c = Cache(torch_cuda, g, 3, *S, 16, [40, 9])
     q = _queries(g, 60, c)
-    got = c.prefill(q, [48, 9])
+    got = c.prefill(q[:57], [48, 9])
     assert int(c.status) == B.MOE_STATUS_BAD_LENGTH
     assert not got[:8].any()
     c.check(got[8:48], q[8:48], 0, c.rows[0], np.arange(40) + 1)
