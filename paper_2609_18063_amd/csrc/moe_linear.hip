@@ -3,9 +3,9 @@
 //
 // Per 64-input group g of an output row the products are summed as
 //   y += s_g (q_g . x_g) + z_g sum(x_g):
-// the codes q enter the matrix cores as exact fp16 numbers (the nibble as a
-// subnormal, q 2^-24, whose 2^24 goes into s), x is fp16, the sums are fp32 and s
-// and z are applied in fp32, so that no weight is rounded.
+// the codes q enter the matrix cores as exact fp16 numbers (q 2^-9, whose 2^9 goes
+// into s), x is fp16, the sums are fp32 and s and z are applied in fp32, so that no
+// weight is rounded.
 #include <hip/hip_runtime.h>
 
 #include "moe_linear.h"
@@ -14,9 +14,12 @@
 namespace moe {
 namespace {
 
-constexpr float kCodeUnit = 16777216.f;  // 2^24
+constexpr float kCodeUnit = 512.f;
 
-// Eight codes (one dword, even input in the low nibble) as halves q 2^-24, in order.
+// Eight codes (one dword, even input in the low nibble) as halves q 2^-9, in order: the
+// nibble is the subnormal q 2^-24, times 2^15. (The matrix cores take the subnormals
+// themselves too, but align their products to the smallest normal number's exponent:
+// a group's sum then loses up to 10 of its bits, 1.2e-6 of a row against 1e-7.)
 __device__ __forceinline__ h8 codes8(uint32_t w) {
   const uint32_t lo = w & 0x0F0F0F0Fu, hi = (w >> 4) & 0x0F0F0F0Fu;
   u4 v;
@@ -24,7 +27,7 @@ __device__ __forceinline__ h8 codes8(uint32_t w) {
   v.y = __builtin_amdgcn_perm(hi, lo, 0x0C050C01u);
   v.z = __builtin_amdgcn_perm(hi, lo, 0x0C060C02u);
   v.w = __builtin_amdgcn_perm(hi, lo, 0x0C070C03u);
-  return __builtin_bit_cast(h8, v);
+  return __builtin_bit_cast(h8, v) * (_Float16)32768.f;
 }
 
 __device__ __forceinline__ h8 ones8() {
