@@ -5,7 +5,8 @@
 
 namespace moe {
 
-constexpr int kTile = 64;        // cached tokens a tile of the attention kernels takes
+constexpr int kTile = 64;        // context tokens of a tile of the expanded form
+constexpr int kStep = 32;        // and of the absorbed form
 
 struct LatentArgs {
   int H, Dc, Dr, Dn, Dv, page;   // page: tokens a page, a power of two >= 16

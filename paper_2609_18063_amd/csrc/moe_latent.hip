@@ -18,6 +18,7 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr int kCus = 256;
+constexpr float kSlack = 8.f;    // (as a power of two)
 
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
 
@@ -84,7 +85,7 @@ __device__ __forceinline__ int own_len(const DecodeArgs& a, int b, bool report) 
   if (report && a.l.status) atomicOr(a.l.status, MOE_STATUS_BAD_LENGTH);
   return n < 0 ? 0 : most;
 }
-__device__ __forceinline__ int tiles_of(int len) { return (len + kTile - 1) / kTile; }
+__device__ __forceinline__ int tiles_of(int len) { return (len + kStep - 1) / kStep; }
 
 struct Item {
   int index, start, tiles;  // order number, first tile on the line, tiles
@@ -101,7 +102,7 @@ __device__ __forceinline__ Item prefix_item(const DecodeArgs& a, int chunk, int 
   it.start = first * a.p.row_blocks + rb * it.tiles;
   it.row0 = rb * a.p.rows;
   it.rows = min(a.p.rows, a.B * a.l.H - it.row0);
-  it.tok0 = first * kTile;
+  it.tok0 = first * kStep;
   it.last = a.prefix_len - 1;
   it.pages = a.prefix;
   return it;
@@ -211,221 +212,267 @@ __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
 }
 
 // ---- attention over the cache -------------------------------------------------------
-// A workgroup takes its share of the line of tiles, item by item. Tiles of 64 tokens are
-// copied into LDS one ahead; scores are formed transposed (tokens x query rows), each
-// wave for its own tokens (or, at 64 rows, its tokens and half of the rows), with the
-// query in registers. The waves agree on the rows' new maximum through LDS, put the
-// weights there, and each adds up its quarter of the latent columns from the same tile,
-// read transposed. Three barriers a tile. With few heads HBM bounds it, with many the
-// matrix cores and LDS.
+// A workgroup takes its share of the line of tiles (32 tokens each), item by item. Half
+// of its waves form the scores, transposed (tokens x query rows, a wave 16 of the tokens
+// and, of four, half of the rows, with the query in registers), and the weights; the
+// other half add up the weighted latents of the tile before, each its share of the latent
+// columns, read transposed from the same LDS copy. So the products of one tile run beside
+// the exponentials of the next, and with one barrier a tile; the copies are two tiles
+// ahead, in four buffers. With few heads HBM bounds it, with many the matrix cores and
+// LDS.
+// The weights are taken against a reference per row that follows the running maximum only
+// where that passes it by kSlack: until then they are at most 2^kSlack and nothing is
+// rescaled. The waves decide that alike, from the largest scores in LDS.
+// The weights are rounded to fp16 for the product with the latents, which are fp16.
 template <int DC, int DR, int MT>
 struct DecodeShape {
   static constexpr int M = 16 * MT;
-  static constexpr int WT = MT == 4 ? 2 : 4, WR = 4 / WT;      // waves over tokens and over rows
-  static constexpr int TT = 4 / WT, RT = MT / WR;              // 16-token, 16-row tiles of a wave
-  static constexpr int KS = (DC + DR) / 32, CT = DC / 64;
-  static constexpr int LAT = kTile * DC * 2, BUF = LAT + kTile * DR * 2;
-  static constexpr int LDS = 2 * BUF + M * 128 + 2 * WT * M * 4 + 32;
+  static constexpr int WR = MT == 1 ? 1 : 2, RT = MT / WR;     // row blocks, 16-row tiles of a score wave
+  static constexpr int NS = 2 * WR, NW = 2 * NS;               // score waves, waves
+  static constexpr int OWN = kStep / NW;                       // token rows a wave copies
+  static constexpr int KS = (DC + DR) / 32, CT = DC / (16 * NS);
+  static constexpr int LAT = kStep * DC * 2, BUF = LAT + kStep * DR * 2;
+  static constexpr int PT = M * 64;                            // the weights of a tile
+  static constexpr int LDS = 4 * BUF + 2 * PT + 2 * 2 * M * 4 + 2 * M * 4 + 32;
+  // copies of a tile by one wave: latent rows LR at a time, rotated keys RR at a time
+  static constexpr int LP = DC / 8, LR = kWave / LP, RP = DR / 8, RR = kWave / RP;
+  static constexpr int LN = OWN / LR, RN = RR <= OWN ? OWN / RR : 1;
 };
 
 template <int DC, int DR, int MT>
-__global__ void __launch_bounds__(256, 1) latent_decode_kernel(DecodeArgs a) {
+__global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_decode_kernel(DecodeArgs a) {
   using S = DecodeShape<DC, DR, MT>;
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  char* pt = lds + 2 * S::BUF;                                  // weights [M][64] halves
-  float* smax = reinterpret_cast<float*>(pt + S::M * 128);      // [WT][M]
-  float* ssum = smax + S::WT * S::M;                            // [WT][M]
-  int* bad = reinterpret_cast<int*>(ssum + S::WT * S::M);       // [2][4]: 16-token groups without a page
+  char* pt = lds + 4 * S::BUF;                                  // weights [2][M][32] halves
+  float* smax = reinterpret_cast<float*>(pt + 2 * S::PT);       // [2][2][M]: largest scores, by tile and token half
+  float* ssum = smax + 4 * S::M;                                // [2][M]: sums, by token half
+  int* bad = reinterpret_cast<int*>(ssum + 2 * S::M);           // [4][2]: 16-token groups without a page
   const LatentArgs& l = a.l;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int c = lane & 15, g = lane >> 4;
-  const int wt = wave % S::WT, wr = wave / S::WT;
+  const bool scores = wave < S::NS;
+  const int wt = wave % 2, wr = wave / 2, wo = wave - S::NS;    // token half, row block; share of the columns
   // neighbours on the line share a chiplet and its L2
   const int wg = (blockIdx.x % 8) * (a.p.wgs / 8) + blockIdx.x / 8;
   const int all = a.starts[a.B], per = (all + a.p.wgs - 1) / a.p.wgs;
   int t = wg * per;
   const int end = min(all, t + per);
+  const float unit = l.scale * kLog2e;
+  const uint32_t at0 = lds_at(lds);
+  const int shift = 31 - __clz(l.page);
 
-  // rows of 16 tokens of tile `tile` (this wave's group) into buffer `buf`
-  auto copy = [&](const Item& it, int tile, int buf) {
-    const int want = it.tok0 + tile * kTile + 16 * wave;
-    const int base = min(want, it.last & ~15);                  // (past the end: the last group again)
-    const int page = it.pages[base / l.page];
+  // this wave copies rows own0 .. own0 + OWN - 1 of a tile, of the 16-token group at
+  // group() (past the end: the last group again), and its part of the rotated keys
+  // (where a copy of those is several waves' rows, one of them takes it)
+  const int own0 = S::OWN * wave;
+  const bool ropes = S::RR <= S::OWN || own0 % S::RR == 0;
+  auto group = [&](const Item& it, int tile) { return min(it.tok0 + tile * kStep + (own0 & ~15), it.last & ~15); };
+  auto page_of = [&](const Item& it, int tile) { return ld_scalar(it.pages + (group(it, tile) >> shift)); };
+  auto copy = [&](const Item& it, int tile, int buf, int page) {
+    const int base = group(it, tile);
     const bool ok = page >= 0 && page < l.n_pages;
-    char* lat = lds + buf * S::BUF + 16 * wave * DC * 2;
-    char* rope = lds + buf * S::BUF + S::LAT + 16 * wave * DR * 2;
-    if (lane == 0) bad[4 * buf + wave] = !ok;
+    if (lane == 0 && own0 % 16 == 0) bad[2 * buf + own0 / 16] = !ok;
     if (!ok) {
+      // (zeros, and the scores are masked; the waits for copies find fewer than they allow)
       if (lane == 0 && l.status) atomicOr(l.status, MOE_STATUS_BAD_PAGE);
-      for (int e = lane; e < 16 * DC / 8; e += kWave) *reinterpret_cast<U4*>(lat + 16 * e) = U4{};
-      for (int e = lane; e < 16 * DR / 8; e += kWave) *reinterpret_cast<U4*>(rope + 16 * e) = U4{};
+      char* lat = lds + buf * S::BUF;
+      for (int e = lane; e < S::OWN * DC / 8; e += kWave) *reinterpret_cast<U4*>(lat + own0 * DC * 2 + 16 * e) = U4{};
+      for (int e = lane; e < S::OWN * DR / 8; e += kWave)
+        *reinterpret_cast<U4*>(lat + S::LAT + own0 * DR * 2 + 16 * e) = U4{};
+      vm_wait<0>();
       return;
     }
+    const uint32_t lat = at0 + buf * S::BUF, rope = lat + S::LAT;
     const char* from = reinterpret_cast<const char*>(l.pages) +
-                       ((size_t)page * l.page + base % l.page) * (DC + DR) * 2;
+                       ((size_t)page * l.page + (base & (l.page - 1))) * (DC + DR) * 2;
     const int most = it.last - base;                            // rows past the end repeat the last one
-    constexpr int LP = DC / 8, LR = kWave / LP;                 // pieces of a row, rows of a copy
+    int ln = lane;                                              // (offsets formed here, not held in registers)
+    asm volatile("" : "+v"(ln));
 #pragma unroll
-    for (int j = 0; j < 16 / LR; ++j) {
-      const int r = j * LR + lane / LP;
-      dma16(from + (size_t)min(r, most) * (DC + DR) * 2 + 16 * ((lane % LP) ^ tile_key<LP>(r)),
-            lat + j * 1024);
+    for (int j = 0; j < S::LN; ++j) {
+      const int r0 = own0 + j * S::LR, r = S::LR == 1 ? r0 : r0 + ln / S::LP;
+      dma16(from, min(r & 15, most) * (DC + DR) * 2 + 16 * ((ln % S::LP) ^ tile_key<S::LP>(r)), lat + r0 * DC * 2);
     }
-    constexpr int RP = DR / 8, RR = kWave / RP;
+    if (ropes)
 #pragma unroll
-    for (int j = 0; j < 16 / RR; ++j) {
-      const int r = j * RR + lane / RP;
-      dma16(from + (size_t)min(r, most) * (DC + DR) * 2 + DC * 2 + 16 * ((lane % RP) ^ tile_key<RP>(r)),
-            rope + j * 1024);
-    }
+      for (int j = 0; j < S::RN; ++j) {
+        const int r0 = own0 + j * S::RR, r = r0 + ln / S::RP;
+        dma16(from + DC * 2, min(r & 15, most) * (DC + DR) * 2 + 16 * ((ln % S::RP) ^ tile_key<S::RP>(r)),
+              rope + r0 * DR * 2);
+      }
+  };
+  // all but the newest tile's copies of this wave are there (or all)
+  auto landed = [&](bool newest_too) {
+    if (newest_too)
+      vm_wait<0>();
+    else if (ropes)
+      vm_wait<S::LN + S::RN>();
+    else
+      vm_wait<S::LN>();
   };
 
   while (t < end) {
     const Item it = item_at(a, t);
     const int first = t - it.start, n = min(end - t, it.tiles - first);
-    copy(it, first, 0);
-    h8 q[S::RT][S::KS];
-#pragma unroll
-    for (int r = 0; r < S::RT; ++r) {
-      const size_t row = it.row0 + min((wr * S::RT + r) * 16 + c, it.rows - 1);
-#pragma unroll
-      for (int k = 0; k < S::KS; ++k) q[r][k] = ld_h8(a.ql + row * (DC + DR) + 32 * k + 8 * g);
-    }
-    float m[MT], sum[S::RT];
-    f4 o[S::CT][MT] = {};
-#pragma unroll
-    for (int r = 0; r < MT; ++r) m[r] = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < S::RT; ++r) sum[r] = 0.f;
-    const float unit = l.scale * kLog2e;
-    for (int i = 0; i < n; ++i) {
-      const char* buf = lds + (i & 1) * S::BUF;
-      vm_wait<0>();
-      lds_barrier();                                            // tile i is there; tile i - 1 is done with
-      if (i + 1 < n) copy(it, first + i + 1, (i + 1) & 1);
-      f4 s[S::TT][S::RT] = {};
-#pragma unroll
-      for (int k = 0; k < S::KS; ++k) {
-#pragma unroll
-        for (int tt = 0; tt < S::TT; ++tt) {
-          const int tok = (wt * S::TT + tt) * 16 + c;
-          const char* p = k < DC / 32
-                              ? buf + tok * DC * 2 + 16 * ((4 * k + g) ^ tile_key<DC / 8>(tok))
-                              : buf + S::LAT + tok * DR * 2 + 16 * ((4 * (k - DC / 32) + g) ^ tile_key<DR / 8>(tok));
-          const h8 kk = ld_h8(p);
-#pragma unroll
-          for (int r = 0; r < S::RT; ++r) s[tt][r] = mfma16(kk, q[r][k], s[tt][r]);
-        }
+    // steps 0 .. n: scores of tile s beside the latents of tile s - 1; tile s + 2 is asked for
+    copy(it, first, 0, page_of(it, first));
+    if (n > 1) copy(it, first + 1, 1, page_of(it, first + 1));
+    int page = page_of(it, first + min(2, n - 1));
+    auto ahead = [&](int s) {
+      if (s + 2 < n) {
+        copy(it, first + s + 2, (s + 2) & 3, page);
+        page = page_of(it, first + min(s + 3, n - 1));
       }
-      const int left = it.last - (it.tok0 + (first + i) * kTile);  // tokens of this tile, less one
-      float top[S::RT];
-#pragma unroll
-      for (int r = 0; r < S::RT; ++r) top[r] = -INFINITY;
-#pragma unroll
-      for (int tt = 0; tt < S::TT; ++tt) {
-        const int grp = wt * S::TT + tt;
-        const bool lost = bad[4 * (i & 1) + grp];
-#pragma unroll
-        for (int r = 0; r < S::RT; ++r)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float v = lost || 16 * grp + 4 * g + e > left ? -INFINITY : s[tt][r][e] * unit;
-            s[tt][r][e] = v;
-            top[r] = fmaxf(top[r], v);
-          }
-      }
-#pragma unroll
-      for (int r = 0; r < S::RT; ++r) {
-        const float v = col_max(top[r]);
-        if (g == 0) smax[wt * S::M + (wr * S::RT + r) * 16 + c] = v;
-      }
-      lds_barrier();
-      float keep[MT], mu[MT];
-#pragma unroll
-      for (int r = 0; r < MT; ++r) {
-        float v = m[r];
-#pragma unroll
-        for (int w = 0; w < S::WT; ++w) v = fmaxf(v, smax[w * S::M + 16 * r + c]);
-        mu[r] = v == -INFINITY ? 0.f : v;
-        keep[r] = exp2_fast(m[r] - mu[r]);
-        m[r] = v;
-      }
-#pragma unroll
-      for (int r = 0; r < S::RT; ++r) {
-        const int rr = wr * S::RT + r;                          // (a select below: rr is not a constant)
-        float mr = mu[r], kr = keep[r];
-        if constexpr (S::WR > 1) {
-          mr = wr ? mu[S::RT + r] : mu[r];
-          kr = wr ? keep[S::RT + r] : keep[r];
-        }
-        float add = 0.f;
-#pragma unroll
-        for (int tt = 0; tt < S::TT; ++tt) {
-          h4 p;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float v = exp2_fast(s[tt][r][e] - mr);
-            add += v;
-            p[e] = (_Float16)v;
-          }
-          const int row = rr * 16 + c, tok = (wt * S::TT + tt) * 16 + 4 * g;
-          *reinterpret_cast<h4*>(pt + row * 128 + 16 * ((tok >> 3) ^ tile_key<8>(row)) + 2 * (tok & 7)) = p;
-        }
-        sum[r] = fmaf(sum[r], kr, add);
-      }
-      bool same = true;
-#pragma unroll
-      for (int r = 0; r < MT; ++r) same = same && keep[r] == 1.f;
-      if (!__all(same))
-#pragma unroll
-        for (int r = 0; r < MT; ++r)
-#pragma unroll
-          for (int k = 0; k < S::CT; ++k) o[k][r] *= keep[r];
-      lds_barrier();
-#pragma unroll
-      for (int ks = 0; ks < kTile / 32; ++ks) {
-        h8 p[MT];
-#pragma unroll
-        for (int r = 0; r < MT; ++r) {
-          const int row = 16 * r + c;
-          p[r] = ld_h8(pt + row * 128 + 16 * ((4 * ks + g) ^ tile_key<8>(row)));
-        }
-#pragma unroll
-        for (int k = 0; k < S::CT; ++k) {
-          h4 part[2];
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const int tok = 32 * ks + 8 * g + 4 * u + (c >> 2), col = wave * (DC / 4) + 16 * k + 4 * (c & 3);
-            part[u] = ld_tr(buf + tok * DC * 2 + 16 * ((col >> 3) ^ tile_key<DC / 8>(tok)) + 2 * (col & 7));
-          }
-          const h8 v = join(part[0], part[1]);
-#pragma unroll
-          for (int r = 0; r < MT; ++r) o[k][r] = mfma16(v, p[r], o[k][r]);
-        }
-      }
-    }
-    // this workgroup's partial result of the item
+    };
+    float mref = -INFINITY;                                     // the reference of row lane % M (unscaled)
+    // after step s: does a row's largest score pass its reference by too much?
+    auto passed = [&](int s, float& top) {
+      const float* p = smax + (s & 1) * 2 * S::M + lane % S::M;
+      top = fmaxf(p[0], p[S::M]);
+      return __any((top - mref) * unit > kSlack);
+    };
+    auto follow = [&](float top) {                              // the factor of what was summed so far
+      const float v = fmaxf(mref, top), mu = v == -INFINITY ? 0.f : v * unit;
+      const float keep = exp2_fast(fmaf(mref, unit, -mu));
+      mref = v;
+      return keep;
+    };
     const size_t seg = (size_t)wg + it.index;
+    if (scores) {
+      h8 q[S::RT][S::KS];
 #pragma unroll
-    for (int r = 0; r < S::RT; ++r) {
-      const float v = col_sum(sum[r]);
-      if (g == 0) ssum[wt * S::M + (wr * S::RT + r) * 16 + c] = v;
-    }
+      for (int r = 0; r < S::RT; ++r) {
+        const size_t row = it.row0 + min((wr * S::RT + r) * 16 + c, it.rows - 1);
 #pragma unroll
-    for (int r = 0; r < MT; ++r)
-#pragma unroll
-      for (int k = 0; k < S::CT; ++k)
-        *reinterpret_cast<f4*>(a.part_o + (seg * S::M + 16 * r + c) * DC + wave * (DC / 4) + 16 * k + 4 * g) = o[k][r];
-    lds_barrier();                                              // (also: the last tile is done with)
-    if (wave == 0 && g == 0)
-#pragma unroll
-      for (int r = 0; r < MT; ++r) {
-        float v = 0.f;
-#pragma unroll
-        for (int w = 0; w < S::WT; ++w) v += ssum[w * S::M + 16 * r + c];
-        *reinterpret_cast<float2*>(a.part_ml + (seg * S::M + 16 * r + c) * 2) = float2{m[r], v};
+        for (int k = 0; k < S::KS; ++k) q[r][k] = ld_h8(a.ql + row * (DC + DR) + 32 * k + 8 * g);
       }
-    lds_barrier();
+      float sum[S::RT], mu[S::RT];
+#pragma unroll
+      for (int r = 0; r < S::RT; ++r) sum[r] = mu[r] = 0.f;
+      vm_drain();
+      lds_barrier();
+      for (int s = 0; s <= n; ++s) {
+        ahead(s);
+        if (s < n) {
+          const char* buf = lds + (s & 3) * S::BUF;
+          f4 x[S::RT] = {};
+          const int tok = wt * 16 + c;
+#pragma unroll
+          for (int k = 0; k < S::KS; ++k) {
+            const char* p = k < DC / 32
+                                ? buf + tok * DC * 2 + 256 * (k >> 2) + 16 * ((4 * (k & 3) + g) ^ tile_key<S::LP>(c))
+                                : buf + S::LAT + tok * DR * 2 + 16 * ((4 * (k - DC / 32) + g) ^ tile_key<S::RP>(c));
+            const h8 kk = ld_h8(p);
+#pragma unroll
+            for (int r = 0; r < S::RT; ++r) x[r] = mfma16(kk, q[r][k], x[r]);
+          }
+          const int left = it.last - (it.tok0 + (first + s) * kStep + 16 * wt);  // tokens of the group, less one
+          if (bad[2 * (s & 3) + wt] || left < 15) {
+            const int most = bad[2 * (s & 3) + wt] ? -1 : left - 4 * g;
+#pragma unroll
+            for (int r = 0; r < S::RT; ++r)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (e > most) x[r][e] = -INFINITY;
+          }
+          // the weights, where the latents are read in the same order: of the tile's tokens,
+          // 16 u + 4 g .. + 3 at 8 g + 4 u
+          float add[S::RT];
+          auto weights = [&]() {
+#pragma unroll
+            for (int r = 0; r < S::RT; ++r) {
+              h4 p;
+              add[r] = 0.f;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float v = exp2_fast(fmaf(x[r][e], unit, -mu[r]));
+                add[r] += v;
+                p[e] = (_Float16)v;
+              }
+              *reinterpret_cast<h4*>(pt + (s & 1) * S::PT + ((wr * S::RT + r) * 16 + c) * 64 +
+                                     16 * (g ^ tile_key<4>(c)) + 8 * wt) = p;
+            }
+          };
+          weights();
+#pragma unroll
+          for (int r = 0; r < S::RT; ++r) {
+            const float v = col_max(fmaxf(fmaxf(x[r][0], x[r][1]), fmaxf(x[r][2], x[r][3])));
+            if (g == 0) smax[((s & 1) * 2 + wt) * S::M + (wr * S::RT + r) * 16 + c] = v;
+          }
+          landed(s + 2 >= n);
+          lds_barrier();
+          float top;
+          if (passed(s, top)) {
+            const float keep = follow(top), ref = mref == -INFINITY ? 0.f : mref * unit;
+#pragma unroll
+            for (int r = 0; r < S::RT; ++r) {
+              sum[r] *= __shfl(keep, (wr * S::RT + r) * 16 + c, kWave);
+              mu[r] = __shfl(ref, (wr * S::RT + r) * 16 + c, kWave);
+            }
+            weights();
+            lds_barrier();
+          }
+#pragma unroll
+          for (int r = 0; r < S::RT; ++r) sum[r] += add[r];
+        } else {
+          lds_barrier();
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < S::RT; ++r) {
+        const float v = col_sum(sum[r]);
+        if (g == 0) ssum[wt * S::M + (wr * S::RT + r) * 16 + c] = v;
+      }
+      lds_barrier();
+      if (wave == 0 && lane < S::M)
+        *reinterpret_cast<float2*>(a.part_ml + (seg * S::M + lane) * 2) =
+            float2{mref * unit, ssum[lane] + ssum[S::M + lane]};
+    } else {
+      f4 o[S::CT][MT] = {};
+      vm_drain();
+      lds_barrier();
+      for (int s = 0; s <= n; ++s) {
+        ahead(s);
+        if (s > 0) {
+          const char* buf = lds + ((s - 1) & 3) * S::BUF;
+          h8 p[MT];
+#pragma unroll
+          for (int r = 0; r < MT; ++r)
+            p[r] = ld_h8(pt + ((s - 1) & 1) * S::PT + (16 * r + c) * 64 + 16 * (g ^ tile_key<4>(c)));
+#pragma unroll
+          for (int k = 0; k < S::CT; ++k) {
+            h4 part[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const int t0 = 4 * g + (c >> 2), col = 16 * (wo * S::CT + k) + 4 * (c & 3);
+              part[u] = ld_tr(buf + (16 * u + t0) * DC * 2 + 16 * ((col >> 3) ^ tile_key<S::LP>(t0)) + 2 * (col & 7));
+            }
+            const h8 v = join(part[0], part[1]);
+#pragma unroll
+            for (int r = 0; r < MT; ++r) o[k][r] = mfma16(v, p[r], o[k][r]);
+          }
+        }
+        if (s < n) landed(s + 2 >= n);
+        lds_barrier();
+        float top;
+        if (s < n && passed(s, top)) {
+          const float keep = follow(top);
+#pragma unroll
+          for (int r = 0; r < MT; ++r) {
+            const float kr = __shfl(keep, (16 * r + c) % S::M, kWave);
+#pragma unroll
+            for (int k = 0; k < S::CT; ++k) o[k][r] *= kr;
+          }
+          lds_barrier();
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < MT; ++r)
+#pragma unroll
+        for (int k = 0; k < S::CT; ++k)
+          *reinterpret_cast<f4*>(a.part_o + (seg * S::M + 16 * r + c) * DC + 16 * (wo * S::CT + k) + 4 * g) = o[k][r];
+      lds_barrier();
+    }
     t += n;
   }
 }
@@ -496,7 +543,7 @@ __global__ void __launch_bounds__(256) latent_up_kernel(DecodeArgs a) {
   }
 }
 
-int tiles_host(int len) { return (len + kTile - 1) / kTile; }
+int tiles_host(int len) { return (len + kStep - 1) / kStep; }
 size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
 template <int DC, int DR, int MT>
@@ -506,7 +553,7 @@ hipError_t launch_attention(const DecodeArgs& a, hipStream_t st) {
   auto kernel = latent_decode_kernel<DC, DR, MT>;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3(a.p.wgs), dim3(256), lds, st, a);
+  hipLaunchKernelGGL(kernel, dim3(a.p.wgs), dim3(64 * DecodeShape<DC, DR, MT>::NW), lds, st, a);
   return hipGetLastError();
 }
 template <int DC, int DR>
@@ -627,9 +674,9 @@ bool decode_shape_ok(const moe_latent_spec* s, int B, int max_len, int prefix_le
   if (moe_latent_spec_check(s) != MOE_OK || B < 0 || B > kMaxBatch || max_len < 0 || max_len > kMaxLen ||
       prefix_len < 0 || prefix_len > kMaxLen)
     return false;
-  // tiles on the plan's line, with their row blocks (16 query rows the smallest)
+  // tiles on the plan's line, with their row blocks (16 query rows and 32 tokens the smallest)
   const int64_t rows = ((int64_t)B * s->heads + 15) / 16 + B;
-  return rows * (((int64_t)max_len + prefix_len + 63) / 64 + 1) < (int64_t(1) << 30);
+  return rows * (((int64_t)max_len + prefix_len + 31) / 32 + 1) < (int64_t(1) << 30);
 }
 
 }  // namespace

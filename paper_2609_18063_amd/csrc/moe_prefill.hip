@@ -13,7 +13,7 @@ namespace moe {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr int kRows = 128;       // query rows a workgroup (32 a wave)
+constexpr int kWaves = 8, kRows = 32 * kWaves;  // of a workgroup of the attention: waves, query rows
 
 struct Span {
   int first, len;
@@ -163,17 +163,19 @@ __global__ void __launch_bounds__(256) latent_expand_kernel(PrefillArgs a, int s
 }
 
 // ---- attention ------------------------------------------------------------------------
-// 128 query rows of one head a workgroup, 32 a wave, with the query in registers; tiles of
+// 256 query rows of one head a workgroup, 32 a wave, with the query in registers; tiles of
 // 64 context tokens in LDS, copied one ahead, one barrier each. Scores are formed
 // transposed (tokens x rows): a lane then holds its row's weights of the tokens
 // 16 t + 4 g .. + 3, which are the operand of the product with the values as they are,
 // when the values' rows are read (transposed) in the same order. The running maximum and
 // sum of a row are in the four lanes of its column. Late tiles first, and the heads of a
 // tile next to each other, so that one head's workgroups share a chiplet's L2.
+// Between a tile's copies and the next barrier no load is waited for: loads come back in
+// order, and the wait would be for the copies.
 template <int DN, int DR, int DV>
-__global__ void __launch_bounds__(256, 2) latent_prefill_kernel(PrefillArgs a) {
+__global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillArgs a) {
   constexpr int KB = kTile * DN * 2, RB = kTile * DR * 2, VB = kTile * DV * 2, BUF = KB + RB + VB;
-  constexpr int KS = (DN + DR) / 32, CT = DV / 16, RT = 2;
+  constexpr int KS = (DN + DR) / 32, CT = DV / 16, RT = 2, OWN = kTile / kWaves;  // OWN: token rows a wave copies
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const LatentArgs& l = a.l;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -185,8 +187,8 @@ __global__ void __launch_bounds__(256, 2) latent_prefill_kernel(PrefillArgs a) {
   const int shift = ks.len - qs.len;                     // position of query row 0
   const int row0 = qt * kRows + 32 * wave;               // this wave's first row
   const int last_row = min(qt * kRows + kRows, qs.len) - 1;
-  const int tiles = max(0, (shift + last_row) / kTile + 1) * (shift + last_row >= 0);
-  const int mine = shift + min(row0 + 31, qs.len - 1);   // last position this wave's rows see
+  const int tiles = shift + last_row >= 0 ? (shift + last_row) / kTile + 1 : 0;
+  const int mine = row0 < qs.len ? shift + min(row0 + 31, qs.len - 1) : -1;  // last position that the wave's rows see
   h8 q[RT][KS];
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
@@ -197,22 +199,27 @@ __global__ void __launch_bounds__(256, 2) latent_prefill_kernel(PrefillArgs a) {
   const char* kb = reinterpret_cast<const char*>(a.k + ((size_t)h * a.kv_total + ks.first) * DN);
   const char* vb = reinterpret_cast<const char*>(a.v + ((size_t)h * a.kv_total + ks.first) * DV);
   const char* rb = reinterpret_cast<const char*>(a.kr + (size_t)ks.first * DR);
-  auto rows = [&](const char* from, int tile, char* to, auto pieces) {
+  // rows of P pieces of 16 bytes, R rows a copy; rows past the context repeat its last one
+  auto rows = [&](const char* from, int tile, uint32_t to, auto pieces) {
     constexpr int P = decltype(pieces)::value, R = kWave / P;
+    const char* base = from + (size_t)tile * kTile * (P * 16);
+    const int most = ks.len - 1 - tile * kTile;
 #pragma unroll
-    for (int j = 0; j < 16 / R; ++j) {
-      const int r = 16 * wave + j * R + lane / P, tok = min(tile * kTile + r, ks.len - 1);
-      dma16(from + (size_t)tok * (P * 16) + 16 * ((lane % P) ^ tile_key<P>(r)), to + (16 * wave + j * R) * P * 16);
+    for (int j = 0; j < (OWN + R - 1) / R; ++j) {
+      const int r0 = OWN * wave + j * R, r = r0 + lane / P;
+      if (R <= OWN || wave % (R / OWN) == 0)             // (a copy of 16 rows is two waves' share)
+        dma16(base, (uint32_t)min(r, most) * (P * 16) + 16 * ((lane % P) ^ tile_key<P>(r)), to + r0 * P * 16);
     }
   };
+  const uint32_t at0 = lds_at(lds);
   auto copy = [&](int tile) {
-    char* buf = lds + (tile & 1) * BUF;
+    const uint32_t buf = at0 + (tile & 1) * BUF;
     rows(kb, tile, buf, std::integral_constant<int, DN / 8>());
     rows(rb, tile, buf + KB, std::integral_constant<int, DR / 8>());
     rows(vb, tile, buf + KB + RB, std::integral_constant<int, DV / 8>());
   };
   f4 o[CT][RT] = {};
-  float m[RT], sum[RT];
+  float m[RT], sum[RT];                                  // running maximum (of unscaled scores) and sum
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     m[r] = -INFINITY;
@@ -220,12 +227,20 @@ __global__ void __launch_bounds__(256, 2) latent_prefill_kernel(PrefillArgs a) {
   }
   const float unit = l.scale * kLog2e;
   const uint32_t* lost_of = a.lost + tile_base(a, b);
-  if (tiles > 0) copy(0);
+  uint32_t lost_next = 0;
+  if (tiles > 0) {
+    lost_next = lost_of[0];
+    copy(0);
+  }
   for (int i = 0; i < tiles; ++i) {
     const char* buf = lds + (i & 1) * BUF;
-    vm_wait<0>();
+    vm_drain();
     lds_barrier();
-    if (i + 1 < tiles) copy(i + 1);
+    const uint32_t lost = __builtin_amdgcn_readfirstlane(lost_next);
+    if (i + 1 < tiles) {
+      lost_next = lost_of[i + 1];
+      copy(i + 1);
+    }
     if (i * kTile > mine) continue;
     f4 s[4][RT] = {};
 #pragma unroll
@@ -233,37 +248,39 @@ __global__ void __launch_bounds__(256, 2) latent_prefill_kernel(PrefillArgs a) {
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const int tok = 16 * t + c;
-        const char* p = k < DN / 32 ? buf + tok * DN * 2 + 16 * ((4 * k + g) ^ tile_key<DN / 8>(tok))
-                                    : buf + KB + tok * DR * 2 + 16 * ((4 * (k - DN / 32) + g) ^ tile_key<DR / 8>(tok));
+        const char* p = k < DN / 32 ? buf + tok * DN * 2 + 16 * ((4 * k + g) ^ tile_key<DN / 8>(c))
+                                    : buf + KB + tok * DR * 2 + 16 * ((4 * (k - DN / 32) + g) ^ tile_key<DR / 8>(c));
         const h8 kk = ld_h8(p);
 #pragma unroll
         for (int r = 0; r < RT; ++r) s[t][r] = mfma16(kk, q[r][k], s[t][r]);
       }
-    const uint32_t lost = lost_of[i];
-    const bool edge = lost || (i + 1) * kTile > shift + row0 + 1;  // some row does not see the whole tile
+    if (lost || (i + 1) * kTile > shift + row0 + 1) {    // some row does not see the whole tile
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const int see = shift + row0 + 16 * r + c - i * kTile - 4 * g;  // the row sees tokens 0 .. see + 4 g of the tile
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (16 * t + e > see || (lost >> t & 1)) s[t][r][e] = -INFINITY;
+      }
+    }
     h8 p[2][RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      const int see = shift + row0 + 16 * r + c - i * kTile;       // the row sees tokens 0 .. see of the tile
-      float top = -INFINITY;
+      float top = fmaxf(s[0][r][0], s[0][r][1]);
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float v = s[t][r][e] * unit;
-          if (edge && (16 * t + 4 * g + e > see || (lost >> t & 1))) v = -INFINITY;
-          s[t][r][e] = v;
-          top = fmaxf(top, v);
-        }
-      const float mx = fmaxf(m[r], col_max(top)), mu = mx == -INFINITY ? 0.f : mx;
-      const float keep = __builtin_amdgcn_exp2f(m[r] - mu);
+      for (int e = 2; e < 16; e += 2) top = max3(top, s[e >> 2][r][e & 3], s[e >> 2][r][(e & 3) + 1]);
+      const float mx = fmaxf(m[r], col_max(top));
+      const float mu = mx == -INFINITY ? 0.f : mx * unit;
+      const float keep = __builtin_amdgcn_exp2f(fmaf(m[r], unit, -mu));
       m[r] = mx;
       float add = 0.f;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float v = __builtin_amdgcn_exp2f(s[t][r][e] - mu);
+          const float v = __builtin_amdgcn_exp2f(fmaf(s[t][r][e], unit, -mu));
           add += v;
           p[t >> 1][r][4 * (t & 1) + e] = (_Float16)v;
         }
@@ -273,6 +290,7 @@ __global__ void __launch_bounds__(256, 2) latent_prefill_kernel(PrefillArgs a) {
         for (int k = 0; k < CT; ++k) o[k][r] *= keep;
     }
     const char* vt = buf + KB + RB;
+    const int t0 = 4 * g + (c >> 2);
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
@@ -280,8 +298,8 @@ __global__ void __launch_bounds__(256, 2) latent_prefill_kernel(PrefillArgs a) {
         h4 part[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const int tok = 32 * hf + 16 * u + 4 * g + (c >> 2), col = 16 * k + 4 * (c & 3);
-          part[u] = ld_tr(vt + tok * DV * 2 + 16 * ((col >> 3) ^ tile_key<DV / 8>(tok)) + 2 * (col & 7));
+          const int tok = 32 * hf + 16 * u + t0, col = 16 * k + 4 * (c & 3);
+          part[u] = ld_tr(vt + tok * DV * 2 + 16 * ((col >> 3) ^ tile_key<DV / 8>(t0)) + 2 * (col & 7));
         }
         const h8 v = join(part[0], part[1]);
 #pragma unroll
@@ -311,7 +329,7 @@ hipError_t launch_attention(const PrefillArgs& a, hipStream_t st) {
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
   const unsigned tiles = (a.max_q + kRows - 1) / kRows;
-  hipLaunchKernelGGL(kernel, dim3(tiles * a.l.H * a.B), dim3(256), lds, st, a);
+  hipLaunchKernelGGL(kernel, dim3(tiles * a.l.H * a.B), dim3(64 * kWaves), lds, st, a);
   return hipGetLastError();
 }
 template <int DN, int DR>

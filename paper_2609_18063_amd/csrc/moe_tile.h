@@ -54,11 +54,37 @@ __device__ __forceinline__ void dma16(const void* g, const void* lds) {
       : "s"(to), "v"(g)
       : "memory");
 }
+// The same from a base that the wave shares, with a byte offset per lane, to LDS address
+// `to` (lds_at).
+__device__ __forceinline__ uint32_t lds_at(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+__device__ __forceinline__ void dma16(const void* base, uint32_t off, uint32_t to) {
+  uint32_t saved;
+  to = __builtin_amdgcn_readfirstlane(to);
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, %3\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "s"(to), "v"(off), "s"(base)
+      : "memory");
+}
+// An int that the whole wave reads and nothing writes while the kernel runs, through the
+// scalar unit: waited for apart from the copies into LDS.
+__device__ __forceinline__ int ld_scalar(const int32_t* p) {
+  return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)p;
+}
 template <int N>
 __device__ __forceinline__ void vm_wait() {
   static_assert(N >= 0 && N <= 63, "vmcnt range");
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
+// All of this wave's loads and stores, in a form that the compiler counts too: behind it,
+// a loop needs no waits for what was asked for before it.
+__device__ __forceinline__ void vm_drain() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 // Workgroup barrier that leaves copies into LDS in flight: LDS reads and writes of this
 // wave are complete, its global loads need not be.
 __device__ __forceinline__ void lds_barrier() {
@@ -80,14 +106,21 @@ __device__ __forceinline__ int tile_key(int row) {
 
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
-// Sum and largest over the four lanes of a wave that share c = lane % 16.
+// Sum and largest over the four lanes of a wave that share c = lane % 16: a lane swap
+// with a register's own copy leaves the lower and the upper half's values side by side.
 __device__ __forceinline__ float col_sum(float v) {
-  v += __shfl_xor(v, 16, kWave);
-  return v + __shfl_xor(v, 32, kWave);
+  const uint32_t x = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  const uint32_t y = __float_as_uint(__uint_as_float(a[0]) + __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(y, y, false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 __device__ __forceinline__ float col_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16, kWave));
-  return fmaxf(v, __shfl_xor(v, 32, kWave));
+  const uint32_t x = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  const uint32_t y = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+  const auto b = __builtin_amdgcn_permlane16_swap(y, y, false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 }  // namespace moe
