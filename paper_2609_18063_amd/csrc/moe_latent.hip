@@ -216,27 +216,28 @@ __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
 // of its waves form the scores, transposed (tokens x query rows, a wave 16 of the tokens
 // and, of four, half of the rows, with the query in registers), and the weights; the
 // other half add up the weighted latents of the tile before, each its share of the latent
-// columns, read transposed from the same LDS copy. So the products of one tile run beside
-// the exponentials of the next, and with one barrier a tile; the copies are two tiles
-// ahead, in four buffers. With few heads HBM bounds it, with many the matrix cores and
-// LDS.
+// columns, read transposed from the same LDS copy, and make the copies, two tiles ahead in
+// four buffers. So the products of one tile run beside the exponentials of the next, with
+// one barrier a tile. With few heads HBM bounds it, with many the scores' chain of one
+// wave (its products, exponentials and the barrier).
 // The weights are taken against a reference per row that follows the running maximum only
 // where that passes it by kSlack: until then they are at most 2^kSlack and nothing is
-// rescaled. The waves decide that alike, from the largest scores in LDS.
-// The weights are rounded to fp16 for the product with the latents, which are fp16.
+// rescaled. The weights are rounded to fp16 for the product with the latents, which are
+// fp16.
 template <int DC, int DR, int MT>
 struct DecodeShape {
   static constexpr int M = 16 * MT;
   static constexpr int WR = MT == 1 ? 1 : 2, RT = MT / WR;     // row blocks, 16-row tiles of a score wave
-  static constexpr int NS = 2 * WR, NW = 2 * NS;               // score waves, waves
-  static constexpr int OWN = kStep / NW;                       // token rows a wave copies
+  static constexpr int NS = 2 * WR, NW = 2 * NS;               // score waves (as many add up), waves
+  static constexpr int OWN = kStep / NS;                       // token rows that a wave of the others copies
   static constexpr int KS = (DC + DR) / 32, CT = DC / (16 * NS);
   static constexpr int LAT = kStep * DC * 2, BUF = LAT + kStep * DR * 2;
   static constexpr int PT = M * 64;                            // the weights of a tile
-  static constexpr int LDS = 4 * BUF + 2 * PT + 2 * 2 * M * 4 + 2 * M * 4 + 32;
+  static constexpr int LDS = 4 * BUF + 2 * PT + 4 * M * 4 + 32;
   // copies of a tile by one wave: latent rows LR at a time, rotated keys RR at a time
   static constexpr int LP = DC / 8, LR = kWave / LP, RP = DR / 8, RR = kWave / RP;
   static constexpr int LN = OWN / LR, RN = RR <= OWN ? OWN / RR : 1;
+  static_assert(OWN % LR == 0 && OWN <= 16, "rows of a wave's copies lie in one group");
 };
 
 template <int DC, int DR, int MT>
@@ -244,36 +245,151 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
   using S = DecodeShape<DC, DR, MT>;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   char* pt = lds + 4 * S::BUF;                                  // weights [2][M][32] halves
-  float* smax = reinterpret_cast<float*>(pt + 2 * S::PT);       // [2][2][M]: largest scores, by tile and token half
-  float* ssum = smax + 4 * S::M;                                // [2][M]: sums, by token half
-  int* bad = reinterpret_cast<int*>(ssum + 2 * S::M);           // [4][2]: 16-token groups without a page
+  float* smax = reinterpret_cast<float*>(pt + 2 * S::PT);       // [2][M], by token half
+  float* skeep = smax + 2 * S::M;                               // [M]
+  float* ssum = skeep + S::M;                                   // [M]
+  int* passed = reinterpret_cast<int*>(ssum + S::M);            // [2]: the last step with a row past its reference
   const LatentArgs& l = a.l;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int c = lane & 15, g = lane >> 4;
-  const bool scores = wave < S::NS;
   const int wt = wave % 2, wr = wave / 2, wo = wave - S::NS;    // token half, row block; share of the columns
   // neighbours on the line share a chiplet and its L2
   const int wg = (blockIdx.x % 8) * (a.p.wgs / 8) + blockIdx.x / 8;
   const int all = a.starts[a.B], per = (all + a.p.wgs - 1) / a.p.wgs;
-  int t = wg * per;
-  const int end = min(all, t + per);
+  const int begin = wg * per, end = min(all, begin + per);
   const float unit = l.scale * kLog2e;
-  const uint32_t at0 = lds_at(lds);
   const int shift = 31 - __clz(l.page);
+  // 16-token group `grp` (0 or 1) of a tile, from its first token (past the end: the last group)
+  auto group = [&](const Item& it, int tile, int grp) { return min(it.tok0 + tile * kStep + 16 * grp, it.last & ~15); };
+  auto page_of = [&](const Item& it, int tile, int grp) { return ld_scalar(it.pages + (group(it, tile, grp) >> shift)); };
+  auto known = [&](int page) { return page >= 0 && page < l.n_pages; };
+  if (threadIdx.x < 2) passed[threadIdx.x] = -1;
 
-  // this wave copies rows own0 .. own0 + OWN - 1 of a tile, of the 16-token group at
-  // group() (past the end: the last group again), and its part of the rotated keys
+  if (wave < S::NS) {
+    __builtin_amdgcn_s_setprio(2);
+    for (int t = begin; t < end;) {
+      const Item it = item_at(a, t);
+      const int first = t - it.start, n = min(end - t, it.tiles - first);
+      h8 q[S::RT][S::KS];
+#pragma unroll
+      for (int r = 0; r < S::RT; ++r) {
+        const size_t row = it.row0 + min((wr * S::RT + r) * 16 + c, it.rows - 1);
+#pragma unroll
+        for (int k = 0; k < S::KS; ++k) q[r][k] = ld_h8(a.ql + row * (DC + DR) + 32 * k + 8 * g);
+      }
+      float sum[S::RT], m[S::RT], ref[S::RT];                   // m: the reference, unscaled; ref: m unit, or 0
+#pragma unroll
+      for (int r = 0; r < S::RT; ++r) {
+        m[r] = -INFINITY;
+        sum[r] = ref[r] = 0.f;
+      }
+      int page = page_of(it, first, wt);
+      vm_drain();
+      lds_barrier();
+      for (int s = 0; s < n; ++s) {
+        const char* buf = lds + (s & 3) * S::BUF;
+        f4 x[S::RT] = {};
+        const int tok = wt * 16 + c;
+#pragma unroll
+        for (int k = 0; k < S::KS; ++k) {
+          const char* p = k < DC / 32
+                              ? buf + tok * DC * 2 + 256 * (k >> 2) + 16 * ((4 * (k & 3) + g) ^ tile_key<S::LP>(c))
+                              : buf + S::LAT + tok * DR * 2 + 16 * ((4 * (k - DC / 32) + g) ^ tile_key<S::RP>(c));
+          const h8 kk = ld_h8(p);
+#pragma unroll
+          for (int r = 0; r < S::RT; ++r) x[r] = mfma16(kk, q[r][k], x[r]);
+        }
+        const bool lost = !known(page);
+        page = page_of(it, first + min(s + 1, n - 1), wt);
+        const int left = it.last - (it.tok0 + (first + s) * kStep + 16 * wt);  // tokens of the group, less one
+        if (lost || left < 15) {
+          const int most = lost ? -1 : left - 4 * g;
+#pragma unroll
+          for (int r = 0; r < S::RT; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (e > most) x[r][e] = -INFINITY;
+        }
+        // the weights, where the latents are read in the same order: of the tile's tokens,
+        // 16 u + 4 g .. + 3 at 8 g + 4 u
+        float add[S::RT];
+        auto weights = [&]() {
+#pragma unroll
+          for (int r = 0; r < S::RT; ++r) {
+            h4 p;
+            add[r] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float v = exp2_fast(fmaf(x[r][e], unit, -ref[r]));
+              add[r] += v;
+              p[e] = (_Float16)v;
+            }
+            *reinterpret_cast<h4*>(pt + (s & 1) * S::PT + ((wr * S::RT + r) * 16 + c) * 64 + 16 * (g ^ tile_key<4>(c)) +
+                                   8 * wt) = p;
+          }
+        };
+        weights();
+        bool far = false;
+        float top[S::RT];
+#pragma unroll
+        for (int r = 0; r < S::RT; ++r) {
+          top[r] = fmaxf(fmaxf(x[r][0], x[r][1]), fmaxf(x[r][2], x[r][3]));
+          far = far || (top[r] - m[r]) * unit > kSlack;         // (no token so far: any score is)
+        }
+        if (__any(far) && lane == 0) passed[s & 1] = t + s;
+        lds_barrier();
+        if (__builtin_amdgcn_readfirstlane(passed[s & 1]) == t + s) {
+          // every row takes its largest score as its reference
+#pragma unroll
+          for (int r = 0; r < S::RT; ++r) {
+            top[r] = col_max(top[r]);
+            if (g == 0) smax[wt * S::M + (wr * S::RT + r) * 16 + c] = top[r];
+          }
+          lds_barrier();
+#pragma unroll
+          for (int r = 0; r < S::RT; ++r) {
+            const int row = (wr * S::RT + r) * 16 + c;
+            const float most = max3(m[r], top[r], smax[(1 - wt) * S::M + row]);
+            const float now = most == -INFINITY ? 0.f : most * unit;
+            const float keep = m[r] == -INFINITY ? 0.f : exp2_fast(ref[r] - now);
+            m[r] = most;
+            sum[r] *= keep;
+            ref[r] = now;
+            if (g == 0 && wt == 0) skeep[row] = keep;
+          }
+          weights();
+          lds_barrier();
+        }
+#pragma unroll
+        for (int r = 0; r < S::RT; ++r) sum[r] += add[r];
+      }
+      const size_t seg = (size_t)wg + it.index;
+#pragma unroll
+      for (int r = 0; r < S::RT; ++r) {
+        sum[r] = col_sum(sum[r]);
+        if (g == 0 && wt == 1) ssum[(wr * S::RT + r) * 16 + c] = sum[r];
+      }
+      lds_barrier();
+      if (g == 0 && wt == 0)
+#pragma unroll
+        for (int r = 0; r < S::RT; ++r) {
+          const int row = (wr * S::RT + r) * 16 + c;
+          *reinterpret_cast<float2*>(a.part_ml + (seg * S::M + row) * 2) = float2{m[r] * unit, sum[r] + ssum[row]};
+        }
+      t += n;
+    }
+    return;
+  }
+
+  // this wave copies rows own0 .. own0 + OWN - 1 of a tile and its part of the rotated keys
   // (where a copy of those is several waves' rows, one of them takes it)
-  const int own0 = S::OWN * wave;
+  const int own0 = S::OWN * wo, grp = own0 / 16;
   const bool ropes = S::RR <= S::OWN || own0 % S::RR == 0;
-  auto group = [&](const Item& it, int tile) { return min(it.tok0 + tile * kStep + (own0 & ~15), it.last & ~15); };
-  auto page_of = [&](const Item& it, int tile) { return ld_scalar(it.pages + (group(it, tile) >> shift)); };
+  const uint32_t at0 = lds_at(lds);
   auto copy = [&](const Item& it, int tile, int buf, int page) {
-    const int base = group(it, tile);
-    const bool ok = page >= 0 && page < l.n_pages;
-    if (lane == 0 && own0 % 16 == 0) bad[2 * buf + own0 / 16] = !ok;
-    if (!ok) {
-      // (zeros, and the scores are masked; the waits for copies find fewer than they allow)
+    const int base = group(it, tile, grp);
+    if (!known(page)) {
+      // (zeros, whose scores are masked; the waits for copies find fewer than they allow)
       if (lane == 0 && l.status) atomicOr(l.status, MOE_STATUS_BAD_PAGE);
       char* lat = lds + buf * S::BUF;
       for (int e = lane; e < S::OWN * DC / 8; e += kWave) *reinterpret_cast<U4*>(lat + own0 * DC * 2 + 16 * e) = U4{};
@@ -285,194 +401,92 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
     const uint32_t lat = at0 + buf * S::BUF, rope = lat + S::LAT;
     const char* from = reinterpret_cast<const char*>(l.pages) +
                        ((size_t)page * l.page + (base & (l.page - 1))) * (DC + DR) * 2;
-    const int most = it.last - base;                            // rows past the end repeat the last one
     int ln = lane;                                              // (offsets formed here, not held in registers)
     asm volatile("" : "+v"(ln));
+    auto rows = [&](auto at_most) {
 #pragma unroll
-    for (int j = 0; j < S::LN; ++j) {
-      const int r0 = own0 + j * S::LR, r = S::LR == 1 ? r0 : r0 + ln / S::LP;
-      dma16(from, min(r & 15, most) * (DC + DR) * 2 + 16 * ((ln % S::LP) ^ tile_key<S::LP>(r)), lat + r0 * DC * 2);
-    }
-    if (ropes)
-#pragma unroll
-      for (int j = 0; j < S::RN; ++j) {
-        const int r0 = own0 + j * S::RR, r = r0 + ln / S::RP;
-        dma16(from + DC * 2, min(r & 15, most) * (DC + DR) * 2 + 16 * ((ln % S::RP) ^ tile_key<S::RP>(r)),
-              rope + r0 * DR * 2);
+      for (int j = 0; j < S::LN; ++j) {
+        const int r0 = j * S::LR, r = S::LR == 1 ? r0 : r0 + ln / S::LP;
+        dma16(from, at_most((own0 & 15) + r) * ((DC + DR) * 2) + 16 * ((ln % S::LP) ^ tile_key<S::LP>(own0 + r)),
+              lat + (own0 + r0) * DC * 2);
       }
-  };
-  // all but the newest tile's copies of this wave are there (or all)
-  auto landed = [&](bool newest_too) {
-    if (newest_too)
-      vm_wait<0>();
-    else if (ropes)
-      vm_wait<S::LN + S::RN>();
+      if (ropes)
+#pragma unroll
+        for (int j = 0; j < S::RN; ++j) {
+          const int r0 = j * S::RR, r = r0 + ln / S::RP;
+          dma16(from + DC * 2,
+                at_most((own0 & 15) + r) * ((DC + DR) * 2) + 16 * ((ln % S::RP) ^ tile_key<S::RP>(own0 + r)),
+                rope + (own0 + r0) * DR * 2);
+        }
+    };
+    const int most = it.last - base;                            // rows past the end repeat the last one
+    if (most >= 15)
+      rows([](int r) { return r; });
     else
-      vm_wait<S::LN>();
+      rows([most](int r) { return min(r, most); });
   };
-
-  while (t < end) {
+  for (int t = begin; t < end;) {
     const Item it = item_at(a, t);
     const int first = t - it.start, n = min(end - t, it.tiles - first);
-    // steps 0 .. n: scores of tile s beside the latents of tile s - 1; tile s + 2 is asked for
-    copy(it, first, 0, page_of(it, first));
-    if (n > 1) copy(it, first + 1, 1, page_of(it, first + 1));
-    int page = page_of(it, first + min(2, n - 1));
-    auto ahead = [&](int s) {
-      if (s + 2 < n) {
+    copy(it, first, 0, page_of(it, first, grp));
+    if (n > 1) copy(it, first + 1, 1, page_of(it, first + 1, grp));
+    int page = page_of(it, first + min(2, n - 1), grp);
+    f4 o[S::CT][MT] = {};
+    vm_drain();
+    lds_barrier();
+    // step s: the latents of tile s - 1, and tile s + 2 is asked for; step n has no scores beside it
+    for (int s = 0; s <= n; ++s) {
+      const bool more = s + 2 < n;
+      if (more) {
         copy(it, first + s + 2, (s + 2) & 3, page);
-        page = page_of(it, first + min(s + 3, n - 1));
+        page = page_of(it, first + min(s + 3, n - 1), grp);
       }
-    };
-    float mref = -INFINITY;                                     // the reference of row lane % M (unscaled)
-    // after step s: does a row's largest score pass its reference by too much?
-    auto passed = [&](int s, float& top) {
-      const float* p = smax + (s & 1) * 2 * S::M + lane % S::M;
-      top = fmaxf(p[0], p[S::M]);
-      return __any((top - mref) * unit > kSlack);
-    };
-    auto follow = [&](float top) {                              // the factor of what was summed so far
-      const float v = fmaxf(mref, top), mu = v == -INFINITY ? 0.f : v * unit;
-      const float keep = exp2_fast(fmaf(mref, unit, -mu));
-      mref = v;
-      return keep;
-    };
-    const size_t seg = (size_t)wg + it.index;
-    if (scores) {
-      h8 q[S::RT][S::KS];
+      if (s > 0) {
+        const char* buf = lds + ((s - 1) & 3) * S::BUF;
+        h8 p[MT];
 #pragma unroll
-      for (int r = 0; r < S::RT; ++r) {
-        const size_t row = it.row0 + min((wr * S::RT + r) * 16 + c, it.rows - 1);
+        for (int r = 0; r < MT; ++r)
+          p[r] = ld_h8(pt + ((s - 1) & 1) * S::PT + (16 * r + c) * 64 + 16 * (g ^ tile_key<4>(c)));
 #pragma unroll
-        for (int k = 0; k < S::KS; ++k) q[r][k] = ld_h8(a.ql + row * (DC + DR) + 32 * k + 8 * g);
-      }
-      float sum[S::RT], mu[S::RT];
+        for (int k = 0; k < S::CT; ++k) {
+          h4 part[2];
 #pragma unroll
-      for (int r = 0; r < S::RT; ++r) sum[r] = mu[r] = 0.f;
-      vm_drain();
-      lds_barrier();
-      for (int s = 0; s <= n; ++s) {
-        ahead(s);
-        if (s < n) {
-          const char* buf = lds + (s & 3) * S::BUF;
-          f4 x[S::RT] = {};
-          const int tok = wt * 16 + c;
-#pragma unroll
-          for (int k = 0; k < S::KS; ++k) {
-            const char* p = k < DC / 32
-                                ? buf + tok * DC * 2 + 256 * (k >> 2) + 16 * ((4 * (k & 3) + g) ^ tile_key<S::LP>(c))
-                                : buf + S::LAT + tok * DR * 2 + 16 * ((4 * (k - DC / 32) + g) ^ tile_key<S::RP>(c));
-            const h8 kk = ld_h8(p);
-#pragma unroll
-            for (int r = 0; r < S::RT; ++r) x[r] = mfma16(kk, q[r][k], x[r]);
+          for (int u = 0; u < 2; ++u) {
+            const int t0 = 4 * g + (c >> 2), col = 16 * (wo * S::CT + k) + 4 * (c & 3);
+            part[u] = ld_tr(buf + (16 * u + t0) * DC * 2 + 16 * ((col >> 3) ^ tile_key<S::LP>(t0)) + 2 * (col & 7));
           }
-          const int left = it.last - (it.tok0 + (first + s) * kStep + 16 * wt);  // tokens of the group, less one
-          if (bad[2 * (s & 3) + wt] || left < 15) {
-            const int most = bad[2 * (s & 3) + wt] ? -1 : left - 4 * g;
+          const h8 v = join(part[0], part[1]);
 #pragma unroll
-            for (int r = 0; r < S::RT; ++r)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (e > most) x[r][e] = -INFINITY;
-          }
-          // the weights, where the latents are read in the same order: of the tile's tokens,
-          // 16 u + 4 g .. + 3 at 8 g + 4 u
-          float add[S::RT];
-          auto weights = [&]() {
-#pragma unroll
-            for (int r = 0; r < S::RT; ++r) {
-              h4 p;
-              add[r] = 0.f;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float v = exp2_fast(fmaf(x[r][e], unit, -mu[r]));
-                add[r] += v;
-                p[e] = (_Float16)v;
-              }
-              *reinterpret_cast<h4*>(pt + (s & 1) * S::PT + ((wr * S::RT + r) * 16 + c) * 64 +
-                                     16 * (g ^ tile_key<4>(c)) + 8 * wt) = p;
-            }
-          };
-          weights();
-#pragma unroll
-          for (int r = 0; r < S::RT; ++r) {
-            const float v = col_max(fmaxf(fmaxf(x[r][0], x[r][1]), fmaxf(x[r][2], x[r][3])));
-            if (g == 0) smax[((s & 1) * 2 + wt) * S::M + (wr * S::RT + r) * 16 + c] = v;
-          }
-          landed(s + 2 >= n);
-          lds_barrier();
-          float top;
-          if (passed(s, top)) {
-            const float keep = follow(top), ref = mref == -INFINITY ? 0.f : mref * unit;
-#pragma unroll
-            for (int r = 0; r < S::RT; ++r) {
-              sum[r] *= __shfl(keep, (wr * S::RT + r) * 16 + c, kWave);
-              mu[r] = __shfl(ref, (wr * S::RT + r) * 16 + c, kWave);
-            }
-            weights();
-            lds_barrier();
-          }
-#pragma unroll
-          for (int r = 0; r < S::RT; ++r) sum[r] += add[r];
-        } else {
-          lds_barrier();
+          for (int r = 0; r < MT; ++r) o[k][r] = mfma16(v, p[r], o[k][r]);
         }
       }
-#pragma unroll
-      for (int r = 0; r < S::RT; ++r) {
-        const float v = col_sum(sum[r]);
-        if (g == 0) ssum[wt * S::M + (wr * S::RT + r) * 16 + c] = v;
-      }
+      if (s == n) break;
+      // tile s + 1 is there: all but this step's copies
+      if (!more)
+        vm_wait<0>();
+      else if (ropes)
+        vm_wait<S::LN + S::RN>();
+      else
+        vm_wait<S::LN>();
       lds_barrier();
-      if (wave == 0 && lane < S::M)
-        *reinterpret_cast<float2*>(a.part_ml + (seg * S::M + lane) * 2) =
-            float2{mref * unit, ssum[lane] + ssum[S::M + lane]};
-    } else {
-      f4 o[S::CT][MT] = {};
-      vm_drain();
-      lds_barrier();
-      for (int s = 0; s <= n; ++s) {
-        ahead(s);
-        if (s > 0) {
-          const char* buf = lds + ((s - 1) & 3) * S::BUF;
-          h8 p[MT];
-#pragma unroll
-          for (int r = 0; r < MT; ++r)
-            p[r] = ld_h8(pt + ((s - 1) & 1) * S::PT + (16 * r + c) * 64 + 16 * (g ^ tile_key<4>(c)));
-#pragma unroll
-          for (int k = 0; k < S::CT; ++k) {
-            h4 part[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const int t0 = 4 * g + (c >> 2), col = 16 * (wo * S::CT + k) + 4 * (c & 3);
-              part[u] = ld_tr(buf + (16 * u + t0) * DC * 2 + 16 * ((col >> 3) ^ tile_key<S::LP>(t0)) + 2 * (col & 7));
-            }
-            const h8 v = join(part[0], part[1]);
-#pragma unroll
-            for (int r = 0; r < MT; ++r) o[k][r] = mfma16(v, p[r], o[k][r]);
-          }
-        }
-        if (s < n) landed(s + 2 >= n);
+      if (__builtin_amdgcn_readfirstlane(passed[s & 1]) == t + s) {
         lds_barrier();
-        float top;
-        if (s < n && passed(s, top)) {
-          const float keep = follow(top);
+        lds_barrier();
 #pragma unroll
-          for (int r = 0; r < MT; ++r) {
-            const float kr = __shfl(keep, (16 * r + c) % S::M, kWave);
+        for (int r = 0; r < MT; ++r) {
+          const float keep = skeep[16 * r + c];
 #pragma unroll
-            for (int k = 0; k < S::CT; ++k) o[k][r] *= kr;
-          }
-          lds_barrier();
+          for (int k = 0; k < S::CT; ++k) o[k][r] *= keep;
         }
       }
-#pragma unroll
-      for (int r = 0; r < MT; ++r)
-#pragma unroll
-        for (int k = 0; k < S::CT; ++k)
-          *reinterpret_cast<f4*>(a.part_o + (seg * S::M + 16 * r + c) * DC + 16 * (wo * S::CT + k) + 4 * g) = o[k][r];
-      lds_barrier();
     }
+    const size_t seg = (size_t)wg + it.index;
+#pragma unroll
+    for (int r = 0; r < MT; ++r)
+#pragma unroll
+      for (int k = 0; k < S::CT; ++k)
+        *reinterpret_cast<f4*>(a.part_o + (seg * S::M + 16 * r + c) * DC + 16 * (wo * S::CT + k) + 4 * g) = o[k][r];
+    lds_barrier();
     t += n;
   }
 }

@@ -39,18 +39,16 @@ __device__ __forceinline__ h8 join(h4 a, h4 b) {
 
 // Each lane copies 16 bytes from its own global address to lds + 16 * lane (lds the
 // same for the wave). The compiler does not see it as a memory instruction: vm_wait
-// orders it, and every wave waits before the barrier behind which the data is read.
+// orders it, and every wave waits before the barrier behind which the data is read. (The
+// LDS address goes through m0, which nothing else in these kernels uses.)
 __device__ __forceinline__ void dma16(const void* g, const void* lds) {
-  uint32_t saved;
   const uint32_t to = __builtin_amdgcn_readfirstlane(
       (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)lds);
   asm volatile(
-      "s_mov_b32 %0, m0\n\t"
-      "s_mov_b32 m0, %1\n\t"
+      "s_mov_b32 m0, %0\n\t"
       "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %2, off\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(saved)
+      "global_load_lds_dwordx4 %1, off"
+      :
       : "s"(to), "v"(g)
       : "memory");
 }
@@ -60,16 +58,12 @@ __device__ __forceinline__ uint32_t lds_at(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
 }
 __device__ __forceinline__ void dma16(const void* base, uint32_t off, uint32_t to) {
-  uint32_t saved;
-  to = __builtin_amdgcn_readfirstlane(to);
   asm volatile(
-      "s_mov_b32 %0, m0\n\t"
-      "s_mov_b32 m0, %1\n\t"
+      "s_mov_b32 m0, %0\n\t"
       "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %2, %3\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(saved)
-      : "s"(to), "v"(off), "s"(base)
+      "global_load_lds_dwordx4 %1, %2"
+      :
+      : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(base)
       : "memory");
 }
 // An int that the whole wave reads and nothing writes while the kernel runs, through the
