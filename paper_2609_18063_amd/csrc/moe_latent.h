@@ -40,12 +40,13 @@ hipError_t launch_latent_append(const AppendArgs& a, hipStream_t st);
 // How a decode call is cut: rows of one workgroup, workgroups, and what the workspace
 // holds. The tiles of all items (the shared prefix's row blocks by token chunks, then
 // every sequence's head blocks) lie on one line that the workgroups share evenly; a
-// workgroup writes one partial result (m, l, O) per item that it touches.
+// workgroup writes one partial result per item that it has tiles of: O, and (m, l) from
+// either half of its tokens.
 struct DecodePlan {
   int rows;                      // query rows of an item: 16, 32 or 64
   int head_blocks;               // items of one sequence
   int chunks, row_blocks;        // prefix: token chunks x row blocks
-  int chunk_tiles, prefix_tiles;
+  int chunk_tiles, prefix_places;
   int wgs;
   size_t ql, lat, starts, part_o, part_ml, total;  // byte offsets in the workspace
 };
@@ -59,9 +60,9 @@ struct DecodeArgs {
   DecodePlan p;
   __half* ql;                    // [B * H][Dc + Dr]: q in latent space, and its rope part
   __half* lat;                   // [B * H][Dc]: softmax-weighted latents
-  int32_t* starts;               // [B + 1]: first tile of each sequence
+  int32_t* starts;               // [B + 1]: first place of each sequence
   float* part_o;                 // [wgs + items][rows][Dc]
-  float* part_ml;                // [wgs + items][rows][2]
+  float* part_ml;                // [wgs + items][2][rows][2]
 };
 hipError_t launch_latent_decode(const DecodeArgs& a, hipStream_t st);
 

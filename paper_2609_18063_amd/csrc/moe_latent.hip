@@ -19,6 +19,7 @@ namespace {
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr int kCus = 256;
 constexpr float kSlack = 8.f;    // (as a power of two)
+constexpr int kItemCost = 2;
 
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
 
@@ -78,17 +79,18 @@ __global__ void __launch_bounds__(256) latent_append_kernel(AppendArgs a) {
 }
 
 // ---- the decode call's plan -----------------------------------------------------
-__device__ __forceinline__ int own_len(const DecodeArgs& a, int b, bool report) {
+__device__ __forceinline__ int clamp_len(const DecodeArgs& a, int n) {
   const int64_t cap = (int64_t)a.l.max_pages * a.l.page;
-  const int most = (int)(cap < a.max_len ? cap : a.max_len), n = a.kv_len[b];
-  if (n >= 0 && n <= most) return n;
-  if (report && a.l.status) atomicOr(a.l.status, MOE_STATUS_BAD_LENGTH);
-  return n < 0 ? 0 : most;
+  return min(max(n, 0), (int)(cap < a.max_len ? cap : a.max_len));
 }
 __device__ __forceinline__ int tiles_of(int len) { return (len + kStep - 1) / kStep; }
 
+// An item takes its tiles and kItemCost places more on the line (nothing without tiles):
+// what its query's loads and its partial result cost a workgroup, in tiles.
+__device__ __forceinline__ int places(int tiles) { return tiles > 0 ? tiles + kItemCost : 0; }
+
 struct Item {
-  int index, start, tiles;  // order number, first tile on the line, tiles
+  int index, start, tiles;  // order number, first place on the line, tiles
   int row0, rows;           // query rows
   int tok0, last;           // first token, last token that may be read
   const int32_t* pages;
@@ -99,7 +101,7 @@ __device__ __forceinline__ Item prefix_item(const DecodeArgs& a, int chunk, int 
   const int all = tiles_of(a.prefix_len), first = chunk * a.p.chunk_tiles;
   it.index = chunk * a.p.row_blocks + rb;
   it.tiles = min(a.p.chunk_tiles, all - first);
-  it.start = first * a.p.row_blocks + rb * it.tiles;
+  it.start = chunk * a.p.row_blocks * places(a.p.chunk_tiles) + rb * places(it.tiles);
   it.row0 = rb * a.p.rows;
   it.rows = min(a.p.rows, a.B * a.l.H - it.row0);
   it.tok0 = first * kStep;
@@ -107,38 +109,60 @@ __device__ __forceinline__ Item prefix_item(const DecodeArgs& a, int chunk, int 
   it.pages = a.prefix;
   return it;
 }
-__device__ __forceinline__ Item own_item(const DecodeArgs& a, int b, int hb, int start, int tiles) {
+__device__ __forceinline__ Item own_item(const DecodeArgs& a, int b, int hb, int start, int len) {
   Item it;
   it.index = a.p.chunks * a.p.row_blocks + b * a.p.head_blocks + hb;
-  it.tiles = tiles;
-  it.start = start + hb * tiles;
+  it.tiles = tiles_of(len);
+  it.start = start + hb * places(it.tiles);
   it.row0 = b * a.l.H + hb * a.p.rows;
   it.rows = min(a.p.rows, a.l.H - hb * a.p.rows);
   it.tok0 = 0;
-  it.last = own_len(a, b, false) - 1;
+  it.last = len - 1;
   it.pages = a.l.table + b * a.l.table_stride;
   return it;
 }
-// the item that tile t of the line belongs to
-__device__ __forceinline__ Item item_at(const DecodeArgs& a, int t) {
-  if (t < a.p.prefix_tiles) {
-    const int chunk = t / (a.p.chunk_tiles * a.p.row_blocks);
+// the item that place t of the line belongs to; b: the sequence looked at last
+__device__ __forceinline__ Item item_at(const DecodeArgs& a, int t, int& b) {
+  if (t < a.p.prefix_places) {
+    const int chunk = t / (a.p.row_blocks * places(a.p.chunk_tiles));
     const Item first = prefix_item(a, chunk, 0);
-    return prefix_item(a, chunk, (t - first.start) / first.tiles);
+    return prefix_item(a, chunk, (t - first.start) / places(first.tiles));
   }
-  int lo = 0, hi = a.B;                                  // starts[lo] <= t < starts[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (a.starts[mid] <= t)
-      lo = mid;
-    else
-      hi = mid;
+  // starts[b] <= t < starts[b + 1] (sequences without a tile share their start with the
+  // next one: the last of equals is the one that has the tile)
+  if (!(ld_scalar(a.starts + b) <= t && t < ld_scalar(a.starts + b + 1))) {
+    int lo = 0, hi = a.B;
+    if (b + 1 < a.B && ld_scalar(a.starts + b + 1) <= t && t < ld_scalar(a.starts + b + 2)) lo = b + 1, hi = b + 2;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (ld_scalar(a.starts + mid) <= t)
+        lo = mid;
+      else
+        hi = mid;
+    }
+    b = lo;
   }
-  // (sequences without a tile share their start with the next one: the last of equals
-  // is the one that has the tile)
-  const int tiles = (a.starts[lo + 1] - a.starts[lo]) / a.p.head_blocks;
-  return own_item(a, lo, (t - a.starts[lo]) / tiles, a.starts[lo], tiles);
+  const int start = ld_scalar(a.starts + b), len = clamp_len(a, ld_scalar(a.kv_len + b));
+  return own_item(a, b, (t - start) / places(tiles_of(len)), start, len);
 }
+// A workgroup's tiles of one item after the other: [begin, end) of the line.
+struct Walk {
+  Item it;
+  int first, n;             // its tiles of the item
+  int t, end, b;
+  __device__ __forceinline__ bool next(const DecodeArgs& a) {
+    while (t < end) {
+      it = item_at(a, t, b);
+      const int begin = it.start + kItemCost, to = min(end, begin + it.tiles);
+      first = max(t - begin, 0);
+      n = to - begin - first;
+      t = max(to, t + 1);
+      if (to < end) t = begin + it.tiles;
+      if (n > 0) return true;
+    }
+    return false;
+  }
+};
 
 // ---- q into the latent space ------------------------------------------------------
 // qt_h = W_uk,h^T q_n,h for 64 latent columns of one head and 64 sequences a workgroup;
@@ -153,10 +177,15 @@ __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
   const int h = blockIdx.y, b0 = blockIdx.z * 64, b1 = min(b0 + 64, a.B);
   if ((int)blockIdx.x == l.Dc / 64) {
     if (blockIdx.y || blockIdx.z) return;
-    int base = a.p.prefix_tiles;
+    int base = a.p.prefix_places;
     for (int c0 = 0; c0 < a.B; c0 += 256) {
       const int b = c0 + threadIdx.x;
-      const int n = b < a.B ? tiles_of(own_len(a, b, true)) * a.p.head_blocks : 0;
+      int n = 0;
+      if (b < a.B) {
+        const int len = clamp_len(a, a.kv_len[b]);
+        if (len != a.kv_len[b] && l.status) atomicOr(l.status, MOE_STATUS_BAD_LENGTH);
+        n = places(tiles_of(len)) * a.p.head_blocks;
+      }
       scan[threadIdx.x] = n;
       __syncthreads();
       for (int o = 1; o < 256; o <<= 1) {
@@ -233,7 +262,7 @@ struct DecodeShape {
   static constexpr int KS = (DC + DR) / 32, CT = DC / (16 * NS);
   static constexpr int LAT = kStep * DC * 2, BUF = LAT + kStep * DR * 2;
   static constexpr int PT = M * 64;                            // the weights of a tile
-  static constexpr int LDS = 4 * BUF + 2 * PT + 4 * M * 4 + 32;
+  static constexpr int LDS = 4 * BUF + 2 * PT + 3 * M * 4 + 32;
   // copies of a tile by one wave: latent rows LR at a time, rotated keys RR at a time
   static constexpr int LP = DC / 8, LR = kWave / LP, RP = DR / 8, RR = kWave / RP;
   static constexpr int LN = OWN / LR, RN = RR <= OWN ? OWN / RR : 1;
@@ -247,16 +276,18 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
   char* pt = lds + 4 * S::BUF;                                  // weights [2][M][32] halves
   float* smax = reinterpret_cast<float*>(pt + 2 * S::PT);       // [2][M], by token half
   float* skeep = smax + 2 * S::M;                               // [M]
-  float* ssum = skeep + S::M;                                   // [M]
-  int* passed = reinterpret_cast<int*>(ssum + S::M);            // [2]: the last step with a row past its reference
+  int* passed = reinterpret_cast<int*>(skeep + S::M);           // [2]: the last step with a row past its reference
   const LatentArgs& l = a.l;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int c = lane & 15, g = lane >> 4;
   const int wt = wave % 2, wr = wave / 2, wo = wave - S::NS;    // token half, row block; share of the columns
   // neighbours on the line share a chiplet and its L2
   const int wg = (blockIdx.x % 8) * (a.p.wgs / 8) + blockIdx.x / 8;
-  const int all = a.starts[a.B], per = (all + a.p.wgs - 1) / a.p.wgs;
-  const int begin = wg * per, end = min(all, begin + per);
+  const int all = ld_scalar(a.starts + a.B), per = (all + a.p.wgs - 1) / a.p.wgs;
+  Walk at;
+  at.t = min(all, wg * per);
+  at.end = min(all, at.t + per);
+  at.b = 0;
   const float unit = l.scale * kLog2e;
   const int shift = 31 - __clz(l.page);
   // 16-token group `grp` (0 or 1) of a tile, from its first token (past the end: the last group)
@@ -267,9 +298,11 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
 
   if (wave < S::NS) {
     __builtin_amdgcn_s_setprio(2);
-    for (int t = begin; t < end;) {
-      const Item it = item_at(a, t);
-      const int first = t - it.start, n = min(end - t, it.tiles - first);
+    lds_barrier();
+    int u = 0;                                                  // steps of this workgroup
+    while (at.next(a)) {
+      const Item& it = at.it;
+      const int first = at.first, n = at.n;
       h8 q[S::RT][S::KS];
 #pragma unroll
       for (int r = 0; r < S::RT; ++r) {
@@ -285,9 +318,8 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
       }
       int page = page_of(it, first, wt);
       vm_drain();
-      lds_barrier();
-      for (int s = 0; s < n; ++s) {
-        const char* buf = lds + (s & 3) * S::BUF;
+      for (int s = 0; s < n; ++s, ++u) {
+        const char* buf = lds + (u & 3) * S::BUF;
         f4 x[S::RT] = {};
         const int tok = wt * 16 + c;
 #pragma unroll
@@ -324,7 +356,7 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
               add[r] += v;
               p[e] = (_Float16)v;
             }
-            *reinterpret_cast<h4*>(pt + (s & 1) * S::PT + ((wr * S::RT + r) * 16 + c) * 64 + 16 * (g ^ tile_key<4>(c)) +
+            *reinterpret_cast<h4*>(pt + (u & 1) * S::PT + ((wr * S::RT + r) * 16 + c) * 64 + 16 * (g ^ tile_key<4>(c)) +
                                    8 * wt) = p;
           }
         };
@@ -336,9 +368,9 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
           top[r] = fmaxf(fmaxf(x[r][0], x[r][1]), fmaxf(x[r][2], x[r][3]));
           far = far || (top[r] - m[r]) * unit > kSlack;         // (no token so far: any score is)
         }
-        if (__any(far) && lane == 0) passed[s & 1] = t + s;
+        if (__any(far) && lane == 0) passed[u & 1] = u;
         lds_barrier();
-        if (__builtin_amdgcn_readfirstlane(passed[s & 1]) == t + s) {
+        if (__builtin_amdgcn_readfirstlane(passed[u & 1]) == u) {
           // every row takes its largest score as its reference
 #pragma unroll
           for (int r = 0; r < S::RT; ++r) {
@@ -367,16 +399,10 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
 #pragma unroll
       for (int r = 0; r < S::RT; ++r) {
         sum[r] = col_sum(sum[r]);
-        if (g == 0 && wt == 1) ssum[(wr * S::RT + r) * 16 + c] = sum[r];
+        if (g == 0)
+          *reinterpret_cast<float2*>(a.part_ml + ((seg * 2 + wt) * S::M + (wr * S::RT + r) * 16 + c) * 2) =
+              float2{m[r] * unit, sum[r]};
       }
-      lds_barrier();
-      if (g == 0 && wt == 0)
-#pragma unroll
-        for (int r = 0; r < S::RT; ++r) {
-          const int row = (wr * S::RT + r) * 16 + c;
-          *reinterpret_cast<float2*>(a.part_ml + (seg * S::M + row) * 2) = float2{m[r] * unit, sum[r] + ssum[row]};
-        }
-      t += n;
     }
     return;
   }
@@ -425,69 +451,91 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
     else
       rows([most](int r) { return min(r, most); });
   };
-  for (int t = begin; t < end;) {
-    const Item it = item_at(a, t);
-    const int first = t - it.start, n = min(end - t, it.tiles - first);
-    copy(it, first, 0, page_of(it, first, grp));
-    if (n > 1) copy(it, first + 1, 1, page_of(it, first + 1, grp));
-    int page = page_of(it, first + min(2, n - 1), grp);
-    f4 o[S::CT][MT] = {};
-    vm_drain();
-    lds_barrier();
-    // step s: the latents of tile s - 1, and tile s + 2 is asked for; step n has no scores beside it
-    for (int s = 0; s <= n; ++s) {
-      const bool more = s + 2 < n;
-      if (more) {
-        copy(it, first + s + 2, (s + 2) & 3, page);
-        page = page_of(it, first + min(s + 3, n - 1), grp);
+  // the tiles asked for so far, and the next one
+  Walk ask = at;
+  int asked = 0, k = 0;
+  bool more = ask.next(a);
+  int page = more ? page_of(ask.it, ask.first, grp) : 0;
+  auto ask_next = [&]() {
+    if (!more) return false;
+    copy(ask.it, ask.first + k, asked & 3, page);
+    ++asked;
+    if (++k == ask.n) {
+      k = 0;
+      more = ask.next(a);
+    }
+    if (more) page = page_of(ask.it, ask.first + k, grp);
+    return true;
+  };
+  ask_next();
+  ask_next();
+  f4 o[S::CT][MT] = {};
+  vm_drain();
+  lds_barrier();
+  int left = 0;                                                 // tiles of the item that are not added up yet
+  // step u: the latents of tile u - 1, and tile u + 2 is asked for; the last step has no scores beside it
+  for (int u = 0;; ++u) {
+    const bool newer = ask_next();
+    bool stored = false;
+    if (u > 0) {
+      if (left == 0) {
+        at.next(a);
+        left = at.n;
       }
-      if (s > 0) {
-        const char* buf = lds + ((s - 1) & 3) * S::BUF;
-        h8 p[MT];
+      const char* buf = lds + ((u - 1) & 3) * S::BUF;
+      h8 p[MT];
+#pragma unroll
+      for (int r = 0; r < MT; ++r)
+        p[r] = ld_h8(pt + ((u - 1) & 1) * S::PT + (16 * r + c) * 64 + 16 * (g ^ tile_key<4>(c)));
+#pragma unroll
+      for (int k = 0; k < S::CT; ++k) {
+        h4 part[2];
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const int t0 = 4 * g + (c >> 2), col = 16 * (wo * S::CT + k) + 4 * (c & 3);
+          part[v] = ld_tr(buf + (16 * v + t0) * DC * 2 + 16 * ((col >> 3) ^ tile_key<S::LP>(t0)) + 2 * (col & 7));
+        }
+        const h8 v = join(part[0], part[1]);
+#pragma unroll
+        for (int r = 0; r < MT; ++r) o[k][r] = mfma16(v, p[r], o[k][r]);
+      }
+      if (--left == 0) {
+        const size_t seg = (size_t)wg + at.it.index;
 #pragma unroll
         for (int r = 0; r < MT; ++r)
-          p[r] = ld_h8(pt + ((s - 1) & 1) * S::PT + (16 * r + c) * 64 + 16 * (g ^ tile_key<4>(c)));
 #pragma unroll
-        for (int k = 0; k < S::CT; ++k) {
-          h4 part[2];
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const int t0 = 4 * g + (c >> 2), col = 16 * (wo * S::CT + k) + 4 * (c & 3);
-            part[u] = ld_tr(buf + (16 * u + t0) * DC * 2 + 16 * ((col >> 3) ^ tile_key<S::LP>(t0)) + 2 * (col & 7));
+          for (int k = 0; k < S::CT; ++k) {
+            *reinterpret_cast<f4*>(a.part_o + (seg * S::M + 16 * r + c) * DC + 16 * (wo * S::CT + k) + 4 * g) = o[k][r];
+            o[k][r] = f4{};
           }
-          const h8 v = join(part[0], part[1]);
-#pragma unroll
-          for (int r = 0; r < MT; ++r) o[k][r] = mfma16(v, p[r], o[k][r]);
-        }
-      }
-      if (s == n) break;
-      // tile s + 1 is there: all but this step's copies
-      if (!more)
-        vm_wait<0>();
-      else if (ropes)
-        vm_wait<S::LN + S::RN>();
-      else
-        vm_wait<S::LN>();
-      lds_barrier();
-      if (__builtin_amdgcn_readfirstlane(passed[s & 1]) == t + s) {
-        lds_barrier();
-        lds_barrier();
-#pragma unroll
-        for (int r = 0; r < MT; ++r) {
-          const float keep = skeep[16 * r + c];
-#pragma unroll
-          for (int k = 0; k < S::CT; ++k) o[k][r] *= keep;
-        }
+        stored = true;
       }
     }
-    const size_t seg = (size_t)wg + it.index;
-#pragma unroll
-    for (int r = 0; r < MT; ++r)
-#pragma unroll
-      for (int k = 0; k < S::CT; ++k)
-        *reinterpret_cast<f4*>(a.part_o + (seg * S::M + 16 * r + c) * DC + 16 * (wo * S::CT + k) + 4 * g) = o[k][r];
+    if (u >= asked) break;
+    // tile u + 1 is there: all but this step's copies and, behind them, the stores (16 bytes
+    // a lane each: no fewer than these)
+    constexpr int ST = S::CT * MT;
+    if (!newer)
+      vm_wait<0>();
+    else if (ropes && stored)
+      vm_wait<S::LN + S::RN + ST>();
+    else if (ropes)
+      vm_wait<S::LN + S::RN>();
+    else if (stored)
+      vm_wait<S::LN + ST>();
+    else
+      vm_wait<S::LN>();
     lds_barrier();
-    t += n;
+    if (__builtin_amdgcn_readfirstlane(passed[u & 1]) == u) {
+      lds_barrier();
+      lds_barrier();
+#pragma unroll
+      for (int r = 0; r < MT; ++r) {
+        const float keep = skeep[16 * r + c];
+#pragma unroll
+        for (int k = 0; k < S::CT; ++k) o[k][r] *= keep;
+      }
+    }
   }
 }
 
@@ -504,21 +552,22 @@ __global__ void __launch_bounds__(128) latent_join_kernel(DecodeArgs a) {
   f4 o = {};
   auto add = [&](const Item& it, int r) {
     if (it.tiles <= 0) return;
-    const int w0 = it.start / per, w1 = (it.start + it.tiles - 1) / per;
+    const int from = it.start + kItemCost, w0 = from / per, w1 = (from + it.tiles - 1) / per;
     for (int w = w0; w <= w1; ++w) {
       const size_t seg = (size_t)w + it.index;
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (seg * M + r) * 2);
-      if (ml.x == -INFINITY) continue;                       // (every token of it was lost)
+      const float2 a0 = *reinterpret_cast<const float2*>(a.part_ml + (seg * 2 * M + r) * 2);
+      const float2 a1 = *reinterpret_cast<const float2*>(a.part_ml + ((seg * 2 + 1) * M + r) * 2);
+      if (a0.x == -INFINITY) continue;                       // (every token of it was lost)
       f4 v = {};
       if (col < l.Dc) v = *reinterpret_cast<const f4*>(a.part_o + (seg * M + r) * l.Dc + col);
-      const float m = fmaxf(top, ml.x), x = exp2_fast(top - m), y = exp2_fast(ml.x - m);
+      const float m = fmaxf(top, a0.x), x = exp2_fast(top - m), y = exp2_fast(a0.x - m);
       o = o * x + v * y;
-      sum = sum * x + ml.y * y;
+      sum = sum * x + (a0.y + a1.y) * y;
       top = m;
     }
   };
   for (int k = 0; k < a.p.chunks; ++k) add(prefix_item(a, k, row / M), row % M);
-  add(own_item(a, b, h / M, a.starts[b], (a.starts[b + 1] - a.starts[b]) / a.p.head_blocks), h % M);
+  add(own_item(a, b, h / M, a.starts[b], clamp_len(a, a.kv_len[b])), h % M);
   if (col < l.Dc) {
     const float inv = sum > 0.f ? 1.f / sum : sum != sum ? sum : 0.f;
     const h4 v = {(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
@@ -593,8 +642,8 @@ DecodePlan decode_plan(int H, int Dc, int Dr, int B, int max_len, int prefix_len
   p.chunks = prefix_len > 0 ? (p.row_blocks >= 8 ? std::min(8, pt) : 1) : 0;
   p.chunk_tiles = p.chunks ? (pt + p.chunks - 1) / p.chunks : 0;
   if (p.chunk_tiles) p.chunks = (pt + p.chunk_tiles - 1) / p.chunk_tiles;
-  p.prefix_tiles = pt * p.row_blocks;
-  const long long tiles = p.prefix_tiles + (long long)B * p.head_blocks * tiles_host(max_len);
+  p.prefix_places = (pt + p.chunks * kItemCost) * p.row_blocks;
+  const long long tiles = (long long)pt * p.row_blocks + (long long)B * p.head_blocks * tiles_host(max_len);
   const int wgs = kCus * (Dc <= 128 ? 3 : Dc <= 256 ? 2 : 1);
   p.wgs = (int)std::min<long long>(wgs, (std::max<long long>(tiles, 1) + 7) / 8 * 8);
   const size_t rows = (size_t)B * H, parts = (size_t)p.wgs + (size_t)p.chunks * p.row_blocks + (size_t)B * p.head_blocks;
@@ -608,7 +657,7 @@ DecodePlan decode_plan(int H, int Dc, int Dr, int B, int max_len, int prefix_len
   p.lat = take(rows * Dc * 2);
   p.starts = take(((size_t)B + 1) * 4);
   p.part_o = take(parts * p.rows * Dc * 4);
-  p.part_ml = take(parts * p.rows * 8);
+  p.part_ml = take(parts * p.rows * 16);
   p.total = off;
   return p;
 }
@@ -690,7 +739,7 @@ bool decode_shape_ok(const moe_latent_spec* s, int B, int max_len, int prefix_le
     return false;
   // tiles on the plan's line, with their row blocks (16 query rows and 32 tokens the smallest)
   const int64_t rows = ((int64_t)B * s->heads + 15) / 16 + B;
-  return rows * (((int64_t)max_len + prefix_len + 31) / 32 + 1) < (int64_t(1) << 30);
+  return rows * (((int64_t)max_len + prefix_len + 31) / 32 + 32) < (int64_t(1) << 30);
 }
 
 }  // namespace
