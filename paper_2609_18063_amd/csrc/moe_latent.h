@@ -47,7 +47,7 @@ struct DecodePlan {
   int head_blocks;               // items of one sequence
   int chunks, row_blocks;        // prefix: token chunks x row blocks
   int chunk_tiles, prefix_places;
-  int wgs;
+  int wgs, least;                // workgroups, and the least share of the line of one
   size_t ql, lat, starts, part_o, part_ml, total;  // byte offsets in the workspace
 };
 DecodePlan decode_plan(int H, int Dc, int Dr, int B, int max_len, int prefix_len);

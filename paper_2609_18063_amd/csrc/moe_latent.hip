@@ -19,7 +19,8 @@ namespace {
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr int kCus = 256;
 constexpr float kSlack = 8.f;    // (as a power of two)
-constexpr int kItemCost = 2;
+constexpr int kItemCost = 8;     // (measured: an item costs a workgroup 4 to 9 us, a tile 1 to 1.4)
+constexpr int kChunks = 15;
 
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
 
@@ -89,6 +90,11 @@ __device__ __forceinline__ int tiles_of(int len) { return (len + kStep - 1) / kS
 // what its query's loads and its partial result cost a workgroup, in tiles.
 __device__ __forceinline__ int places(int tiles) { return tiles > 0 ? tiles + kItemCost : 0; }
 
+// Places of the line that a workgroup takes.
+__device__ __forceinline__ int share(const DecodeArgs& a) {
+  return max(a.p.least, (ld_scalar(a.starts + a.B) + a.p.wgs - 1) / a.p.wgs);
+}
+
 struct Item {
   int index, start, tiles;  // order number, first place on the line, tiles
   int row0, rows;           // query rows
@@ -121,46 +127,67 @@ __device__ __forceinline__ Item own_item(const DecodeArgs& a, int b, int hb, int
   it.pages = a.l.table + b * a.l.table_stride;
   return it;
 }
-// the item that place t of the line belongs to; b: the sequence looked at last
-__device__ __forceinline__ Item item_at(const DecodeArgs& a, int t, int& b) {
-  if (t < a.p.prefix_places) {
-    const int chunk = t / (a.p.row_blocks * places(a.p.chunk_tiles));
-    const Item first = prefix_item(a, chunk, 0);
-    return prefix_item(a, chunk, (t - first.start) / places(first.tiles));
-  }
-  // starts[b] <= t < starts[b + 1] (sequences without a tile share their start with the
-  // next one: the last of equals is the one that has the tile)
-  if (!(ld_scalar(a.starts + b) <= t && t < ld_scalar(a.starts + b + 1))) {
-    int lo = 0, hi = a.B;
-    if (b + 1 < a.B && ld_scalar(a.starts + b + 1) <= t && t < ld_scalar(a.starts + b + 2)) lo = b + 1, hi = b + 2;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (ld_scalar(a.starts + mid) <= t)
-        lo = mid;
-      else
-        hi = mid;
-    }
-    b = lo;
-  }
-  const int start = ld_scalar(a.starts + b), len = clamp_len(a, ld_scalar(a.kv_len + b));
-  return own_item(a, b, (t - start) / places(tiles_of(len)), start, len);
-}
-// A workgroup's tiles of one item after the other: [begin, end) of the line.
+// A workgroup's tiles of one item after the other: [t, end) of the line. What the next
+// sequence's item needs is read while the one at hand is worked on.
 struct Walk {
   Item it;
   int first, n;             // its tiles of the item
-  int t, end, b;
+  int t, end;
+  int b, s0, s1, s2;        // the sequence at hand, its start, and the next two
+  int len0, len1;
+  __device__ __forceinline__ void begin(const DecodeArgs& a, int wg) {
+    const int all = ld_scalar(a.starts + a.B), per = share(a);
+    t = (int)min((int64_t)all, (int64_t)wg * per);
+    end = min(all, t + per);
+    b = -1;
+    s1 = s2 = 0;
+  }
   __device__ __forceinline__ bool next(const DecodeArgs& a) {
     while (t < end) {
-      it = item_at(a, t, b);
-      const int begin = it.start + kItemCost, to = min(end, begin + it.tiles);
-      first = max(t - begin, 0);
-      n = to - begin - first;
-      t = max(to, t + 1);
-      if (to < end) t = begin + it.tiles;
+      if (t < a.p.prefix_places) {
+        const int chunk = t / (a.p.row_blocks * places(a.p.chunk_tiles));
+        const Item one = prefix_item(a, chunk, 0);
+        it = prefix_item(a, chunk, (t - one.start) / places(one.tiles));
+      } else {
+        sequence_at(a);
+        it = own_item(a, b, (t - s0) / places(tiles_of(len0)), s0, len0);
+      }
+      const int from = it.start + kItemCost, to = min(end, from + it.tiles);
+      first = max(t - from, 0);
+      n = to - from - first;
+      t = to < end ? from + it.tiles : end;
       if (n > 0) return true;
     }
     return false;
+  }
+
+ private:
+  // the sequence with starts[b] <= t < starts[b + 1] (sequences without a tile share their
+  // start with the next one: the last of equals is the one that has the tile)
+  __device__ __forceinline__ void sequence_at(const DecodeArgs& a) {
+    if (t < s1) return;
+    if (t < s2) {
+      ++b;
+      s0 = s1;
+      s1 = s2;
+      len0 = len1;
+    } else {
+      // 64 starts at a time, each lane one
+      int lo = 0, count = a.B;
+      while (count > 1) {
+        const int step = (count + kWave - 1) / kWave, i = lo + (int)(threadIdx.x & 63) * step;
+        const bool below = i < lo + count && a.starts[min(i, a.B)] <= t;
+        const int k = __popcll(__ballot(below)) - 1;
+        count = min(step, lo + count - (lo + k * step));
+        lo += k * step;
+      }
+      b = lo;
+      s0 = ld_scalar(a.starts + b);
+      s1 = ld_scalar(a.starts + b + 1);
+      len0 = clamp_len(a, ld_scalar(a.kv_len + b));
+    }
+    s2 = ld_scalar(a.starts + min(b + 2, a.B));
+    len1 = clamp_len(a, ld_scalar(a.kv_len + min(b + 1, a.B - 1)));
   }
 };
 
@@ -283,11 +310,8 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
   const int wt = wave % 2, wr = wave / 2, wo = wave - S::NS;    // token half, row block; share of the columns
   // neighbours on the line share a chiplet and its L2
   const int wg = (blockIdx.x % 8) * (a.p.wgs / 8) + blockIdx.x / 8;
-  const int all = ld_scalar(a.starts + a.B), per = (all + a.p.wgs - 1) / a.p.wgs;
   Walk at;
-  at.t = min(all, wg * per);
-  at.end = min(all, at.t + per);
-  at.b = 0;
+  at.begin(a, wg);
   const float unit = l.scale * kLog2e;
   const int shift = 31 - __clz(l.page);
   // 16-token group `grp` (0 or 1) of a tile, from its first token (past the end: the last group)
@@ -298,110 +322,126 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
 
   if (wave < S::NS) {
     __builtin_amdgcn_s_setprio(2);
-    lds_barrier();
-    int u = 0;                                                  // steps of this workgroup
-    while (at.next(a)) {
-      const Item& it = at.it;
-      const int first = at.first, n = at.n;
-      h8 q[S::RT][S::KS];
+    bool more = at.next(a);
+    h8 q[S::RT][S::KS];
+    auto queries = [&]() {
 #pragma unroll
       for (int r = 0; r < S::RT; ++r) {
-        const size_t row = it.row0 + min((wr * S::RT + r) * 16 + c, it.rows - 1);
+        const size_t row = at.it.row0 + min((wr * S::RT + r) * 16 + c, at.it.rows - 1);
 #pragma unroll
         for (int k = 0; k < S::KS; ++k) q[r][k] = ld_h8(a.ql + row * (DC + DR) + 32 * k + 8 * g);
       }
-      float sum[S::RT], m[S::RT], ref[S::RT];                   // m: the reference, unscaled; ref: m unit, or 0
+    };
+    float sum[S::RT], m[S::RT], ref[S::RT];                     // m: the reference, unscaled; ref: m unit, or 0
+    auto start = [&]() {
 #pragma unroll
       for (int r = 0; r < S::RT; ++r) {
         m[r] = -INFINITY;
         sum[r] = ref[r] = 0.f;
       }
-      int page = page_of(it, first, wt);
-      vm_drain();
-      for (int s = 0; s < n; ++s, ++u) {
-        const char* buf = lds + (u & 3) * S::BUF;
-        f4 x[S::RT] = {};
-        const int tok = wt * 16 + c;
+    };
+    int page = 0;
+    if (more) {
+      queries();
+      page = page_of(at.it, at.first, wt);
+    }
+    start();
+    vm_drain();
+    lds_barrier();
+    // step u: the scores of tile u, the k-th of its item
+    for (int u = 0, k = 0; more; ++u) {
+      const char* buf = lds + (u & 3) * S::BUF;
+      f4 x[S::RT] = {};
+      const int tok = wt * 16 + c;
 #pragma unroll
-        for (int k = 0; k < S::KS; ++k) {
-          const char* p = k < DC / 32
-                              ? buf + tok * DC * 2 + 256 * (k >> 2) + 16 * ((4 * (k & 3) + g) ^ tile_key<S::LP>(c))
-                              : buf + S::LAT + tok * DR * 2 + 16 * ((4 * (k - DC / 32) + g) ^ tile_key<S::RP>(c));
-          const h8 kk = ld_h8(p);
+      for (int k = 0; k < S::KS; ++k) {
+        const char* p = k < DC / 32
+                            ? buf + tok * DC * 2 + 256 * (k >> 2) + 16 * ((4 * (k & 3) + g) ^ tile_key<S::LP>(c))
+                            : buf + S::LAT + tok * DR * 2 + 16 * ((4 * (k - DC / 32) + g) ^ tile_key<S::RP>(c));
+        const h8 kk = ld_h8(p);
 #pragma unroll
-          for (int r = 0; r < S::RT; ++r) x[r] = mfma16(kk, q[r][k], x[r]);
-        }
-        const bool lost = !known(page);
-        page = page_of(it, first + min(s + 1, n - 1), wt);
-        const int left = it.last - (it.tok0 + (first + s) * kStep + 16 * wt);  // tokens of the group, less one
-        if (lost || left < 15) {
-          const int most = lost ? -1 : left - 4 * g;
+        for (int r = 0; r < S::RT; ++r) x[r] = mfma16(kk, q[r][k], x[r]);
+      }
+      const bool lost = !known(page);
+      const int left = at.it.last - (at.it.tok0 + (at.first + k) * kStep + 16 * wt);  // tokens of the group, less one
+      const size_t seg = (size_t)wg + at.it.index;
+      // (the next item's query is asked for while this step's weights are formed)
+      const bool ends = ++k == at.n;
+      if (ends) {
+        k = 0;
+        more = at.next(a);
+        if (more) queries();
+      }
+      if (more) page = page_of(at.it, at.first + k, wt);
+      if (lost || left < 15) {
+        const int most = lost ? -1 : left - 4 * g;
 #pragma unroll
-          for (int r = 0; r < S::RT; ++r)
+        for (int r = 0; r < S::RT; ++r)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (e > most) x[r][e] = -INFINITY;
-        }
-        // the weights, where the latents are read in the same order: of the tile's tokens,
-        // 16 u + 4 g .. + 3 at 8 g + 4 u
-        float add[S::RT];
-        auto weights = [&]() {
-#pragma unroll
-          for (int r = 0; r < S::RT; ++r) {
-            h4 p;
-            add[r] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float v = exp2_fast(fmaf(x[r][e], unit, -ref[r]));
-              add[r] += v;
-              p[e] = (_Float16)v;
-            }
-            *reinterpret_cast<h4*>(pt + (u & 1) * S::PT + ((wr * S::RT + r) * 16 + c) * 64 + 16 * (g ^ tile_key<4>(c)) +
-                                   8 * wt) = p;
-          }
-        };
-        weights();
-        bool far = false;
-        float top[S::RT];
+          for (int e = 0; e < 4; ++e)
+            if (e > most) x[r][e] = -INFINITY;
+      }
+      // the weights, where the latents are read in the same order: of the tile's tokens,
+      // 16 v + 4 g .. + 3 at 8 g + 4 v
+      float add[S::RT];
+      auto weights = [&]() {
 #pragma unroll
         for (int r = 0; r < S::RT; ++r) {
-          top[r] = fmaxf(fmaxf(x[r][0], x[r][1]), fmaxf(x[r][2], x[r][3]));
-          far = far || (top[r] - m[r]) * unit > kSlack;         // (no token so far: any score is)
-        }
-        if (__any(far) && lane == 0) passed[u & 1] = u;
-        lds_barrier();
-        if (__builtin_amdgcn_readfirstlane(passed[u & 1]) == u) {
-          // every row takes its largest score as its reference
+          h4 p;
+          add[r] = 0.f;
 #pragma unroll
-          for (int r = 0; r < S::RT; ++r) {
-            top[r] = col_max(top[r]);
-            if (g == 0) smax[wt * S::M + (wr * S::RT + r) * 16 + c] = top[r];
+          for (int e = 0; e < 4; ++e) {
+            const float v = exp2_fast(fmaf(x[r][e], unit, -ref[r]));
+            add[r] += v;
+            p[e] = (_Float16)v;
           }
-          lds_barrier();
-#pragma unroll
-          for (int r = 0; r < S::RT; ++r) {
-            const int row = (wr * S::RT + r) * 16 + c;
-            const float most = max3(m[r], top[r], smax[(1 - wt) * S::M + row]);
-            const float now = most == -INFINITY ? 0.f : most * unit;
-            const float keep = m[r] == -INFINITY ? 0.f : exp2_fast(ref[r] - now);
-            m[r] = most;
-            sum[r] *= keep;
-            ref[r] = now;
-            if (g == 0 && wt == 0) skeep[row] = keep;
-          }
-          weights();
-          lds_barrier();
+          *reinterpret_cast<h4*>(pt + (u & 1) * S::PT + ((wr * S::RT + r) * 16 + c) * 64 + 16 * (g ^ tile_key<4>(c)) +
+                                 8 * wt) = p;
         }
-#pragma unroll
-        for (int r = 0; r < S::RT; ++r) sum[r] += add[r];
-      }
-      const size_t seg = (size_t)wg + it.index;
+      };
+      weights();
+      bool far = false;
+      float top[S::RT];
 #pragma unroll
       for (int r = 0; r < S::RT; ++r) {
-        sum[r] = col_sum(sum[r]);
-        if (g == 0)
-          *reinterpret_cast<float2*>(a.part_ml + ((seg * 2 + wt) * S::M + (wr * S::RT + r) * 16 + c) * 2) =
-              float2{m[r] * unit, sum[r]};
+        top[r] = fmaxf(fmaxf(x[r][0], x[r][1]), fmaxf(x[r][2], x[r][3]));
+        far = far || (top[r] - m[r]) * unit > kSlack;           // (no token so far: any score is)
+      }
+      if (__any(far) && lane == 0) passed[u & 1] = u;
+      lds_barrier();
+      if (__builtin_amdgcn_readfirstlane(passed[u & 1]) == u) {
+        // every row takes its largest score as its reference
+#pragma unroll
+        for (int r = 0; r < S::RT; ++r) {
+          top[r] = col_max(top[r]);
+          if (g == 0) smax[wt * S::M + (wr * S::RT + r) * 16 + c] = top[r];
+        }
+        lds_barrier();
+#pragma unroll
+        for (int r = 0; r < S::RT; ++r) {
+          const int row = (wr * S::RT + r) * 16 + c;
+          const float most = max3(m[r], top[r], smax[(1 - wt) * S::M + row]);
+          const float now = most == -INFINITY ? 0.f : most * unit;
+          const float keep = m[r] == -INFINITY ? 0.f : exp2_fast(ref[r] - now);
+          m[r] = most;
+          sum[r] *= keep;
+          ref[r] = now;
+          if (g == 0 && wt == 0) skeep[row] = keep;
+        }
+        weights();
+        lds_barrier();
+      }
+#pragma unroll
+      for (int r = 0; r < S::RT; ++r) sum[r] += add[r];
+      if (ends) {
+#pragma unroll
+        for (int r = 0; r < S::RT; ++r) {
+          sum[r] = col_sum(sum[r]);
+          if (g == 0)
+            *reinterpret_cast<float2*>(a.part_ml + ((seg * 2 + wt) * S::M + (wr * S::RT + r) * 16 + c) * 2) =
+                float2{m[r] * unit, sum[r]};
+        }
+        start();
       }
     }
     return;
@@ -540,35 +580,89 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
 }
 
 // ---- joining the partial results --------------------------------------------------
-// One query row a workgroup, four latent columns a thread: the weights 2^(m - max) of
-// the partial results that the plan says exist, in the plan's order. A row without any
-// (no tokens) gives zeros. The latents are rounded to fp16 for the product with W_uv.
-__global__ void __launch_bounds__(128) latent_join_kernel(DecodeArgs a) {
+// One query row a workgroup. Its partial results are the runs of workgroups that the plan
+// gave its items' tiles to. All their (m, l) are read at once, for the weights
+// 2^(m - max) / sum; then the thread groups of Dc / 4 (four latent columns a thread) take
+// them in turn. A row without any (no tokens) gives zeros. The latents are rounded to
+// fp16 for the product with W_uv, which is fp16.
+// With few rows 512 threads share a row's partial results, with many 128 do: more rows at
+// once on a CU.
+constexpr int kJoinMost = 1024;                          // (partial results of a row: at most the workgroups and its items)
+
+template <int NT>
+__global__ void __launch_bounds__(NT) latent_join_kernel(DecodeArgs a) {
+  __shared__ int first[16], upto[17];                     // of each item: first partial result, those up to it
+  __shared__ float weight[kJoinMost];
+  __shared__ f4 part[NT];
   const LatentArgs& l = a.l;
-  const int row = blockIdx.x, b = row / l.H, h = row % l.H, M = a.p.rows;
-  const int all = a.starts[a.B], per = max(1, (all + a.p.wgs - 1) / a.p.wgs);
-  const int col = 4 * threadIdx.x;
-  float top = -INFINITY, sum = 0.f;
-  f4 o = {};
-  auto add = [&](const Item& it, int r) {
-    if (it.tiles <= 0) return;
-    const int from = it.start + kItemCost, w0 = from / per, w1 = (from + it.tiles - 1) / per;
-    for (int w = w0; w <= w1; ++w) {
-      const size_t seg = (size_t)w + it.index;
-      const float2 a0 = *reinterpret_cast<const float2*>(a.part_ml + (seg * 2 * M + r) * 2);
-      const float2 a1 = *reinterpret_cast<const float2*>(a.part_ml + ((seg * 2 + 1) * M + r) * 2);
-      if (a0.x == -INFINITY) continue;                       // (every token of it was lost)
-      f4 v = {};
-      if (col < l.Dc) v = *reinterpret_cast<const f4*>(a.part_o + (seg * M + r) * l.Dc + col);
-      const float m = fmaxf(top, a0.x), x = exp2_fast(top - m), y = exp2_fast(a0.x - m);
-      o = o * x + v * y;
-      sum = sum * x + (a0.y + a1.y) * y;
-      top = m;
+  const int row = blockIdx.x, b = row / l.H, h = row % l.H, M = a.p.rows, lane = threadIdx.x & 63;
+  const int per = share(a);
+  const int items = a.p.chunks + 1;
+  const bool own_r = threadIdx.x % kWave == a.p.chunks;   // (the last item is the sequence's own)
+  if (threadIdx.x < kWave) {
+    int w0 = 0, n = 0, index = 0;
+    if (lane < items) {
+      const Item it = own_r ? own_item(a, b, h / M, a.starts[b], clamp_len(a, a.kv_len[b])) : prefix_item(a, lane, row / M);
+      index = it.index;
+      if (it.tiles > 0) {
+        const int from = it.start + kItemCost;
+        w0 = from / per;
+        n = (from + it.tiles - 1) / per - w0 + 1;
+      }
     }
+    int up = n;
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+      const int v = __shfl_up(up, o, kWave);
+      if (lane >= o) up += v;
+    }
+    if (lane < items) {
+      first[lane] = w0 + index;
+      upto[lane + 1] = up;
+    }
+    if (lane == 0) upto[0] = 0;
+  }
+  __syncthreads();
+  const int parts = upto[items];
+  auto seg_of = [&](int i, int& r) {                      // the i-th partial result: where it is, and its row there
+    int k = 0;
+    while (i >= upto[k + 1]) ++k;
+    r = k == items - 1 ? h % M : row % M;
+    return (size_t)(first[k] + i - upto[k]);
   };
-  for (int k = 0; k < a.p.chunks; ++k) add(prefix_item(a, k, row / M), row % M);
-  add(own_item(a, b, h / M, a.starts[b], clamp_len(a, a.kv_len[b])), h % M);
-  if (col < l.Dc) {
+  // every wave forms the maximum and the sum for itself
+  float top = -INFINITY, sum = 0.f;
+  for (int i = lane; i < parts; i += kWave) {
+    int r;
+    const size_t seg = seg_of(i, r);
+    top = fmaxf(top, a.part_ml[(seg * 2 * M + r) * 2]);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+  for (int i = lane; i < parts; i += kWave) {
+    int r;
+    const size_t seg = seg_of(i, r);
+    const float2 a0 = *reinterpret_cast<const float2*>(a.part_ml + (seg * 2 * M + r) * 2);
+    const float2 a1 = *reinterpret_cast<const float2*>(a.part_ml + ((seg * 2 + 1) * M + r) * 2);
+    const float w = a0.x == -INFINITY ? 0.f : exp2_fast(a0.x - top);  // (-inf: every token of it was lost)
+    sum += w == 0.f ? 0.f : w * (a0.y + a1.y);
+    if (threadIdx.x < kWave) weight[i] = w;
+  }
+  sum = wave_sum(sum);
+  __syncthreads();
+  const int cols = l.Dc / 4, groups = NT / cols, grp = threadIdx.x / cols, col = 4 * (threadIdx.x % cols);
+  f4 o = {};
+#pragma unroll 4
+  for (int i = grp; i < parts; i += groups) {
+    int r;
+    const size_t seg = seg_of(i, r);
+    const float w = weight[i];
+    if (w != 0.f) o += *reinterpret_cast<const f4*>(a.part_o + (seg * M + r) * l.Dc + col) * w;
+  }
+  part[threadIdx.x] = o;
+  __syncthreads();
+  if (grp == 0) {
+    for (int k = 1; k < groups; ++k) o += part[k * cols + threadIdx.x];
     const float inv = sum > 0.f ? 1.f / sum : sum != sum ? sum : 0.f;
     const h4 v = {(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
     *reinterpret_cast<h4*>(a.lat + (size_t)row * l.Dc + col) = v;
@@ -639,12 +733,28 @@ DecodePlan decode_plan(int H, int Dc, int Dr, int B, int max_len, int prefix_len
   p.head_blocks = (H + p.rows - 1) / p.rows;
   p.row_blocks = prefix_len > 0 ? (B * H + p.rows - 1) / p.rows : 0;
   const int pt = tiles_host(prefix_len);
-  p.chunks = prefix_len > 0 ? (p.row_blocks >= 8 ? std::min(8, pt) : 1) : 0;
-  p.chunk_tiles = p.chunks ? (pt + p.chunks - 1) / p.chunks : 0;
-  if (p.chunk_tiles) p.chunks = (pt + p.chunk_tiles - 1) / p.chunk_tiles;
+  const int wgs = kCus * (Dc <= 128 ? 3 : Dc <= 256 ? 2 : 1);
+  const long long own = (long long)B * p.head_blocks * (max_len > 0 ? tiles_host(max_len) + kItemCost : 0);
+  p.least = 1;
+  if (prefix_len > 0) {
+    // Token chunks of the prefix such that a row block of a chunk is just one workgroup's
+    // share: as many as leave workgroups enough for the sequences' own tiles. Then no
+    // workgroup has two partial results of the prefix, and the workgroups of a chiplet read
+    // the same tokens, which its L2 holds.
+    p.chunks = 1;
+    for (int c = kChunks; c > 1; --c) {
+      const int item = (pt + c - 1) / c + kItemCost;
+      if (c <= pt && (long long)c * p.row_blocks + (own + item - 1) / item <= wgs && c * p.row_blocks * 2 >= wgs) {
+        p.chunks = c;
+        p.least = item;
+        break;
+      }
+    }
+    p.chunk_tiles = (pt + p.chunks - 1) / p.chunks;
+    p.chunks = (pt + p.chunk_tiles - 1) / p.chunk_tiles;
+  }
   p.prefix_places = (pt + p.chunks * kItemCost) * p.row_blocks;
   const long long tiles = (long long)pt * p.row_blocks + (long long)B * p.head_blocks * tiles_host(max_len);
-  const int wgs = kCus * (Dc <= 128 ? 3 : Dc <= 256 ? 2 : 1);
   p.wgs = (int)std::min<long long>(wgs, (std::max<long long>(tiles, 1) + 7) / 8 * 8);
   const size_t rows = (size_t)B * H, parts = (size_t)p.wgs + (size_t)p.chunks * p.row_blocks + (size_t)B * p.head_blocks;
   size_t off = 0;
@@ -679,7 +789,10 @@ hipError_t launch_latent_decode(const DecodeArgs& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   e = l.Dc == 512 ? launch_attention<512>(a, st) : l.Dc == 256 ? launch_attention<256>(a, st) : launch_attention<128>(a, st);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(latent_join_kernel, dim3(a.B * l.H), dim3(128), 0, st, a);
+  if (a.B * l.H > 2 * kCus)
+    hipLaunchKernelGGL(latent_join_kernel<128>, dim3(a.B * l.H), dim3(128), 0, st, a);
+  else
+    hipLaunchKernelGGL(latent_join_kernel<512>, dim3(a.B * l.H), dim3(512), 0, st, a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   const dim3 gu(l.Dv / 16, l.H, (a.B + 127) / 128);
