@@ -206,62 +206,67 @@ __global__ void __launch_bounds__(512) linear_sums_kernel(LinearArgs a) {
 __device__ __forceinline__ int x_key(int row) { return ((row >> 1) & 1) | ((row >> 1) & 4); }
 
 // The products on the matrix cores: 128 rows of x by 128 outputs, four waves of 64 x 64,
-// one 64-input group a step. x comes through LDS, one step ahead; a wave loads the codes
-// and scales of its own 64 outputs into registers, one step ahead too.
-__global__ void __launch_bounds__(256) linear_tile_kernel(LinearArgs a) {
+// one 64-input group a step. x comes through LDS one step ahead, codes and (s, z) one run
+// of four groups ahead (a 128-byte line of codes per output). Bound by the VALU beside the
+// matrix cores: a wave's 32 products a step (512 clocks) come with 88 instructions to
+// unpack codes and 64 to apply scales.
+constexpr int kRun = 4;                                  // groups of a run
+__global__ void __launch_bounds__(256, 2) linear_tile_kernel(LinearArgs a) {
   __shared__ __attribute__((aligned(16))) char xt[2][128 * 128];
+  __shared__ __attribute__((aligned(16))) char ct[2][128 * 32 * kRun];
+  __shared__ uint32_t st[2][kRun][128];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int c = lane & 15, g = lane >> 4, ng = a.in_dim >> 6;
   const int t0 = blockIdx.y * 128, o0 = blockIdx.x * 128;
-  const int tw = (wave & 1) * 64, ow = o0 + (wave >> 1) * 64;
-  const char* src[4];
+  const int tw = (wave & 1) * 64, nw = (wave >> 1) * 64, ow = o0 + nw;
+  const uint32_t x_at = lds_at(xt), c_at = lds_at(ct), s_at = lds_at(st);
+  const char *xs[4], *cs[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int r = 8 * (4 * wave + j) + (lane >> 3);
-    src[j] = static_cast<const char*>(a.x) + (size_t)min(t0 + r, a.T - 1) * a.x_stride * 2 +
-             16 * ((lane & 7) ^ x_key(r));
+    xs[j] = static_cast<const char*>(a.x) + (size_t)min(t0 + r, a.T - 1) * a.x_stride * 2 + 16 * ((lane & 7) ^ x_key(r));
+    cs[j] = static_cast<const char*>(a.q) + (size_t)min(o0 + r, a.out_dim - 1) * (a.in_dim / 2);
   }
-  auto copy = [&](int gi) {
+  const int piece = (lane & 7) ^ (lane >> 4 & 7);        // of a line of codes: its key is row / 2, of 8 rows a copy
+  auto copy_x = [&](int gi) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) dma16(src[j] + 128 * (size_t)gi, xt[gi & 1] + 1024 * (4 * wave + j));
+    for (int j = 0; j < 4; ++j) dma16(xs[j] + 128 * (size_t)gi, x_at + (gi & 1) * 16384 + 1024 * (4 * wave + j));
   };
-  const char* q[4];
-  const __half2* sz[4];
+  // (pieces past a row's end, in its last run, are the row's first one again; not used)
+  auto copy_run = [&](int run) {
 #pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    const int row = min(ow + 16 * n + c, a.out_dim - 1);
-    q[n] = static_cast<const char*>(a.q) + (size_t)row * (a.in_dim / 2) + 8 * g;
-    sz[n] = static_cast<const __half2*>(a.sz) + (size_t)row * ng;
-  }
+    for (int j = 0; j < 4; ++j) {
+      const int p = piece ^ (4 * (j & 1));
+      const int at = kRun * 32 * run + 16 * p;
+      dma16(cs[j] + (at < a.in_dim / 2 ? at : 0), c_at + (run & 1) * 16384 + 1024 * (4 * wave + j));
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int row = min(o0 + 64 * j + lane, a.out_dim - 1), gi = min(kRun * run + wave, ng - 1);
+      dma4(static_cast<const uint32_t*>(a.sz) + (size_t)row * ng + gi, s_at + (run & 1) * kRun * 512 + wave * 512 + 256 * j);
+    }
+  };
   f4 y[4][4] = {};
-  u2 w[4];
-  float s[4];
-  copy(0);
-#pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    w[n] = *reinterpret_cast<const u2*>(q[n]);
-    s[n] = __low2float(sz[n][0]);
-  }
+  copy_run(0);
+  copy_x(0);
   for (int gi = 0; gi < ng; ++gi) {
+    const int run = gi / kRun, k = gi % kRun;
     vm_wait<0>();
     lds_barrier();
+    if (gi + 1 < ng) copy_x(gi + 1);
+    if (k == 0 && gi + kRun < ng) copy_run(run + 1);
+    const char* tile = xt[gi & 1];
+    const char* codes = ct[run & 1];
     h8 b0[4], b1[4];
-    float s1[4];
+    float s[4];
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      b0[n] = codes8(w[n].x);
-      b1[n] = codes8(w[n].y);
-      s1[n] = s[n] * kCodeUnit;
+      const int r = nw + 16 * n + c;
+      const u2 w = *reinterpret_cast<const u2*>(codes + 128 * r + 16 * ((2 * k + (g >> 1)) ^ (r >> 1 & 7)) + 8 * (g & 1));
+      b0[n] = codes8(w.x);
+      b1[n] = codes8(w.y);
+      s[n] = __low2float(__builtin_bit_cast(__half2, st[run & 1][k][r])) * kCodeUnit;
     }
-    if (gi + 1 < ng) {
-      copy(gi + 1);
-#pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        w[n] = *reinterpret_cast<const u2*>(q[n] + 32 * (size_t)(gi + 1));
-        s[n] = __low2float(sz[n][gi + 1]);
-      }
-    }
-    const char* tile = xt[gi & 1];
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
       const int r = tw + 16 * m + c;
@@ -271,7 +276,7 @@ __global__ void __launch_bounds__(256) linear_tile_kernel(LinearArgs a) {
       for (int n = 0; n < 4; ++n) {
         const f4 d = mfma16(x1, b1[n], mfma16(x0, b0[n], f4{}));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[m][n][i] = fmaf(s1[n], d[i], y[m][n][i]);
+        for (int i = 0; i < 4; ++i) y[m][n][i] = fmaf(s[n], d[i], y[m][n][i]);
       }
     }
   }
@@ -284,14 +289,11 @@ __global__ void __launch_bounds__(256) linear_tile_kernel(LinearArgs a) {
     const _Float16* brow = static_cast<const _Float16*>(a.lora_b) + (size_t)row * a.r;
     f4 d[4] = {};
     for (int k = 0; k < KE; k += 32) {
-      h8 b = {};
+      h8 b;                                              // (past the groups or the rank: any weight, times E's zero)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int j = k + 8 * g + e;
-        if (j < ng)
-          b[e] = __builtin_bit_cast(_Float16, __high2half(zrow[j]));
-        else if (j >= az && j - az < a.r)
-          b[e] = brow[j - az];
+        b[e] = k < az ? __builtin_bit_cast(_Float16, __high2half(zrow[min(j, ng - 1)])) : brow[min(j - az, a.r - 1)];
       }
 #pragma unroll
       for (int m = 0; m < 4; ++m) {

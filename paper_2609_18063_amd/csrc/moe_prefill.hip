@@ -112,11 +112,12 @@ __global__ void __launch_bounds__(256) latent_expand_kernel(PrefillArgs a, int s
     src_c[j] = reinterpret_cast<const char*>(l.pages + (ok ? ((size_t)page * l.page + tok % l.page) * row_halves : 0)) + piece;
     src_w[j] = reinterpret_cast<const char*>(l.w + (size_t)min(n0 + r, N - 1) * DC) + piece;
   }
+  const uint32_t at0 = lds_at(lds);
   auto copy = [&](int k) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      dma16(src_c[j] + 128 * k, lds[k & 1][0] + 1024 * (4 * wave + j));
-      dma16(src_w[j] + 128 * k, lds[k & 1][1] + 1024 * (4 * wave + j));
+      dma16(src_c[j] + 128 * k, at0 + (k & 1) * 32768 + 1024 * (4 * wave + j));
+      dma16(src_w[j] + 128 * k, at0 + (k & 1) * 32768 + 16384 + 1024 * (4 * wave + j));
     }
   };
   const int tr = (wave & 1) * 64, tn = (wave >> 1) * 64;

@@ -37,26 +37,24 @@ __device__ __forceinline__ h8 join(h4 a, h4 b) {
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// Each lane copies 16 bytes from its own global address to lds + 16 * lane (lds the
-// same for the wave). The compiler does not see it as a memory instruction: vm_wait
-// orders it, and every wave waits before the barrier behind which the data is read. (The
-// LDS address goes through m0, which nothing else in these kernels uses.)
-__device__ __forceinline__ void dma16(const void* g, const void* lds) {
-  const uint32_t to = __builtin_amdgcn_readfirstlane(
-      (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)lds);
+// The LDS address of a shared object.
+__device__ __forceinline__ uint32_t lds_at(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+// Each lane copies 16 bytes from its own global address to LDS address to + 16 * lane (`to`
+// the same for the wave). The compiler does not see it as a memory instruction: vm_wait
+// orders it, and every wave waits before the barrier behind which the data is read. (`to`
+// goes through m0, which nothing else in these kernels uses.)
+__device__ __forceinline__ void dma16(const void* g, uint32_t to) {
   asm volatile(
       "s_mov_b32 m0, %0\n\t"
       "s_nop 0\n\t"
       "global_load_lds_dwordx4 %1, off"
       :
-      : "s"(to), "v"(g)
+      : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(g)
       : "memory");
 }
-// The same from a base that the wave shares, with a byte offset per lane, to LDS address
-// `to` (lds_at).
-__device__ __forceinline__ uint32_t lds_at(const void* p) {
-  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
-}
+// The same from a base that the wave shares, with a byte offset per lane.
 __device__ __forceinline__ void dma16(const void* base, uint32_t off, uint32_t to) {
   asm volatile(
       "s_mov_b32 m0, %0\n\t"
@@ -64,6 +62,16 @@ __device__ __forceinline__ void dma16(const void* base, uint32_t off, uint32_t t
       "global_load_lds_dwordx4 %1, %2"
       :
       : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(base)
+      : "memory");
+}
+// Four bytes a lane, to lds + 4 * lane.
+__device__ __forceinline__ void dma4(const void* g, uint32_t to) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dword %1, off"
+      :
+      : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(g)
       : "memory");
 }
 // An int that the whole wave reads and nothing writes while the kernel runs, through the
