@@ -15,7 +15,11 @@ struct LinearArgs {
   // workspace, for many rows: [T][linear_extra] and [T]
   __half *e_hi, *e_lo;
   float* e_scale;
+  float* sums;                           // of tiles split along the inputs
 };
+
+constexpr int kRowsMost = 64;            // rows up to which the weights are read once for all
+constexpr size_t kLinearSums = 32u << 20;
 
 // Inputs that the group sums and the adapter add to a row's products.
 constexpr int linear_extra(int in_dim, int r) { return (in_dim / 64 + 31) / 32 * 32 + (r + 31) / 32 * 32; }

@@ -8,6 +8,8 @@
 // weight is rounded.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "moe_linear.h"
 #include "moe_tile.h"
 
@@ -70,31 +72,49 @@ __global__ void __launch_bounds__(64 * NW) linear_rows_kernel(LinearArgs a) {
     ad[n] = static_cast<const _Float16*>(a.lora_a) + (size_t)min(16 * n + c, a.r - 1) * a.in_dim + 16 * g;
   f4 y[TT] = {}, ax[TT][RT ? RT : 1] = {};
   const h8 one = ones8();
-  for (int quad = wave; quad * 4 < ng; quad += NW) {
+  // N groups from g0 on: everything is asked for before the first product
+  auto groups = [&](int g0, auto count) {
+    constexpr int N = decltype(count)::value;
+    u2 w[N];
+    float2 s[N];
+    h8 x0[N][TT], x1[N][TT], b0[N][RT ? RT : 1], b1[N][RT ? RT : 1];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int gi = quad * 4 + k;
-      if (gi >= ng) break;
-      const u2 w = *reinterpret_cast<const u2*>(q + 32 * gi);
-      const float2 s = __half22float2(sz[gi]);
-      const h8 w0 = codes8(w.x), w1 = codes8(w.y);
-      h8 b0[RT ? RT : 1], b1[RT ? RT : 1];
-#pragma unroll
-      for (int n = 0; n < RT; ++n) {
-        b0[n] = ld_h8(ad[n] + 64 * gi);
-        b1[n] = ld_h8(ad[n] + 64 * gi + 8);
-      }
+    for (int k = 0; k < N; ++k) {
+      w[k] = *reinterpret_cast<const u2*>(q + 32 * (g0 + k));
+      s[k] = __half22float2(sz[g0 + k]);
 #pragma unroll
       for (int m = 0; m < TT; ++m) {
-        const h8 x0 = ld_h8(x[m] + 64 * gi), x1 = ld_h8(x[m] + 64 * gi + 8);
-        const f4 d = mfma16(x1, w1, mfma16(x0, w0, f4{}));
-        const f4 xs = mfma16(x1, one, mfma16(x0, one, f4{}));
+        x0[k][m] = ld_h8(x[m] + 64 * (g0 + k));
+        x1[k][m] = ld_h8(x[m] + 64 * (g0 + k) + 8);
+      }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[m][i] = fmaf(s.x * kCodeUnit, d[i], fmaf(s.y, xs[i], y[m][i]));
-#pragma unroll
-        for (int n = 0; n < RT; ++n) ax[m][n] = mfma16(x1, b1[n], mfma16(x0, b0[n], ax[m][n]));
+      for (int n = 0; n < RT; ++n) {
+        b0[k][n] = ld_h8(ad[n] + 64 * (g0 + k));
+        b1[k][n] = ld_h8(ad[n] + 64 * (g0 + k) + 8);
       }
     }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const h8 w0 = codes8(w[k].x), w1 = codes8(w[k].y);
+#pragma unroll
+      for (int m = 0; m < TT; ++m) {
+        const f4 d = mfma16(x1[k][m], w1, mfma16(x0[k][m], w0, f4{}));
+        const f4 xs = mfma16(x1[k][m], one, mfma16(x0[k][m], one, f4{}));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[m][i] = fmaf(s[k].x * kCodeUnit, d[i], fmaf(s[k].y, xs[i], y[m][i]));
+#pragma unroll
+        for (int n = 0; n < RT; ++n) ax[m][n] = mfma16(x1[k][m], b1[k][n], mfma16(x0[k][m], b0[k][n], ax[m][n]));
+      }
+    }
+  };
+  // (the registers that a run of N groups takes: 4 for codes and scales, 8 for each tile of x and A)
+  constexpr int N = TT + RT <= 2 ? 4 : TT + RT <= 3 ? 2 : 1;
+  for (int quad = wave; quad * 4 < ng; quad += NW) {
+    const int end = min(quad * 4 + 4, ng);
+    int gi = quad * 4;
+    for (; gi + N <= end; gi += N) groups(gi, std::integral_constant<int, N>());
+    if constexpr (N > 1)
+      for (; gi < end; ++gi) groups(gi, std::integral_constant<int, 1>());
   }
 #pragma unroll
   for (int m = 0; m < TT; ++m)
@@ -124,9 +144,16 @@ __global__ void __launch_bounds__(64 * NW) linear_rows_kernel(LinearArgs a) {
     if (t >= a.T || o >= a.out_dim) continue;
     float v = total(m, i, l);
     if constexpr (RT > 0) {
-      const __half* lb = static_cast<const __half*>(a.lora_b) + (size_t)o * a.r;
+      const _Float16* lb = static_cast<const _Float16*>(a.lora_b) + (size_t)o * a.r;
       float delta = 0.f;
-      for (int k = 0; k < a.r; ++k) delta = fmaf(__half2float(lb[k]), axs[tl][k], delta);
+      if (a.r % 8 == 0)
+        for (int k = 0; k < a.r; k += 8) {
+          const h8 v = ld_h8(lb + k);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) delta = fmaf((float)v[e], axs[tl][k + e], delta);
+        }
+      else
+        for (int k = 0; k < a.r; ++k) delta = fmaf((float)lb[k], axs[tl][k], delta);
       v = fmaf(a.lora_scale, delta, v);
     }
     store_out(a, t, o, v);
@@ -206,72 +233,93 @@ __global__ void __launch_bounds__(512) linear_sums_kernel(LinearArgs a) {
 __device__ __forceinline__ int x_key(int row) { return ((row >> 1) & 1) | ((row >> 1) & 4); }
 
 // The products on the matrix cores: 128 rows of x by 128 outputs, four waves of 64 x 64,
-// one 64-input group a step. x comes through LDS one step ahead, codes and (s, z) one run
-// of four groups ahead (a 128-byte line of codes per output). Bound by the VALU beside the
-// matrix cores: a wave's 32 products a step (512 clocks) come with 88 instructions to
-// unpack codes and 64 to apply scales.
-constexpr int kRun = 4;                                  // groups of a run
-__global__ void __launch_bounds__(256, 2) linear_tile_kernel(LinearArgs a) {
-  __shared__ __attribute__((aligned(16))) char xt[2][128 * 128];
-  __shared__ __attribute__((aligned(16))) char ct[2][128 * 32 * kRun];
-  __shared__ uint32_t st[2][kRun][128];
+// one 64-input group a step. x, codes and (s, z) come through LDS, two steps ahead in three
+// slots. Bound by the VALU beside the matrix cores: a wave's 32 products a step (512
+// clocks) come with 88 instructions to unpack codes and 64 to apply scales.
+// Workgroups come in rounds of kSlots. The tiles that do not fill a round are split along
+// the inputs into as many parts as fill it (first in the grid, so that whole tiles follow
+// the short parts); a part writes fp32 sums, which one more launch adds in order.
+struct TilePlan {
+  int cols, tiles, rest, parts;   // tiles of a row block, all tiles; of them split, and into how many parts
+  int workgroups() const { return tiles - rest + rest * parts; }
+};
+constexpr int kSlots = 512, kMostParts = 16, kTileSums = 128 * 128;
+static_assert(kSlots * kTileSums * sizeof(float) <= kLinearSums, "parts fit the workspace");
+
+TilePlan tile_plan(int out_dim, int T, int ng) {
+  TilePlan p{};
+  p.cols = (out_dim + 127) / 128;
+  p.tiles = p.cols * ((T + 127) / 128);
+  p.rest = p.tiles % kSlots;
+  p.parts = p.rest ? std::min({kSlots / p.rest, kMostParts, std::max(1, ng / 4)}) : 1;
+  if (p.parts < 2) p.rest = 0, p.parts = 1;
+  return p;
+}
+
+__global__ void __launch_bounds__(256, 2) linear_tile_kernel(LinearArgs a, TilePlan p) {
+  constexpr int XB = 128 * 128, CB = 128 * 32, SB = 128 * 4, SLOT = XB + CB + SB;
+  __shared__ __attribute__((aligned(16))) char ring[3][SLOT];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int c = lane & 15, g = lane >> 4, ng = a.in_dim >> 6;
-  const int t0 = blockIdx.y * 128, o0 = blockIdx.x * 128;
+  const int split = p.rest * p.parts;
+  int tile = blockIdx.x - split + p.rest, part = 0, from = 0, to = ng;
+  if ((int)blockIdx.x < split) {
+    tile = blockIdx.x / p.parts;
+    part = blockIdx.x % p.parts;
+    from = ng * part / p.parts;
+    to = ng * (part + 1) / p.parts;
+  }
+  const int t0 = tile / p.cols * 128, o0 = tile % p.cols * 128;
   const int tw = (wave & 1) * 64, nw = (wave >> 1) * 64, ow = o0 + nw;
-  const uint32_t x_at = lds_at(xt), c_at = lds_at(ct), s_at = lds_at(st);
-  const char *xs[4], *cs[4];
+  const char* xs[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int r = 8 * (4 * wave + j) + (lane >> 3);
     xs[j] = static_cast<const char*>(a.x) + (size_t)min(t0 + r, a.T - 1) * a.x_stride * 2 + 16 * ((lane & 7) ^ x_key(r));
-    cs[j] = static_cast<const char*>(a.q) + (size_t)min(o0 + r, a.out_dim - 1) * (a.in_dim / 2);
   }
-  const int piece = (lane & 7) ^ (lane >> 4 & 7);        // of a line of codes: its key is row / 2, of 8 rows a copy
-  auto copy_x = [&](int gi) {
+  // codes: 32 rows of two pieces a copy, a row's pieces swapped in every other four rows
+  const int cr = 32 * wave + (lane >> 1);
+  const char* cs = static_cast<const char*>(a.q) + (size_t)min(o0 + cr, a.out_dim - 1) * (a.in_dim / 2) +
+                   16 * ((lane & 1) ^ (cr >> 2 & 1));
+  const uint32_t* ss = static_cast<const uint32_t*>(a.sz) + (size_t)min(o0 + 64 * (wave & 1) + lane, a.out_dim - 1) * ng;
+  const uint32_t at0 = lds_at(ring);
+  auto copy = [&](int gi, int slot) {
+    const uint32_t at = at0 + slot * SLOT;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) dma16(xs[j] + 128 * (size_t)gi, x_at + (gi & 1) * 16384 + 1024 * (4 * wave + j));
+    for (int j = 0; j < 4; ++j) dma16(xs[j] + 128 * (size_t)gi, at + 1024 * (4 * wave + j));
+    dma16(cs + 32 * (size_t)gi, at + XB + 1024 * wave);
+    dma4(ss + gi, at + XB + CB + 256 * (wave & 1));      // (two waves each write the same scales)
   };
-  // (pieces past a row's end, in its last run, are the row's first one again; not used)
-  auto copy_run = [&](int run) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int p = piece ^ (4 * (j & 1));
-      const int at = kRun * 32 * run + 16 * p;
-      dma16(cs[j] + (at < a.in_dim / 2 ? at : 0), c_at + (run & 1) * 16384 + 1024 * (4 * wave + j));
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int row = min(o0 + 64 * j + lane, a.out_dim - 1), gi = min(kRun * run + wave, ng - 1);
-      dma4(static_cast<const uint32_t*>(a.sz) + (size_t)row * ng + gi, s_at + (run & 1) * kRun * 512 + wave * 512 + 256 * j);
-    }
-  };
+  constexpr int kCopies = 6;
   f4 y[4][4] = {};
-  copy_run(0);
-  copy_x(0);
-  for (int gi = 0; gi < ng; ++gi) {
-    const int run = gi / kRun, k = gi % kRun;
-    vm_wait<0>();
+  int slot = 0;
+  copy(from, 0);
+  if (from + 1 < to) copy(from + 1, 1);
+  for (int gi = from; gi < to; ++gi) {
+    if (gi + 1 < to)
+      vm_wait<kCopies>();
+    else
+      vm_wait<0>();
     lds_barrier();
-    if (gi + 1 < ng) copy_x(gi + 1);
-    if (k == 0 && gi + kRun < ng) copy_run(run + 1);
-    const char* tile = xt[gi & 1];
-    const char* codes = ct[run & 1];
+    if (gi + 2 < to) copy(gi + 2, slot >= 1 ? slot - 1 : 2);
+    const char* xt = ring[slot];
+    const char* codes = xt + XB;
+    const uint32_t* scales = reinterpret_cast<const uint32_t*>(codes + CB);
     h8 b0[4], b1[4];
     float s[4];
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const int r = nw + 16 * n + c;
-      const u2 w = *reinterpret_cast<const u2*>(codes + 128 * r + 16 * ((2 * k + (g >> 1)) ^ (r >> 1 & 7)) + 8 * (g & 1));
+      const u2 w = *reinterpret_cast<const u2*>(codes + 32 * r + 16 * ((g >> 1) ^ (r >> 2 & 1)) + 8 * (g & 1));
       b0[n] = codes8(w.x);
       b1[n] = codes8(w.y);
-      s[n] = __low2float(__builtin_bit_cast(__half2, st[run & 1][k][r])) * kCodeUnit;
+      s[n] = __low2float(__builtin_bit_cast(__half2, scales[r])) * kCodeUnit;
     }
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
       const int r = tw + 16 * m + c;
-      const h8 x0 = ld_h8(tile + 128 * r + 16 * ((2 * g) ^ x_key(r)));
-      const h8 x1 = ld_h8(tile + 128 * r + 16 * ((2 * g + 1) ^ x_key(r)));
+      const h8 x0 = ld_h8(xt + 128 * r + 16 * ((2 * g) ^ x_key(r)));
+      const h8 x1 = ld_h8(xt + 128 * r + 16 * ((2 * g + 1) ^ x_key(r)));
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         const f4 d = mfma16(x1, b1[n], mfma16(x0, b0[n], f4{}));
@@ -279,36 +327,79 @@ __global__ void __launch_bounds__(256, 2) linear_tile_kernel(LinearArgs a) {
         for (int i = 0; i < 4; ++i) y[m][n][i] = fmaf(s[n], d[i], y[m][n][i]);
       }
     }
+    slot = slot == 2 ? 0 : slot + 1;
   }
   // the group sums by z and lora_scale A x by B
-  const int KE = linear_extra(a.in_dim, a.r), az = (ng + 31) / 32 * 32;
+  const int KE = part ? 0 : linear_extra(a.in_dim, a.r), az = (ng + 31) / 32 * 32;
+  f4 d[4][4] = {};
+  for (int k = 0; k < KE; k += 32) {
+    h8 w[4];                                             // (past the groups or the rank: any weight, times E's zero)
+    const int j = k + 8 * g;
 #pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    const int row = min(ow + 16 * n + c, a.out_dim - 1);
-    const __half2* zrow = static_cast<const __half2*>(a.sz) + (size_t)row * ng;
-    const _Float16* brow = static_cast<const _Float16*>(a.lora_b) + (size_t)row * a.r;
-    f4 d[4] = {};
-    for (int k = 0; k < KE; k += 32) {
-      h8 b;                                              // (past the groups or the rank: any weight, times E's zero)
+    for (int n = 0; n < 4; ++n) {
+      const size_t row = min(ow + 16 * n + c, a.out_dim - 1);
+      if (k < az) {
+        const uint32_t* z = static_cast<const uint32_t*>(a.sz) + row * ng;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int j = k + 8 * g + e;
-        b[e] = k < az ? __builtin_bit_cast(_Float16, __high2half(zrow[min(j, ng - 1)])) : brow[min(j - az, a.r - 1)];
-      }
+        for (int e = 0; e < 8; ++e) w[n][e] = __builtin_bit_cast(_Float16, (uint16_t)(z[min(j + e, ng - 1)] >> 16));
+      } else {
+        const _Float16* lb = static_cast<const _Float16*>(a.lora_b) + row * a.r;
+        if (a.r % 8 == 0)
+          w[n] = ld_h8(lb + min(j - az, a.r - 8));
+        else
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const size_t at = (size_t)min(t0 + tw + 16 * m + c, a.T - 1) * KE + k + 8 * g;
-        d[m] = mfma16(ld_h8(a.e_lo + at), b, mfma16(ld_h8(a.e_hi + at), b, d[m]));
+          for (int e = 0; e < 8; ++e) w[n][e] = lb[min(j + e - az, a.r - 1)];
       }
     }
 #pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const size_t at = (size_t)min(t0 + tw + 16 * m + c, a.T - 1) * KE + j;
+      const h8 hi = ld_h8(a.e_hi + at), lo = ld_h8(a.e_lo + at);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) d[m][n] = mfma16(lo, w[n], mfma16(hi, w[n], d[m][n]));
+    }
+  }
+  if (KE)
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const f4 es = *reinterpret_cast<const f4*>(a.e_scale + t0 + tw + 16 * m + 4 * g);  // (rows past T: not stored)
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[m][n][i] = fmaf(es[i], d[m][n][i], y[m][n][i]);
+    }
+  if ((int)blockIdx.x < split) {
+    // a tile's sums as the lanes hold them: [m][n] of each wave, four rows a lane
+    float* sums = a.sums + (size_t)blockIdx.x * kTileSums + threadIdx.x * 4;
+#pragma unroll
     for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int n = 0; n < 4; ++n) *reinterpret_cast<f4*>(sums + (4 * m + n) * 1024) = y[m][n];
+    return;
+  }
+#pragma unroll
+  for (int m = 0; m < 4; ++m)
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int t = t0 + tw + 16 * m + 4 * g + i, o = ow + 16 * n + c;
-        if (t < a.T && o < a.out_dim) store_out(a, t, o, fmaf(a.e_scale[t], d[m][i], y[m][n][i]));
+        if (t < a.T && o < a.out_dim) store_out(a, t, o, y[m][n][i]);
       }
-  }
+}
+
+// The parts of the split tiles, added in order: one of a tile's sixteen [m][n] a workgroup.
+__global__ void __launch_bounds__(256) linear_parts_kernel(LinearArgs a, TilePlan p) {
+  const int tile = blockIdx.x / 16, mn = blockIdx.x % 16;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const float* sums = a.sums + (size_t)tile * p.parts * kTileSums + mn * 1024 + threadIdx.x * 4;
+  f4 y = {};
+  for (int k = 0; k < p.parts; ++k) y += *reinterpret_cast<const f4*>(sums + (size_t)k * kTileSums);
+  const int t0 = tile / p.cols * 128 + (wave & 1) * 64 + 16 * (mn >> 2) + 4 * (lane >> 4);
+  const int o = tile % p.cols * 128 + (wave >> 1) * 64 + 16 * (mn & 3) + (lane & 15);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (t0 + i < a.T && o < a.out_dim) store_out(a, t0 + i, o, y[i]);
 }
 
 template <int TT, int RT>
@@ -328,7 +419,7 @@ hipError_t launch_rows(const LinearArgs& a, hipStream_t st) {
 
 hipError_t launch_linear(const LinearArgs& a, hipStream_t st) {
   if (a.T <= 16) return launch_rows<1>(a, st);
-  if (a.T <= 64) return launch_rows<2>(a, st);
+  if (a.T <= kRowsMost) return launch_rows<2>(a, st);
   const size_t lds = 16 * (size_t)linear_extra(a.in_dim, a.r) * sizeof(float);
   const dim3 grid((a.T + 15) / 16), block(512);
   if (a.r == 0)
@@ -339,7 +430,11 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((linear_sums_kernel<4>), grid, block, lds, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(linear_tile_kernel, dim3((a.out_dim + 127) / 128, (a.T + 127) / 128), dim3(256), 0, st, a);
+  const TilePlan p = tile_plan(a.out_dim, a.T, a.in_dim / 64);
+  hipLaunchKernelGGL(linear_tile_kernel, dim3(p.workgroups()), dim3(256), 0, st, a, p);
+  e = hipGetLastError();
+  if (e != hipSuccess || !p.rest) return e;
+  hipLaunchKernelGGL(linear_parts_kernel, dim3(16 * p.rest), dim3(256), 0, st, a, p);
   return hipGetLastError();
 }
 
@@ -365,7 +460,8 @@ extern "C" {
 size_t moe_linear_workspace_bytes(int out_dim, int in_dim, int rank, int T) {
   if (!linear_shape_ok(out_dim, in_dim, rank, T)) return 0;
   const size_t t = T < 1 ? 1 : T, ke = moe::linear_extra(in_dim, rank);
-  return 2 * round256(t * ke * 2) + round256(t * 4);
+  const size_t sums = T > moe::kRowsMost ? (size_t)moe::kLinearSums : 0;
+  return 2 * round256(t * ke * 2) + round256(t * 4) + sums;
 }
 
 int moe_linear_int4_lora(const moe_proj* w, int out_dim, int in_dim, int rank, float lora_scale,
@@ -404,6 +500,7 @@ int moe_linear_int4_lora(const moe_proj* w, int out_dim, int in_dim, int rank, f
   a.e_hi = static_cast<__half*>(workspace);
   a.e_lo = reinterpret_cast<__half*>(static_cast<char*>(workspace) + part);
   a.e_scale = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * part);
+  a.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * part + round256((size_t)T * 4));
   return moe::launch_linear(a, static_cast<hipStream_t>(stream)) == hipSuccess ? MOE_OK : MOE_EHIP;
 }
 
