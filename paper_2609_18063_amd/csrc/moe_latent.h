@@ -66,13 +66,17 @@ struct DecodeArgs {
 };
 hipError_t launch_latent_decode(const DecodeArgs& a, hipStream_t st);
 
+constexpr int kPartGroups = 256, kPartRows = 256;  // workgroups that leave partial results, and their rows
+
 struct PrefillArgs {
   LatentArgs l;
-  int T, B, kv_total, max_q;
+  int T, B, kv_total, max_q, parts;
   const int32_t *q_start, *kv_start;  // [B + 1]
   __half *k, *v, *kr;            // [H][kv_total][Dn], [H][kv_total][Dv], [kv_total][Dr]
+  float *part_o, *part_ml;       // [kPartGroups][kPartRows][Dv] and [..][2], with parts > 1
   uint32_t* lost;                // per 64-token tile: its 16-token groups without a page
 };
+int prefill_parts(int max_q, int H, int B, int kv_total);
 hipError_t launch_latent_prefill(const PrefillArgs& a, hipStream_t st);
 
 }  // namespace moe

@@ -16,6 +16,7 @@
 namespace moe {
 namespace {
 
+constexpr int kCus = 256;
 constexpr float kCodeUnit = 512.f;
 
 // Eight codes (one dword, even input in the low nibble) as halves q 2^-9, in order: the
@@ -47,21 +48,27 @@ __device__ __forceinline__ void store_out(const LinearArgs& a, int t, int o, flo
     static_cast<float*>(a.y)[at] += v;
 }
 
-// ---- few rows: the weights are read once, 16 output rows a workgroup -----------
+// ---- few rows: the weights are read once, 16 NT output rows a workgroup --------
 // The NW waves take quads of groups in turn (a 128-byte line of codes per output row)
 // and their sums meet in LDS. A lane holds the codes of output row c = lane % 16,
 // inputs 16 g .. + 15 of a group (g = lane / 16). sum(x_g) is the product with ones,
 // and A x rides along as RT further tiles of 16 adapter rows, formed again by every
-// workgroup (from L2) rather than by a launch of its own.
-template <int TT, int RT, int NW>
+// workgroup (from L2) rather than by a launch of its own. Latency bounds it: every
+// load of a run of groups, and B's, is asked for before the first product.
+template <int TT, int RT, int NT, int NW>
 __global__ void __launch_bounds__(64 * NW) linear_rows_kernel(LinearArgs a) {
-  __shared__ float red[NW][TT * (1 + RT)][4][kWave];
+  __shared__ float red[NW][TT * (NT + RT)][4][kWave];
   __shared__ float axs[RT ? TT * 16 : 1][RT ? RT * 16 + 1 : 1];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int ng = a.in_dim >> 6, t0 = blockIdx.y * TT * 16;
-  const int row = min((int)blockIdx.x * 16 + c, a.out_dim - 1);
-  const char* q = static_cast<const char*>(a.q) + (size_t)row * (a.in_dim / 2) + 8 * g;
-  const __half2* sz = static_cast<const __half2*>(a.sz) + (size_t)row * ng;
+  const int ng = a.in_dim >> 6, t0 = blockIdx.y * TT * 16, o0 = blockIdx.x * NT * 16;
+  const char* q[NT];
+  const __half2* sz[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const size_t row = min(o0 + 16 * n + c, a.out_dim - 1);
+    q[n] = static_cast<const char*>(a.q) + row * (a.in_dim / 2) + 8 * g;
+    sz[n] = static_cast<const __half2*>(a.sz) + row * ng;
+  }
   const _Float16* x[TT];
 #pragma unroll
   for (int m = 0; m < TT; ++m)  // (a row past T repeats the last one and is not stored)
@@ -70,18 +77,36 @@ __global__ void __launch_bounds__(64 * NW) linear_rows_kernel(LinearArgs a) {
 #pragma unroll
   for (int n = 0; n < RT; ++n)
     ad[n] = static_cast<const _Float16*>(a.lora_a) + (size_t)min(16 * n + c, a.r - 1) * a.in_dim + 16 * g;
-  f4 y[TT] = {}, ax[TT][RT ? RT : 1] = {};
+  // this thread's first output, for the adapter's B
+  constexpr int OUTS = TT * NT * 256;
+  auto output = [&](int e, int& tl, int& o) {  // output e: its row of the tile and its column
+    const int l = e & 63, i = (e >> 6) & 3, tile = e >> 8;
+    tl = 16 * (tile / NT) + 4 * (l >> 4) + i;
+    o = o0 + 16 * (tile % NT) + (l & 15);
+  };
+  h8 lb[2] = {};
+  const bool early = RT == 1 && (a.r == 8 || a.r == 16);
+  if (early) {
+    int tl, o;
+    output(min((int)threadIdx.x, OUTS - 1), tl, o);
+    const _Float16* p = static_cast<const _Float16*>(a.lora_b) + (size_t)min(o, a.out_dim - 1) * a.r;
+    lb[0] = ld_h8(p);
+    if (a.r == 16) lb[1] = ld_h8(p + 8);
+  }
+  f4 y[TT][NT] = {}, ax[TT][RT ? RT : 1] = {};
   const h8 one = ones8();
-  // N groups from g0 on: everything is asked for before the first product
-  auto groups = [&](int g0, auto count) {
+  auto groups = [&](int g0, auto count) {      // N groups from g0 on
     constexpr int N = decltype(count)::value;
-    u2 w[N];
-    float2 s[N];
+    u2 w[N][NT];
+    float2 s[N][NT];
     h8 x0[N][TT], x1[N][TT], b0[N][RT ? RT : 1], b1[N][RT ? RT : 1];
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      w[k] = *reinterpret_cast<const u2*>(q + 32 * (g0 + k));
-      s[k] = __half22float2(sz[g0 + k]);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        w[k][n] = *reinterpret_cast<const u2*>(q[n] + 32 * (g0 + k));
+        s[k][n] = __half22float2(sz[n][g0 + k]);
+      }
 #pragma unroll
       for (int m = 0; m < TT; ++m) {
         x0[k][m] = ld_h8(x[m] + 64 * (g0 + k));
@@ -94,21 +119,24 @@ __global__ void __launch_bounds__(64 * NW) linear_rows_kernel(LinearArgs a) {
       }
     }
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const h8 w0 = codes8(w[k].x), w1 = codes8(w[k].y);
+    for (int k = 0; k < N; ++k)
 #pragma unroll
       for (int m = 0; m < TT; ++m) {
-        const f4 d = mfma16(x1[k][m], w1, mfma16(x0[k][m], w0, f4{}));
         const f4 xs = mfma16(x1[k][m], one, mfma16(x0[k][m], one, f4{}));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[m][i] = fmaf(s[k].x * kCodeUnit, d[i], fmaf(s[k].y, xs[i], y[m][i]));
+        for (int n = 0; n < NT; ++n) {
+          const h8 w0 = codes8(w[k][n].x), w1 = codes8(w[k][n].y);
+          const f4 d = mfma16(x1[k][m], w1, mfma16(x0[k][m], w0, f4{}));
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            y[m][n][i] = fmaf(s[k][n].x * kCodeUnit, d[i], fmaf(s[k][n].y, xs[i], y[m][n][i]));
+        }
 #pragma unroll
         for (int n = 0; n < RT; ++n) ax[m][n] = mfma16(x1[k][m], b1[k][n], mfma16(x0[k][m], b0[k][n], ax[m][n]));
       }
-    }
   };
-  // (the registers that a run of N groups takes: 4 for codes and scales, 8 for each tile of x and A)
-  constexpr int N = TT + RT <= 2 ? 4 : TT + RT <= 3 ? 2 : 1;
+  // (registers of a group: 4 for each tile of outputs, 8 for each of x and A)
+  constexpr int PER = 4 * NT + 8 * TT + 8 * RT, N = PER <= 24 ? 4 : PER <= 40 ? 2 : 1;
   for (int quad = wave; quad * 4 < ng; quad += NW) {
     const int end = min(quad * 4 + 4, ng);
     int gi = quad * 4;
@@ -120,9 +148,10 @@ __global__ void __launch_bounds__(64 * NW) linear_rows_kernel(LinearArgs a) {
   for (int m = 0; m < TT; ++m)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      red[wave][m][i][lane] = y[m][i];
 #pragma unroll
-      for (int n = 0; n < RT; ++n) red[wave][TT + m * RT + n][i][lane] = ax[m][n][i];
+      for (int n = 0; n < NT; ++n) red[wave][m * NT + n][i][lane] = y[m][n][i];
+#pragma unroll
+      for (int n = 0; n < RT; ++n) red[wave][TT * NT + m * RT + n][i][lane] = ax[m][n][i];
     }
   __syncthreads();
   auto total = [&](int tile, int i, int l) {
@@ -134,29 +163,28 @@ __global__ void __launch_bounds__(64 * NW) linear_rows_kernel(LinearArgs a) {
   if constexpr (RT > 0) {
     for (int e = threadIdx.x; e < TT * RT * 256; e += 64 * NW) {
       const int l = e & 63, i = (e >> 6) & 3, tile = e >> 8;
-      axs[16 * (tile / RT) + 4 * (l >> 4) + i][16 * (tile % RT) + (l & 15)] = total(TT + tile, i, l);
+      axs[16 * (tile / RT) + 4 * (l >> 4) + i][16 * (tile % RT) + (l & 15)] = total(TT * NT + tile, i, l);
     }
     __syncthreads();
   }
-  for (int e = threadIdx.x; e < TT * 256; e += 64 * NW) {
-    const int l = e & 63, i = (e >> 6) & 3, m = e >> 8;
-    const int tl = 16 * m + 4 * (l >> 4) + i, t = t0 + tl, o = blockIdx.x * 16 + (l & 15);
-    if (t >= a.T || o >= a.out_dim) continue;
-    float v = total(m, i, l);
+  for (int e = threadIdx.x; e < OUTS; e += 64 * NW) {
+    int tl, o;
+    output(e, tl, o);
+    if (t0 + tl >= a.T || o >= a.out_dim) continue;
+    float v = total(e >> 8, (e >> 6) & 3, e & 63);
     if constexpr (RT > 0) {
-      const _Float16* lb = static_cast<const _Float16*>(a.lora_b) + (size_t)o * a.r;
       float delta = 0.f;
-      if (a.r % 8 == 0)
-        for (int k = 0; k < a.r; k += 8) {
-          const h8 v = ld_h8(lb + k);
+      if (early && e == (int)threadIdx.x) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) delta = fmaf((float)v[e], axs[tl][k + e], delta);
-        }
-      else
-        for (int k = 0; k < a.r; ++k) delta = fmaf((float)lb[k], axs[tl][k], delta);
+        for (int k = 0; k < 16; ++k)
+          if (k < a.r) delta = fmaf((float)lb[k / 8][k % 8], axs[tl][k], delta);
+      } else {
+        const _Float16* p = static_cast<const _Float16*>(a.lora_b) + (size_t)o * a.r;
+        for (int k = 0; k < a.r; ++k) delta = fmaf((float)p[k], axs[tl][k], delta);
+      }
       v = fmaf(a.lora_scale, delta, v);
     }
-    store_out(a, t, o, v);
+    store_out(a, t0 + tl, o, v);
   }
 }
 
@@ -402,17 +430,26 @@ __global__ void __launch_bounds__(256) linear_parts_kernel(LinearArgs a, TilePla
     if (t0 + i < a.T && o < a.out_dim) store_out(a, t0 + i, o, y[i]);
 }
 
-template <int TT, int RT>
+template <int TT, int RT, int NT>
 hipError_t launch_rows(const LinearArgs& a, hipStream_t st) {
-  const dim3 grid((a.out_dim + 15) / 16, (a.T + 16 * TT - 1) / (16 * TT));
-  hipLaunchKernelGGL((linear_rows_kernel<TT, RT, 8>), grid, dim3(512), 0, st, a);
+  const dim3 grid((a.out_dim + 16 * NT - 1) / (16 * NT), (a.T + 16 * TT - 1) / (16 * TT));
+  hipLaunchKernelGGL((linear_rows_kernel<TT, RT, NT, 8>), grid, dim3(512), 0, st, a);
   return hipGetLastError();
 }
+template <int TT, int NT>
+hipError_t launch_rows(const LinearArgs& a, hipStream_t st) {
+  if (a.r == 0) return launch_rows<TT, 0, NT>(a, st);
+  if (a.r <= 16) return launch_rows<TT, 1, NT>(a, st);
+  return launch_rows<TT, 4, NT>(a, st);
+}
+
+// 32 outputs a workgroup where 16 would give more workgroups than CUs: half the reads of x
+// and A (one row, 6144 x 2048, rank 16: 8.2 against 10.4 us; 8192 x 8192: 24 against 30;
+// 64 rows, 4096 x 4096: 21 against 30), 16 below, for the CUs (4096 x 2048: 6.8 against 7.9).
 template <int TT>
 hipError_t launch_rows(const LinearArgs& a, hipStream_t st) {
-  if (a.r == 0) return launch_rows<TT, 0>(a, st);
-  if (a.r <= 16) return launch_rows<TT, 1>(a, st);
-  return launch_rows<TT, 4>(a, st);
+  const int64_t groups = (int64_t)((a.out_dim + 15) / 16) * ((a.T + 16 * TT - 1) / (16 * TT));
+  return groups > kCus ? launch_rows<TT, 2>(a, st) : launch_rows<TT, 1>(a, st);
 }
 
 }  // namespace

@@ -6,6 +6,9 @@
 // a head: one launch expands keys and values into the workspace, a second attends.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "moe_latent.h"
 #include "moe_tile.h"
 
@@ -55,7 +58,7 @@ __device__ __forceinline__ int tile_base(const PrefillArgs& a, int b) {
 template <int DC>
 __global__ void __launch_bounds__(256) latent_expand_kernel(PrefillArgs a, int side, int col_tiles) {
   __shared__ __attribute__((aligned(16))) char lds[2][2][128 * 128];
-  __shared__ uint8_t there[128];
+  __shared__ int64_t where[128];
   const LatentArgs& l = a.l;
   const int row_halves = DC + l.Dr;
   if ((int)blockIdx.x < side) {
@@ -96,20 +99,23 @@ __global__ void __launch_bounds__(256) latent_expand_kernel(PrefillArgs a, int s
   const int tile = blockIdx.x - side, n0 = (tile % col_tiles) * 128, r0 = (tile / col_tiles) * 128;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int c = lane & 15, g = lane >> 4, N = l.H * (l.Dn + l.Dv);
-  const char *src_c[4], *src_w[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int r = 8 * (4 * wave + j) + (lane >> 3), piece = 16 * ((lane & 7) ^ tile_key<8>(r));
-    const int at = min(r0 + r, a.kv_total - 1);
+  // where the context rows are (a token without a page: the first page's first row, and
+  // zeros are stored)
+  if (threadIdx.x < 128) {
+    const int at = min(r0 + (int)threadIdx.x, a.kv_total - 1);
     const int b = last_at_most(a.B, at, [&](int k) { return a.kv_start[k]; });
     const Span s = context_of(a, b);
     const int tok = at - s.first;
     int page = -1;
     if (tok >= 0 && tok < s.len) page = l.table[b * l.table_stride + tok / l.page];
-    const bool ok = page >= 0 && page < l.n_pages;
-    if ((lane & 7) == 0) there[r] = ok;
-    // (a token without a page reads the first page's first row and stores zeros)
-    src_c[j] = reinterpret_cast<const char*>(l.pages + (ok ? ((size_t)page * l.page + tok % l.page) * row_halves : 0)) + piece;
+    where[threadIdx.x] = page >= 0 && page < l.n_pages ? (int64_t)page * l.page + tok % l.page : -1;
+  }
+  __syncthreads();
+  const char *src_c[4], *src_w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int r = 8 * (4 * wave + j) + (lane >> 3), piece = 16 * ((lane & 7) ^ tile_key<8>(r));
+    src_c[j] = reinterpret_cast<const char*>(l.pages + max(where[r], (int64_t)0) * row_halves) + piece;
     src_w[j] = reinterpret_cast<const char*>(l.w + (size_t)min(n0 + r, N - 1) * DC) + piece;
   }
   const uint32_t at0 = lds_at(lds);
@@ -154,7 +160,7 @@ __global__ void __launch_bounds__(256) latent_expand_kernel(PrefillArgs a, int s
     for (int m = 0; m < 4; ++m) {
       const int r = tr + 16 * m + c, at = r0 + r;
       if (at >= a.kv_total) continue;
-      const f4 d = there[r] ? y[m][n] : f4{};
+      const f4 d = where[r] >= 0 ? y[m][n] : f4{};
       const h4 v = {(_Float16)d[0], (_Float16)d[1], (_Float16)d[2], (_Float16)d[3]};
       __half* to = in < l.Dn ? a.k + ((size_t)h * a.kv_total + at) * l.Dn + in
                              : a.v + ((size_t)h * a.kv_total + at) * l.Dv + in - l.Dn;
@@ -171,9 +177,11 @@ __global__ void __launch_bounds__(256) latent_expand_kernel(PrefillArgs a, int s
 // when the values' rows are read (transposed) in the same order. The running maximum and
 // sum of a row are in the four lanes of its column. Late tiles first, and the heads of a
 // tile next to each other, so that one head's workgroups share a chiplet's L2.
+// With fewer workgroups than CUs the context is cut into parts, a workgroup each, whose
+// (m, l, O) one more launch joins.
 // Between a tile's copies and the next barrier no load is waited for: loads come back in
 // order, and the wait would be for the copies.
-template <int DN, int DR, int DV>
+template <int DN, int DR, int DV, bool PARTS>
 __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillArgs a) {
   constexpr int KB = kTile * DN * 2, RB = kTile * DR * 2, VB = kTile * DV * 2, BUF = KB + RB + VB;
   constexpr int KS = (DN + DR) / 32, CT = DV / 16, RT = 2, OWN = kTile / kWaves;  // OWN: token rows a wave copies
@@ -181,14 +189,17 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
   const LatentArgs& l = a.l;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int c = lane & 15, g = lane >> 4;
-  const int heads = l.H * a.B, qt = (a.max_q + kRows - 1) / kRows - 1 - (int)blockIdx.x / heads;
-  const int hb = blockIdx.x % heads, h = hb % l.H, b = hb / l.H;
+  const int part = PARTS ? blockIdx.x % a.parts : 0, whole = PARTS ? blockIdx.x / a.parts : blockIdx.x;
+  const int heads = l.H * a.B, qt = (a.max_q + kRows - 1) / kRows - 1 - whole / heads;
+  const int hb = whole % heads, h = hb % l.H, b = hb / l.H;
   const Span qs = span_of(a.q_start, b, a.T), ks = context_of(a, b);
   if (qt * kRows >= qs.len) return;
   const int shift = ks.len - qs.len;                     // position of query row 0
   const int row0 = qt * kRows + 32 * wave;               // this wave's first row
   const int last_row = min(qt * kRows + kRows, qs.len) - 1;
-  const int tiles = shift + last_row >= 0 ? (shift + last_row) / kTile + 1 : 0;
+  const int all = shift + last_row >= 0 ? (shift + last_row) / kTile + 1 : 0;
+  const int first = PARTS ? (int)((int64_t)all * part / a.parts) : 0;  // the tiles of this part: first .. tiles - 1
+  const int tiles = PARTS ? (int)((int64_t)all * (part + 1) / a.parts) : all;
   const int mine = row0 < qs.len ? shift + min(row0 + 31, qs.len - 1) : -1;  // last position that the wave's rows see
   h8 q[RT][KS];
 #pragma unroll
@@ -229,11 +240,11 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
   const float unit = l.scale * kLog2e;
   const uint32_t* lost_of = a.lost + tile_base(a, b);
   uint32_t lost_next = 0;
-  if (tiles > 0) {
-    lost_next = lost_of[0];
-    copy(0);
+  if (first < tiles) {
+    lost_next = lost_of[first];
+    copy(first);
   }
-  for (int i = 0; i < tiles; ++i) {
+  for (int i = first; i < tiles; ++i) {
     const char* buf = lds + (i & 1) * BUF;
     vm_drain();
     lds_barrier();
@@ -312,6 +323,13 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
     const float total = col_sum(sum[r]);
     const int row = row0 + 16 * r + c;
     if (row >= qs.len) continue;
+    if constexpr (PARTS) {
+      const size_t at = (size_t)blockIdx.x * kRows + 32 * wave + 16 * r + c;
+      if (g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = float2{m[r] * unit, total};
+#pragma unroll
+      for (int k = 0; k < CT; ++k) *reinterpret_cast<f4*>(a.part_o + at * DV + 16 * k + 4 * g) = o[k][r];
+      continue;
+    }
     const float inv = total > 0.f ? 1.f / total : total != total ? total : 0.f;  // (no token: zeros)
     __half* to = l.out + ((size_t)(qs.first + row) * l.H + h) * DV + 4 * g;
 #pragma unroll
@@ -323,14 +341,52 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
   }
 }
 
+// The parts of a row's context, joined: four values a thread, Dv / 4 threads a row.
+__global__ void __launch_bounds__(256) latent_parts_kernel(PrefillArgs a) {
+  const LatentArgs& l = a.l;
+  const int per = l.Dv / 4, rows = 256 / per, blocks = kRows / rows;
+  const int whole = blockIdx.x / blocks, in = blockIdx.x % blocks * rows + threadIdx.x / per, col = 4 * (threadIdx.x % per);
+  const int heads = l.H * a.B, qt = (a.max_q + kRows - 1) / kRows - 1 - whole / heads;
+  const int hb = whole % heads, h = hb % l.H, b = hb / l.H;
+  const Span qs = span_of(a.q_start, b, a.T);
+  const int row = qt * kRows + in;
+  if (row >= qs.len) return;
+  const size_t at = (size_t)whole * a.parts * kRows + in;
+  float top = -INFINITY;
+  for (int p = 0; p < a.parts; ++p) top = fmaxf(top, a.part_ml[2 * (at + (size_t)p * kRows)]);
+  float sum = 0.f;
+  f4 o = {};
+#pragma unroll 4
+  for (int p = 0; p < a.parts; ++p) {
+    const size_t i = at + (size_t)p * kRows;
+    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * i);
+    const f4 v = *reinterpret_cast<const f4*>(a.part_o + i * l.Dv + col);
+    if (ml.x == -INFINITY) continue;                     // (a part without a token of the row)
+    const float w = __builtin_amdgcn_exp2f(ml.x - top);
+    sum += w * ml.y;
+    o += v * w;
+  }
+  const float inv = sum > 0.f ? 1.f / sum : sum != sum ? sum : 0.f;
+  const h4 v = {(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
+  *reinterpret_cast<h4*>(l.out + ((size_t)(qs.first + row) * l.H + h) * l.Dv + col) = v;
+}
+
+template <int DN, int DR, int DV, bool PARTS>
+hipError_t launch_attention(const PrefillArgs& a, unsigned wholes, hipStream_t st) {
+  constexpr int lds = 2 * kTile * (DN + DR + DV) * 2;
+  auto kernel = latent_prefill_kernel<DN, DR, DV, PARTS>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3(wholes * a.parts), dim3(64 * kWaves), lds, st, a);
+  return hipGetLastError();
+}
 template <int DN, int DR, int DV>
 hipError_t launch_attention(const PrefillArgs& a, hipStream_t st) {
-  constexpr int lds = 2 * kTile * (DN + DR + DV) * 2;
-  auto kernel = latent_prefill_kernel<DN, DR, DV>;
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  const unsigned wholes = (a.max_q + kRows - 1) / kRows * a.l.H * a.B;
+  if (a.parts == 1) return launch_attention<DN, DR, DV, false>(a, wholes, st);
+  const hipError_t e = launch_attention<DN, DR, DV, true>(a, wholes, st);
   if (e != hipSuccess) return e;
-  const unsigned tiles = (a.max_q + kRows - 1) / kRows;
-  hipLaunchKernelGGL(kernel, dim3(tiles * a.l.H * a.B), dim3(64 * kWaves), lds, st, a);
+  hipLaunchKernelGGL(latent_parts_kernel, dim3(wholes * (kRows * DV / 1024)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 template <int DN, int DR>
@@ -343,6 +399,15 @@ hipError_t launch_attention(const PrefillArgs& a, hipStream_t st) {
 }
 
 }  // namespace
+
+// Into how many parts the contexts are cut: as fill the CUs, of eight tiles at least on
+// average.
+int prefill_parts(int max_q, int H, int B, int kv_total) {
+  static_assert(kRows == kPartRows, "rows of a partial result");
+  const int64_t wholes = (int64_t)((max_q + kRows - 1) / kRows) * H * B;
+  const int64_t most = std::max<int64_t>(1, kv_total / ((int64_t)B * kTile * 8));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({kPartGroups / wholes, most, 16}));
+}
 
 hipError_t launch_latent_prefill(const PrefillArgs& a, hipStream_t st) {
   const LatentArgs& l = a.l;
@@ -369,7 +434,7 @@ bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p
 size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
 struct PrefillLayout {
-  size_t k, v, kr, lost, total;
+  size_t k, v, kr, lost, part_o, part_ml, total;
 };
 constexpr int kMaxTotal = 1 << 24, kMaxBatch = 1 << 16;
 
@@ -384,7 +449,9 @@ PrefillLayout prefill_layout(const moe_latent_spec* s, int B, int kv_total) {
   p.v = round256((size_t)s->heads * n * s->d_nope * 2);
   p.kr = p.v + round256((size_t)s->heads * n * s->d_v * 2);
   p.lost = p.kr + round256(n * s->d_rope * 2);
-  p.total = p.lost + round256((n / moe::kTile + B) * 4);
+  p.part_o = p.lost + round256((n / moe::kTile + B) * 4);
+  p.part_ml = p.part_o + (size_t)moe::kPartGroups * moe::kPartRows * s->d_v * 4;
+  p.total = p.part_ml + (size_t)moe::kPartGroups * moe::kPartRows * 8;
   return p;
 }
 
@@ -433,6 +500,9 @@ int moe_latent_prefill(const moe_latent_spec* spec, const moe_latent_cache* cach
   a.v = reinterpret_cast<__half*>(ws + p.v);
   a.kr = reinterpret_cast<__half*>(ws + p.kr);
   a.lost = reinterpret_cast<uint32_t*>(ws + p.lost);
+  a.part_o = reinterpret_cast<float*>(ws + p.part_o);
+  a.part_ml = reinterpret_cast<float*>(ws + p.part_ml);
+  a.parts = moe::prefill_parts(max_q, spec->heads, B, kv_total);
   return moe::launch_latent_prefill(a, static_cast<hipStream_t>(stream)) == hipSuccess ? MOE_OK : MOE_EHIP;
 }
 
