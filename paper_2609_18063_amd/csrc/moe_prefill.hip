@@ -214,13 +214,15 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
   // rows of P pieces of 16 bytes, R rows a copy; rows past the context repeat its last one
   auto rows = [&](const char* from, int tile, uint32_t to, auto pieces) {
     constexpr int P = decltype(pieces)::value, R = kWave / P;
+    int ln = lane;
+    if constexpr (PARTS) asm volatile("" : "+v"(ln));
     const char* base = from + (size_t)tile * kTile * (P * 16);
     const int most = ks.len - 1 - tile * kTile;
 #pragma unroll
     for (int j = 0; j < (OWN + R - 1) / R; ++j) {
-      const int r0 = OWN * wave + j * R, r = r0 + lane / P;
+      const int r0 = OWN * wave + j * R, r = r0 + ln / P;
       if (R <= OWN || wave % (R / OWN) == 0)             // (a copy of 16 rows is two waves' share)
-        dma16(base, (uint32_t)min(r, most) * (P * 16) + 16 * ((lane % P) ^ tile_key<P>(r)), to + r0 * P * 16);
+        dma16(base, (uint32_t)min(r, most) * (P * 16) + 16 * ((ln % P) ^ tile_key<P>(r)), to + r0 * P * 16);
     }
   };
   const uint32_t at0 = lds_at(lds);
@@ -254,14 +256,18 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
       copy(i + 1);
     }
     if (i * kTile > mine) continue;
+    // (with parts the addresses are formed tile by tile: held, they would spill, and a
+    // register that comes back from memory waits for the copies)
+    int c1 = c, g1 = g, c2 = c, g2 = g;
+    if constexpr (PARTS) asm volatile("" : "+v"(c1), "+v"(g1));
     f4 s[4][RT] = {};
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const int tok = 16 * t + c;
-        const char* p = k < DN / 32 ? buf + tok * DN * 2 + 16 * ((4 * k + g) ^ tile_key<DN / 8>(c))
-                                    : buf + KB + tok * DR * 2 + 16 * ((4 * (k - DN / 32) + g) ^ tile_key<DR / 8>(c));
+        const int tok = 16 * t + c1;
+        const char* p = k < DN / 32 ? buf + tok * DN * 2 + 16 * ((4 * k + g1) ^ tile_key<DN / 8>(c1))
+                                    : buf + KB + tok * DR * 2 + 16 * ((4 * (k - DN / 32) + g1) ^ tile_key<DR / 8>(c1));
         const h8 kk = ld_h8(p);
 #pragma unroll
         for (int r = 0; r < RT; ++r) s[t][r] = mfma16(kk, q[r][k], s[t][r]);
@@ -302,7 +308,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
         for (int k = 0; k < CT; ++k) o[k][r] *= keep;
     }
     const char* vt = buf + KB + RB;
-    const int t0 = 4 * g + (c >> 2);
+    if constexpr (PARTS) asm volatile("" : "+v"(c2), "+v"(g2));
+    const int t0 = 4 * g2 + (c2 >> 2);
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
@@ -310,7 +317,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
         h4 part[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const int tok = 32 * hf + 16 * u + t0, col = 16 * k + 4 * (c & 3);
+          const int tok = 32 * hf + 16 * u + t0, col = 16 * k + 4 * (c2 & 3);
           part[u] = ld_tr(vt + tok * DV * 2 + 16 * ((col >> 3) ^ tile_key<DV / 8>(t0)) + 2 * (col & 7));
         }
         const h8 v = join(part[0], part[1]);
@@ -318,16 +325,20 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
         for (int r = 0; r < RT; ++r) o[k][r] = mfma16(v, p[hf][r], o[k][r]);
       }
   }
+  uint32_t mine_at = blockIdx.x;
+  if constexpr (PARTS) asm volatile("" : "+s"(mine_at));
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const float total = col_sum(sum[r]);
     const int row = row0 + 16 * r + c;
     if (row >= qs.len) continue;
     if constexpr (PARTS) {
-      const size_t at = (size_t)blockIdx.x * kRows + 32 * wave + 16 * r + c;
+      const size_t at = (size_t)mine_at * kRows + 32 * wave + 16 * r + c;
       if (g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = float2{m[r] * unit, total};
+      // (divided by its sum: stored as it is, o would be held twice over the loop, and spill)
+      const float inv = total > 0.f ? 1.f / total : 0.f;
 #pragma unroll
-      for (int k = 0; k < CT; ++k) *reinterpret_cast<f4*>(a.part_o + at * DV + 16 * k + 4 * g) = o[k][r];
+      for (int k = 0; k < CT; ++k) *reinterpret_cast<f4*>(a.part_o + at * DV + 16 * k + 4 * g) = o[k][r] * inv;
       continue;
     }
     const float inv = total > 0.f ? 1.f / total : total != total ? total : 0.f;  // (no token: zeros)
@@ -362,8 +373,8 @@ __global__ void __launch_bounds__(256) latent_parts_kernel(PrefillArgs a) {
     const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * i);
     const f4 v = *reinterpret_cast<const f4*>(a.part_o + i * l.Dv + col);
     if (ml.x == -INFINITY) continue;                     // (a part without a token of the row)
-    const float w = __builtin_amdgcn_exp2f(ml.x - top);
-    sum += w * ml.y;
+    const float w = __builtin_amdgcn_exp2f(ml.x - top) * ml.y;
+    sum += w;
     o += v * w;
   }
   const float inv = sum > 0.f ? 1.f / sum : sum != sum ? sum : 0.f;
