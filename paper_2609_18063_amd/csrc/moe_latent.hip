@@ -135,12 +135,16 @@ struct Walk {
   int t, end;
   int b, s0, s1, s2;        // the sequence at hand, its start, and the next two
   int len0, len1;
+  int starts, lens;         // of sequence `lane`, where a wave's lanes hold them all
   __device__ __forceinline__ void begin(const DecodeArgs& a, int wg) {
+    b = -1;
+    s1 = s2 = 0;
+    const int lane = threadIdx.x & 63;
+    starts = a.starts[min(lane, a.B)];
+    lens = a.kv_len[min(lane, a.B - 1)];
     const int all = ld_scalar(a.starts + a.B), per = share(a);
     t = (int)min((int64_t)all, (int64_t)wg * per);
     end = min(all, t + per);
-    b = -1;
-    s1 = s2 = 0;
   }
   __device__ __forceinline__ bool next(const DecodeArgs& a) {
     while (t < end) {
@@ -166,6 +170,14 @@ struct Walk {
   // start with the next one: the last of equals is the one that has the tile)
   __device__ __forceinline__ void sequence_at(const DecodeArgs& a) {
     if (t < s1) return;
+    if (a.B < kWave) {
+      const int lane = threadIdx.x & 63;
+      b = __popcll(__ballot(lane < a.B && starts <= t)) - 1;
+      s0 = __builtin_amdgcn_readlane(starts, b);
+      s1 = __builtin_amdgcn_readlane(starts, b + 1);
+      len0 = clamp_len(a, __builtin_amdgcn_readlane(lens, b));
+      return;
+    }
     if (t < s2) {
       ++b;
       s0 = s1;
@@ -580,29 +592,30 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
 }
 
 // ---- joining the partial results --------------------------------------------------
-// One query row a workgroup. Its partial results are the runs of workgroups that the plan
-// gave its items' tiles to. All their (m, l) are read at once, for the weights
-// 2^(m - max) / sum; then the thread groups of Dc / 4 (four latent columns a thread) take
-// them in turn. A row without any (no tokens) gives zeros. The latents are rounded to
-// fp16 for the product with W_uv, which is fp16.
-// With few rows 512 threads share a row's partial results, with many 128 do: more rows at
-// once on a CU.
+// A query row's partial results are the runs of workgroups that the plan gave its items'
+// tiles to. All their (m, l) are read at once, for the weights 2^(m - max) / sum; then the
+// thread groups of Dc / 4 (four latent columns a thread) take them in turn. A row without
+// any (no tokens) gives zeros. The latents are rounded to fp16 for the product with W_uv,
+// which is fp16.
 constexpr int kJoinMost = 1024;                          // (partial results of a row: at most the workgroups and its items)
 
 template <int NT>
-__global__ void __launch_bounds__(NT) latent_join_kernel(DecodeArgs a) {
-  __shared__ int first[16], upto[17];                     // of each item: first partial result, those up to it
-  __shared__ float weight[kJoinMost];
-  __shared__ f4 part[NT];
+struct JoinShared {
+  int first[16], upto[17];                               // of each item: first partial result, those up to it
+  float weight[kJoinMost];
+  f4 part[NT];
+};
+// The joined latents 4 i .. 4 i + 3 of a row, in threads i < Dc / 4; the whole workgroup calls.
+template <int NT>
+__device__ __forceinline__ h4 join_row(const DecodeArgs& a, int row, JoinShared<NT>& sh) {
   const LatentArgs& l = a.l;
-  const int row = blockIdx.x, b = row / l.H, h = row % l.H, M = a.p.rows, lane = threadIdx.x & 63;
-  const int per = share(a);
-  const int items = a.p.chunks + 1;
-  const bool own_r = threadIdx.x % kWave == a.p.chunks;   // (the last item is the sequence's own)
+  const int b = row / l.H, h = row % l.H, M = a.p.rows, lane = threadIdx.x & 63;
+  const int per = share(a), items = a.p.chunks + 1;
   if (threadIdx.x < kWave) {
     int w0 = 0, n = 0, index = 0;
-    if (lane < items) {
-      const Item it = own_r ? own_item(a, b, h / M, a.starts[b], clamp_len(a, a.kv_len[b])) : prefix_item(a, lane, row / M);
+    if (lane < items) {                                  // (the last item is the sequence's own)
+      const Item it = lane == a.p.chunks ? own_item(a, b, h / M, a.starts[b], clamp_len(a, a.kv_len[b]))
+                                         : prefix_item(a, lane, row / M);
       index = it.index;
       if (it.tiles > 0) {
         const int from = it.start + kItemCost;
@@ -617,18 +630,18 @@ __global__ void __launch_bounds__(NT) latent_join_kernel(DecodeArgs a) {
       if (lane >= o) up += v;
     }
     if (lane < items) {
-      first[lane] = w0 + index;
-      upto[lane + 1] = up;
+      sh.first[lane] = w0 + index;
+      sh.upto[lane + 1] = up;
     }
-    if (lane == 0) upto[0] = 0;
+    if (lane == 0) sh.upto[0] = 0;
   }
   __syncthreads();
-  const int parts = upto[items];
-  auto seg_of = [&](int i, int& r) {                      // the i-th partial result: where it is, and its row there
+  const int parts = sh.upto[items];
+  auto seg_of = [&](int i, int& r) {                     // the i-th partial result: where it is, and its row there
     int k = 0;
-    while (i >= upto[k + 1]) ++k;
+    while (i >= sh.upto[k + 1]) ++k;
     r = k == items - 1 ? h % M : row % M;
-    return (size_t)(first[k] + i - upto[k]);
+    return (size_t)(sh.first[k] + i - sh.upto[k]);
   };
   // every wave forms the maximum and the sum for itself
   float top = -INFINITY, sum = 0.f;
@@ -646,7 +659,7 @@ __global__ void __launch_bounds__(NT) latent_join_kernel(DecodeArgs a) {
     const float2 a1 = *reinterpret_cast<const float2*>(a.part_ml + ((seg * 2 + 1) * M + r) * 2);
     const float w = a0.x == -INFINITY ? 0.f : exp2_fast(a0.x - top);  // (-inf: every token of it was lost)
     sum += w == 0.f ? 0.f : w * (a0.y + a1.y);
-    if (threadIdx.x < kWave) weight[i] = w;
+    if (threadIdx.x < kWave) sh.weight[i] = w;
   }
   sum = wave_sum(sum);
   __syncthreads();
@@ -656,39 +669,63 @@ __global__ void __launch_bounds__(NT) latent_join_kernel(DecodeArgs a) {
   for (int i = grp; i < parts; i += groups) {
     int r;
     const size_t seg = seg_of(i, r);
-    const float w = weight[i];
+    const float w = sh.weight[i];
     if (w != 0.f) o += *reinterpret_cast<const f4*>(a.part_o + (seg * M + r) * l.Dc + col) * w;
   }
-  part[threadIdx.x] = o;
+  sh.part[threadIdx.x] = o;
   __syncthreads();
-  if (grp == 0) {
-    for (int k = 1; k < groups; ++k) o += part[k * cols + threadIdx.x];
-    const float inv = sum > 0.f ? 1.f / sum : sum != sum ? sum : 0.f;
-    const h4 v = {(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
-    *reinterpret_cast<h4*>(a.lat + (size_t)row * l.Dc + col) = v;
-  }
+  if (grp == 0)
+    for (int k = 1; k < groups; ++k) o += sh.part[k * cols + threadIdx.x];
+  const float inv = sum > 0.f ? 1.f / sum : sum != sum ? sum : 0.f;
+  return h4{(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
+}
+
+// With few rows 512 threads share a row's partial results, with many 128 do: more rows at
+// once on a CU.
+template <int NT>
+__global__ void __launch_bounds__(NT) latent_join_kernel(DecodeArgs a) {
+  __shared__ JoinShared<NT> sh;
+  const h4 v = join_row<NT>(a, blockIdx.x, sh);
+  if ((int)threadIdx.x < a.l.Dc / 4) *reinterpret_cast<h4*>(a.lat + (size_t)blockIdx.x * a.l.Dc + 4 * threadIdx.x) = v;
 }
 
 // ---- out of the latent space --------------------------------------------------------
 // o_h = W_uv,h lat_h: 16 values of one head a workgroup, whose four waves split the
-// latent columns and keep their weights in registers for all sequences.
-template <int DC>
+// latent columns and keep their weights in registers for all sequences. For at most
+// kFewSeqs sequences it joins its head's rows itself (JOIN; the workgroups of a head do
+// that over again): a launch less.
+constexpr int kFewSeqs = 4;
+
+template <int DC, bool JOIN>
 __global__ void __launch_bounds__(256) latent_up_kernel(DecodeArgs a) {
+  constexpr int NT = 256, KS = DC / 128;
   __shared__ f4 red[4][kWave];
+  __shared__ JoinShared<JOIN ? NT : 1> sh;
+  __shared__ __attribute__((aligned(16))) _Float16 joined[JOIN ? kFewSeqs : 1][JOIN ? DC : 8];
   const LatentArgs& l = a.l;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int v0 = blockIdx.x * 16, h = blockIdx.y;
   const int b0 = blockIdx.z * 128, b1 = min(b0 + 128, a.B);
-  constexpr int KS = DC / 128;
   h8 w[KS];
   const __half* wv = l.w + ((size_t)h * (l.Dn + l.Dv) + l.Dn + v0 + c) * DC + wave * (DC / 4) + 8 * g;
 #pragma unroll
   for (int k = 0; k < KS; ++k) w[k] = ld_h8(wv + 32 * k);
+  if constexpr (JOIN) {
+    for (int b = 0; b < a.B; ++b) {
+      const h4 v = join_row<NT>(a, b * l.H + h, sh);
+      if (threadIdx.x < DC / 4) *reinterpret_cast<h4*>(&joined[b][4 * threadIdx.x]) = v;
+      __syncthreads();
+    }
+  }
   for (int bt = b0; bt < b1; bt += 16) {
-    const size_t r = (size_t)min(bt + c, b1 - 1) * l.H + h;
+    const int b = min(bt + c, b1 - 1);
+    const size_t r = (size_t)b * l.H + h;
+    const void* lat = a.lat + r * DC;
+    if constexpr (JOIN) lat = joined[b];
     f4 d = {};
 #pragma unroll
-    for (int k = 0; k < KS; ++k) d = mfma16(w[k], ld_h8(a.lat + r * DC + wave * (DC / 4) + 32 * k + 8 * g), d);
+    for (int k = 0; k < KS; ++k)
+      d = mfma16(w[k], ld_h8(static_cast<const _Float16*>(lat) + wave * (DC / 4) + 32 * k + 8 * g), d);
     red[wave][lane] = d;
     __syncthreads();
     if (wave == 0 && bt + c < b1) {
@@ -698,6 +735,24 @@ __global__ void __launch_bounds__(256) latent_up_kernel(DecodeArgs a) {
     }
     __syncthreads();
   }
+}
+
+template <int DC>
+hipError_t launch_up(const DecodeArgs& a, hipStream_t st) {
+  const LatentArgs& l = a.l;
+  const dim3 grid(l.Dv / 16, l.H, (a.B + 127) / 128), block(256);
+  if (a.B <= kFewSeqs) {
+    hipLaunchKernelGGL((latent_up_kernel<DC, true>), grid, block, 0, st, a);
+    return hipGetLastError();
+  }
+  if (a.B * l.H > 2 * kCus)
+    hipLaunchKernelGGL(latent_join_kernel<128>, dim3(a.B * l.H), dim3(128), 0, st, a);
+  else
+    hipLaunchKernelGGL(latent_join_kernel<512>, dim3(a.B * l.H), dim3(512), 0, st, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((latent_up_kernel<DC, false>), grid, block, 0, st, a);
+  return hipGetLastError();
 }
 
 int tiles_host(int len) { return (len + kStep - 1) / kStep; }
@@ -789,20 +844,7 @@ hipError_t launch_latent_decode(const DecodeArgs& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   e = l.Dc == 512 ? launch_attention<512>(a, st) : l.Dc == 256 ? launch_attention<256>(a, st) : launch_attention<128>(a, st);
   if (e != hipSuccess) return e;
-  if (a.B * l.H > 2 * kCus)
-    hipLaunchKernelGGL(latent_join_kernel<128>, dim3(a.B * l.H), dim3(128), 0, st, a);
-  else
-    hipLaunchKernelGGL(latent_join_kernel<512>, dim3(a.B * l.H), dim3(512), 0, st, a);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const dim3 gu(l.Dv / 16, l.H, (a.B + 127) / 128);
-  if (l.Dc == 512)
-    hipLaunchKernelGGL(latent_up_kernel<512>, gu, dim3(256), 0, st, a);
-  else if (l.Dc == 256)
-    hipLaunchKernelGGL(latent_up_kernel<256>, gu, dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL(latent_up_kernel<128>, gu, dim3(256), 0, st, a);
-  return hipGetLastError();
+  return l.Dc == 512 ? launch_up<512>(a, st) : l.Dc == 256 ? launch_up<256>(a, st) : launch_up<128>(a, st);
 }
 
 // ---- arguments of the calls --------------------------------------------------------
