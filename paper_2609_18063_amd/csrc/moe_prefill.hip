@@ -16,6 +16,7 @@ namespace moe {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kSlack = 8.f;    // (as a power of two)
 constexpr int kWaves = 8, kRows = 32 * kWaves;  // of a workgroup of the attention: waves, query rows
 
 struct Span {
@@ -174,7 +175,7 @@ __global__ void __launch_bounds__(256) latent_expand_kernel(PrefillArgs a, int s
 // 64 context tokens in LDS, copied one ahead, one barrier each. Scores are formed
 // transposed (tokens x rows): a lane then holds its row's weights of the tokens
 // 16 t + 4 g .. + 3, which are the operand of the product with the values as they are,
-// when the values' rows are read (transposed) in the same order. The running maximum and
+// when the values' rows are read (transposed) in the same order. The reference and the
 // sum of a row are in the four lanes of its column. Late tiles first, and the heads of a
 // tile next to each other, so that one head's workgroups share a chiplet's L2.
 // With fewer workgroups than CUs the context is cut into parts, a workgroup each, whose
@@ -233,11 +234,11 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
     rows(vb, tile, buf + KB + RB, std::integral_constant<int, DV / 8>());
   };
   f4 o[CT][RT] = {};
-  float m[RT], sum[RT];                                  // running maximum (of unscaled scores) and sum
+  float m[RT], ref[RT], sum[RT];                         // reference (an unscaled score), m unit (or 0), sum
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     m[r] = -INFINITY;
-    sum[r] = 0.f;
+    ref[r] = sum[r] = 0.f;
   }
   const float unit = l.scale * kLog2e;
   const uint32_t* lost_of = a.lost + tile_base(a, b);
@@ -283,29 +284,42 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
             if (16 * t + e > see || (lost >> t & 1)) s[t][r][e] = -INFINITY;
       }
     }
+    // the reference of a row follows its maximum only where that passes it by kSlack: until
+    // then the weights are at most 2^kSlack, and nothing is rescaled
+    float top[RT];
+    bool far = false;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      top[r] = fmaxf(s[0][r][0], s[0][r][1]);
+#pragma unroll
+      for (int e = 2; e < 16; e += 2) top[r] = max3(top[r], s[e >> 2][r][e & 3], s[e >> 2][r][(e & 3) + 1]);
+      far = far || (top[r] - m[r]) * unit > kSlack;      // (no token so far: any score is)
+    }
+    if (__any(far)) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const float mx = fmaxf(m[r], col_max(top[r])), now = mx == -INFINITY ? 0.f : mx * unit;
+        const float keep = m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[r] - now);
+        m[r] = mx;
+        ref[r] = now;
+        sum[r] *= keep;
+#pragma unroll
+        for (int k = 0; k < CT; ++k) o[k][r] *= keep;
+      }
+    }
     h8 p[2][RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      float top = fmaxf(s[0][r][0], s[0][r][1]);
-#pragma unroll
-      for (int e = 2; e < 16; e += 2) top = max3(top, s[e >> 2][r][e & 3], s[e >> 2][r][(e & 3) + 1]);
-      const float mx = fmaxf(m[r], col_max(top));
-      const float mu = mx == -INFINITY ? 0.f : mx * unit;
-      const float keep = __builtin_amdgcn_exp2f(fmaf(m[r], unit, -mu));
-      m[r] = mx;
       float add = 0.f;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float v = __builtin_amdgcn_exp2f(fmaf(s[t][r][e], unit, -mu));
+          const float v = __builtin_amdgcn_exp2f(fmaf(s[t][r][e], unit, -ref[r]));
           add += v;
           p[t >> 1][r][4 * (t & 1) + e] = (_Float16)v;
         }
-      sum[r] = fmaf(sum[r], keep, add);
-      if (!__all(keep == 1.f))
-#pragma unroll
-        for (int k = 0; k < CT; ++k) o[k][r] *= keep;
+      sum[r] += add;
     }
     const char* vt = buf + KB + RB;
     if constexpr (PARTS) asm volatile("" : "+v"(c2), "+v"(g2));
