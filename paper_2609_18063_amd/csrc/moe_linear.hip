@@ -9,6 +9,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "moe_linear.h"
 #include "moe_tile.h"
@@ -211,16 +212,34 @@ __global__ void __launch_bounds__(512) linear_sums_kernel(LinearArgs a) {
     ad[n] = static_cast<const _Float16*>(a.lora_a) + (size_t)min(16 * n + c, a.r - 1) * a.in_dim + 16 * g;
   f4 ax[RT ? RT : 1] = {};
   const h8 one = ones8();
-  for (int gi = wave; gi < ng; gi += NW) {
-    const h8 x0 = ld_h8(x + 64 * gi), x1 = ld_h8(x + 64 * gi + 8);
-    const f4 xs = mfma16(x1, one, mfma16(x0, one, f4{}));
-    if (c == 0)
+  auto groups = [&](int g0, auto count) {                // N groups, NW apart, asked for at once
+    constexpr int N = decltype(count)::value;
+    h8 x0[N], x1[N], b0[N][RT ? RT : 1], b1[N][RT ? RT : 1];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) es[(4 * g + i) * KE + gi] = xs[i];
+    for (int k = 0; k < N; ++k) {
+      const int gi = g0 + NW * k;
+      x0[k] = ld_h8(x + 64 * gi);
+      x1[k] = ld_h8(x + 64 * gi + 8);
 #pragma unroll
-    for (int n = 0; n < RT; ++n)
-      ax[n] = mfma16(x1, ld_h8(ad[n] + 64 * gi + 8), mfma16(x0, ld_h8(ad[n] + 64 * gi), ax[n]));
-  }
+      for (int n = 0; n < RT; ++n) {
+        b0[k][n] = ld_h8(ad[n] + 64 * gi);
+        b1[k][n] = ld_h8(ad[n] + 64 * gi + 8);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const f4 xs = mfma16(x1[k], one, mfma16(x0[k], one, f4{}));
+      if (c == 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) es[(4 * g + i) * KE + g0 + NW * k] = xs[i];
+#pragma unroll
+      for (int n = 0; n < RT; ++n) ax[n] = mfma16(x1[k], b1[k][n], mfma16(x0[k], b0[k][n], ax[n]));
+    }
+  };
+  constexpr int N = RT <= 1 ? 4 : 2;
+  int gi = wave;
+  for (; gi + (N - 1) * NW < ng; gi += N * NW) groups(gi, std::integral_constant<int, N>());
+  for (; gi < ng; gi += NW) groups(gi, std::integral_constant<int, 1>());
   if constexpr (RT > 0) {
 #pragma unroll
     for (int n = 0; n < RT; ++n)
@@ -319,10 +338,64 @@ __global__ void __launch_bounds__(256, 2) linear_tile_kernel(LinearArgs a, TileP
     dma4(ss + gi, at + XB + CB + 256 * (wave & 1));      // (two waves each write the same scales)
   };
   constexpr int kCopies = 6;
-  f4 y[4][4] = {};
-  int slot = 0;
   copy(from, 0);
   if (from + 1 < to) copy(from + 1, 1);
+  f4 y[4][4] = {};
+  // first the group sums by z and lora_scale A x by B, which the sums then start from
+  const int KE = part ? 0 : linear_extra(a.in_dim, a.r), az = (ng + 31) / 32 * 32;
+  for (int k = 0; k < KE; k += 32) {
+    h8 w[4];                                             // (past the groups or the rank: any weight, times E's zero)
+    const int j = k + 8 * g;
+    if (k < az) {
+      // 32 (s, z) of each output through the last slot, two rows a copy, keyed like x
+      char* zt = ring[2];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int r = 2 * (16 * wave + i) + (lane >> 5), d = (lane & 31) ^ (4 * x_key(r));
+        const size_t row = min(o0 + r, a.out_dim - 1);
+        dma4(static_cast<const uint32_t*>(a.sz) + row * ng + min(k + d, ng - 1), at0 + 2 * SLOT + 256 * (16 * wave + i));
+      }
+      vm_wait<0>();
+      lds_barrier();
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const int r = nw + 16 * n + c;
+        const u4 lo = *reinterpret_cast<const u4*>(zt + 128 * r + 16 * ((2 * g) ^ x_key(r)));
+        const u4 hi = *reinterpret_cast<const u4*>(zt + 128 * r + 16 * ((2 * g + 1) ^ x_key(r)));
+        // the upper halves
+        const u4 z = {__builtin_amdgcn_perm(lo.y, lo.x, 0x07060302u), __builtin_amdgcn_perm(lo.w, lo.z, 0x07060302u),
+                      __builtin_amdgcn_perm(hi.y, hi.x, 0x07060302u), __builtin_amdgcn_perm(hi.w, hi.z, 0x07060302u)};
+        w[n] = __builtin_bit_cast(h8, z);
+      }
+      lds_barrier();
+    } else {
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const _Float16* lb = static_cast<const _Float16*>(a.lora_b) + (size_t)min(ow + 16 * n + c, a.out_dim - 1) * a.r;
+        if (a.r % 8 == 0)
+          w[n] = ld_h8(lb + min(j - az, a.r - 8));
+        else
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[n][e] = lb[min(j + e - az, a.r - 1)];
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const size_t at = (size_t)min(t0 + tw + 16 * m + c, a.T - 1) * KE + j;
+      const h8 hi = ld_h8(a.e_hi + at), lo = ld_h8(a.e_lo + at);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) y[m][n] = mfma16(lo, w[n], mfma16(hi, w[n], y[m][n]));
+    }
+  }
+  if (KE)
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const f4 es = *reinterpret_cast<const f4*>(a.e_scale + t0 + tw + 16 * m + 4 * g);  // (rows past T: not stored)
+#pragma unroll
+      for (int n = 0; n < 4; ++n) y[m][n] *= es;
+    }
+  vm_drain();
+  int slot = 0;
   for (int gi = from; gi < to; ++gi) {
     if (gi + 1 < to)
       vm_wait<kCopies>();
@@ -357,45 +430,6 @@ __global__ void __launch_bounds__(256, 2) linear_tile_kernel(LinearArgs a, TileP
     }
     slot = slot == 2 ? 0 : slot + 1;
   }
-  // the group sums by z and lora_scale A x by B
-  const int KE = part ? 0 : linear_extra(a.in_dim, a.r), az = (ng + 31) / 32 * 32;
-  f4 d[4][4] = {};
-  for (int k = 0; k < KE; k += 32) {
-    h8 w[4];                                             // (past the groups or the rank: any weight, times E's zero)
-    const int j = k + 8 * g;
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const size_t row = min(ow + 16 * n + c, a.out_dim - 1);
-      if (k < az) {
-        const uint32_t* z = static_cast<const uint32_t*>(a.sz) + row * ng;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[n][e] = __builtin_bit_cast(_Float16, (uint16_t)(z[min(j + e, ng - 1)] >> 16));
-      } else {
-        const _Float16* lb = static_cast<const _Float16*>(a.lora_b) + row * a.r;
-        if (a.r % 8 == 0)
-          w[n] = ld_h8(lb + min(j - az, a.r - 8));
-        else
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[n][e] = lb[min(j + e - az, a.r - 1)];
-      }
-    }
-#pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      const size_t at = (size_t)min(t0 + tw + 16 * m + c, a.T - 1) * KE + j;
-      const h8 hi = ld_h8(a.e_hi + at), lo = ld_h8(a.e_lo + at);
-#pragma unroll
-      for (int n = 0; n < 4; ++n) d[m][n] = mfma16(lo, w[n], mfma16(hi, w[n], d[m][n]));
-    }
-  }
-  if (KE)
-#pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      const f4 es = *reinterpret_cast<const f4*>(a.e_scale + t0 + tw + 16 * m + 4 * g);  // (rows past T: not stored)
-#pragma unroll
-      for (int n = 0; n < 4; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[m][n][i] = fmaf(es[i], d[m][n][i], y[m][n][i]);
-    }
   if ((int)blockIdx.x < split) {
     // a tile's sums as the lanes hold them: [m][n] of each wave, four rows a lane
     float* sums = a.sums + (size_t)blockIdx.x * kTileSums + threadIdx.x * 4;
@@ -422,6 +456,7 @@ __global__ void __launch_bounds__(256) linear_parts_kernel(LinearArgs a, TilePla
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const float* sums = a.sums + (size_t)tile * p.parts * kTileSums + mn * 1024 + threadIdx.x * 4;
   f4 y = {};
+#pragma unroll 8
   for (int k = 0; k < p.parts; ++k) y += *reinterpret_cast<const f4*>(sums + (size_t)k * kTileSums);
   const int t0 = tile / p.cols * 128 + (wave & 1) * 64 + 16 * (mn >> 2) + 4 * (lane >> 4);
   const int o = tile % p.cols * 128 + (wave >> 1) * 64 + 16 * (mn & 3) + (lane & 15);
