@@ -205,11 +205,11 @@ __global__ void __launch_bounds__(512) linear_sums_kernel(LinearArgs a) {
   const int t0 = blockIdx.x * 16;
   for (int e = threadIdx.x; e < 16 * KE; e += 512) es[e] = 0.f;
   __syncthreads();
-  const _Float16* x = static_cast<const _Float16*>(a.x) + (size_t)min(t0 + c, a.T - 1) * a.x_stride + 16 * g;
+  const _Float16* x = static_cast<const _Float16*>(a.x) + (size_t)min(t0 + c, a.T - 1) * a.x_stride + 8 * g;
   const _Float16* ad[RT ? RT : 1];
 #pragma unroll
   for (int n = 0; n < RT; ++n)
-    ad[n] = static_cast<const _Float16*>(a.lora_a) + (size_t)min(16 * n + c, a.r - 1) * a.in_dim + 16 * g;
+    ad[n] = static_cast<const _Float16*>(a.lora_a) + (size_t)min(16 * n + c, a.r - 1) * a.in_dim + 8 * g;
   f4 ax[RT ? RT : 1] = {};
   const h8 one = ones8();
   auto groups = [&](int g0, auto count) {                // N groups, NW apart, asked for at once
@@ -219,11 +219,11 @@ __global__ void __launch_bounds__(512) linear_sums_kernel(LinearArgs a) {
     for (int k = 0; k < N; ++k) {
       const int gi = g0 + NW * k;
       x0[k] = ld_h8(x + 64 * gi);
-      x1[k] = ld_h8(x + 64 * gi + 8);
+      x1[k] = ld_h8(x + 64 * gi + 32);
 #pragma unroll
       for (int n = 0; n < RT; ++n) {
         b0[k][n] = ld_h8(ad[n] + 64 * gi);
-        b1[k][n] = ld_h8(ad[n] + 64 * gi + 8);
+        b1[k][n] = ld_h8(ad[n] + 64 * gi + 32);
       }
     }
 #pragma unroll
