@@ -18,7 +18,8 @@
  * - The caller owns every buffer passed in: inputs, outputs and workspaces.
  *   Only the slot-table object and its device table belong to the library.
  * - The hot-path calls (moe_rmsnorm_f16 through moe_topk, and the calls of the
- *   attention block) only enqueue work on `stream`. They never allocate, never synchronise the host, and are
+ *   attention block on device arrays) only enqueue work on `stream`. They
+ *   never allocate, never synchronise the host, and are
  *   safe to capture in a HIP graph.
  * - Return value: MOE_OK (0) or a negative MOE_E* code. A failed argument
  *   check enqueues nothing.
@@ -329,7 +330,10 @@ int moe_topk_biased(const moe_layer_spec* spec, const float* logits, const float
  *   MOE_OUT_F16      fp16, rounded once
  *   MOE_OUT_F32_ADD  fp32, y += (the residual's form)
  * y must not overlap x. in_dim: a multiple of 64 up to 32768; out_dim: 1 ..
- * 2^20; T up to 2^20. The order of a row's sums depends on T, not on the other rows.
+ * 2^20; T up to 2^20, T out_dim up to 2^37. The order of a row's sums depends on
+ * T and its place among them, not on the other rows. (s (q . x) and z sum(x) of
+ * a group are formed apart: a row with an infinite input may give NaN where
+ * W x is infinite.)
  * workspace: moe_linear_workspace_bytes(out_dim, in_dim, rank, T) (it grows with T
  * and rank; no initial contents needed). Calls that share one workspace must
  * be ordered on one stream.
@@ -412,8 +416,8 @@ int moe_latent_append(const moe_latent_spec* spec, const moe_latent_cache* cache
  * A prefix that the whole batch shares: prefix_pages, device int32 ids of its
  * ceil(prefix_len / page_tokens) pages (NULL with prefix_len 0). Every sequence
  * attends to the prefix_len tokens of it and to its own kv_len; the prefix is
- * read once for many sequences. A row that has no token gives zeros.
- * B up to n_seqs. workspace: moe_latent_decode_workspace_bytes (no initial
+ * read once for many sequences. A row that has no token, or whose scores are
+ * all minus infinity, gives zeros. B up to n_seqs. workspace: moe_latent_decode_workspace_bytes (no initial
  * contents needed); calls that share one must be ordered on one stream.
  */
 size_t moe_latent_decode_workspace_bytes(const moe_latent_spec* spec, int B, int max_len, int prefix_len);
@@ -430,8 +434,8 @@ int moe_latent_decode(const moe_latent_spec* spec, const moe_latent_cache* cache
  * already written, the chunk's own among them), and each attends to the
  * tokens up to its own position.
  * q_start, kv_start: device int32 [B + 1], ascending from 0 or more. T,
- * kv_total and max_q: bounds on the last q_start, the last kv_start and the
- * longest chunk. q_f16: device fp16 [T][H][d_nope + d_rope], rotated; out_f16:
+ * kv_total and max_q (up to T): bounds on the last q_start, the last kv_start
+ * and the longest chunk. q_f16: device fp16 [T][H][d_nope + d_rope], rotated; out_f16:
  * [T][H][d_v]; rows behind the last sequence are left as they were.
  * Lists that break these rules, a chunk longer than its context or a context
  * longer than the table set MOE_STATUS_BAD_LENGTH, and what is computed then is

@@ -718,12 +718,28 @@ def _need(ok, what):
         raise ValueError(what)
 
 
+def _current_device():
+    import torch
+    return torch.cuda.current_device()
+
+
 def _dense(what, dtype, *tensors):
-    """Contiguous tensors of one dtype on one GPU: the library sees addresses only."""
+    """Contiguous tensors of one dtype on the current GPU: the library sees addresses only, and launches there."""
+    here = _current_device() if tensors[0].is_cuda else -1
     for t in tensors:
-        if t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
-            raise ValueError("%s: a contiguous %s tensor on the GPU is needed, got %s %s on %s"
+        if t.dtype != dtype or not t.is_contiguous() or here < 0 or t.get_device() != here:
+            raise ValueError("%s: a contiguous %s tensor on the current GPU is needed, got %s %s on %s"
                              % (what, dtype, t.dtype, tuple(t.stride()), t.device))
+
+
+def _status(status):
+    if status is not None:
+        import torch
+        _dense("status", torch.int32, status)
+
+
+def _room(workspace):
+    _dense("workspace", workspace.dtype, workspace)
 
 
 def linear_workspace_bytes(out_dim, in_dim, rank, T):
@@ -741,7 +757,8 @@ def linear_int4(proj, out_dim, in_dim, rank, lora_scale, x, y, workspace, add=Fa
     _need((f16 or y.dtype == torch.float32) and tuple(y.shape) == (T, out_dim) and (out_dim == 1 or y.stride(1) == 1),
           "y: fp32 or fp16 [T, out] with unit column stride")
     _need(not (add and f16), "add needs an fp32 y")
-    _need(x.is_cuda and x.device == y.device == workspace.device, "x, y and the workspace on one GPU")
+    _room(workspace)
+    _need(x.device == y.device == workspace.device, "x, y and the workspace on one GPU")
     _check(lib().moe_linear_int4_lora(ctypes.byref(proj), out_dim, in_dim, rank, lora_scale, _ptr(x),
                                       x.stride(0) if T > 1 else in_dim, T, _ptr(y),
                                       MOE_OUT_F16 if f16 else MOE_OUT_F32_ADD if add else MOE_OUT_F32,
@@ -775,8 +792,11 @@ def latent_cache(pages, table):
     return c
 
 
-def _cache_of(spec, cache):
+def _cache_of(spec, cache, status):
+    import torch
     pages = cache.keep[0]
+    _dense("pages", torch.float16, pages)
+    _status(status)
     _need(tuple(pages.shape[1:]) == (spec.page_tokens, spec.d_latent + spec.d_rope),
           "pages of %d tokens of %d" % (spec.page_tokens, spec.d_latent + spec.d_rope))
 
@@ -786,7 +806,7 @@ def latent_append(spec, cache, kv, gamma, rope, seq, pos, status, q=None, q_out=
     d_rope / 2, 2]``, ``seq`` / ``pos`` int32 ``[T]``, ``q`` / ``q_out`` fp16 ``[T, H, d_nope + d_rope]``."""
     import torch
     T = kv.shape[0]
-    _cache_of(spec, cache)
+    _cache_of(spec, cache, status)
     _dense("kv, rope", torch.float32, kv, rope)
     _dense("seq, pos", torch.int32, seq, pos)
     _dense("gamma", torch.float16, gamma)
@@ -807,9 +827,10 @@ def latent_decode_workspace_bytes(spec, B, max_len, prefix_len=0):
     return int(lib().moe_latent_decode_workspace_bytes(ctypes.byref(spec), B, max_len, prefix_len))
 
 
-def _attends(spec, cache, w_kvb, q, out):
+def _attends(spec, cache, w_kvb, q, out, status, workspace):
     import torch
-    _cache_of(spec, cache)
+    _cache_of(spec, cache, status)
+    _room(workspace)
     _dense("w_kvb, q, out", torch.float16, w_kvb, q, out)
     _need(tuple(w_kvb.shape) == (spec.heads, spec.d_nope + spec.d_v, spec.d_latent)
           and tuple(q.shape[1:]) == (spec.heads, spec.d_nope + spec.d_rope)
@@ -823,7 +844,7 @@ def latent_decode(spec, cache, w_kvb, q, kv_len, max_len, out, status, workspace
     ids of ``prefix_len`` tokens that every sequence of the batch begins with."""
     import torch
     B = q.shape[0]
-    _attends(spec, cache, w_kvb, q, out)
+    _attends(spec, cache, w_kvb, q, out, status, workspace)
     _dense("kv_len", torch.int32, kv_len)
     _need(kv_len.numel() == B, "kv_len [B]")
     if prefix_len:
@@ -841,7 +862,7 @@ def latent_prefill_workspace_bytes(spec, B, kv_total):
 def latent_prefill(spec, cache, w_kvb, q, q_start, kv_start, kv_total, max_q, out, status, workspace, stream=None):
     """moe_latent_prefill: ``q`` fp16 ``[T, H, d_nope + d_rope]``, ``q_start`` / ``kv_start`` int32 ``[B + 1]``."""
     import torch
-    _attends(spec, cache, w_kvb, q, out)
+    _attends(spec, cache, w_kvb, q, out, status, workspace)
     _dense("q_start, kv_start", torch.int32, q_start, kv_start)
     _need(q_start.numel() == kv_start.numel() >= 1, "q_start and kv_start [B + 1]")
     _check(lib().moe_latent_prefill(ctypes.byref(spec), ctypes.byref(cache), _ptr(w_kvb), _ptr(q), q.shape[0],
@@ -909,9 +930,11 @@ def page_copy(pages, pairs, status, stream=None):
     """moe_page_copy on ``pages [n_layers, n_pages, ...]`` (pages contiguous, layers may be strided); ``pairs``
     int32 ``[n, 2]`` on the GPU."""
     import torch
+    _need(pages.dim() >= 3 and pages.shape[0] > 0 and pairs.dim() == 2 and pairs.shape[1] == 2,
+          "pages [n_layers, n_pages, ...], pairs [n, 2]")
     _dense("pages of a layer", pages.dtype, pages[0])
     _dense("pairs", torch.int32, pairs)
-    _need(pages.dim() >= 3 and pairs.dim() == 2 and pairs.shape[1] == 2, "pages [n_layers, n_pages, ...], pairs [n, 2]")
+    _status(status)
     size = pages.element_size()
     _check(lib().moe_page_copy(_ptr(pages), pages.shape[0], pages.stride(0) * size, pages.stride(1) * size,
                                pages.shape[1], _ptr(pairs), pairs.shape[0], _ptr(status), _stream(stream)),
@@ -922,6 +945,7 @@ def page_remap(table, remap, table_out, status, stream=None):
     """moe_page_remap: int32 tensors; ``table_out`` may be ``table``."""
     import torch
     _dense("table, remap, table_out", torch.int32, table, remap, table_out)
+    _status(status)
     _need(table_out.numel() == table.numel(), "tables of one size")
     _check(lib().moe_page_remap(_ptr(table), table.numel(), _ptr(remap), remap.numel(), _ptr(table_out), _ptr(status),
                                 _stream(stream)), "moe_page_remap")

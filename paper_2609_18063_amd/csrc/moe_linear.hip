@@ -517,10 +517,11 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t st) {
 namespace {
 
 constexpr int kMaxIn = 32768, kMaxOut = 1 << 20, kMaxRows = 1 << 20;
+constexpr int64_t kMaxOutputs = int64_t(1) << 37;      // (a grid's threads: 2^24 tiles of 128 x 128, 256 each)
 
 bool linear_shape_ok(int out_dim, int in_dim, int rank, int T) {
   return out_dim >= 1 && out_dim <= kMaxOut && in_dim >= 64 && in_dim <= kMaxIn && in_dim % 64 == 0 &&
-         rank >= 0 && rank <= 64 && T >= 0 && T <= kMaxRows;
+         rank >= 0 && rank <= 64 && T >= 0 && T <= kMaxRows && (int64_t)T * out_dim <= kMaxOutputs;
 }
 size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }

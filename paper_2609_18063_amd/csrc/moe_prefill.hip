@@ -498,7 +498,7 @@ int moe_latent_prefill(const moe_latent_spec* spec, const moe_latent_cache* cach
   if (!prefill_shape_ok(spec, T, B, kv_total) || B > cache->n_seqs || max_q < 0 || max_q > T)
     return MOE_EINVAL;
   if (T == 0 || B == 0) return T == 0 ? MOE_OK : MOE_EINVAL;
-  if (max_q < 1 || (int64_t)((max_q + moe::kTile - 1) / moe::kTile) * spec->heads * B * 256 > (int64_t)UINT32_MAX ||
+  if (max_q < 1 || (int64_t)((max_q + moe::kPartRows - 1) / moe::kPartRows) * spec->heads * B * 512 > (int64_t)UINT32_MAX ||
       (int64_t)(kv_total / 128 + 1) * spec->heads * 2 * 256 + ((int64_t)kv_total / moe::kTile + B) * 256 >
           (int64_t)UINT32_MAX)
     return MOE_EINVAL;  // (a grid's threads)

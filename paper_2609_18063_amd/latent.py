@@ -18,7 +18,8 @@ from . import binding as B
 
 
 class LatentCache:
-    """Pages of every layer and the page tables of up to ``n_seqs`` sequences (the same page ids in every layer)."""
+    """Pages of every layer and the page tables of up to ``n_seqs`` sequences (the same page ids in every layer).
+    Tables and pages change on the current stream, which has to be the one that reads them."""
 
     def __init__(self, spec, n_layers, n_pages, n_seqs, max_tokens):
         P = spec.page_tokens
@@ -44,8 +45,15 @@ class LatentCache:
         self.ids[seq], self.tokens[seq] = [], 0
         return seq
 
+    def _live(self, seq):
+        if not 0 <= seq < len(self.ids) or self.ids[seq] is None:
+            raise ValueError("there is no sequence %d" % seq)
+
     def grow(self, seq, n):
         """Room for ``n`` more tokens of ``seq``; returns the position of the first."""
+        self._live(seq)
+        if n < 0:
+            raise ValueError("sequence %d cannot grow by %d tokens" % (seq, n))
         at = self.tokens[seq]
         need = -(-(at + n) // self.spec.page_tokens) - len(self.ids[seq])
         if len(self.ids[seq]) + need > self.max_pages:
@@ -58,6 +66,7 @@ class LatentCache:
 
     def fork(self, seq):
         """A new sequence with ``seq``'s tokens: its full pages shared, the last one copied."""
+        self._live(seq)
         new = self.start()
         try:
             self.ids[new], pairs = self.pool.fork(self.ids[seq], self.tokens[seq])
@@ -71,8 +80,12 @@ class LatentCache:
         return new
 
     def end(self, seq):
+        """Give ``seq``'s pages back. Its table row is cleared: a call that still names it flags
+        ``MOE_STATUS_BAD_PAGE`` and touches no page that another sequence has by then."""
+        self._live(seq)
         self.pool.free(self.ids[seq])
         self.ids[seq], self.tokens[seq] = None, 0
+        self.table[seq].fill_(-1)
 
     def compact(self):
         """Move the live pages to the lowest ids, in the tables too; returns the number of pages moved."""
@@ -150,7 +163,8 @@ class LatentAttention:
         self._out(n, r)
 
     def prefill(self, n, x, r, seq, pos, q_start, kv_start, kv_total, max_q):
-        """Layer ``n`` for chunks of prompts: the ragged batch of ``moe_latent_prefill``, sequence b in table row b."""
+        """Layer ``n`` for chunks of prompts: the ragged batch of ``moe_latent_prefill``, sequence b in table row b.
+        Eager only: its workspace grows with ``kv_total``."""
         q = self._project(n, x, seq, pos)
         need = B.latent_prefill_workspace_bytes(self.spec, q_start.numel() - 1, kv_total)
         if self.ws_prefill is None or self.ws_prefill.nbytes < need:

@@ -241,3 +241,82 @@ def test_binding_checks(B):
         B.linear_int4(p, 64, 128, 0, 0.0, x, y.half(), ws, add=True)
     with pytest.raises(ValueError):
         B.page_copy(torch.zeros(2, 4, 16), torch.zeros(1, 2, dtype=torch.int32), None)
+
+
+def test_grids_past_the_launch_limit(B):
+    """Calls whose grids would hold 2^32 threads or more are refused before any launch."""
+    assert _linear(B, out=1 << 20, ys=1 << 20, T=1 << 18, wb=1 << 40) == B.MOE_EINVAL
+    assert B.linear_workspace_bytes(1 << 20, 128, 4, 1 << 18) == 0
+    assert B.linear_workspace_bytes(1 << 20, 128, 4, 1 << 17) > 0
+    spec, cache = _spec(B, heads=128), _cache(B, n_seqs=1 << 16)
+    assert B.lib().moe_latent_prefill(ctypes.byref(spec), ctypes.byref(cache), P[2], P[3], 1 << 16, P[4], P[5], 1 << 16, 1 << 16, 1,
+                                      P[6], P[7], P[8], 1 << 60, None) == B.MOE_EINVAL
+
+
+class _OnGpu:
+    """What the binding's checks ask of a tensor, for a device that is not there."""
+
+    is_cuda = True
+
+    def __init__(self, dtype, device=0, contiguous=True):
+        self.dtype, self.device, self.contiguous = dtype, device, contiguous
+
+    def is_contiguous(self):
+        return self.contiguous
+
+    def get_device(self):
+        return self.device
+
+    def stride(self):
+        return (1,)
+
+
+def test_binding_wants_the_current_device(B, monkeypatch):
+    import torch
+    monkeypatch.setattr(B, "_current_device", lambda: 1)
+    i32 = torch.int32
+    B._dense("t", i32, _OnGpu(i32, 1), _OnGpu(i32, 1))
+    B._status(None)
+    B._status(_OnGpu(i32, 1))
+    B._room(_OnGpu(torch.uint8, 1))
+    for bad in (_OnGpu(i32, 0), _OnGpu(torch.int64, 1), _OnGpu(i32, 1, False), torch.zeros(2, dtype=i32)):
+        for call in (lambda: B._dense("t", i32, bad), lambda: B._dense("t", i32, _OnGpu(i32, 1), bad), lambda: B._status(bad)):
+            with pytest.raises(ValueError):
+                call()
+    for bad in (_OnGpu(i32, 0), _OnGpu(i32, 1, False), torch.zeros(2)):
+        with pytest.raises(ValueError):
+            B._room(bad)
+    with pytest.raises(ValueError):
+        B.page_copy(torch.zeros(0, 4, 16), torch.zeros(1, 2, dtype=i32), None)
+
+
+def test_sequences_of_a_cache(B, monkeypatch):
+    """The host's side of a cache: growth, ends and forks of sequences that are not there are refused."""
+    import torch
+    from paper_2609_18063_amd import latent
+    made = {n: getattr(torch, n) for n in ("zeros", "full")}
+    for n, f in made.items():
+        monkeypatch.setattr(torch, n, lambda *a, _f=f, device=None, **k: _f(*a, **k))
+    monkeypatch.setattr(B, "latent_cache", lambda pages, table: None)
+    cache = latent.LatentCache(_spec(B), 1, 6, 3, 64)
+    a = cache.start()
+    assert cache.grow(a, 0) == 0 and cache.grow(a, 32) == 0 and cache.grow(a, 16) == 32
+    for call in (lambda: cache.grow(a, -1), lambda: cache.grow(1, 1), lambda: cache.grow(3, 1), lambda: cache.grow(-1, 1),
+                 lambda: cache.end(1), lambda: cache.fork(2), lambda: cache.grow(a, 17)):
+        with pytest.raises(ValueError):
+            call()
+    assert cache.ids == [[0, 1, 2], None, None] and cache.tokens == [48, 0, 0] and cache.pool.available() == 3
+    b = cache.fork(a)                                     # (48 tokens: whole pages, nothing to copy)
+    assert cache.ids[b] == [0, 1, 2] and cache.pool.refs(1) == 2
+    cache.grow(b, 1)
+    cache.end(a)
+    assert cache.table[a].tolist() == [-1] * 4 and cache.table[b].tolist() == [0, 1, 2, 3]
+    with pytest.raises(ValueError):
+        cache.end(a)
+    c = cache.start()
+    assert c == a
+    cache.grow(c, 32)
+    with pytest.raises(B.MoeError):
+        cache.grow(c, 32)                                 # two more pages than are free: nothing changes
+    assert cache.ids[c] == [4, 5] and cache.tokens[c] == 32 and cache.table[c].tolist() == [4, 5, -1, -1]
+    cache.close()
