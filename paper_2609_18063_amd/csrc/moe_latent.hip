@@ -9,6 +9,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "moe_latent.h"
 #include "moe_tile.h"
@@ -605,9 +606,10 @@ struct JoinShared {
   float weight[kJoinMost];
   f4 part[NT];
 };
-// The joined latents 4 i .. 4 i + 3 of a row, in threads i < Dc / 4; the whole workgroup calls.
+// The joined latents of one of `slices` slices of a row: its 4 i .. 4 i + 3 in threads
+// i < Dc / (4 slices); the whole workgroup calls.
 template <int NT>
-__device__ __forceinline__ h4 join_row(const DecodeArgs& a, int row, JoinShared<NT>& sh) {
+__device__ __forceinline__ h4 join_row(const DecodeArgs& a, int row, int slice, int slices, JoinShared<NT>& sh) {
   const LatentArgs& l = a.l;
   const int b = row / l.H, h = row % l.H, M = a.p.rows, lane = threadIdx.x & 63;
   const int per = share(a), items = a.p.chunks + 1;
@@ -663,7 +665,8 @@ __device__ __forceinline__ h4 join_row(const DecodeArgs& a, int row, JoinShared<
   }
   sum = wave_sum(sum);
   __syncthreads();
-  const int cols = l.Dc / 4, groups = NT / cols, grp = threadIdx.x / cols, col = 4 * (threadIdx.x % cols);
+  const int cols = l.Dc / 4 / slices, groups = NT / cols, grp = threadIdx.x / cols;
+  const int col = 4 * (slice * cols + threadIdx.x % cols);
   f4 o = {};
 #pragma unroll 4
   for (int i = grp; i < parts; i += groups) {
@@ -680,28 +683,33 @@ __device__ __forceinline__ h4 join_row(const DecodeArgs& a, int row, JoinShared<
   return h4{(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
 }
 
-// With few rows 512 threads share a row's partial results, with many 128 do: more rows at
-// once on a CU.
+// With few rows 512 threads share a row's partial results, and its columns are cut into
+// slices that are workgroups of their own (16 heads over 16,000 tokens, 250 partial results
+// a row: the whole call in 34 us with four slices, 55 without); with many 128 do, so that
+// more rows are on a CU at once (2048 rows: 13.4 us against 21; 32 rows: 14.6 against 5.9).
+// Bound by the partial results' reads, which the decode launch has just left in the L2s.
 template <int NT>
 __global__ void __launch_bounds__(NT) latent_join_kernel(DecodeArgs a) {
   __shared__ JoinShared<NT> sh;
-  const h4 v = join_row<NT>(a, blockIdx.x, sh);
-  if ((int)threadIdx.x < a.l.Dc / 4) *reinterpret_cast<h4*>(a.lat + (size_t)blockIdx.x * a.l.Dc + 4 * threadIdx.x) = v;
+  const int cols = a.l.Dc / 4 / gridDim.y, i = blockIdx.y * cols + threadIdx.x;
+  const h4 v = join_row<NT>(a, blockIdx.x, blockIdx.y, gridDim.y, sh);
+  if ((int)threadIdx.x < cols) *reinterpret_cast<h4*>(a.lat + (size_t)blockIdx.x * a.l.Dc + 4 * i) = v;
 }
 
 // ---- out of the latent space --------------------------------------------------------
 // o_h = W_uv,h lat_h: 16 values of one head a workgroup, whose four waves split the
-// latent columns and keep their weights in registers for all sequences. For at most
-// kFewSeqs sequences it joins its head's rows itself (JOIN; the workgroups of a head do
-// that over again): a launch less.
-constexpr int kFewSeqs = 4;
+// latent columns and keep their weights in registers for all sequences. For one short
+// sequence it joins its head's row itself (JOIN; the workgroups of a head do that over
+// again): a launch less (16 heads over 100 tokens: the call in 15.6 us against 18.1; 500
+// tokens: 17.3, 18.4; 1,000 tokens: 19.7, 18.6; two sequences of 500: 21.6, 18.4).
+constexpr int kFusedTiles = 24;
 
 template <int DC, bool JOIN>
 __global__ void __launch_bounds__(256) latent_up_kernel(DecodeArgs a) {
   constexpr int NT = 256, KS = DC / 128;
   __shared__ f4 red[4][kWave];
   __shared__ JoinShared<JOIN ? NT : 1> sh;
-  __shared__ __attribute__((aligned(16))) _Float16 joined[JOIN ? kFewSeqs : 1][JOIN ? DC : 8];
+  __shared__ __attribute__((aligned(16))) _Float16 joined[JOIN ? DC : 8];
   const LatentArgs& l = a.l;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int v0 = blockIdx.x * 16, h = blockIdx.y;
@@ -711,17 +719,15 @@ __global__ void __launch_bounds__(256) latent_up_kernel(DecodeArgs a) {
 #pragma unroll
   for (int k = 0; k < KS; ++k) w[k] = ld_h8(wv + 32 * k);
   if constexpr (JOIN) {
-    for (int b = 0; b < a.B; ++b) {
-      const h4 v = join_row<NT>(a, b * l.H + h, sh);
-      if (threadIdx.x < DC / 4) *reinterpret_cast<h4*>(&joined[b][4 * threadIdx.x]) = v;
-      __syncthreads();
-    }
+    const h4 v = join_row<NT>(a, h, 0, 1, sh);
+    if (threadIdx.x < DC / 4) *reinterpret_cast<h4*>(&joined[4 * threadIdx.x]) = v;
+    __syncthreads();
   }
   for (int bt = b0; bt < b1; bt += 16) {
     const int b = min(bt + c, b1 - 1);
     const size_t r = (size_t)b * l.H + h;
     const void* lat = a.lat + r * DC;
-    if constexpr (JOIN) lat = joined[b];
+    if constexpr (JOIN) lat = joined;
     f4 d = {};
 #pragma unroll
     for (int k = 0; k < KS; ++k)
@@ -737,25 +743,27 @@ __global__ void __launch_bounds__(256) latent_up_kernel(DecodeArgs a) {
   }
 }
 
+int tiles_host(int len) { return (len + kStep - 1) / kStep; }
+
 template <int DC>
 hipError_t launch_up(const DecodeArgs& a, hipStream_t st) {
   const LatentArgs& l = a.l;
   const dim3 grid(l.Dv / 16, l.H, (a.B + 127) / 128), block(256);
-  if (a.B <= kFewSeqs) {
+  if (a.B == 1 && a.prefix_len == 0 && tiles_host(a.max_len) <= kFusedTiles) {
     hipLaunchKernelGGL((latent_up_kernel<DC, true>), grid, block, 0, st, a);
     return hipGetLastError();
   }
-  if (a.B * l.H > 2 * kCus)
-    hipLaunchKernelGGL(latent_join_kernel<128>, dim3(a.B * l.H), dim3(128), 0, st, a);
+  const int rows = a.B * l.H;
+  if (rows > 2 * kCus)
+    hipLaunchKernelGGL(latent_join_kernel<128>, dim3(rows), dim3(128), 0, st, a);
   else
-    hipLaunchKernelGGL(latent_join_kernel<512>, dim3(a.B * l.H), dim3(512), 0, st, a);
+    hipLaunchKernelGGL(latent_join_kernel<512>, dim3(rows, rows <= kCus / 2 ? 4 : rows <= kCus ? 2 : 1), dim3(512), 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((latent_up_kernel<DC, false>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 
-int tiles_host(int len) { return (len + kStep - 1) / kStep; }
 size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
 template <int DC, int DR, int MT>
@@ -783,14 +791,24 @@ hipError_t launch_attention(const DecodeArgs& a, hipStream_t st) {
 
 DecodePlan decode_plan(int H, int Dc, int Dr, int B, int max_len, int prefix_len) {
   DecodePlan p{};
-  const int most = prefix_len > 0 ? std::max(H, std::min(B * H, 64)) : H;
-  p.rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
+  const int pt = tiles_host(prefix_len);
+  // The fewest rows that hold a sequence's heads (more would be idle in its own tiles), and
+  // with a prefix as many more as keep its tiles, which all sequences' rows share, under 12 a
+  // CU (16 heads, 8 sequences, 4,000 shared tokens: 29.8 us with 16 rows, 40.8 with 64; 32
+  // sequences, 12,000 tokens: 99.7, 52.6; 32 heads, 16 sequences, 8,000: 47.3 with 32, 45.4).
+  p.rows = H <= 16 ? 16 : H <= 32 ? 32 : 64;
+  while (p.rows < 64 && (int64_t)pt * ((B * H + p.rows - 1) / p.rows) > 12 * kCus) p.rows *= 2;
   p.head_blocks = (H + p.rows - 1) / p.rows;
   p.row_blocks = prefix_len > 0 ? (B * H + p.rows - 1) / p.rows : 0;
-  const int pt = tiles_host(prefix_len);
-  const int wgs = kCus * (Dc <= 128 ? 3 : Dc <= 256 ? 2 : 1);
+  // (one workgroup a CU has the whole LDS and fewer partial results; two pay for the small
+  // tiles of 128 latents: 64 sequences of 4,000 tokens 40.1 us against 44.9, with 256 latents,
+  // 32 heads, 32 of 6,000 47.7 against 40.9)
+  const int wgs = kCus * (Dc <= 128 ? 2 : 1);
   const long long own = (long long)B * p.head_blocks * (max_len > 0 ? tiles_host(max_len) + kItemCost : 0);
-  p.least = 1;
+  // A share of fewer tiles leaves more partial results than it saves time: about
+  // sqrt(tiles) / 6 of a sequence (one of 16,000 tokens, 16 heads: 34 us with 2, 29.6 with 4,
+  // 30.5 with 6; of 3,000: 20.4 with 2, 21.7 with 4).
+  p.least = std::max(1, (int)(0.18 * std::sqrt((double)tiles_host(max_len)) + 0.5));
   if (prefix_len > 0) {
     // Token chunks of the prefix such that a row block of a chunk is just one workgroup's
     // share: as many as leave workgroups enough for the sequences' own tiles. Then no

@@ -18,12 +18,14 @@ struct LinearArgs {
   float* sums;                           // of tiles split along the inputs
 };
 
-constexpr int kRowsMost = 64;            // rows up to which the weights are read once for all
+constexpr int kRowsMost = 192;           // rows that the kernel without tiles takes at most
 constexpr size_t kLinearSums = 32u << 20;
 
 // Inputs that the group sums and the adapter add to a row's products.
 constexpr int linear_extra(int in_dim, int r) { return (in_dim / 64 + 31) / 32 * 32 + (r + 31) / 32 * 32; }
 
+// Whether the call goes without tiles (it does at fewer rows too, then).
+bool linear_by_rows(int out_dim, int in_dim, int T);
 hipError_t launch_linear(const LinearArgs& a, hipStream_t st);
 
 }  // namespace moe

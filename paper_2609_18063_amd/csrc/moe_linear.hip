@@ -489,9 +489,20 @@ hipError_t launch_rows(const LinearArgs& a, hipStream_t st) {
 
 }  // namespace
 
+// The rows kernel as long as its workgroups (32 outputs by 32 rows) are on the CUs at once,
+// or twice that where the inputs are few: it has one launch and reads the weights once per
+// 32 rows, from L2 after the first time. Against the tiles, us: 64 rows 4096 x 4096, rank 32
+// (256 workgroups) 27 : 40, 80 rows (384) 49 : 40; 8192 x 8192, 32 rows (256) 38 : 58, 64
+// rows (512) 73 : 60; 6144 x 2048, 64 rows (384) 22 : 27, 80 rows (576) 29 : 27; 640 x 2048,
+// 192 rows (120) 9.5 : 19.
+bool linear_by_rows(int out_dim, int in_dim, int T) {
+  const int64_t groups = (int64_t)((out_dim + 31) / 32) * ((T + 31) / 32);
+  return T <= 16 || (T <= kRowsMost && groups <= (in_dim <= 2048 ? 2 : 1) * kCus);
+}
+
 hipError_t launch_linear(const LinearArgs& a, hipStream_t st) {
   if (a.T <= 16) return launch_rows<1>(a, st);
-  if (a.T <= kRowsMost) return launch_rows<2>(a, st);
+  if (linear_by_rows(a.out_dim, a.in_dim, a.T)) return launch_rows<2>(a, st);
   const size_t lds = 16 * (size_t)linear_extra(a.in_dim, a.r) * sizeof(float);
   const dim3 grid((a.T + 15) / 16), block(512);
   if (a.r == 0)
@@ -533,7 +544,7 @@ extern "C" {
 size_t moe_linear_workspace_bytes(int out_dim, int in_dim, int rank, int T) {
   if (!linear_shape_ok(out_dim, in_dim, rank, T)) return 0;
   const size_t t = T < 1 ? 1 : T, ke = moe::linear_extra(in_dim, rank);
-  const size_t sums = T > moe::kRowsMost ? (size_t)moe::kLinearSums : 0;
+  const size_t sums = moe::linear_by_rows(out_dim, in_dim, T) ? 0 : (size_t)moe::kLinearSums;
   return 2 * round256(t * ke * 2) + round256(t * 4) + sums;
 }
 

@@ -314,3 +314,9 @@ def test_graphs_of_both_forms(torch_cuda):
         torch.cuda.synchronize()
         assert torch.equal(a, out) and torch.equal(b, out2), n
         assert int(c.status) == 0
+
+
+@pytest.mark.parametrize("H,lens,prefix", [(4, [3, 0] * 35, 6000), (8, [0, 1, 33, 70] * 16, 6300), (2, [40], 6000)])
+def test_decode_prefix_by_more_rows(torch_cuda, H, lens, prefix):
+    """Few heads of many sequences over a prefix: rows of several sequences in a workgroup, 16, 32 and 64 of them."""
+    test_decode_shared_prefix(torch_cuda, H, S, 16, lens, prefix)

@@ -154,3 +154,24 @@ def test_graph_replays_on_a_side_stream(torch_cuda, T):
         torch.cuda.synchronize()
         assert torch.equal(got, y), k
         lin.check(v, got.cpu().numpy())
+
+
+# Either side of the rule for tiles (more than 192 rows, or workgroups of 32 x 32 beyond the CUs), and what the
+# calls above check of few rows.
+@pytest.mark.parametrize("T,out,inn,r", [(192, 65, 2048, 16), (193, 65, 2048, 16), (20, 8200, 128, 3), (33, 4097, 2112, 5),
+                                         (64, 8193, 64, 0), (40, 8193, 2048, 16), (256, 129, 192, 1)])
+def test_types_around_the_tiles(torch_cuda, T, out, inn, r):
+    test_types(torch_cuda, T, out, inn, r)
+
+
+def test_strides_leave_the_rest_with_tiles(torch_cuda):
+    test_strides_leave_the_rest(torch_cuda, 210, 131, 320, 9)
+
+
+@pytest.mark.parametrize("size", [6e4, 1e-4, 6e-8])
+def test_ends_of_fp16_with_tiles(torch_cuda, size):
+    test_ends_of_fp16(torch_cuda, 195, size)
+
+
+def test_graph_replays_with_tiles(torch_cuda):
+    test_graph_replays_on_a_side_stream(torch_cuda, 230)
