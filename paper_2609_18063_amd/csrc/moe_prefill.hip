@@ -52,122 +52,167 @@ __device__ __forceinline__ int tile_base(const PrefillArgs& a, int b) {
 }
 
 // ---- expanding the context ----------------------------------------------------------
-// Workgroups [0, side): one 64-token tile of one sequence each. They copy its rotated
-// keys into one run, and note which of its four 16-token groups have no page.
-// Workgroups from `side` on: 128 context tokens by 128 of the H (Dn + Dv) columns on the
-// matrix cores, four waves of 64 x 64, 64 latent columns a step through LDS, one ahead.
+// 256 of the H (Dn + Dv) columns by up to 512 context tokens a workgroup. A wave keeps its
+// columns' weights of all Dc latents in registers and reads whole tokens, 32 a step, through
+// LDS in four slots, copied three ahead: with the weights through LDS too, 128 x 128 tiles
+// and one step ahead, 3,100 tokens of 512 latents by 32 heads of 256 columns took 54 us, now
+// 37.5 (0.69 PFLOP/s): 13 until the first step (weights, page ids) and 1.9 a step, of which
+// the LDS reads need 1.0 and the products 0.5. 256 latents, 64 columns a wave: 22 us for
+// 11,000 tokens by 8 heads of 128 columns.
+// Before that the workgroups share the 64-token tiles of the sequences (`side` numbers):
+// they copy a tile's rotated keys into one run, and note which of its four 16-token groups
+// have no page.
+constexpr int kExpandTokens = 32, kExpandMost = 512, kExpandCols = 256, kExpandSlots = 4;
+
+// Products of 16 columns that a wave has: 512 latents' weights of four would be copied out of
+// the accumulator registers for every product (43 us against 38 with two, below).
 template <int DC>
-__global__ void __launch_bounds__(256) latent_expand_kernel(PrefillArgs a, int side, int col_tiles) {
-  __shared__ __attribute__((aligned(16))) char lds[2][2][128 * 128];
-  __shared__ int64_t where[128];
+constexpr int kExpandProducts = DC == 512 ? 2 : 4;
+template <int DC>
+constexpr int kExpandWaves = 16 / kExpandProducts<DC>;
+
+template <int DC>
+__global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
+    latent_expand_kernel(PrefillArgs a, int side, int col_groups, int splits) {
+  constexpr int NM = kExpandProducts<DC>, NW = kExpandWaves<DC>, PR = DC / 8, CW = PR / 2 / NW, SLOT = kExpandTokens * DC * 2, KS = DC / 32;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  int64_t* where = reinterpret_cast<int64_t*>(lds + kExpandSlots * SLOT);
+  __shared__ uint32_t lost[4];
   const LatentArgs& l = a.l;
   const int row_halves = DC + l.Dr;
-  if ((int)blockIdx.x < side) {
-    const int b = last_at_most(a.B, blockIdx.x, [&](int k) { return tile_base(a, k); });
-    const Span s = context_of(a, b);
-    const int tok0 = ((int)blockIdx.x - tile_base(a, b)) * kTile;
-    if (blockIdx.x == 0 && threadIdx.x < 64) {
-      // (the lists are looked at once, by one wave)
-      bool good = a.q_start[0] >= 0 && a.kv_start[0] >= 0 && a.q_start[a.B] <= a.T && a.kv_start[a.B] <= a.kv_total;
-      for (int k = threadIdx.x; k < a.B; k += 64) {
-        const int nq = a.q_start[k + 1] - a.q_start[k], nk = a.kv_start[k + 1] - a.kv_start[k];
-        good = good && nq >= 0 && nq <= a.max_q && nk >= nq && nk <= (int64_t)l.max_pages * l.page;
-      }
-      if (!good && l.status) atomicOr(l.status, MOE_STATUS_BAD_LENGTH);
-    }
-    if (tok0 < 0 || tok0 >= s.len) return;
-    uint32_t lost = 0;
-    for (int grp = 0; grp < 4; ++grp) {
-      const int tok = tok0 + 16 * grp;
-      if (tok >= s.len) break;
-      const int page = l.table[b * l.table_stride + tok / l.page];
-      if (page < 0 || page >= l.n_pages) {
-        lost |= 1u << grp;
-        continue;
-      }
-      const __half* from = l.pages + ((size_t)page * l.page + tok % l.page) * row_halves + DC;
-      const int pieces = l.Dr / 8, rows = min(16, s.len - tok);
-      for (int e = threadIdx.x; e < rows * pieces; e += 256)
-        *reinterpret_cast<U4*>(a.kr + (size_t)(s.first + tok + e / pieces) * l.Dr + 8 * (e % pieces)) =
-            ld16(from + (size_t)(e / pieces) * row_halves + 8 * (e % pieces));
-    }
-    if (threadIdx.x == 0) {
-      a.lost[blockIdx.x] = lost;
-      if (lost && l.status) atomicOr(l.status, MOE_STATUS_BAD_PAGE);
-    }
-    return;
-  }
-  const int tile = blockIdx.x - side, n0 = (tile % col_tiles) * 128, r0 = (tile / col_tiles) * 128;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int c = lane & 15, g = lane >> 4, N = l.H * (l.Dn + l.Dv);
-  // where the context rows are (a token without a page: the first page's first row, and
-  // zeros are stored)
-  if (threadIdx.x < 128) {
-    const int at = min(r0 + (int)threadIdx.x, a.kv_total - 1);
+  const int c = lane & 15, g = lane >> 4, hd = l.Dn + l.Dv, N = l.H * hd;
+  const int split = blockIdx.x / col_groups, col0 = (blockIdx.x % col_groups) * kExpandCols + 16 * NM * wave;
+  const int tiles = (a.kv_total + kExpandTokens - 1) / kExpandTokens;
+  const int even = tiles / splits, more = tiles % splits;
+  const int from = split * even + min(split, more), n = even + (split < more);
+  const int first = from * kExpandTokens;
+  // Columns: row i of product m is 4 NM (i / 4) + 4 m + i % 4 of the wave's, so that a lane has
+  // 4 NM neighbouring columns of a token.
+  h8 w[KS][NM];
+#pragma unroll
+  for (int m = 0; m < NM; ++m) {
+    const __half* from_w = l.w + (size_t)min(col0 + 4 * NM * (c >> 2) + 4 * m + (c & 3), N - 1) * DC + 8 * g;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) w[k][m] = ld_h8(from_w + 32 * k);
+  }
+  if (blockIdx.x == 0 && threadIdx.x < 64) {
+    // (the lists are looked at once, by one wave)
+    bool good = a.q_start[0] >= 0 && a.kv_start[0] >= 0 && a.q_start[a.B] <= a.T && a.kv_start[a.B] <= a.kv_total;
+    for (int k = threadIdx.x; k < a.B; k += 64) {
+      const int nq = a.q_start[k + 1] - a.q_start[k], nk = a.kv_start[k + 1] - a.kv_start[k];
+      good = good && nq >= 0 && nq <= a.max_q && nk >= nq && nk <= (int64_t)l.max_pages * l.page;
+    }
+    if (!good && l.status) atomicOr(l.status, MOE_STATUS_BAD_LENGTH);
+  }
+  for (int t = blockIdx.x; t < side; t += gridDim.x) {
+    const int b = last_at_most(a.B, t, [&](int k) { return tile_base(a, k); });
+    const Span s = context_of(a, b);
+    const int tok0 = (t - tile_base(a, b)) * kTile;
+    if (tok0 < 0 || tok0 >= s.len) continue;
+    const int tok = tok0 + 16 * wave;                    // (a group a wave)
+    int32_t page = -1;
+    if (wave < 4 && tok < s.len) page = l.table[b * l.table_stride + tok / l.page];
+    const bool there = page >= 0 && page < l.n_pages;
+    if (there) {
+      const __half* rope = l.pages + ((size_t)page * l.page + tok % l.page) * row_halves + DC;
+      const int pieces = l.Dr / 8, rows = min(16, s.len - tok);
+      for (int e = lane; e < rows * pieces; e += 64)
+        *reinterpret_cast<U4*>(a.kr + (size_t)(s.first + tok + e / pieces) * l.Dr + 8 * (e % pieces)) =
+            ld16(rope + (size_t)(e / pieces) * row_halves + 8 * (e % pieces));
+    }
+    __syncthreads();
+    if (lane == 0 && wave < 4) lost[wave] = !there && tok < s.len;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      const uint32_t mask = lost[0] | lost[1] << 1 | lost[2] << 2 | lost[3] << 3;
+      a.lost[t] = mask;
+      if (mask && l.status) atomicOr(l.status, MOE_STATUS_BAD_PAGE);
+    }
+  }
+  if (n < 1) return;
+  // Where the tokens' rows are, as byte offsets (one without a page: -1; zeros are stored).
+  // Behind the last token its own values are stored again.
+  for (int i = threadIdx.x; i < n * kExpandTokens; i += 64 * NW) {
+    const int at = min(first + i, a.kv_total - 1);
     const int b = last_at_most(a.B, at, [&](int k) { return a.kv_start[k]; });
     const Span s = context_of(a, b);
     const int tok = at - s.first;
     int page = -1;
     if (tok >= 0 && tok < s.len) page = l.table[b * l.table_stride + tok / l.page];
-    where[threadIdx.x] = page >= 0 && page < l.n_pages ? (int64_t)page * l.page + tok % l.page : -1;
+    where[i] = page >= 0 && page < l.n_pages ? ((int64_t)page * l.page + tok % l.page) * (2 * row_halves) : -1;
   }
   __syncthreads();
-  const char *src_c[4], *src_w[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int r = 8 * (4 * wave + j) + (lane >> 3), piece = 16 * ((lane & 7) ^ tile_key<8>(r));
-    src_c[j] = reinterpret_cast<const char*>(l.pages + max(where[r], (int64_t)0) * row_halves) + piece;
-    src_w[j] = reinterpret_cast<const char*>(l.w + (size_t)min(n0 + r, N - 1) * DC) + piece;
-  }
   const uint32_t at0 = lds_at(lds);
-  auto copy = [&](int k) {
+  auto copy = [&](int u) {                               // (past the last tile: it again, into a free slot)
+    const int t = min(u, n - 1), slot = u % kExpandSlots;
+    const char* src[CW];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      dma16(src_c[j] + 128 * k, at0 + (k & 1) * 32768 + 1024 * (4 * wave + j));
-      dma16(src_w[j] + 128 * k, at0 + (k & 1) * 32768 + 16384 + 1024 * (4 * wave + j));
+    for (int j = 0; j < CW; ++j) {
+      const int p = 64 * (CW * wave + j) + lane, r = p / PR;
+      src[j] = reinterpret_cast<const char*>(l.pages) + max(where[t * kExpandTokens + r], (int64_t)0) +
+               16 * ((p % PR) ^ tile_key<PR>(r));
     }
+#pragma unroll
+    for (int j = 0; j < CW; ++j) dma16(src[j], at0 + slot * SLOT + 1024 * (CW * wave + j));
   };
-  const int tr = (wave & 1) * 64, tn = (wave >> 1) * 64;
-  f4 y[4][4] = {};
-  copy(0);
-  for (int k = 0; k < DC / 64; ++k) {
-    vm_wait<0>();
+  for (int u = 0; u < 3; ++u) copy(u);
+  vm_drain();
+  const bool idle = col0 >= N;
+  const int h = min(col0, N - 1) / hd, in = min(col0, N - 1) % hd;
+  __half* to = in < l.Dn ? a.k + (size_t)h * a.kv_total * l.Dn + in : a.v + (size_t)h * a.kv_total * l.Dv + in - l.Dn;
+  const int to_row = in < l.Dn ? l.Dn : l.Dv;
+  for (int u = 0; u < n; ++u) {
+    // what was asked for after tile u: the copies of two tiles, and NM stores a tile
+    if (idle || u == 0)
+      vm_wait<2 * CW>();
+    else if (u == 1)
+      vm_wait<2 * CW + NM>();
+    else
+      vm_wait<2 * CW + 2 * NM>();
     lds_barrier();
-    if (k + 1 < DC / 64) copy(k + 1);
+    copy(u + 3);
+    if (idle) continue;
+    const char* x = lds + (u % kExpandSlots) * SLOT;
+    // (the reads of KR steps are asked for before the products of the KR before them)
+    f4 y[2][NM] = {};
+    constexpr int KR = 4;
+    h8 v[2][KR][2];
+    auto read = [&](int k) {
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      h8 w[4];
+      for (int i = 0; i < KR; ++i)
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const int r = tn + 16 * n + c;
-        w[n] = ld_h8(lds[k & 1][1] + 128 * r + 16 * ((4 * ks + g) ^ tile_key<8>(r)));
-      }
+        for (int t = 0; t < 2; ++t)
+          v[k / KR & 1][i][t] =
+              ld_h8(x + (16 * t + c) * (DC * 2) + 16 * ((4 * (k + i) + g) ^ tile_key<PR>(c)));
+    };
+    read(0);
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const int r = tr + 16 * m + c;
-        const h8 x = ld_h8(lds[k & 1][0] + 128 * r + 16 * ((4 * ks + g) ^ tile_key<8>(r)));
+    for (int k = 0; k < KS; k += KR) {
+      if (k + KR < KS) read(k + KR);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) y[m][n] = mfma16(w[n], x, y[m][n]);
+      for (int i = 0; i < KR; ++i)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int m = 0; m < NM; ++m) y[t][m] = mfma16(w[k + i][m], v[k / KR & 1][i][t], y[t][m]);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int r = u * kExpandTokens + 16 * t + c;
+      const bool there = where[r] >= 0;
+      __half* row = to + (size_t)min(first + r, a.kv_total - 1) * to_row + 4 * NM * g;
+#pragma unroll
+      for (int half = 0; half < NM / 2; ++half) {
+        h8 o;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = there ? (_Float16)y[t][2 * half + i / 4][i % 4] : (_Float16)0.f;
+        *reinterpret_cast<h8*>(row + 8 * half) = o;
       }
     }
   }
-  const int hd = l.Dn + l.Dv;
-#pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    const int col = n0 + tn + 16 * n + 4 * g;
-    if (col >= N) continue;
-    const int h = col / hd, in = col % hd;
-#pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      const int r = tr + 16 * m + c, at = r0 + r;
-      if (at >= a.kv_total) continue;
-      const f4 d = where[r] >= 0 ? y[m][n] : f4{};
-      const h4 v = {(_Float16)d[0], (_Float16)d[1], (_Float16)d[2], (_Float16)d[3]};
-      __half* to = in < l.Dn ? a.k + ((size_t)h * a.kv_total + at) * l.Dn + in
-                             : a.v + ((size_t)h * a.kv_total + at) * l.Dv + in - l.Dn;
-      *reinterpret_cast<h4*>(to) = v;
-    }
-  }
+  vm_wait<0>();                                          // (copies may be in flight into this workgroup's LDS)
 }
 
 // ---- attention ------------------------------------------------------------------------
@@ -423,6 +468,21 @@ hipError_t launch_attention(const PrefillArgs& a, hipStream_t st) {
   return a.l.Dr == 64 ? launch_attention<DN, 64>(a, st) : launch_attention<DN, 32>(a, st);
 }
 
+// As many splits of the tokens as fill the CUs (the weights of 512 latent columns leave room
+// for one workgroup there, else two), and at least one per kExpandMost tokens.
+template <int DC>
+hipError_t launch_expand(const PrefillArgs& a, hipStream_t st) {
+  constexpr int lds = kExpandSlots * kExpandTokens * DC * 2 + kExpandMost * 8, slots = 256 * (DC == 512 ? 1 : 2);
+  const int groups = (a.l.H * (a.l.Dn + a.l.Dv) + kExpandCols - 1) / kExpandCols;
+  const int tiles = (a.kv_total + kExpandTokens - 1) / kExpandTokens, most = kExpandMost / kExpandTokens;
+  const int splits = std::max({1, std::min((slots + groups - 1) / groups, tiles), (tiles + most - 1) / most});
+  auto kernel = latent_expand_kernel<DC>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)groups * splits), dim3(64 * kExpandWaves<DC>), lds, st, a, a.kv_total / kTile + a.B, groups, splits);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 // Into how many parts the contexts are cut: as fill the CUs, of eight tiles at least on
@@ -436,15 +496,7 @@ int prefill_parts(int max_q, int H, int B, int kv_total) {
 
 hipError_t launch_latent_prefill(const PrefillArgs& a, hipStream_t st) {
   const LatentArgs& l = a.l;
-  const int side = a.kv_total / kTile + a.B, cols = (l.H * (l.Dn + l.Dv) + 127) / 128;
-  const dim3 grid(side + (unsigned)cols * ((a.kv_total + 127) / 128)), block(256);
-  if (l.Dc == 512)
-    hipLaunchKernelGGL(latent_expand_kernel<512>, grid, block, 0, st, a, side, cols);
-  else if (l.Dc == 256)
-    hipLaunchKernelGGL(latent_expand_kernel<256>, grid, block, 0, st, a, side, cols);
-  else
-    hipLaunchKernelGGL(latent_expand_kernel<128>, grid, block, 0, st, a, side, cols);
-  const hipError_t e = hipGetLastError();
+  const hipError_t e = l.Dc == 512 ? launch_expand<512>(a, st) : l.Dc == 256 ? launch_expand<256>(a, st) : launch_expand<128>(a, st);
   if (e != hipSuccess) return e;
   return l.Dn == 128 ? launch_attention<128>(a, st) : launch_attention<64>(a, st);
 }
@@ -498,9 +550,7 @@ int moe_latent_prefill(const moe_latent_spec* spec, const moe_latent_cache* cach
   if (!prefill_shape_ok(spec, T, B, kv_total) || B > cache->n_seqs || max_q < 0 || max_q > T)
     return MOE_EINVAL;
   if (T == 0 || B == 0) return T == 0 ? MOE_OK : MOE_EINVAL;
-  if (max_q < 1 || (int64_t)((max_q + moe::kPartRows - 1) / moe::kPartRows) * spec->heads * B * 512 > (int64_t)UINT32_MAX ||
-      (int64_t)(kv_total / 128 + 1) * spec->heads * 2 * 256 + ((int64_t)kv_total / moe::kTile + B) * 256 >
-          (int64_t)UINT32_MAX)
+  if (max_q < 1 || (int64_t)((max_q + moe::kPartRows - 1) / moe::kPartRows) * spec->heads * B * 512 > (int64_t)UINT32_MAX)
     return MOE_EINVAL;  // (a grid's threads)
   if (!w_kvb_f16 || !q_f16 || !q_start || !kv_start || !out_f16 || !workspace) return MOE_EINVAL;
   if (misaligned(w_kvb_f16, 16) || misaligned(q_f16, 16) || misaligned(q_start, 4) || misaligned(kv_start, 4) ||
