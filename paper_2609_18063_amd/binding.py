@@ -718,24 +718,39 @@ def _need(ok, what):
         raise ValueError(what)
 
 
+_device = None
+
+
+def _the_torch():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 def _current_device():
-    import torch
-    return torch.cuda.current_device()
+    """The current GPU, by torch's internal reader where it has one (0.06 us a call; 0.3 us through torch.cuda)."""
+    global _device
+    if _device is None:
+        t = _the_torch()
+        if not t.cuda.is_available():
+            return -2                                    # (no tensor is there; -1 is the CPU)
+        t.cuda.current_device()                          # (the internal one needs what this sets up)
+        _device = getattr(t._C, "_cuda_getDevice", t.cuda.current_device)
+    return _device()
 
 
 def _dense(what, dtype, *tensors):
-    """Contiguous tensors of one dtype on the current GPU: the library sees addresses only, and launches there."""
-    here = _current_device() if tensors[0].is_cuda else -1
+    """Contiguous tensors of one dtype on the current GPU (None: left out): the library sees addresses only, and
+    launches there."""
+    here = _current_device()
     for t in tensors:
-        if t.dtype != dtype or not t.is_contiguous() or here < 0 or t.get_device() != here:
+        if t is None:
+            continue
+        if t.dtype != dtype or not t.is_contiguous() or t.get_device() != here:
             raise ValueError("%s: a contiguous %s tensor on the current GPU is needed, got %s %s on %s"
                              % (what, dtype, t.dtype, tuple(t.stride()), t.device))
-
-
-def _status(status):
-    if status is not None:
-        import torch
-        _dense("status", torch.int32, status)
 
 
 def _room(workspace):
@@ -749,12 +764,12 @@ def linear_workspace_bytes(out_dim, in_dim, rank, T):
 def linear_int4(proj, out_dim, in_dim, rank, lora_scale, x, y, workspace, add=False, stream=None):
     """moe_linear_int4_lora: ``proj`` a MoeProj of device pointers; ``x`` fp16 ``[T, in]`` and ``y`` fp32 or
     fp16 ``[T, out]`` with unit column stride; ``add``: into an fp32 ``y``."""
-    import torch
+    torch = _the_torch()
     T = x.shape[0]
     f16 = y.dtype == torch.float16
     _need(x.dtype == torch.float16 and x.dim() == 2 and x.shape[1] == in_dim and (in_dim == 1 or x.stride(1) == 1),
           "x: fp16 [T, in] with unit column stride")
-    _need((f16 or y.dtype == torch.float32) and tuple(y.shape) == (T, out_dim) and (out_dim == 1 or y.stride(1) == 1),
+    _need((f16 or y.dtype == torch.float32) and y.shape == (T, out_dim) and (out_dim == 1 or y.stride(1) == 1),
           "y: fp32 or fp16 [T, out] with unit column stride")
     _need(not (add and f16), "add needs an fp32 y")
     _room(workspace)
@@ -780,7 +795,7 @@ def latent_spec_check(spec):
 def latent_cache(pages, table):
     """moe_latent_cache of ``pages`` fp16 ``[n_pages, page_tokens, d_latent + d_rope]`` and ``table`` int32
     ``[n_seqs, max_pages]`` (rows may be strided). The struct keeps both alive."""
-    import torch
+    torch = _the_torch()
     _dense("pages", torch.float16, pages)
     _need(pages.dim() == 3 and table.dim() == 2 and table.dtype == torch.int32
           and (table.shape[1] == 1 or table.stride(1) == 1) and table.device == pages.device,
@@ -792,31 +807,29 @@ def latent_cache(pages, table):
     return c
 
 
-def _cache_of(spec, cache, status):
-    import torch
+def _cache_of(spec, cache):
+    """The cache's pages, as the description has them."""
     pages = cache.keep[0]
-    _dense("pages", torch.float16, pages)
-    _status(status)
-    _need(tuple(pages.shape[1:]) == (spec.page_tokens, spec.d_latent + spec.d_rope),
-          "pages of %d tokens of %d" % (spec.page_tokens, spec.d_latent + spec.d_rope))
+    if pages.shape[1:] != (spec.page_tokens, spec.d_latent + spec.d_rope):
+        raise ValueError("pages of %d tokens of %d" % (spec.page_tokens, spec.d_latent + spec.d_rope))
+    return pages
 
 
 def latent_append(spec, cache, kv, gamma, rope, seq, pos, status, q=None, q_out=None, stream=None):
     """moe_latent_append: ``kv`` fp32 ``[T, d_latent + d_rope]``, ``gamma`` fp16, ``rope`` fp32 ``[max_pos,
     d_rope / 2, 2]``, ``seq`` / ``pos`` int32 ``[T]``, ``q`` / ``q_out`` fp16 ``[T, H, d_nope + d_rope]``."""
-    import torch
+    torch = _the_torch()
     T = kv.shape[0]
-    _cache_of(spec, cache, status)
+    _dense("pages, gamma", torch.float16, _cache_of(spec, cache), gamma)
     _dense("kv, rope", torch.float32, kv, rope)
-    _dense("seq, pos", torch.int32, seq, pos)
-    _dense("gamma", torch.float16, gamma)
-    _need(tuple(kv.shape) == (T, spec.d_latent + spec.d_rope) and tuple(rope.shape[1:]) == (spec.d_rope // 2, 2)
+    _dense("seq, pos, status", torch.int32, seq, pos, status)
+    _need(kv.shape == (T, spec.d_latent + spec.d_rope) and rope.shape[1:] == (spec.d_rope // 2, 2)
           and rope.dim() == 3 and gamma.numel() == spec.d_latent and seq.numel() == T and pos.numel() == T,
           "kv [T, d_latent + d_rope], gamma [d_latent], rope [max_pos, d_rope / 2, 2], seq and pos [T]")
     _need((q is None) == (q_out is None), "q and q_out: both or none")
     if q is not None:
         _dense("q, q_out", torch.float16, q, q_out)
-        _need(tuple(q.shape) == tuple(q_out.shape) == (T, spec.heads, spec.d_nope + spec.d_rope),
+        _need(q.shape == q_out.shape == (T, spec.heads, spec.d_nope + spec.d_rope),
               "q and q_out [T, H, d_nope + d_rope]")
     _check(lib().moe_latent_append(ctypes.byref(spec), ctypes.byref(cache), _ptr(kv), _ptr(gamma), _ptr(rope),
                                    rope.shape[0], _ptr(seq), _ptr(pos), T, _ptr(q), _ptr(q_out), _ptr(status),
@@ -827,14 +840,12 @@ def latent_decode_workspace_bytes(spec, B, max_len, prefix_len=0):
     return int(lib().moe_latent_decode_workspace_bytes(ctypes.byref(spec), B, max_len, prefix_len))
 
 
-def _attends(spec, cache, w_kvb, q, out, status, workspace):
-    import torch
-    _cache_of(spec, cache, status)
+def _attends(spec, cache, w_kvb, q, out, workspace):
     _room(workspace)
-    _dense("w_kvb, q, out", torch.float16, w_kvb, q, out)
-    _need(tuple(w_kvb.shape) == (spec.heads, spec.d_nope + spec.d_v, spec.d_latent)
-          and tuple(q.shape[1:]) == (spec.heads, spec.d_nope + spec.d_rope)
-          and tuple(out.shape) == (q.shape[0], spec.heads, spec.d_v),
+    _dense("pages, w_kvb, q, out", _the_torch().float16, _cache_of(spec, cache), w_kvb, q, out)
+    _need(w_kvb.shape == (spec.heads, spec.d_nope + spec.d_v, spec.d_latent)
+          and q.shape[1:] == (spec.heads, spec.d_nope + spec.d_rope)
+          and out.shape == (q.shape[0], spec.heads, spec.d_v),
           "w_kvb [H, d_nope + d_v, d_latent], q [T, H, d_nope + d_rope], out [T, H, d_v]")
 
 
@@ -842,10 +853,10 @@ def latent_decode(spec, cache, w_kvb, q, kv_len, max_len, out, status, workspace
                   stream=None):
     """moe_latent_decode: ``q`` fp16 ``[B, H, d_nope + d_rope]``, ``kv_len`` int32 ``[B]``; ``prefix``: int32 page
     ids of ``prefix_len`` tokens that every sequence of the batch begins with."""
-    import torch
+    torch = _the_torch()
     B = q.shape[0]
-    _attends(spec, cache, w_kvb, q, out, status, workspace)
-    _dense("kv_len", torch.int32, kv_len)
+    _attends(spec, cache, w_kvb, q, out, workspace)
+    _dense("kv_len, status", torch.int32, kv_len, status)
     _need(kv_len.numel() == B, "kv_len [B]")
     if prefix_len:
         _need(prefix is not None and prefix.numel() * spec.page_tokens >= prefix_len, "the prefix's page ids")
@@ -861,9 +872,9 @@ def latent_prefill_workspace_bytes(spec, B, kv_total):
 
 def latent_prefill(spec, cache, w_kvb, q, q_start, kv_start, kv_total, max_q, out, status, workspace, stream=None):
     """moe_latent_prefill: ``q`` fp16 ``[T, H, d_nope + d_rope]``, ``q_start`` / ``kv_start`` int32 ``[B + 1]``."""
-    import torch
-    _attends(spec, cache, w_kvb, q, out, status, workspace)
-    _dense("q_start, kv_start", torch.int32, q_start, kv_start)
+    torch = _the_torch()
+    _attends(spec, cache, w_kvb, q, out, workspace)
+    _dense("q_start, kv_start, status", torch.int32, q_start, kv_start, status)
     _need(q_start.numel() == kv_start.numel() >= 1, "q_start and kv_start [B + 1]")
     _check(lib().moe_latent_prefill(ctypes.byref(spec), ctypes.byref(cache), _ptr(w_kvb), _ptr(q), q.shape[0],
                                     _ptr(q_start), _ptr(kv_start), q_start.numel() - 1, kv_total, max_q, _ptr(out),
@@ -929,12 +940,11 @@ class PagePool:
 def page_copy(pages, pairs, status, stream=None):
     """moe_page_copy on ``pages [n_layers, n_pages, ...]`` (pages contiguous, layers may be strided); ``pairs``
     int32 ``[n, 2]`` on the GPU."""
-    import torch
+    torch = _the_torch()
     _need(pages.dim() >= 3 and pages.shape[0] > 0 and pairs.dim() == 2 and pairs.shape[1] == 2,
           "pages [n_layers, n_pages, ...], pairs [n, 2]")
-    _dense("pages of a layer", pages.dtype, pages[0])
-    _dense("pairs", torch.int32, pairs)
-    _status(status)
+    _dense("pages of a layer", pages.dtype, pages if pages.is_contiguous() else pages[0])
+    _dense("pairs, status", torch.int32, pairs, status)
     size = pages.element_size()
     _check(lib().moe_page_copy(_ptr(pages), pages.shape[0], pages.stride(0) * size, pages.stride(1) * size,
                                pages.shape[1], _ptr(pairs), pairs.shape[0], _ptr(status), _stream(stream)),
@@ -943,9 +953,8 @@ def page_copy(pages, pairs, status, stream=None):
 
 def page_remap(table, remap, table_out, status, stream=None):
     """moe_page_remap: int32 tensors; ``table_out`` may be ``table``."""
-    import torch
-    _dense("table, remap, table_out", torch.int32, table, remap, table_out)
-    _status(status)
+    torch = _the_torch()
+    _dense("table, remap, table_out, status", torch.int32, table, remap, table_out, status)
     _need(table_out.numel() == table.numel(), "tables of one size")
     _check(lib().moe_page_remap(_ptr(table), table.numel(), _ptr(remap), remap.numel(), _ptr(table_out), _ptr(status),
                                 _stream(stream)), "moe_page_remap")

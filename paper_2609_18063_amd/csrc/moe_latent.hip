@@ -27,7 +27,8 @@ __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_ex
 
 // ---- cache writes -------------------------------------------------------------
 // Block (t, 0) normalizes and rotates token t's row into its page; blocks (t, 1 ..)
-// rotate the query, 8 halves a thread. One pass; bound by the bytes read and written.
+// rotate the query, 8 halves a thread. One pass; bound by the bytes read and written (3,100
+// tokens of 32 heads: 87 MB in 19 us, 4.6 TB/s; 16 tokens: 3.5 us, latency).
 __global__ void __launch_bounds__(256) latent_append_kernel(AppendArgs a) {
   const LatentArgs& l = a.l;
   const int t = blockIdx.x, seq = a.seq[t], pos = a.pos[t], row = l.Dc + l.Dr;
@@ -208,7 +209,8 @@ struct Walk {
 // qt_h = W_uk,h^T q_n,h for 64 latent columns of one head and 64 sequences a workgroup;
 // W_uk,h's columns are staged in LDS and read transposed. qt is rounded to fp16, the
 // type of the rows that it meets. The first column block copies q_r beside it; one
-// further block adds up the tiles of the sequences for the plan.
+// further block adds up the tiles of the sequences for the plan. Bound by latency (weights,
+// LDS, queries in turn): 48 sequences of 32 heads, 4.2 MB of weights, 7.0 us.
 template <int DN>
 __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
   __shared__ __attribute__((aligned(16))) char wt[DN * 128];
@@ -287,8 +289,10 @@ __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
 // other half add up the weighted latents of the tile before, each its share of the latent
 // columns, read transposed from the same LDS copy, and make the copies, two tiles ahead in
 // four buffers. So the products of one tile run beside the exponentials of the next, with
-// one barrier a tile. With few heads HBM bounds it, with many the scores' chain of one
-// wave (its products, exponentials and the barrier).
+// one barrier a tile. With few heads HBM bounds it (32 heads, 48 sequences, 378,000 tokens:
+// 445 MB in 88 us, 5.05 TB/s), with many, or a shared prefix, the scores' chain of one wave
+// (its products, exponentials and the barrier): 32 sequences of 64 heads on 12,000 shared
+// tokens in 91 us, 0.6 PFLOP/s.
 // The weights are taken against a reference per row that follows the running maximum only
 // where that passes it by kSlack: until then they are at most 2^kSlack and nothing is
 // rescaled. The weights are rounded to fp16 for the product with the latents, which are
@@ -697,7 +701,8 @@ __global__ void __launch_bounds__(NT) latent_join_kernel(DecodeArgs a) {
 }
 
 // ---- out of the latent space --------------------------------------------------------
-// o_h = W_uv,h lat_h: 16 values of one head a workgroup, whose four waves split the
+// o_h = W_uv,h lat_h (48 sequences of 32 heads: 6.2 us, bound by latency as the way in is):
+// 16 values of one head a workgroup, whose four waves split the
 // latent columns and keep their weights in registers for all sequences. For one short
 // sequence it joins its head's row itself (JOIN; the workgroups of a head do that over
 // again): a launch less (16 heads over 100 tokens: the call in 15.6 us against 18.1; 500

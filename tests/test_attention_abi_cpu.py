@@ -276,11 +276,10 @@ def test_binding_wants_the_current_device(B, monkeypatch):
     monkeypatch.setattr(B, "_current_device", lambda: 1)
     i32 = torch.int32
     B._dense("t", i32, _OnGpu(i32, 1), _OnGpu(i32, 1))
-    B._status(None)
-    B._status(_OnGpu(i32, 1))
+    B._dense("t", i32, _OnGpu(i32, 1), None)
     B._room(_OnGpu(torch.uint8, 1))
     for bad in (_OnGpu(i32, 0), _OnGpu(torch.int64, 1), _OnGpu(i32, 1, False), torch.zeros(2, dtype=i32)):
-        for call in (lambda: B._dense("t", i32, bad), lambda: B._dense("t", i32, _OnGpu(i32, 1), bad), lambda: B._status(bad)):
+        for call in (lambda: B._dense("t", i32, bad), lambda: B._dense("t", i32, _OnGpu(i32, 1), None, bad)):
             with pytest.raises(ValueError):
                 call()
     for bad in (_OnGpu(i32, 0), _OnGpu(i32, 1, False), torch.zeros(2)):
