@@ -432,7 +432,8 @@ int moe_latent_decode(const moe_latent_spec* spec, const moe_latent_cache* cache
  * query rows q_start[b] .. q_start[b + 1] of q, which are the last tokens of
  * its context of kv_start[b + 1] - kv_start[b] cached tokens (table row b;
  * already written, the chunk's own among them), and each attends to the
- * tokens up to its own position.
+ * tokens up to its own position. (An expanded value beyond fp16's range is
+ * taken as its largest; what a later token holds does not reach a row.)
  * q_start, kv_start: device int32 [B + 1], ascending from 0 or more. T,
  * kv_total and max_q (up to T): bounds on the last q_start, the last kv_start
  * and the longest chunk. q_f16: device fp16 [T][H][d_nope + d_rope], rotated; out_f16:

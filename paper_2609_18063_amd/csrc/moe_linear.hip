@@ -285,7 +285,7 @@ __device__ __forceinline__ int x_key(int row) { return ((row >> 1) & 1) | ((row 
 // one 64-input group a step. x, codes and (s, z) come through LDS, two steps ahead in three
 // slots. Bound by LDS and the VALU: a step of a CU's two workgroups reads 128 KB of LDS
 // (about 1,200 clocks), unpacks codes and applies scales (1,100 a SIMD) beside its products
-// (64 a SIMD, 550), and takes 2,600. 1,555 rows, 5001 x 4096, rank 16: 113 us, 0.57 PFLOP/s.
+// (64 a SIMD, 550), and takes 2,600. 1,555 rows, 5001 x 4096, rank 16: 109 us, 0.59 PFLOP/s.
 // Workgroups come in rounds of kSlots. The tiles that do not fill a round are split along
 // the inputs into as many parts as fill it (first in the grid, so that whole tiles follow
 // the short parts); a part writes fp32 sums, which one more launch adds in order.

@@ -56,7 +56,7 @@ __device__ __forceinline__ int tile_base(const PrefillArgs& a, int b) {
 // columns' weights of all Dc latents in registers and reads whole tokens, 32 a step, through
 // LDS in four slots, copied three ahead: with the weights through LDS too, 128 x 128 tiles
 // and one step ahead, 3,100 tokens of 512 latents by 32 heads of 256 columns took 54 us, now
-// 37.5 (0.69 PFLOP/s): 13 until the first step (weights, page ids) and 1.9 a step, of which
+// 39 (0.67 PFLOP/s): 13 until the first step (weights, page ids) and 1.9 a step, of which
 // the LDS reads need 1.0 and the products 0.5. 256 latents, 64 columns a wave: 22 us for
 // 14,500 tokens by 8 heads of 128 columns.
 // Before that the workgroups share the 64-token tiles of the sequences (`side` numbers):
@@ -162,6 +162,9 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
   const int h = min(col0, N - 1) / hd, in = min(col0, N - 1) % hd;
   __half* to = in < l.Dn ? a.k + (size_t)h * a.kv_total * l.Dn + in : a.v + (size_t)h * a.kv_total * l.Dv + in - l.Dn;
   const int to_row = in < l.Dn ? l.Dn : l.Dv;
+  // Values are stored finite: a row's weight 0 of a token that it does not see then gives 0,
+  // whatever the token holds. (Its keys stay as they are, and make NaN of the rows that see it.)
+  const bool values = in >= l.Dn;
   for (int u = 0; u < n; ++u) {
     // what was asked for after tile u: the copies of two tiles, and NM stores a tile
     if (idle || u == 0)
@@ -207,7 +210,11 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
       for (int half = 0; half < NM / 2; ++half) {
         h8 o;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = there ? (_Float16)y[t][2 * half + i / 4][i % 4] : (_Float16)0.f;
+        for (int i = 0; i < 8; ++i) {
+          float e = y[t][2 * half + i / 4][i % 4];
+          if (values) e = fminf(fmaxf(e, -65504.f), 65504.f);
+          o[i] = there ? (_Float16)e : (_Float16)0.f;
+        }
         *reinterpret_cast<h8*>(row + 8 * half) = o;
       }
     }

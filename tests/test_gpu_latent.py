@@ -320,3 +320,22 @@ def test_graphs_of_both_forms(torch_cuda):
 def test_decode_prefix_by_more_rows(torch_cuda, H, lens, prefix):
     """Few heads of many sequences over a prefix: rows of several sequences in a workgroup, 16, 32 and 64 of them."""
     test_decode_shared_prefix(torch_cuda, H, S, 16, lens, prefix)
+
+
+@pytest.mark.parametrize("dims,H", [(S, 3), (W, 8), ((256, 32, 64, 128), 2)])
+@pytest.mark.parametrize("what,part", [(np.nan, 0), (np.inf, 0), (-np.inf, 1), (np.nan, 1), (6e4, 0)])
+def test_prefill_later_tokens_stay_out(torch_cuda, dims, H, what, part):
+    """A token that is not finite, or whose values are beyond fp16, changes no row before it and no other sequence."""
+    g = np.random.default_rng(17)
+    lens, counts, bad = [300, 90], [120, 90], 250
+    c = Cache(torch_cuda, g, H, *dims, 16, lens)
+    q = _queries(g, sum(counts), c)
+    clean = c.prefill(q, counts)
+    row = int(c.table_np[0, bad // 16]) * 16 + bad % 16
+    flat = c.pages.view(-1, dims[0] + dims[1])
+    flat[row, dims[0] * part:dims[0] + dims[1] if part else dims[0]] = float(what)
+    got = c.prefill(q, counts)
+    seen = bad - (lens[0] - counts[0])                    # the first row that sees the token
+    assert np.array_equal(got[:seen], clean[:seen]) and np.array_equal(got[counts[0]:], clean[counts[0]:])
+    if np.isnan(what):
+        assert np.isnan(got[seen:counts[0]]).all()
