@@ -339,3 +339,41 @@ def test_prefill_later_tokens_stay_out(torch_cuda, dims, H, what, part):
     assert np.array_equal(got[:seen], clean[:seen]) and np.array_equal(got[counts[0]:], clean[counts[0]:])
     if np.isnan(what):
         assert np.isnan(got[seen:counts[0]]).all()
+
+
+@pytest.mark.parametrize("H,dims,page,lens,counts", [(1, S, 64, [40000], [3]), (2, S, 16, [20001, 15000], [1, 40])])
+def test_long_contexts(torch_cuda, H, dims, page, lens, counts):
+    test_prefill(torch_cuda, H, dims, page, lens, counts)
+    test_decode(torch_cuda, H, *dims, page, lens)
+
+
+def test_cache_past_32_bits(torch_cuda):
+    """Rows at byte and element offsets beyond 2^32 and 2^31: written, copied to another page and read by both forms."""
+    torch, g = torch_cuda, np.random.default_rng(18)
+    from paper_2609_18063_amd import binding as B
+    c = Cache(torch, g, 3, *S, 1024, [90])
+    n_pages, row = 14000, S[0] + S[1]
+    big = torch.empty(n_pages, 1024, row, dtype=torch.float16, device="cuda")
+    assert big.numel() > 1 << 31
+    far = n_pages - 3
+    table = torch.tensor([[far], [far + 1]], dtype=torch.int32, device="cuda")
+    cache = B.latent_cache(big, table)
+    kv = torch.from_numpy(g.standard_normal((90, row)).astype(np.float32)).cuda()
+    rope = torch.zeros(90, S[1] // 2, 2, device="cuda")
+    rope[..., 0] = 1
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    B.latent_append(c.spec, cache, kv, torch.ones(S[0], dtype=torch.float16, device="cuda"), rope, i32([0] * 90), i32(list(range(90))),
+                    c.status)
+    x = kv.cpu().numpy().astype(np.float64)
+    want = np.concatenate([x[:, :S[0]] / np.sqrt((x[:, :S[0]] ** 2).mean(-1, keepdims=True) + 1e-6), x[:, S[0]:]], 1)
+    rows = big[far, :90].cpu().numpy()
+    assert (np.abs(rows - want) <= np.abs(want) * (A.HALF + 1e-5) + 1e-7).all()  # one rounding to fp16, fp32 before it
+    B.page_copy(big[None], i32([[far, far + 1], [far, 5]]), c.status)
+    for p in (far + 1, 5):
+        assert np.array_equal(big[p, :90].cpu().numpy(), rows)
+    c.cache, c.lens, c.rows = cache, [90, 90], [rows, rows]
+    q = _queries(g, 2, c)
+    for got in (c.decode(q), c.prefill(q, [1, 1])):
+        for b in range(2):
+            c.check(got[b:b + 1], q[b:b + 1], b, rows)
+    assert int(c.status) == 0
