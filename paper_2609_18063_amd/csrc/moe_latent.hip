@@ -210,7 +210,8 @@ struct Walk {
 // W_uk,h's columns are staged in LDS and read transposed. qt is rounded to fp16, the
 // type of the rows that it meets. The first column block copies q_r beside it; one
 // further block adds up the tiles of the sequences for the plan. Bound by latency (weights,
-// LDS, queries in turn): 48 sequences of 32 heads, 4.2 MB of weights, 7.0 us.
+// LDS, products): 48 sequences of 32 heads, 4.2 MB of weights, 5.7 us (7.5 with the queries
+// asked for after the weights).
 template <int DN>
 __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
   __shared__ __attribute__((aligned(16))) char wt[DN * 128];
@@ -245,10 +246,21 @@ __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
   }
   const int hd = l.Dn + l.Dr, row = l.Dc + l.Dr, c0 = blockIdx.x * 64;
   const __half* w = l.w + (size_t)h * (l.Dn + l.Dv) * l.Dc + c0;
-  for (int e = threadIdx.x; e < DN * 8; e += 256) {
-    const int n = e >> 3, p = e & 7;
-    *reinterpret_cast<U4*>(wt + n * 128 + 16 * (p ^ tile_key<8>(n))) = ld16(w + (size_t)n * l.Dc + 8 * p);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  // (the weights, the first queries and q_r are asked for together)
+  U4 wl[DN / 32];
+#pragma unroll
+  for (int i = 0; i < DN / 32; ++i) {
+    const int e = threadIdx.x + 256 * i;
+    wl[i] = ld16(w + (size_t)(e >> 3) * l.Dc + 8 * (e & 7));
   }
+  h8 x[DN / 32];
+  auto queries = [&](int bt) {
+    const __half* q = l.q + ((size_t)min(bt + c, b1 - 1) * l.H + h) * hd + 8 * g;
+#pragma unroll
+    for (int k = 0; k < DN / 32; ++k) x[k] = ld_h8(q + 32 * k);
+  };
+  queries(b0);
   if (blockIdx.x == 0) {
     const int pieces = l.Dr / 8;
     for (int e = threadIdx.x; e < (b1 - b0) * pieces; e += 256) {
@@ -257,8 +269,12 @@ __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
       *reinterpret_cast<U4*>(a.ql + r * row + l.Dc + p) = ld16(l.q + r * hd + l.Dn + p);
     }
   }
+#pragma unroll
+  for (int i = 0; i < DN / 32; ++i) {
+    const int e = threadIdx.x + 256 * i, n = e >> 3;
+    *reinterpret_cast<U4*>(wt + n * 128 + 16 * ((e & 7) ^ tile_key<8>(n))) = wl[i];
+  }
   __syncthreads();
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   h8 wa[DN / 32];
 #pragma unroll
   for (int k = 0; k < DN / 32; ++k) {
@@ -274,7 +290,8 @@ __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
     const size_t r = (size_t)min(bt + c, b1 - 1) * l.H + h;
     f4 d = {};
 #pragma unroll
-    for (int k = 0; k < DN / 32; ++k) d = mfma16(wa[k], ld_h8(l.q + r * hd + 32 * k + 8 * g), d);
+    for (int k = 0; k < DN / 32; ++k) d = mfma16(wa[k], x[k], d);
+    if (bt + 16 < b1) queries(bt + 16);
     if (bt + c < b1) {
       const h4 v = {(_Float16)d[0], (_Float16)d[1], (_Float16)d[2], (_Float16)d[3]};
       *reinterpret_cast<h4*>(a.ql + r * row + c0 + 16 * wave + 4 * g) = v;
@@ -701,7 +718,7 @@ __global__ void __launch_bounds__(NT) latent_join_kernel(DecodeArgs a) {
 }
 
 // ---- out of the latent space --------------------------------------------------------
-// o_h = W_uv,h lat_h (48 sequences of 32 heads: 6.2 us, bound by latency as the way in is):
+// o_h = W_uv,h lat_h (48 sequences of 32 heads: 5.3 us, bound by latency as the way in is):
 // 16 values of one head a workgroup, whose four waves split the
 // latent columns and keep their weights in registers for all sequences. For one short
 // sequence it joins its head's row itself (JOIN; the workgroups of a head do that over
@@ -728,15 +745,20 @@ __global__ void __launch_bounds__(256) latent_up_kernel(DecodeArgs a) {
     if (threadIdx.x < DC / 4) *reinterpret_cast<h4*>(&joined[4 * threadIdx.x]) = v;
     __syncthreads();
   }
-  for (int bt = b0; bt < b1; bt += 16) {
-    const int b = min(bt + c, b1 - 1);
-    const size_t r = (size_t)b * l.H + h;
-    const void* lat = a.lat + r * DC;
+  h8 x[KS];                                              // (the next 16 sequences' are asked for early)
+  auto latents = [&](int bt) {
+    const void* lat = a.lat + ((size_t)min(bt + c, b1 - 1) * l.H + h) * DC;
     if constexpr (JOIN) lat = joined;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) x[k] = ld_h8(static_cast<const _Float16*>(lat) + wave * (DC / 4) + 32 * k + 8 * g);
+  };
+  latents(b0);
+  for (int bt = b0; bt < b1; bt += 16) {
+    const size_t r = (size_t)min(bt + c, b1 - 1) * l.H + h;
     f4 d = {};
 #pragma unroll
-    for (int k = 0; k < KS; ++k)
-      d = mfma16(w[k], ld_h8(static_cast<const _Float16*>(lat) + wave * (DC / 4) + 32 * k + 8 * g), d);
+    for (int k = 0; k < KS; ++k) d = mfma16(w[k], x[k], d);
+    if (bt + 16 < b1) latents(bt + 16);
     red[wave][lane] = d;
     __syncthreads();
     if (wave == 0 && bt + c < b1) {
