@@ -417,7 +417,8 @@ int moe_latent_append(const moe_latent_spec* spec, const moe_latent_cache* cache
  * ceil(prefix_len / page_tokens) pages (NULL with prefix_len 0). Every sequence
  * attends to the prefix_len tokens of it and to its own kv_len; the prefix is
  * read once for many sequences. A row that has no token, or whose scores are
- * all minus infinity, gives zeros. B up to n_seqs. workspace: moe_latent_decode_workspace_bytes (no initial
+ * all minus infinity, gives zeros; one with a NaN among its scores is NaN.
+ * B up to n_seqs. workspace: moe_latent_decode_workspace_bytes (no initial
  * contents needed); calls that share one must be ordered on one stream.
  */
 size_t moe_latent_decode_workspace_bytes(const moe_latent_spec* spec, int B, int max_len, int prefix_len);

@@ -680,8 +680,9 @@ __device__ __forceinline__ h4 join_row(const DecodeArgs& a, int row, int slice, 
     const size_t seg = seg_of(i, r);
     const float2 a0 = *reinterpret_cast<const float2*>(a.part_ml + (seg * 2 * M + r) * 2);
     const float2 a1 = *reinterpret_cast<const float2*>(a.part_ml + ((seg * 2 + 1) * M + r) * 2);
-    const float w = a0.x == -INFINITY ? 0.f : exp2_fast(a0.x - top);  // (-inf: every token of it was lost)
-    sum += w == 0.f ? 0.f : w * (a0.y + a1.y);
+    // (-inf: no score of it is above that, and its sum is 0, or NaN, which a weight of 0 keeps)
+    const float w = a0.x == -INFINITY ? 0.f : exp2_fast(a0.x - top);
+    sum += w * (a0.y + a1.y);
     if (threadIdx.x < kWave) sh.weight[i] = w;
   }
   sum = wave_sum(sum);
