@@ -441,7 +441,10 @@ __global__ void __launch_bounds__(256) latent_parts_kernel(PrefillArgs a) {
     const size_t i = at + (size_t)p * kRows;
     const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * i);
     const f4 v = *reinterpret_cast<const f4*>(a.part_o + i * l.Dv + col);
-    if (ml.x == -INFINITY) continue;                     // (a part without a token of the row)
+    if (ml.x == -INFINITY) {                             // (no score of it is above that: its sum is 0, or NaN)
+      sum += ml.y;
+      continue;
+    }
     const float w = __builtin_amdgcn_exp2f(ml.x - top) * ml.y;
     sum += w;
     o += v * w;

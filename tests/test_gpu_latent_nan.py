@@ -87,3 +87,31 @@ def test_decode_nan_in_a_shared_prefix(torch_cuda, dims, H, prefix):
     last = c.pages[int(c.prefix_ids[(prefix - 1) // 16]), (prefix - 1) % 16]
     last[0] = float("nan")
     assert np.isnan(c.decode(q, prefix=prefix)).all()
+
+
+@pytest.mark.parametrize("dims,H", [(S, 3), (W, 2)])
+def test_prefill_nan_in_cut_contexts(torch_cuda, dims, H):
+    """Contexts cut into parts: the first token that a row sees in its part (128: the first row block has four tiles in
+    two parts), one further on, and a query."""
+    g = np.random.default_rng(24)
+    lens = counts = [2100, 90]
+    assert sum(lens) // (len(lens) * 512) >= 2             # (from there on contexts are cut)
+    c = Cache(torch_cuda, g, H, *dims, 16, lens)
+    q = _queries(g, sum(counts), c)
+    clean = c.prefill(q, counts)
+    for bad in (128, 1000):
+        row = _at(c, 0, bad)
+        was = row.clone()
+        row[:c.Dc] = float("nan")
+        got = c.prefill(q, counts)
+        row.copy_(was)
+        assert np.array_equal(got[:bad], clean[:bad]) and np.array_equal(got[counts[0]:], clean[counts[0]:])
+        assert np.isnan(got[bad:counts[0]]).all()
+    for i in (0, 130, 2099, 2150):
+        p = q.copy()
+        p[i, 1, 0] = np.nan
+        got = c.prefill(p, counts)
+        assert np.isnan(got[i, 1]).all()
+        same = np.ones(got.shape[:2], bool)
+        same[i, 1] = False
+        assert np.array_equal(got[same], clean[same])
