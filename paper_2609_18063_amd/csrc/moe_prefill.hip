@@ -164,7 +164,14 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
   const int to_row = in < l.Dn ? l.Dn : l.Dv;
   // Values are stored finite: a row's weight 0 of a token that it does not see then gives 0,
   // whatever the token holds. (Its keys stay as they are, and make NaN of the rows that see it.)
-  const bool values = in >= l.Dn;
+  // Not so where the weights of the wave's columns are not finite, which no key would show:
+  // times zeros they add up to NaN, else to 0.
+  f4 whole = {};
+#pragma unroll
+  for (int k = 0; k < KS; ++k)
+#pragma unroll
+    for (int m = 0; m < NM; ++m) whole = mfma16(w[k][m], h8{}, whole);
+  const bool values = in >= l.Dn && !__any(whole[0] + whole[1] + whole[2] + whole[3] != 0.f);
   for (int u = 0; u < n; ++u) {
     // what was asked for after tile u: the copies of two tiles, and NM stores a tile
     if (idle || u == 0)
