@@ -157,21 +157,27 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
     for (int j = 0; j < CW; ++j) dma16(src[j], at0 + slot * SLOT + 1024 * (CW * wave + j));
   };
   for (int u = 0; u < 3; ++u) copy(u);
-  vm_drain();
-  const bool idle = col0 >= N;
   const int h = min(col0, N - 1) / hd, in = min(col0, N - 1) % hd;
-  __half* to = in < l.Dn ? a.k + (size_t)h * a.kv_total * l.Dn + in : a.v + (size_t)h * a.kv_total * l.Dv + in - l.Dn;
-  const int to_row = in < l.Dn ? l.Dn : l.Dv;
   // Values are stored finite: a row's weight 0 of a token that it does not see then gives 0,
   // whatever the token holds. (Its keys stay as they are, and make NaN of the rows that see it.)
   // Not so where the weights of the wave's columns are not finite, which no key would show:
-  // times zeros they add up to NaN, else to 0.
-  f4 whole = {};
+  // times zeros they add up to NaN, else to 0. (Formed while the copies are on their way.)
+  __builtin_amdgcn_sched_barrier(0);
+  f4 whole[4] = {};
+  if (in >= l.Dn)
 #pragma unroll
-  for (int k = 0; k < KS; ++k)
+    for (int k = 0; k < KS; ++k)
 #pragma unroll
-    for (int m = 0; m < NM; ++m) whole = mfma16(w[k][m], h8{}, whole);
-  const bool values = in >= l.Dn && !__any(whole[0] + whole[1] + whole[2] + whole[3] != 0.f);
+      for (int m = 0; m < NM; ++m) {
+        f4& sum = whole[(k * NM + m) % 4];
+        sum = mfma16(w[k][m], h8{}, sum);
+      }
+  const f4 odd = whole[0] + whole[1] + whole[2] + whole[3];
+  const bool values = in >= l.Dn && !__any(odd[0] + odd[1] + odd[2] + odd[3] != 0.f);
+  vm_drain();
+  const bool idle = col0 >= N;
+  __half* to = in < l.Dn ? a.k + (size_t)h * a.kv_total * l.Dn + in : a.v + (size_t)h * a.kv_total * l.Dv + in - l.Dn;
+  const int to_row = in < l.Dn ? l.Dn : l.Dv;
   for (int u = 0; u < n; ++u) {
     // what was asked for after tile u: the copies of two tiles, and NM stores a tile
     if (idle || u == 0)
