@@ -444,7 +444,8 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
       if (__any(far) && lane == 0) passed[u & 1] = u;
       lds_barrier();
       if (__builtin_amdgcn_readfirstlane(passed[u & 1]) == u) {
-        // every row takes its largest score as its reference
+        // every row that is past its reference takes its largest score as the new one (the others
+        // keep theirs: a row's roundings are its own)
 #pragma unroll
         for (int r = 0; r < S::RT; ++r) {
           top[r] = col_max(top[r]);
@@ -455,11 +456,14 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
         for (int r = 0; r < S::RT; ++r) {
           const int row = (wr * S::RT + r) * 16 + c;
           const float most = max3(m[r], top[r], smax[(1 - wt) * S::M + row]);
-          const float now = most == -INFINITY ? 0.f : most * unit;
-          const float keep = m[r] == -INFINITY ? 0.f : exp2_fast(ref[r] - now);
-          m[r] = most;
-          sum[r] *= keep;
-          ref[r] = now;
+          float keep = 1.f;
+          if ((most - m[r]) * unit > kSlack) {
+            const float now = most * unit;
+            keep = m[r] == -INFINITY ? 0.f : exp2_fast(ref[r] - now);
+            m[r] = most;
+            sum[r] *= keep;
+            ref[r] = now;
+          }
           if (g == 0 && wt == 0) skeep[row] = keep;
         }
         weights();

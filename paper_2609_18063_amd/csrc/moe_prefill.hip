@@ -365,9 +365,11 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
     if (__any(far)) {
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const float mx = fmaxf(m[r], col_max(top[r])), now = mx == -INFINITY ? 0.f : mx * unit;
-        const float keep = m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[r] - now);
-        m[r] = mx;
+        const float mx = fmaxf(m[r], col_max(top[r]));
+        const bool past = (mx - m[r]) * unit > kSlack;   // (a row's roundings are its own)
+        const float now = past ? mx * unit : ref[r];
+        const float keep = !past ? 1.f : m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[r] - now);
+        m[r] = past ? mx : m[r];
         ref[r] = now;
         sum[r] *= keep;
 #pragma unroll

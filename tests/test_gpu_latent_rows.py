@@ -1,4 +1,5 @@
-"""Latent attention's rows: weights of the model that are not finite show."""
+"""What else of a latent attention row's result may depend on: not on its neighbours' scores. Weights of the model that are not finite
+show."""
 
 import numpy as np
 import pytest
@@ -25,6 +26,59 @@ def _place(c, torch, b, rows):
     i = np.arange(len(rows))
     at = c.table_np[b, i // c.page].astype(np.int64) * c.page + i % c.page
     c.pages.view(-1, c.Dc + c.Dr)[torch.from_numpy(at).cuda()] = torch.from_numpy(rows).cuda()
+
+
+@pytest.mark.parametrize("dims,H,lens", [(S, 5, [700, 65, 33]), (W, 32, [400, 40])])
+def test_decode_rows_for_themselves(torch_cuda, dims, H, lens):
+    """Head 1's scores rise a hundredfold, or are infinite: the other heads' bits stay."""
+    g = np.random.default_rng(51)
+    c = Cache(torch_cuda, g, H, *dims, 16, lens)
+    q = _queries(g, len(lens), c)
+    clean = c.decode(q)
+    rest = np.setdiff1d(np.arange(H), [1])
+    for what in (100, np.inf):
+        p = q.copy()
+        p[:, 1] *= np.float16(what)
+        assert np.array_equal(c.decode(p)[:, rest], clean[:, rest]), what
+
+
+@pytest.mark.parametrize("dims,H,prefix", [(S, 5, 600), (W, 16, 300)])
+def test_decode_sequences_for_themselves(torch_cuda, dims, H, prefix):
+    """The same over a prefix that the batch shares, where rows of several sequences are in a workgroup."""
+    g = np.random.default_rng(52)
+    c = Cache(torch_cuda, g, H, *dims, 16, [65, 0, 200, 5], prefix=prefix)
+    q = _queries(g, 4, c)
+    clean = c.decode(q, prefix=prefix)
+    p = q.copy()
+    p[1] *= np.float16(100)
+    rest = [0, 2, 3]
+    assert np.array_equal(c.decode(p, prefix=prefix)[rest], clean[rest])
+
+
+@pytest.mark.parametrize("dims,H,lens", [(S, 2, [300]), (W, 2, [300]), (S, 2, [2100])])
+def test_prefill_rows_for_themselves(torch_cuda, dims, H, lens):
+    """A token with far larger scores, or infinite ones, inside a wave's rows and tile: the rows before it keep their
+    bits; and so do a row's neighbours where its query grows."""
+    torch, g = torch_cuda, np.random.default_rng(53)
+    c = Cache(torch, g, H, *dims, 16, lens)
+    q = _queries(g, lens[0], c)
+    q[:, :, c.Dn] = np.abs(q[:, :, c.Dn]) + np.float16(0.5)
+    clean, original = c.prefill(q, lens), c.rows[0]
+    for bad in (5, 40, 150, 250):
+        rows = original.copy()
+        for what in (200, np.inf):
+            rows[bad, c.Dc] = what
+            _place(c, torch, 0, rows)
+            got = c.prefill(q, lens)
+            assert np.array_equal(got[:bad], clean[:bad]), (bad, what)
+            if np.isinf(what):
+                assert np.isnan(got[bad:]).all()
+    _place(c, torch, 0, original)
+    for i in (7, 100, 299):
+        p = q.copy()
+        p[i] *= np.float16(100)
+        rest = np.setdiff1d(np.arange(lens[0]), [i])
+        assert np.array_equal(c.prefill(p, lens)[rest], clean[rest]), i
 
 
 @pytest.mark.parametrize("dims", [S, W])
