@@ -142,6 +142,7 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
     if (tok >= 0 && tok < s.len) page = l.table[b * l.table_stride + tok / l.page];
     where[i] = page >= 0 && page < l.n_pages ? ((int64_t)page * l.page + tok % l.page) * (2 * row_halves) : -1;
   }
+  vm_drain();                                            // (the weights: asked for before the page ids)
   __syncthreads();
   const uint32_t at0 = lds_at(lds);
   auto copy = [&](int u) {                               // (past the last tile: it again, into a free slot)
@@ -174,7 +175,6 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
       }
   const f4 odd = whole[0] + whole[1] + whole[2] + whole[3];
   const bool values = in >= l.Dn && !__any(odd[0] + odd[1] + odd[2] + odd[3] != 0.f);
-  vm_drain();
   const bool idle = col0 >= N;
   __half* to = in < l.Dn ? a.k + (size_t)h * a.kv_total * l.Dn + in : a.v + (size_t)h * a.kv_total * l.Dv + in - l.Dn;
   const int to_row = in < l.Dn ? l.Dn : l.Dv;
