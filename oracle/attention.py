@@ -17,6 +17,7 @@ EPS = 1e-6
 HALF = 2.0 ** -11        # largest relative rounding error of fp16
 SINGLE = 2.0 ** -24      # of fp32
 TINY = 2.0 ** -25        # half of fp16's smallest step
+WEIGHT = TINY / 128      # the same of a softmax weight that is held times 2^7, the row's largest at 2^7 or more
 
 
 def projection(qsz, lora, lora_scale, x):
@@ -95,7 +96,8 @@ def attend(q, rows, w_uk, w_uv, scale, seen=None):
     ds = absq.max(-1, keepdims=True)                     # (softmax: |dp / p| <= 2 max |ds|)
     mag = (p @ np.abs(lat)) @ np.abs(w_uv).T
     rel = 2 * ds + 3 * HALF + (len(rows) + Dc) * SINGLE  # + weights, latents or values, the output
-    out[live], bound[live] = o, rel * mag + TINY
+    far = ((p > 0) @ np.abs(lat)) @ np.abs(w_uv).T       # (p's largest is at most 1: each is off by WEIGHT at most)
+    out[live], bound[live] = o, rel * mag + WEIGHT * far + TINY
     return out, bound
 
 

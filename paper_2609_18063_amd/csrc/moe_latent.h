@@ -8,6 +8,15 @@ namespace moe {
 constexpr int kTile = 64;        // context tokens of a tile of the expanded form
 constexpr int kStep = 32;        // and of the absorbed form
 
+// A row's softmax weights are held as 2^(score log2(e) - reference + kRaise). The reference
+// is the row's running maximum, but follows it only where that passes it by kSlack: until
+// then nothing is rescaled. In fp16 a weight so has all bits down to 2^-(14 + kRaise) of the
+// largest, is off by at most 2^-(25 + kRaise) of it below, and is at most 2^(kSlack +
+// kRaise), which is in range. (4 and 11 would hold four more bits, but rescale more often:
+// 32 sequences of 64 heads on 12,000 shared tokens 125 us against 113.) A row's sum and all
+// its partial results are raised alike.
+constexpr float kSlack = 8.f, kRaise = 7.f;
+
 struct LatentArgs {
   int H, Dc, Dr, Dn, Dv, page;   // page: tokens a page, a power of two >= 16
   float scale;

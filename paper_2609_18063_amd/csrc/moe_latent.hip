@@ -19,7 +19,6 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr int kCus = 256;
-constexpr float kSlack = 8.f;    // (as a power of two)
 constexpr int kItemCost = 8;     // (measured: an item costs a workgroup 4 to 9 us, a tile 1 to 1.4)
 constexpr int kChunks = 15;
 
@@ -310,10 +309,8 @@ __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
 // 445 MB in 88 us, 5.05 TB/s), with many, or a shared prefix, the scores' chain of one wave
 // (its products, exponentials and the barrier): 32 sequences of 64 heads on 12,000 shared
 // tokens in 91 us, 0.6 PFLOP/s.
-// The weights are taken against a reference per row that follows the running maximum only
-// where that passes it by kSlack: until then they are at most 2^kSlack and nothing is
-// rescaled. The weights are rounded to fp16 for the product with the latents, which are
-// fp16.
+// The weights are taken against a reference per row (see kSlack), and rounded to fp16 for
+// the product with the latents, which are fp16.
 template <int DC, int DR, int MT>
 struct DecodeShape {
   static constexpr int M = 16 * MT;
@@ -366,7 +363,7 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
         for (int k = 0; k < S::KS; ++k) q[r][k] = ld_h8(a.ql + row * (DC + DR) + 32 * k + 8 * g);
       }
     };
-    float sum[S::RT], m[S::RT], ref[S::RT];                     // m: the reference, unscaled; ref: m unit, or 0
+    float sum[S::RT], m[S::RT], ref[S::RT];                     // m: the reference, unscaled; ref: m unit - kRaise, or 0
     auto start = [&]() {
 #pragma unroll
       for (int r = 0; r < S::RT; ++r) {
@@ -458,7 +455,7 @@ __global__ void __launch_bounds__((64 * DecodeShape<DC, DR, MT>::NW)) latent_dec
           const float most = max3(m[r], top[r], smax[(1 - wt) * S::M + row]);
           float keep = 1.f;
           if ((most - m[r]) * unit > kSlack) {
-            const float now = most * unit;
+            const float now = most * unit - kRaise;
             keep = m[r] == -INFINITY ? 0.f : exp2_fast(ref[r] - now);
             m[r] = most;
             sum[r] *= keep;

@@ -16,7 +16,6 @@ namespace moe {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr float kSlack = 8.f;    // (as a power of two)
 constexpr int kWaves = 8, kRows = 32 * kWaves;  // of a workgroup of the attention: waves, query rows
 
 struct Span {
@@ -301,7 +300,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
     rows(vb, tile, buf + KB + RB, std::integral_constant<int, DV / 8>());
   };
   f4 o[CT][RT] = {};
-  float m[RT], ref[RT], sum[RT];                         // reference (an unscaled score), m unit (or 0), sum
+  float m[RT], ref[RT], sum[RT];                         // reference (an unscaled score), m unit - kRaise (or 0), sum
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     m[r] = -INFINITY;
@@ -351,8 +350,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
             if (16 * t + e > see || (lost >> t & 1)) s[t][r][e] = -INFINITY;
       }
     }
-    // the reference of a row follows its maximum only where that passes it by kSlack: until
-    // then the weights are at most 2^kSlack, and nothing is rescaled
+    // the reference of a row follows its maximum only where that passes it by kSlack
     float top[RT];
     bool far = false;
 #pragma unroll
@@ -367,7 +365,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
       for (int r = 0; r < RT; ++r) {
         const float mx = fmaxf(m[r], col_max(top[r]));
         const bool past = (mx - m[r]) * unit > kSlack;   // (a row's roundings are its own)
-        const float now = past ? mx * unit : ref[r];
+        const float now = past ? mx * unit - kRaise : ref[r];
         const float keep = !past ? 1.f : m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[r] - now);
         m[r] = past ? mx : m[r];
         ref[r] = now;
@@ -417,7 +415,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
     if (row >= qs.len) continue;
     if constexpr (PARTS) {
       const size_t at = (size_t)mine_at * kRows + 32 * wave + 16 * r + c;
-      if (g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = float2{m[r] * unit, total};
+      if (g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = float2{m[r] == -INFINITY ? m[r] : ref[r], total};
       // (divided by its sum: stored as it is, o would be held twice over the loop, and spill)
       const float inv = total > 0.f ? 1.f / total : 0.f;
 #pragma unroll

@@ -1,5 +1,5 @@
-"""What else of a latent attention row's result may depend on: not on its neighbours' scores. Weights of the model that are not finite
-show."""
+"""What else of a latent attention row's result may depend on: not on its neighbours' scores, not on how far its weights
+lie apart; weights of the model that are not finite show."""
 
 import numpy as np
 import pytest
@@ -79,6 +79,28 @@ def test_prefill_rows_for_themselves(torch_cuda, dims, H, lens):
         p[i] *= np.float16(100)
         rest = np.setdiff1d(np.arange(lens[0]), [i])
         assert np.array_equal(c.prefill(p, lens)[rest], clean[rest]), i
+
+
+@pytest.mark.parametrize("dims", [S, W])
+@pytest.mark.parametrize("nats", [0, 8, 12, 14, 16])
+@pytest.mark.parametrize("form", ["decode", "prefill"])
+def test_weights_far_below_the_largest(torch_cuda, dims, nats, form):
+    """One token with a score ``nats`` above all others and a value of zero: the output is what the others add up to,
+    at weights down to e^-16 of the largest (2^-23.1: held times 2^7 they are off by 2^-25 / 2^-16.1 = 4.2 A.HALF at
+    most, alike for all of them, beside the roundings that 8 A.HALF are there for). All in one share of the work (a bound that large gives a workgroup 260
+    tiles; contexts below 1,024 tokens are not cut)."""
+    torch, g = torch_cuda, np.random.default_rng(54)
+    n = 8000 if form == "decode" else 1000
+    c = Cache(torch, g, 2, *dims, 64, [n])
+    rows = np.zeros((n, c.Dc + c.Dr), np.float16)
+    rows[1:, :c.Dc] = 1 + 0.25 * g.standard_normal((n - 1, c.Dc))
+    rows[0, c.Dc] = nats / (8 * c.scale)                   # (its latent stays 0)
+    _place(c, torch, 0, rows)
+    q = np.zeros((1, 2, c.Dn + c.Dr), np.float16)
+    q[0, :, c.Dn] = 8
+    got = c.decode(q, most=1 << 26) if form == "decode" else c.prefill(q, [1])
+    assert int(c.status) == 0
+    c.check(got, q, 0, rows)
 
 
 @pytest.mark.parametrize("dims", [S, W])
