@@ -18,6 +18,7 @@ struct LinearArgs {
   float* sums;                           // of tiles split along the inputs
 };
 
+constexpr int kMostIn = 32768, kMostRank = 64;
 constexpr int kRowsMost = 192;           // rows that the kernel without tiles takes at most
 constexpr size_t kLinearSums = 32u << 20;
 

@@ -483,6 +483,21 @@ hipError_t launch_rows(const LinearArgs& a, hipStream_t st) {
   return launch_rows<TT, 4, NT>(a, st);
 }
 
+// E of 16 rows lies beside the partial sums of A x, which above rank 16 take half of the 64 KB
+// that a launch has without being asked (68 KB at the most inputs and adapter rows).
+template <int RT>
+hipError_t launch_sums(const LinearArgs& a, hipStream_t st) {
+  auto kernel = linear_sums_kernel<RT>;
+  if constexpr (RT > 1) {
+    constexpr int most = 16 * linear_extra(kMostIn, kMostRank) * sizeof(float);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (e != hipSuccess) return e;
+  }
+  const size_t lds = 16 * (size_t)linear_extra(a.in_dim, a.r) * sizeof(float);
+  hipLaunchKernelGGL(kernel, dim3((a.T + 15) / 16), dim3(512), lds, st, a);
+  return hipGetLastError();
+}
+
 // 32 outputs a workgroup where 16 would give more workgroups than CUs: half the reads of x
 // and A (one row, 6144 x 2048, rank 16: 8.2 against 10.4 us; 8192 x 8192: 24 against 30;
 // 64 rows, 4096 x 4096: 21 against 30), 16 below, for the CUs (4096 x 2048: 6.8 against 7.9).
@@ -508,15 +523,7 @@ bool linear_by_rows(int out_dim, int in_dim, int T) {
 hipError_t launch_linear(const LinearArgs& a, hipStream_t st) {
   if (a.T <= 16) return launch_rows<1>(a, st);
   if (linear_by_rows(a.out_dim, a.in_dim, a.T)) return launch_rows<2>(a, st);
-  const size_t lds = 16 * (size_t)linear_extra(a.in_dim, a.r) * sizeof(float);
-  const dim3 grid((a.T + 15) / 16), block(512);
-  if (a.r == 0)
-    hipLaunchKernelGGL((linear_sums_kernel<0>), grid, block, lds, st, a);
-  else if (a.r <= 16)
-    hipLaunchKernelGGL((linear_sums_kernel<1>), grid, block, lds, st, a);
-  else
-    hipLaunchKernelGGL((linear_sums_kernel<4>), grid, block, lds, st, a);
-  hipError_t e = hipGetLastError();
+  hipError_t e = a.r == 0 ? launch_sums<0>(a, st) : a.r <= 16 ? launch_sums<1>(a, st) : launch_sums<4>(a, st);
   if (e != hipSuccess) return e;
   const TilePlan p = tile_plan(a.out_dim, a.T, a.in_dim / 64);
   hipLaunchKernelGGL(linear_tile_kernel, dim3(p.workgroups()), dim3(256), 0, st, a, p);
@@ -532,12 +539,12 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t st) {
 
 namespace {
 
-constexpr int kMaxIn = 32768, kMaxOut = 1 << 20, kMaxRows = 1 << 20;
+constexpr int kMaxOut = 1 << 20, kMaxRows = 1 << 20;
 constexpr int64_t kMaxOutputs = int64_t(1) << 37;      // (a grid's threads: 2^24 tiles of 128 x 128, 256 each)
 
 bool linear_shape_ok(int out_dim, int in_dim, int rank, int T) {
-  return out_dim >= 1 && out_dim <= kMaxOut && in_dim >= 64 && in_dim <= kMaxIn && in_dim % 64 == 0 &&
-         rank >= 0 && rank <= 64 && T >= 0 && T <= kMaxRows && (int64_t)T * out_dim <= kMaxOutputs;
+  return out_dim >= 1 && out_dim <= kMaxOut && in_dim >= 64 && in_dim <= moe::kMostIn && in_dim % 64 == 0 &&
+         rank >= 0 && rank <= moe::kMostRank && T >= 0 && T <= kMaxRows && (int64_t)T * out_dim <= kMaxOutputs;
 }
 size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
