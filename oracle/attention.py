@@ -41,7 +41,7 @@ def projection(qsz, lora, lora_scale, x):
 def projection_bound(y, mag, in_dim, rank, f16):
     """Sums of at most 64 products, in_dim / 64 groups (two terms each), rank more and 16 partial sums in fp32,
     each rounding at most SINGLE of the magnitude; 2^-21 of it for the group sums and A x held as two halves
-    (22 bits of the row's largest, which the magnitude bounds); one rounding to fp16."""
+    (22 bits of each); one rounding to fp16."""
     e = (64 + 2 * (in_dim // 64) + 2 * rank + 16) * SINGLE * mag + 2.0 ** -21 * mag
     return e + (HALF * np.abs(y) + TINY if f16 else 0.0)
 

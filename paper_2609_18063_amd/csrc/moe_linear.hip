@@ -193,9 +193,10 @@ __global__ void __launch_bounds__(64 * NW) linear_rows_kernel(LinearArgs a) {
 // ---- many rows -------------------------------------------------------------------
 // What multiplies z and B is small: per row the group sums of x and lora_scale A x.
 // One launch forms them (16 rows a workgroup) as E [T][KE] = (group sums, zeros to a
-// multiple of 32, lora_scale A x, zeros), scaled per row by a power of two to at most
-// 2 and split into two halves, hi + lo (22 bits of the row's largest): the tile
-// products then add them as KE more inputs whose weights z and B are exact in fp16.
+// multiple of 32, lora_scale A x, zeros), scaled per row by a power of two to less than
+// 2^15 and split into two halves, hi + lo (22 bits of each number down to 2^-18 of the row's
+// largest, and 2^-39 of that below): the tile products then add them as KE more inputs whose
+// weights z and B are exact in fp16.
 // Bound by latency, few workgroups for x's reads: 1,555 rows of 4,096, rank 16 (13 MB), 10 us.
 template <int RT>
 __global__ void __launch_bounds__(512) linear_sums_kernel(LinearArgs a) {
@@ -265,7 +266,7 @@ __global__ void __launch_bounds__(512) linear_sums_kernel(LinearArgs a) {
     float top = 0.f;
     for (int j = lane; j < KE; j += kWave) top = fmaxf(top, fabsf(e[j]));
     top = __uint_as_float(wave_max_u32(__float_as_uint(top)));  // (of numbers >= 0)
-    const int ex = top > 0.f && top < INFINITY ? max(ilogbf(top), -100) : 0;
+    const int ex = top > 0.f && top < INFINITY ? max(ilogbf(top), -86) - 14 : 0;
     for (int j = lane; j < KE; j += kWave) {
       const float v = ldexpf(e[j], -ex);
       const _Float16 hi = (_Float16)v;

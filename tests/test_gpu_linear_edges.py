@@ -42,3 +42,29 @@ def test_most_inputs(torch_cuda, T):
     lin = Linear(torch_cuda, g, 40, 32768, 64)
     x = g.standard_normal((T, 32768)).astype(np.float16)
     lin.check(x, _run(torch_cuda, lin, x))
+
+
+@pytest.mark.parametrize("T", [3, 40, 200])
+def test_large_inputs_of_a_group_without_weights(torch_cuda, T):
+    """A group whose scales and zeros are 0 under inputs near fp16's largest: it adds nothing, and takes no bits of what
+    the other groups add."""
+    g = np.random.default_rng(41)
+    lin = Linear(torch_cuda, g, 150, 320, 16)
+    q, s, z = lin.qsz
+    s[:, 2], z[:, 2] = 0, 0
+    lin.lora[0][:, 128:192] = 0
+    lin.proj, lin.keep = lin.B.upload_projection(lin.qsz, lin.lora, "cuda")
+    x = g.standard_normal((T, 320)).astype(np.float16)
+    x[:, 128:192] = 60000
+    lin.check(x, _run(torch_cuda, lin, x))
+
+
+@pytest.mark.parametrize("T", [3, 200])
+def test_large_adapter_inputs_without_outputs(torch_cuda, T):
+    """B = 0, as an adapter starts, under a large A x."""
+    g = np.random.default_rng(42)
+    lin = Linear(torch_cuda, g, 150, 320, 16, scale=64.0)
+    lin.lora = (np.float16(1000) * lin.lora[0], 0 * lin.lora[1])
+    lin.proj, lin.keep = lin.B.upload_projection(lin.qsz, lin.lora, "cuda")
+    x = g.standard_normal((T, 320)).astype(np.float16)
+    lin.check(x, _run(torch_cuda, lin, x))
