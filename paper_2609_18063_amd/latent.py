@@ -164,13 +164,15 @@ class LatentAttention:
 
     def prefill(self, n, x, r, seq, pos, q_start, kv_start, kv_total, max_q):
         """Layer ``n`` for chunks of prompts: the ragged batch of ``moe_latent_prefill``, sequence b in table row b.
-        Eager only: its workspace grows with ``kv_total``."""
+        Rows of padding behind the last sequence (``seq`` -1) keep their ``r``. Eager only: its workspace grows with
+        ``kv_total``, ``H (d_nope + d_v)`` halves a token, for one layer at a time."""
         q = self._project(n, x, seq, pos)
         need = B.latent_prefill_workspace_bytes(self.spec, q_start.numel() - 1, kv_total)
         if self.ws_prefill is None or self.ws_prefill.nbytes < need:
             self.ws_prefill = self._ws(need)
-        B.latent_prefill(self.spec, self.cache.layers[n], self.blocks[n].w_kvb, q, q_start, kv_start, kv_total, max_q,
-                         self.ob[:x.shape[0]], self.cache.status, self.ws_prefill)
+        o = self.ob[:x.shape[0]].zero_()                 # (rows of padding are not written, and W_o 0 = 0)
+        B.latent_prefill(self.spec, self.cache.layers[n], self.blocks[n].w_kvb, q, q_start, kv_start, kv_total, max_q, o,
+                         self.cache.status, self.ws_prefill)
         self._out(n, r)
 
 
