@@ -51,9 +51,10 @@ extern "C" {
 
 /* ---- device status bits (OR-ed into *status_dev by the kernels) ---------- */
 #define MOE_STATUS_SLOT_MISS 1u  /* routed expert has no resident slot       */
-#define MOE_STATUS_BAD_INDEX 2u  /* expert id outside [0, E)                  */
+#define MOE_STATUS_BAD_INDEX 2u  /* expert id outside [0, E); sequence or position
+                                    out of range (moe_latent_append)          */
 #define MOE_STATUS_BAD_PAGE   8u  /* page id outside [0, n_pages)             */
-#define MOE_STATUS_BAD_LENGTH 16u /* length or position outside its bounds    */
+#define MOE_STATUS_BAD_LENGTH 16u /* length or list of starts outside its bounds */
 #define MOE_STATUS_ENGINE_ABORT 4u /* decode engine left a wait on its time limit,
                                       or ran on an unexpected CU/XCD layout     */
 
@@ -416,7 +417,11 @@ int moe_latent_append(const moe_latent_spec* spec, const moe_latent_cache* cache
  * A prefix that the whole batch shares: prefix_pages, device int32 ids of its
  * ceil(prefix_len / page_tokens) pages (NULL with prefix_len 0). Every sequence
  * attends to the prefix_len tokens of it and to its own kv_len; the prefix is
- * read once for many sequences. A row that has no token, or whose scores are
+ * read once for many sequences. Its own tokens stand in its table row from the
+ * first column on, whatever the prefix. (For table rows that hold the whole
+ * sequence, a prefix of whole pages first, moe_latent_append takes the rows as
+ * they are, with positions counted from the prefix's first token, and this call
+ * a cache whose table begins prefix_len / page_tokens columns further on.) A row that has no token, or whose scores are
  * all minus infinity, gives zeros; one with a NaN among its scores is NaN.
  * B up to n_seqs. workspace: moe_latent_decode_workspace_bytes (no initial
  * contents needed); calls that share one must be ordered on one stream.

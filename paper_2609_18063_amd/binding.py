@@ -852,7 +852,9 @@ def _attends(spec, cache, w_kvb, q, out, workspace):
 def latent_decode(spec, cache, w_kvb, q, kv_len, max_len, out, status, workspace, prefix=None, prefix_len=0,
                   stream=None):
     """moe_latent_decode: ``q`` fp16 ``[B, H, d_nope + d_rope]``, ``kv_len`` int32 ``[B]``; ``prefix``: int32 page
-    ids of ``prefix_len`` tokens that every sequence of the batch begins with."""
+    ids of ``prefix_len`` tokens that every sequence of the batch begins with. ``cache`` and ``kv_len`` are of the
+    tokens behind the prefix: where table rows hold the prefix's k whole pages too, as those of forks do, a cache of
+    the view ``table[:, k:]``."""
     torch = _the_torch()
     B = q.shape[0]
     _attends(spec, cache, w_kvb, q, out, workspace)
