@@ -284,9 +284,10 @@ __device__ __forceinline__ int x_key(int row) { return ((row >> 1) & 1) | ((row 
 
 // The products on the matrix cores: 128 rows of x by 128 outputs, four waves of 64 x 64,
 // one 64-input group a step. x, codes and (s, z) come through LDS, two steps ahead in three
-// slots. Bound by LDS and the VALU: a step of a CU's two workgroups reads 128 KB of LDS
-// (about 1,200 clocks), unpacks codes and applies scales (1,100 a SIMD) beside its products
-// (64 a SIMD, 550), and takes 2,600. 1,555 rows, 5001 x 4096, rank 16: 109 us, 0.59 PFLOP/s.
+// slots. Bound by three pipes that overlap in part: a step of a CU's two workgroups reads 88 KB
+// of LDS and has 41 KB copied in (about 1,200 clocks), unpacks codes and applies scales (1,100 a
+// SIMD) and has 64 products a SIMD (1,030), and takes 2,600. 1,555 rows, 5001 x 4096, rank 16:
+// 109 us, 0.59 PFLOP/s.
 // Workgroups come in rounds of kSlots. The tiles that do not fill a round are split along
 // the inputs into as many parts as fill it (first in the grid, so that whole tiles follow
 // the short parts); a part writes fp32 sums, which one more launch adds in order.

@@ -178,7 +178,8 @@ class LatentAttention:
 
 class ChainAttention:
     """The blocks as a decode chain's attention: one sequence, one token a step. ``pos`` and ``kv_len`` live on
-    the GPU, so that captured steps replay at any token; ``at`` sets them before a token."""
+    the GPU, so that captured steps replay at any token; ``at`` sets them before a token. What the calls find wrong
+    is in ``cache.status``, not in the chain's."""
 
     def __init__(self, d, spec, blocks, n_tokens):
         self.cache = LatentCache(spec, len(blocks), -(-n_tokens // spec.page_tokens), 1, n_tokens)
