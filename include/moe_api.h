@@ -406,7 +406,8 @@ int moe_latent_append(const moe_latent_spec* spec, const moe_latent_cache* cache
 
 /*
  * One query token per sequence, in the absorbed form: the query is taken into
- * the latent space (rounded to fp16, the type of the rows it meets), all heads
+ * the latent space (rounded to fp16, the type of the rows it meets: beyond its
+ * range it is infinite, and what scores come of that are infinite or NaN), all heads
  * read each cached row once, and the weighted latents (rounded to fp16) go
  * through W_uv.
  * w_kvb_f16: device fp16 [H][d_nope + d_v][d_latent], W_uk,h above W_uv,h.
@@ -439,7 +440,8 @@ int moe_latent_decode(const moe_latent_spec* spec, const moe_latent_cache* cache
  * its context of kv_start[b + 1] - kv_start[b] cached tokens (table row b;
  * already written, the chunk's own among them), and each attends to the
  * tokens up to its own position. (An expanded value beyond fp16's range is
- * taken as its largest; what a later token holds does not reach a row.)
+ * taken as its largest, also by rows that see its token, and an expanded key is
+ * infinite there; what a later token holds does not reach a row.)
  * q_start, kv_start: device int32 [B + 1], ascending from 0 or more. T,
  * kv_total and max_q (up to T): bounds on the last q_start, the last kv_start
  * and the longest chunk. q_f16: device fp16 [T][H][d_nope + d_rope], rotated; out_f16:

@@ -308,7 +308,7 @@ __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
 // one barrier a tile. With few heads HBM bounds it (32 heads, 48 sequences, 378,000 tokens:
 // 445 MB in 88 us, 5.05 TB/s), with many, or a shared prefix, the scores' chain of one wave
 // (its products, exponentials and the barrier): 32 sequences of 64 heads on 12,000 shared
-// tokens in 91 us, 0.6 PFLOP/s.
+// tokens in 88 us, 0.62 PFLOP/s.
 // The weights are taken against a reference per row (see kSlack), and rounded to fp16 for
 // the product with the latents, which are fp16.
 template <int DC, int DR, int MT>

@@ -56,8 +56,10 @@ __device__ __forceinline__ int tile_base(const PrefillArgs& a, int b) {
 // LDS in four slots, copied three ahead: with the weights through LDS too, 128 x 128 tiles
 // and one step ahead, 3,100 tokens of 512 latents by 32 heads of 256 columns took 54 us, now
 // 39 (0.67 PFLOP/s): 13 until the first step (weights, page ids) and 1.9 a step, of which
-// the LDS reads need 1.0 and the products 0.5. 256 latents, 64 columns a wave: 22 us for
+// the LDS reads need 1.0 and the products 0.9. 256 latents, 64 columns a wave: 22 us for
 // 14,500 tokens by 8 heads of 128 columns.
+// Keys and values are rounded to fp16, as operands of the matrix cores: held as two halves
+// each, the workspace and the attention's products and LDS reads, which bound it, would double.
 // Before that the workgroups share the 64-token tiles of the sequences (`side` numbers):
 // they copy a tile's rotated keys into one run, and note which of its four 16-token groups
 // have no page.
@@ -512,7 +514,8 @@ hipError_t launch_expand(const PrefillArgs& a, hipStream_t st) {
 }  // namespace
 
 // Into how many parts the contexts are cut: as fill the CUs, of eight tiles at least on
-// average (777 tokens in five chunks on 14,500, 8 heads: the call in 62 us, uncut 121).
+// average (777 tokens in five chunks on 14,500, 8 heads: the call in 53 us; uncut, with an
+// earlier expansion, 121 against 62).
 int prefill_parts(int max_q, int H, int B, int kv_total) {
   static_assert(kRows == kPartRows, "rows of a partial result");
   const int64_t wholes = (int64_t)((max_q + kRows - 1) / kRows) * H * B;
