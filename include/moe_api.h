@@ -407,9 +407,9 @@ int moe_latent_append(const moe_latent_spec* spec, const moe_latent_cache* cache
 /*
  * One query token per sequence, in the absorbed form: the query is taken into
  * the latent space (rounded to fp16, the type of the rows it meets: beyond its
- * range it is infinite, and what scores come of that are infinite or NaN), all heads
- * read each cached row once, and the weighted latents (rounded to fp16) go
- * through W_uv.
+ * range it is infinite, and the scores that come of it are infinite or NaN), all
+ * heads read each cached row once, and the weighted latents (rounded to fp16)
+ * go through W_uv.
  * w_kvb_f16: device fp16 [H][d_nope + d_v][d_latent], W_uk,h above W_uv,h.
  * q_f16: device fp16 [B][H][d_nope + d_rope], rotated. out_f16: [B][H][d_v].
  * kv_len: device int32 [B], tokens of sequence b = table row b (0: none);
@@ -422,8 +422,9 @@ int moe_latent_append(const moe_latent_spec* spec, const moe_latent_cache* cache
  * first column on, whatever the prefix. (For table rows that hold the whole
  * sequence, a prefix of whole pages first, moe_latent_append takes the rows as
  * they are, with positions counted from the prefix's first token, and this call
- * a cache whose table begins prefix_len / page_tokens columns further on.) A row that has no token, or whose scores are
- * all minus infinity, gives zeros; one with a NaN among its scores is NaN.
+ * a cache whose table begins prefix_len / page_tokens columns further on.)
+ * A row that has no token, or whose scores are all minus infinity, gives zeros;
+ * one with a NaN among its scores is NaN.
  * B up to n_seqs. workspace: moe_latent_decode_workspace_bytes (no initial
  * contents needed); calls that share one must be ordered on one stream.
  */
