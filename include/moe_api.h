@@ -461,6 +461,99 @@ int moe_latent_prefill(const moe_latent_spec* spec, const moe_latent_cache* cach
                        size_t workspace_bytes, void* stream);
 
 /*
+ * The latent cache held in 4 bits, beside the fp16 one: the same tables, and pages
+ * of moe_latent4_page_bytes(spec) bytes. A row's values stand in groups of 64 (the
+ * last group is the rotated key): a group has a step s and a middle z (fp16), a
+ * value a code q of 0..15 and is s (q - 8) + z. A page of P tokens, in order, with
+ * G = d_latent / 64 + 1 groups:
+ *   uint8 [P][d_latent / 2]   the latents' codes, element 2j in the low half of byte j
+ *   uint8 [P][d_rope / 2]     the keys' codes
+ *   fp16  [G][P]              s of each group and token
+ *   fp16  [G][P]              z
+ * (576 values: 324 bytes, against 1152 of the fp16 cache.) moe_latent_cache describes
+ * it, with these pages. Pages of one cache and calls of the other must not be mixed.
+ */
+size_t moe_latent4_page_bytes(const moe_latent_spec* spec);
+
+/*
+ * As moe_latent_append, into a 4-bit cache: the row (c / sqrt(mean(c^2) + 1e-6) *
+ * gamma, rot(k_r)) is quantized by groups,
+ *   s = fp16((hi - lo) / 15), z = fp16(lo + 8 s), q = clamp(rint((v - z) / s) + 8, 0, 15)
+ * with lo and hi the group's smallest and largest value (s = 0: q = 8), all of it
+ * formed in 64 bits from the fp32 inputs. A group with a value that is not finite, or whose s or z is
+ * beyond fp16, is NaN throughout.
+ * slot: device int32 [T], the token's place in its sequence; pos its position, which gives the
+ * angles. They are the same until tokens of the sequence are evicted.
+ */
+int moe_latent4_append(const moe_latent_spec* spec, const moe_latent_cache* cache, const float* kv,
+                       const void* gamma_f16, const float* rope, int max_pos, const int32_t* seq,
+                       const int32_t* slot, const int32_t* pos, int T, const void* q_f16, void* q_out_f16,
+                       uint32_t* status, void* stream);
+
+/*
+ * T cached rows as fp16, each value rounded once: rows device fp16 [T][d_latent +
+ * d_rope], row t the token at place slot[t] of sequence seq[t] (which may be read
+ * more than once). seq < 0, and tokens out of range or without a page (status as of
+ * moe_latent_append), leave their row as it was.
+ */
+int moe_latent4_read(const moe_latent_spec* spec, const moe_latent_cache* cache, const int32_t* seq,
+                     const int32_t* slot, int T, void* rows_f16, uint32_t* status, void* stream);
+
+/*
+ * As moe_latent_decode, over a 4-bit cache and without a shared prefix (forks share pages
+ * through their tables). The values are rounded to fp16, the type of the products.
+ * sums: device fp32 or NULL, sequence b's row at sums + b sums_stride (sums_stride >=
+ * max_len): the weights of its tokens over all heads are added to it,
+ *   sums[b][j] += sum over h of softmax_h(j),  j < kv_len[b],
+ * in one order, so that equal calls give equal sums. Heads without a weight (all scores minus
+ * infinity) and tokens without a page add nothing; a head with a NaN among its scores makes
+ * NaN of all its sequence's tokens. Entries at kv_len[b] and beyond stay as they were.
+ */
+size_t moe_latent4_decode_workspace_bytes(const moe_latent_spec* spec, int B, int max_len, int sums);
+int moe_latent4_decode(const moe_latent_spec* spec, const moe_latent_cache* cache, const void* w_kvb_f16,
+                       const void* q_f16, int B, const int32_t* kv_len, int max_len, void* out_f16, float* sums,
+                       int64_t sums_stride, uint32_t* status, void* workspace, size_t workspace_bytes,
+                       void* stream);
+
+/*
+ * As moe_latent_prefill, over a 4-bit cache. sums: as of moe_latent4_decode, over all rows of a
+ * sequence's chunk and all heads; a row has room for sums_len tokens (1 .. sums_stride),
+ * and those beyond get none. `sums` of the workspace size: whether the call has them; it grows
+ * with T too then.
+ */
+size_t moe_latent4_prefill_workspace_bytes(const moe_latent_spec* spec, int T, int B, int kv_total, int sums);
+int moe_latent4_prefill(const moe_latent_spec* spec, const moe_latent_cache* cache, const void* w_kvb_f16,
+                        const void* q_f16, int T, const int32_t* q_start, const int32_t* kv_start, int B,
+                        int kv_total, int max_q, void* out_f16, float* sums, int64_t sums_stride, int sums_len,
+                        uint32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Which tokens of a sequence stay when it goes back to `budget` of them, per layer: the
+ * first `sinks`, the last `recent` (sinks + recent <= budget), and of the others those
+ * with the largest sums, ties to the lower place (NaN counts as minus infinity). A sequence of no
+ * more than `budget` tokens keeps all.
+ * sums: device fp32 [n_layers][B][width]. kv_len: device int32 [B], up to width (else
+ * MOE_STATUS_BAD_LENGTH, and the nearest that is not). keep: device int32
+ * [n_layers][B][budget], the places that stay, ascending, then -1. sums_out: the
+ * shape of sums, which may be sums: the sums of the tokens that stay, then zeros.
+ */
+int moe_evict_select(const float* sums, float* sums_out, int n_layers, int B, int width, const int32_t* kv_len,
+                     int budget, int sinks, int recent, int32_t* keep, uint32_t* status, void* stream);
+
+/*
+ * Move the tokens that stay: in each of n_layers arrays of 4-bit pages (layer_bytes
+ * apart, cache: the first of them), row keep[layer][b][i] of table row b goes to place i of
+ * the pages to_table[b] (device int32, to_stride >= ceil(budget / page_tokens) apart). No
+ * page of to_table may be one that a kept token stands in, or stand there twice; others may share the old pages
+ * (forks), which stay as they are. keep < 0: nothing is moved. A place out of range sets
+ * MOE_STATUS_BAD_INDEX, a bad page of either table MOE_STATUS_BAD_PAGE, and its token is not
+ * moved.
+ */
+int moe_latent4_move(const moe_latent_spec* spec, const moe_latent_cache* cache, int n_layers,
+                     int64_t layer_bytes, const int32_t* keep, int B, int budget, const int32_t* to_table,
+                     int64_t to_stride, uint32_t* status, void* stream);
+
+/*
  * Pages of a paged cache, on the host: reference counts and the lowest free
  * ids first. One pool serves all layers (a page id means the same page in
  * every layer's array). Not thread-safe for concurrent calls on one pool.

@@ -158,6 +158,25 @@ SIGNATURES = {
     "moe_latent_prefill": (c_int, [ctypes.POINTER(MoeLatentSpec), ctypes.POINTER(MoeLatentCache), c_void_p,
                                    c_void_p, c_int, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p,
                                    c_void_p, c_void_p, c_size_t, c_void_p]),
+    "moe_latent4_page_bytes": (c_size_t, [ctypes.POINTER(MoeLatentSpec)]),
+    "moe_latent4_append": (c_int, [ctypes.POINTER(MoeLatentSpec), ctypes.POINTER(MoeLatentCache), c_void_p,
+                                   c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_int, c_void_p,
+                                   c_void_p, c_void_p, c_void_p]),
+    "moe_latent4_read": (c_int, [ctypes.POINTER(MoeLatentSpec), ctypes.POINTER(MoeLatentCache), c_void_p,
+                                 c_void_p, c_int, c_void_p, c_void_p, c_void_p]),
+    "moe_latent4_decode_workspace_bytes": (c_size_t, [ctypes.POINTER(MoeLatentSpec), c_int, c_int, c_int]),
+    "moe_latent4_decode": (c_int, [ctypes.POINTER(MoeLatentSpec), ctypes.POINTER(MoeLatentCache), c_void_p,
+                                   c_void_p, c_int, c_void_p, c_int, c_void_p, c_void_p, c_int64, c_void_p,
+                                   c_void_p, c_size_t, c_void_p]),
+    "moe_latent4_prefill_workspace_bytes": (c_size_t, [ctypes.POINTER(MoeLatentSpec), c_int, c_int, c_int,
+                                                       c_int]),
+    "moe_latent4_prefill": (c_int, [ctypes.POINTER(MoeLatentSpec), ctypes.POINTER(MoeLatentCache), c_void_p,
+                                    c_void_p, c_int, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p,
+                                    c_void_p, c_int64, c_int, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "moe_evict_select": (c_int, [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_int, c_int, c_int,
+                                 c_void_p, c_void_p, c_void_p]),
+    "moe_latent4_move": (c_int, [ctypes.POINTER(MoeLatentSpec), ctypes.POINTER(MoeLatentCache), c_int, c_int64,
+                                 c_void_p, c_int, c_int, c_void_p, c_int64, c_void_p, c_void_p]),
     "moe_page_pool_create": (c_int, [c_int, c_int, ctypes.POINTER(c_void_p)]),
     "moe_page_pool_destroy": (c_int, [c_void_p]),
     "moe_page_pool_available": (c_int, [c_void_p]),
@@ -795,11 +814,14 @@ def latent_spec_check(spec):
 def latent_cache(pages, table):
     """moe_latent_cache of ``pages`` fp16 ``[n_pages, page_tokens, d_latent + d_rope]`` and ``table`` int32
     ``[n_seqs, max_pages]`` (rows may be strided). The struct keeps both alive."""
-    torch = _the_torch()
-    _dense("pages", torch.float16, pages)
-    _need(pages.dim() == 3 and table.dim() == 2 and table.dtype == torch.int32
-          and (table.shape[1] == 1 or table.stride(1) == 1) and table.device == pages.device,
-          "pages [n_pages, page_tokens, row] and an int32 table [n_seqs, max_pages] on one GPU")
+    _dense("pages", _the_torch().float16, pages)
+    _need(pages.dim() == 3, "pages [n_pages, page_tokens, row]")
+    return _cache_struct(pages, table)
+
+
+def _cache_struct(pages, table):
+    _need(table.dim() == 2 and table.dtype == _the_torch().int32 and (table.shape[1] == 1 or table.stride(1) == 1)
+          and table.device == pages.device, "an int32 table [n_seqs, max_pages] on the pages' GPU")
     c = MoeLatentCache(pages.data_ptr(), table.data_ptr(),
                        table.stride(0) if table.shape[0] > 1 else table.shape[1], pages.shape[0], table.shape[0],
                        table.shape[1], 0)
@@ -810,7 +832,7 @@ def latent_cache(pages, table):
 def _cache_of(spec, cache):
     """The cache's pages, as the description has them."""
     pages = cache.keep[0]
-    if pages.shape[1:] != (spec.page_tokens, spec.d_latent + spec.d_rope):
+    if pages.dim() != 3 or pages.shape[1:] != (spec.page_tokens, spec.d_latent + spec.d_rope):
         raise ValueError("pages of %d tokens of %d" % (spec.page_tokens, spec.d_latent + spec.d_rope))
     return pages
 
@@ -882,6 +904,139 @@ def latent_prefill(spec, cache, w_kvb, q, q_start, kv_start, kv_total, max_q, ou
                                     _ptr(q_start), _ptr(kv_start), q_start.numel() - 1, kv_total, max_q, _ptr(out),
                                     _ptr(status), _ptr(workspace), workspace.nbytes, _stream(stream)),
            "moe_latent_prefill")
+
+
+def latent4_page_bytes(spec):
+    return int(lib().moe_latent4_page_bytes(ctypes.byref(spec)))
+
+
+def latent4_cache(spec, pages, table):
+    """moe_latent_cache of 4-bit ``pages`` uint8 ``[n_pages, latent4_page_bytes(spec)]`` and ``table`` int32 ``[n_seqs,
+    max_pages]`` (rows may be strided), for the ``latent4_`` calls. The struct keeps both alive."""
+    torch = _the_torch()
+    _dense("pages", torch.uint8, pages)
+    _need(pages.dim() == 2 and pages.shape[1] == latent4_page_bytes(spec), "uint8 pages [n_pages, %d]" % latent4_page_bytes(spec))
+    return _cache_struct(pages, table)
+
+
+def _cache4(spec, cache):
+    pages = cache.keep[0]
+    _dense("pages", _the_torch().uint8, pages)
+    _need(pages.dim() == 2 and pages.shape[1] == latent4_page_bytes(spec), "a cache of latent4_cache with this description")
+
+
+def latent4_append(spec, cache, kv, gamma, rope, seq, slot, pos, status, q=None, q_out=None, stream=None):
+    """moe_latent4_append: as ``latent_append``, with each token's place ``slot`` int32 ``[T]`` beside its position."""
+    torch = _the_torch()
+    T = kv.shape[0]
+    _cache4(spec, cache)
+    _dense("gamma", torch.float16, gamma)
+    _dense("kv, rope", torch.float32, kv, rope)
+    _dense("seq, slot, pos, status", torch.int32, seq, slot, pos, status)
+    _need(kv.shape == (T, spec.d_latent + spec.d_rope) and rope.shape[1:] == (spec.d_rope // 2, 2)
+          and rope.dim() == 3 and gamma.numel() == spec.d_latent and seq.numel() == slot.numel() == pos.numel() == T,
+          "kv [T, d_latent + d_rope], gamma [d_latent], rope [max_pos, d_rope / 2, 2], seq, slot and pos [T]")
+    _need((q is None) == (q_out is None), "q and q_out: both or none")
+    if q is not None:
+        _dense("q, q_out", torch.float16, q, q_out)
+        _need(q.shape == q_out.shape == (T, spec.heads, spec.d_nope + spec.d_rope),
+              "q and q_out [T, H, d_nope + d_rope]")
+    _check(lib().moe_latent4_append(ctypes.byref(spec), ctypes.byref(cache), _ptr(kv), _ptr(gamma), _ptr(rope),
+                                    rope.shape[0], _ptr(seq), _ptr(slot), _ptr(pos), T, _ptr(q), _ptr(q_out),
+                                    _ptr(status), _stream(stream)), "moe_latent4_append")
+
+
+def latent4_read(spec, cache, seq, slot, rows, status, stream=None):
+    """moe_latent4_read: the rows at ``seq`` / ``slot`` int32 ``[T]`` into ``rows`` fp16 ``[T, d_latent + d_rope]``."""
+    torch = _the_torch()
+    T = rows.shape[0]
+    _cache4(spec, cache)
+    _dense("rows", torch.float16, rows)
+    _dense("seq, slot, status", torch.int32, seq, slot, status)
+    _need(rows.shape == (T, spec.d_latent + spec.d_rope) and seq.numel() == slot.numel() == T,
+          "rows [T, d_latent + d_rope], seq and slot [T]")
+    _check(lib().moe_latent4_read(ctypes.byref(spec), ctypes.byref(cache), _ptr(seq), _ptr(slot), T, _ptr(rows),
+                                  _ptr(status), _stream(stream)), "moe_latent4_read")
+
+
+def _attends4(spec, cache, w_kvb, q, out, workspace, sums, B, least):
+    """The checks that both forms share; the stride of the sums' rows."""
+    torch = _the_torch()
+    _room(workspace)
+    _cache4(spec, cache)
+    _dense("w_kvb, q, out", torch.float16, w_kvb, q, out)
+    _need(w_kvb.shape == (spec.heads, spec.d_nope + spec.d_v, spec.d_latent)
+          and q.shape[1:] == (spec.heads, spec.d_nope + spec.d_rope)
+          and out.shape == (q.shape[0], spec.heads, spec.d_v),
+          "w_kvb [H, d_nope + d_v, d_latent], q [T, H, d_nope + d_rope], out [T, H, d_v]")
+    if sums is None:
+        return 0
+    _need(sums.dtype == torch.float32 and sums.dim() == 2 and sums.shape[0] >= B and sums.shape[1] >= least
+          and (sums.shape[1] == 1 or sums.stride(1) == 1) and sums.get_device() == _current_device(),
+          "sums: fp32 [B, at least %d] with unit column stride on the current GPU" % least)
+    return sums.stride(0) if sums.shape[0] > 1 else sums.shape[1]
+
+
+def latent4_decode_workspace_bytes(spec, B, max_len, sums=False):
+    return int(lib().moe_latent4_decode_workspace_bytes(ctypes.byref(spec), B, max_len, int(sums)))
+
+
+def latent4_decode(spec, cache, w_kvb, q, kv_len, max_len, out, status, workspace, sums=None, stream=None):
+    """moe_latent4_decode: as ``latent_decode``; ``sums`` fp32 ``[B, >= max_len]`` or None, to which each token's weights
+    over all heads are added."""
+    B = q.shape[0]
+    stride = _attends4(spec, cache, w_kvb, q, out, workspace, sums, B, max_len)
+    _dense("kv_len, status", _the_torch().int32, kv_len, status)
+    _need(kv_len.numel() == B, "kv_len [B]")
+    _check(lib().moe_latent4_decode(ctypes.byref(spec), ctypes.byref(cache), _ptr(w_kvb), _ptr(q), B, _ptr(kv_len),
+                                    max_len, _ptr(out), _ptr(sums), stride, _ptr(status), _ptr(workspace),
+                                    workspace.nbytes, _stream(stream)), "moe_latent4_decode")
+
+
+def latent4_prefill_workspace_bytes(spec, T, B, kv_total, sums=False):
+    return int(lib().moe_latent4_prefill_workspace_bytes(ctypes.byref(spec), T, B, kv_total, int(sums)))
+
+
+def latent4_prefill(spec, cache, w_kvb, q, q_start, kv_start, kv_total, max_q, out, status, workspace, sums=None,
+                    stream=None):
+    """moe_latent4_prefill: as ``latent_prefill``; ``sums`` fp32 ``[B, tokens]`` or None (tokens beyond it get none)."""
+    B = q_start.numel() - 1
+    stride = _attends4(spec, cache, w_kvb, q, out, workspace, sums, B, 1)
+    _dense("q_start, kv_start, status", _the_torch().int32, q_start, kv_start, status)
+    _need(q_start.numel() == kv_start.numel() >= 1, "q_start and kv_start [B + 1]")
+    _check(lib().moe_latent4_prefill(ctypes.byref(spec), ctypes.byref(cache), _ptr(w_kvb), _ptr(q), q.shape[0],
+                                     _ptr(q_start), _ptr(kv_start), B, kv_total, max_q, _ptr(out), _ptr(sums), stride,
+                                     0 if sums is None else sums.shape[1], _ptr(status), _ptr(workspace),
+                                     workspace.nbytes, _stream(stream)), "moe_latent4_prefill")
+
+
+def evict_select(sums, kv_len, budget, sinks, recent, keep, sums_out, status, stream=None):
+    """moe_evict_select: ``sums`` fp32 ``[layers, B, width]``, ``kv_len`` int32 ``[B]``, ``keep`` int32 ``[layers, B,
+    budget]``; ``sums_out`` may be ``sums``."""
+    torch = _the_torch()
+    _dense("sums, sums_out", torch.float32, sums, sums_out)
+    _dense("kv_len, keep, status", torch.int32, kv_len, keep, status)
+    _need(sums.dim() == 3 and sums_out.shape == sums.shape and kv_len.numel() == sums.shape[1]
+          and keep.shape == (sums.shape[0], sums.shape[1], budget),
+          "sums and sums_out [layers, B, width], kv_len [B], keep [layers, B, budget]")
+    _check(lib().moe_evict_select(_ptr(sums), _ptr(sums_out), sums.shape[0], sums.shape[1], sums.shape[2], _ptr(kv_len),
+                                  budget, sinks, recent, _ptr(keep), _ptr(status), _stream(stream)), "moe_evict_select")
+
+
+def latent4_move(spec, pages, table, keep, to_table, status, stream=None):
+    """moe_latent4_move on 4-bit ``pages`` uint8 ``[layers, n_pages, page bytes]`` (a layer contiguous, layers may be
+    strided): the rows ``keep`` int32 ``[layers, B, budget]`` of the sequences of ``table`` go to the pages ``to_table``
+    int32 ``[B, >= ceil(budget / page_tokens)]``."""
+    torch = _the_torch()
+    _need(pages.dim() == 3 and keep.dim() == 3 and pages.shape[0] == keep.shape[0] > 0 and to_table.dim() == 2
+          and to_table.shape[0] == keep.shape[1], "pages [layers, n_pages, bytes], keep [layers, B, budget], to_table [B, pages]")
+    cache = latent4_cache(spec, pages[0], table)
+    need = -(-keep.shape[2] // spec.page_tokens)
+    _need(to_table.shape[1] >= need, "to_table: %d pages a sequence" % need)
+    _dense("keep, to_table, status", torch.int32, keep, to_table, status)
+    _check(lib().moe_latent4_move(ctypes.byref(spec), ctypes.byref(cache), pages.shape[0], pages.stride(0), _ptr(keep),
+                                  keep.shape[1], keep.shape[2], _ptr(to_table), to_table.shape[1], _ptr(status),
+                                  _stream(stream)), "moe_latent4_move")
 
 
 class PagePool:

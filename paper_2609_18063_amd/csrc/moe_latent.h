@@ -72,6 +72,7 @@ struct DecodeArgs {
   int32_t* starts;               // [B + 1]: first place of each sequence
   float* part_o;                 // [wgs + items][rows][Dc]
   float* part_ml;                // [wgs + items][2][rows][2]
+  float* row_ml;                 // [B * H][2]: a row's reference and 1 / sum, or null
 };
 hipError_t launch_latent_decode(const DecodeArgs& a, hipStream_t st);
 
@@ -84,6 +85,12 @@ struct PrefillArgs {
   __half *k, *v, *kr;            // [H][kv_total][Dn], [H][kv_total][Dv], [kv_total][Dr]
   float *part_o, *part_ml;       // [kPartGroups][kPartRows][Dv] and [..][2], with parts > 1
   uint32_t* lost;                // per 64-token tile: its 16-token groups without a page
+  bool four;                     // the cache holds 4-bit rows (moe_latent4.h)
+  float* row_ml;                 // [T][H][2]: a row's reference and 1 / sum, or null
+  float* part_sums;              // [H][kv_total]: a head's weights of each token over the rows, with row_ml
+  float* sums;                   // [B][sums_stride], the first sums_len used; with row_ml
+  int64_t sums_stride;
+  int sums_len;
 };
 int prefill_parts(int max_q, int H, int B, int kv_total);
 hipError_t launch_latent_prefill(const PrefillArgs& a, hipStream_t st);

@@ -1,0 +1,771 @@
+// Latent attention for single tokens over a cache held in 4 bits (moe_latent4.h), the
+// writes of that cache, and rows read back from it. The formulas are moe_latent.hip's; a
+// cached row is (Dc + Dr) / 2 + 4 (Dc / 64 + 1) bytes instead of 2 (Dc + Dr), 324 instead of
+// 1152 for 512 + 64.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "moe_decode.h"
+#include "moe_latent4.h"
+
+namespace moe {
+namespace {
+
+// ---- cache writes -------------------------------------------------------------
+// Of a group: s = fp16((hi - lo) / 15), z = fp16(lo + 8 s), q = rint((v - z) / s) + 8. The
+// values are formed in 64 bits, as a code beside a border goes one way or the other by the
+// last bit: so a row's codes are those of its definition, but for exact ties.
+struct Append4Args {
+  AppendArgs a;                  // (a.pos: the angle's position)
+  const int32_t* slot;           // [T]: the place in the sequence
+  char* pages;
+};
+
+__device__ __forceinline__ double pair_min(double v, double o) { return o < v ? o : v; }
+__device__ __forceinline__ double pair_max(double v, double o) { return o > v ? o : v; }
+
+// Two neighbouring values of a group a thread, `lanes` (16 or 32) threads a group.
+__device__ __forceinline__ void store_group(double x, double y, int lanes, char* code, __half* s_at, __half* z_at) {
+  double lo = pair_min(x, y), hi = pair_max(x, y);
+  int odd = !isfinite(x) || !isfinite(y);
+  for (int o = 1; o < lanes; o <<= 1) {
+    lo = pair_min(lo, __shfl_xor(lo, o, kWave));
+    hi = pair_max(hi, __shfl_xor(hi, o, kWave));
+    odd |= __shfl_xor(odd, o, kWave);
+  }
+  __half s = __float2half_rn((float)((hi - lo) / 15.0));
+  const double step = (double)__half2float(s);
+  __half z = __float2half_rn((float)(lo + 8.0 * step));
+  // (a value that is not finite, or beyond fp16, makes NaN of its group)
+  if (odd || !isfinite(__half2float(s)) || !isfinite(__half2float(z))) s = z = __ushort_as_half(0x7E00);
+  const double base = (double)__half2float(z), div = step == 0.0 ? 1.0 : step;
+  auto q = [&](double v) { return (int)fmin(fmax(rint((v - base) / div) + 8.0, 0.0), 15.0); };
+  *code = (char)(q(x) | q(y) << 4);
+  if ((threadIdx.x & (lanes - 1)) == 0) {
+    *s_at = s;
+    *z_at = z;
+  }
+}
+
+// Block (t, 0) normalizes, rotates and quantizes token t's row into its page; blocks (t, 1 ..)
+// rotate the query.
+__global__ void __launch_bounds__(256) latent4_append_kernel(Append4Args b) {
+  const AppendArgs& a = b.a;
+  const LatentArgs& l = a.l;
+  const int t = blockIdx.x, seq = a.seq[t], pos = a.pos[t], slot = b.slot[t];
+  if (seq < 0) return;                                   // a padding row
+  int32_t page = -1;
+  const bool in = seq < l.n_seqs && pos >= 0 && pos < a.max_pos && slot >= 0 && slot / l.page < l.max_pages;
+  if (in) page = l.table[seq * l.table_stride + slot / l.page];
+  if (page < 0 || page >= l.n_pages) {
+    if (blockIdx.y == 0 && threadIdx.x == 0 && l.status)
+      atomicOr(l.status, in ? MOE_STATUS_BAD_PAGE : MOE_STATUS_BAD_INDEX);
+    return;
+  }
+  const float2* cs = reinterpret_cast<const float2*>(a.rope) + (size_t)pos * (l.Dr / 2);
+  if (blockIdx.y > 0) {
+    rotate_query(a, t, blockIdx.y - 1, cs);
+    return;
+  }
+  __shared__ double red[4];
+  const float* kv = a.kv + (size_t)t * (l.Dc + l.Dr);
+  const Page4 p4 = page4(l.Dc, l.Dr, l.page);
+  char* to = b.pages + (size_t)page * p4.bytes;
+  const int at = slot & (l.page - 1), G = l.Dc / 64 + 1, e = 2 * threadIdx.x;
+  __half* s_to = reinterpret_cast<__half*>(to + p4.steps) + at;
+  __half* z_to = s_to + (size_t)G * l.page;
+  float2 v = {0.f, 0.f}, x = {0.f, 0.f}, r = {0.f, 0.f}; // two of Dc <= 512 a thread
+  float2 gm = {0.f, 0.f};
+  if (e < l.Dc) {
+    v = *reinterpret_cast<const float2*>(kv + e);
+    gm = __half22float2(*reinterpret_cast<const __half2*>(a.gamma + e));
+  }
+  if (e < l.Dr) {
+    x = *reinterpret_cast<const float2*>(kv + l.Dc + e);
+    r = cs[threadIdx.x];
+  }
+  double s = (double)v.x * v.x + (double)v.y * v.y;
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, kWave);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  const double root = sqrt((red[0] + red[1] + red[2] + red[3]) / (double)l.Dc + 1e-6);
+  if (e < l.Dc) {
+    const int grp = threadIdx.x >> 5;
+    store_group(v.x / root * gm.x, v.y / root * gm.y, 32, to + at * (l.Dc / 2) + threadIdx.x, s_to + grp * l.page,
+                z_to + grp * l.page);
+  }
+  if (e < l.Dr)
+    store_group((double)x.x * r.x - (double)x.y * r.y, (double)x.x * r.y + (double)x.y * r.x, l.Dr / 2,
+                to + p4.keys + at * (l.Dr / 2) + threadIdx.x, s_to + (G - 1) * l.page, z_to + (G - 1) * l.page);
+}
+
+// Rows as fp16, each value rounded once; eight a thread.
+__global__ void __launch_bounds__(256) latent4_read_kernel(LatentArgs l, const int32_t* seq, const int32_t* slot, int T,
+                                                           __half* rows) {
+  const int row = l.Dc + l.Dr, per = row / 8;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int t = (int)(i / per), e = 8 * (int)(i % per);
+  if (t >= T) return;
+  const int b = seq[t], at = slot[t];
+  if (b < 0) return;
+  int32_t page = -1;
+  const bool in = b < l.n_seqs && at >= 0 && at / l.page < l.max_pages;
+  if (in) page = l.table[b * l.table_stride + at / l.page];
+  if (page < 0 || page >= l.n_pages) {
+    if (e == 0 && l.status) atomicOr(l.status, in ? MOE_STATUS_BAD_PAGE : MOE_STATUS_BAD_INDEX);
+    return;
+  }
+  const Page4 p4 = page4(l.Dc, l.Dr, l.page);
+  const char* from = reinterpret_cast<const char*>(l.pages) + (size_t)page * p4.bytes;
+  const int k = at & (l.page - 1), G = l.Dc / 64 + 1, grp = min(e / 64, G - 1);
+  const char* code = e < l.Dc ? from + k * (l.Dc / 2) + e / 2 : from + p4.keys + k * (l.Dr / 2) + (e - l.Dc) / 2;
+  const _Float16* s = reinterpret_cast<const _Float16*>(from + p4.steps) + (size_t)grp * l.page + k;
+  const h8 v = values8(*reinterpret_cast<const uint32_t*>(code), splat8(s[0]), splat8(s[(size_t)G * l.page]));
+  *reinterpret_cast<h8*>(rows + (size_t)t * row + e) = in_value_order(v);
+}
+
+// ---- attention over the cache ---------------------------------------------------
+// The schedule is moe_latent.hip's: of eight waves four form the scores and weights of a tile
+// of 64 tokens, the other four add up the weighted latents of the tile before, each a quarter
+// of the latent columns, and make the copies, two tiles ahead in four buffers. The codes stay
+// codes in LDS: a wave takes those it needs out of it, along a token for the scores and across
+// 16 tokens (the 4-bit transposing read) for the sums, and forms the values in registers, so
+// that LDS and HBM carry 4 bits a value.
+template <int DC, int DR, int MT>
+struct Decode4Shape {
+  static constexpr int M = 16 * MT, G = DC / 64 + 1;
+  static constexpr int NS = 4, NW = 2 * NS;                    // score waves (as many add up), waves
+  static constexpr int WR = MT == 4 ? 2 : 1, TW = NS / WR;     // row blocks by token shares of the score waves
+  static constexpr int RT = MT / WR, TT = 4 / TW;              // 16-row and 16-token tiles of one
+  static constexpr int KS = (DC + DR) / 32, CT = DC / 64;      // products of a score, 16-column tiles of an adding wave
+  // a group of 16 tokens: latents' codes, keys' codes, s and z
+  static constexpr int LAT = 8 * DC, KEY = 8 * DR, TAIL = (KEY + 64 * G + 1023) / 1024 * 1024, GRP = LAT + TAIL;
+  static constexpr int BUF = 4 * GRP, LN = LAT / 1024, CN = GRP / 1024;  // copies of a wave
+  static constexpr int PT = M * 128;                           // the weights of a tile
+  static constexpr int LDS = 4 * BUF + 2 * PT + (TW + 1) * M * 4 + 32;
+  static constexpr int PC = DC / 32;                           // 16-byte pieces of a row of codes
+};
+// XOR key of a row's pieces: 16 rows at one piece lie on all banks.
+template <int PC>
+__device__ __forceinline__ int code_key(int row) { return row * PC / 16; }
+
+struct Decode4Args {
+  DecodeArgs d;
+  float* sums;                   // [B][sums_stride], or null
+  int64_t sums_stride;
+};
+
+template <int DC, int DR, int MT>
+__global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_decode_kernel(DecodeArgs a) {
+  using S = Decode4Shape<DC, DR, MT>;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  char* pt = lds + 4 * S::BUF;                                  // weights [2][M][64] halves
+  float* smax = reinterpret_cast<float*>(pt + 2 * S::PT);       // [TW][M], by token share
+  float* skeep = smax + S::TW * S::M;                           // [M]
+  int* passed = reinterpret_cast<int*>(skeep + S::M);           // [2]: the last step with a row past its reference
+  const LatentArgs& l = a.l;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int c = lane & 15, g = lane >> 4;
+  const int wt = wave % S::TW, wr = wave / S::TW, wo = wave - S::NS;  // token share, row block; share of the columns
+  // neighbours on the line share a chiplet and its L2
+  const int wg = (blockIdx.x % 8) * (a.p.wgs / 8) + blockIdx.x / 8;
+  Walk<kStep4> at;
+  at.begin(a, wg);
+  const float unit = l.scale * kLog2e;
+  const int shift = 31 - __clz(l.page);
+  // 16-token group `grp` (0 .. 3) of a tile, from its first token (past the end: the last group)
+  auto group = [&](const Item& it, int tile, int grp) { return min(it.tok0 + tile * kStep4 + 16 * grp, it.last & ~15); };
+  auto page_of = [&](const Item& it, int tile, int grp) { return ld_scalar(it.pages + (group(it, tile, grp) >> shift)); };
+  auto known = [&](int page) { return page >= 0 && page < l.n_pages; };
+  if (threadIdx.x < 2) passed[threadIdx.x] = -1;
+
+  if (wave < S::NS) {
+    __builtin_amdgcn_s_setprio(2);
+    bool more = at.next(a);
+    h8 q[S::RT][S::KS];
+    // (a product's k: of a word's eight codes in their order, of 16 (32-value keys: 8) a lane group)
+    auto queries = [&]() {
+#pragma unroll
+      for (int r = 0; r < S::RT; ++r) {
+        const size_t row = at.it.row0 + min((wr * S::RT + r) * 16 + c, at.it.rows - 1);
+#pragma unroll
+        for (int k = 0; k < S::KS; ++k) {
+          const int e = DR == 32 && k == S::KS - 1 ? DC + 8 * g : 64 * (k / 2) + 16 * g + 8 * (k % 2);
+          q[r][k] = in_code_order(ld_h8(a.ql + row * (DC + DR) + e));
+        }
+      }
+    };
+    float sum[S::TT][S::RT], m[S::RT], ref[S::RT];              // m: the reference, unscaled; ref: m unit - kRaise, or 0
+    auto start = [&]() {
+#pragma unroll
+      for (int r = 0; r < S::RT; ++r) {
+        m[r] = -INFINITY;
+        ref[r] = 0.f;
+#pragma unroll
+        for (int t = 0; t < S::TT; ++t) sum[t][r] = 0.f;
+      }
+    };
+    int page[S::TT] = {};
+    auto pages = [&](int tile) {
+#pragma unroll
+      for (int t = 0; t < S::TT; ++t) page[t] = page_of(at.it, tile, wt * S::TT + t);
+    };
+    if (more) {
+      queries();
+      pages(at.first);
+    }
+    start();
+    vm_drain();
+    lds_barrier();
+    // row i of a product is token 8 (i / 8) + code_order(i % 8), so that a lane has the weights
+    // of four tokens that follow each other in code order
+    const int tok = 8 * (c >> 3) + code_order(c & 7);
+    // step u: the scores of tile u, the k-th of its item
+    for (int u = 0, k = 0; more; ++u) {
+      const char* buf = lds + (u & 3) * S::BUF + wt * S::TT * S::GRP;
+      f4 x[S::TT][S::RT] = {};
+#pragma unroll
+      for (int t = 0; t < S::TT; ++t) {
+        const char* lat = buf + t * S::GRP + tok * (DC / 2);
+        const char* key = buf + t * S::GRP + S::LAT + tok * (DR / 2);
+        const _Float16* sz = reinterpret_cast<const _Float16*>(buf + t * S::GRP + S::LAT + S::KEY) + tok;
+#pragma unroll
+        for (int n = 0; n < S::G; ++n) {
+          const h8 s = splat8(sz[16 * n]), z = splat8(sz[16 * (S::G + n)]);
+          if (n < S::G - 1 || DR == 64) {
+            const char* p = n < S::G - 1 ? lat + 16 * ((2 * n + (g >> 1)) ^ code_key<S::PC>(tok)) + 8 * (g & 1) : key + 8 * g;
+            const u2 w = *reinterpret_cast<const u2*>(p);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const h8 kk = values8(w[i], s, z);
+#pragma unroll
+              for (int r = 0; r < S::RT; ++r) x[t][r] = mfma16(kk, q[r][2 * n + i], x[t][r]);
+            }
+          } else {
+            const h8 kk = values8(*reinterpret_cast<const uint32_t*>(key + 4 * g), s, z);
+#pragma unroll
+            for (int r = 0; r < S::RT; ++r) x[t][r] = mfma16(kk, q[r][S::KS - 1], x[t][r]);
+          }
+        }
+      }
+      bool lost[S::TT];
+      int left[S::TT];                                          // tokens of the group, less one
+#pragma unroll
+      for (int t = 0; t < S::TT; ++t) {
+        lost[t] = !known(page[t]);
+        left[t] = at.it.last - (at.it.tok0 + (at.first + k) * kStep4 + 16 * (wt * S::TT + t));
+      }
+      const size_t seg = (size_t)wg + at.it.index;
+      // (the next item's query is asked for while this step's weights are formed)
+      const bool ends = ++k == at.n;
+      if (ends) {
+        k = 0;
+        more = at.next(a);
+        if (more) queries();
+      }
+      if (more) pages(at.first + k);
+#pragma unroll
+      for (int t = 0; t < S::TT; ++t)
+        if (lost[t] || left[t] < 15) {
+          const int most = lost[t] ? -1 : left[t];
+#pragma unroll
+          for (int r = 0; r < S::RT; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (8 * (g >> 1) + code_order(4 * (g & 1) + e) > most) x[t][r][e] = -INFINITY;
+        }
+      // the weights: of the tile's tokens in code order, eight at a time
+      float add[S::TT][S::RT];
+      auto weights = [&]() {
+#pragma unroll
+        for (int t = 0; t < S::TT; ++t)
+#pragma unroll
+          for (int r = 0; r < S::RT; ++r) {
+            h4 p;
+            add[t][r] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float v = exp2_fast(fmaf(x[t][r][e], unit, -ref[r]));
+              add[t][r] += v;
+              p[e] = (_Float16)v;
+            }
+            *reinterpret_cast<h4*>(pt + (u & 1) * S::PT + ((wr * S::RT + r) * 16 + c) * 128 +
+                                   16 * ((2 * (wt * S::TT + t) + (g >> 1)) ^ tile_key<8>(c)) + 8 * (g & 1)) = p;
+          }
+      };
+      weights();
+      bool far = false;
+      float top[S::RT];
+#pragma unroll
+      for (int r = 0; r < S::RT; ++r) {
+        top[r] = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < S::TT; ++t) top[r] = max3(max3(top[r], x[t][r][0], x[t][r][1]), x[t][r][2], x[t][r][3]);
+        far = far || (top[r] - m[r]) * unit > kSlack;           // (no token so far: any score is)
+      }
+      if (__any(far) && lane == 0) passed[u & 1] = u;
+      lds_barrier();
+      if (__builtin_amdgcn_readfirstlane(passed[u & 1]) == u) {
+        // every row that is past its reference takes its largest score as the new one (the others
+        // keep theirs: a row's roundings are its own)
+#pragma unroll
+        for (int r = 0; r < S::RT; ++r) {
+          top[r] = col_max(top[r]);
+          if (g == 0) smax[wt * S::M + (wr * S::RT + r) * 16 + c] = top[r];
+        }
+        lds_barrier();
+#pragma unroll
+        for (int r = 0; r < S::RT; ++r) {
+          const int row = (wr * S::RT + r) * 16 + c;
+          float most = m[r];
+#pragma unroll
+          for (int t = 0; t < S::TW; ++t) most = fmaxf(most, smax[t * S::M + row]);
+          float keep = 1.f;
+          if ((most - m[r]) * unit > kSlack) {
+            const float now = most * unit - kRaise;
+            keep = m[r] == -INFINITY ? 0.f : exp2_fast(ref[r] - now);
+            m[r] = most;
+#pragma unroll
+            for (int t = 0; t < S::TT; ++t) sum[t][r] *= keep;
+            ref[r] = now;
+          }
+          if (g == 0 && wt == 0) skeep[row] = keep;
+        }
+        weights();
+        lds_barrier();
+      }
+#pragma unroll
+      for (int t = 0; t < S::TT; ++t)
+#pragma unroll
+        for (int r = 0; r < S::RT; ++r) sum[t][r] += add[t][r];
+      if (ends) {
+#pragma unroll
+        for (int r = 0; r < S::RT; ++r)
+#pragma unroll
+          for (int t = 0; t < S::TT; ++t) {
+            const float all = col_sum(sum[t][r]);
+            if (g == 0)
+              *reinterpret_cast<float2*>(a.part_ml + ((seg * 4 + wt * S::TT + t) * S::M + (wr * S::RT + r) * 16 + c) * 2) =
+                  float2{m[r] * unit, all};
+          }
+        start();
+      }
+    }
+    return;
+  }
+
+  // this wave copies 16-token group wo of a tile
+  const uint32_t at0 = lds_at(lds);
+  const Page4 p4 = page4(DC, DR, l.page);
+  auto copy = [&](const Item& it, int tile, int buf, int page) {
+    if (!known(page)) {
+      // (zeros, whose scores are masked; the waits for copies find fewer than they allow)
+      if (lane == 0 && l.status) atomicOr(l.status, MOE_STATUS_BAD_PAGE);
+      char* to = lds + buf * S::BUF + wo * S::GRP;
+      for (int e = lane; e < S::GRP / 16; e += kWave) *reinterpret_cast<U4*>(to + 16 * e) = U4{};
+      vm_wait<0>();
+      return;
+    }
+    const uint32_t to = at0 + buf * S::BUF + wo * S::GRP;
+    const char* from = reinterpret_cast<const char*>(l.pages) + (size_t)page * p4.bytes;
+    const uint32_t in = group(it, tile, wo) & (l.page - 1);
+    int ln = lane;                                              // (offsets formed here, not held in registers)
+    asm volatile("" : "+v"(ln));
+#pragma unroll
+    for (int j = 0; j < S::LN; ++j) {
+      const int n = 64 * j + ln, row = n / S::PC;
+      dma16(from, in * (DC / 2) + row * (DC / 2) + 16 * ((n % S::PC) ^ code_key<S::PC>(row)), to + 1024 * j);
+    }
+    // keys' codes in one run, then 32 bytes of each s and z (past the last: it again)
+#pragma unroll
+    for (int j = 0; j < S::CN - S::LN; ++j) {
+      const int n = 64 * j + ln, k = min(n - DR / 2, 4 * S::G - 1);
+      dma16(from, n < DR / 2 ? p4.keys + in * (DR / 2) + 16 * n : p4.steps + (k >> 1) * 2 * l.page + 2 * in + 16 * (k & 1),
+            to + S::LAT + 1024 * j);
+    }
+  };
+  // the tiles asked for so far, and the next one
+  Walk<kStep4> ask = at;
+  int asked = 0, k = 0;
+  bool more = ask.next(a);
+  int page = more ? page_of(ask.it, ask.first, wo) : 0;
+  auto ask_next = [&]() {
+    if (!more) return false;
+    copy(ask.it, ask.first + k, asked & 3, page);
+    ++asked;
+    if (++k == ask.n) {
+      k = 0;
+      more = ask.next(a);
+    }
+    if (more) page = page_of(ask.it, ask.first + k, wo);
+    return true;
+  };
+  ask_next();
+  ask_next();
+  f4 o[S::CT][MT] = {};
+  vm_drain();
+  lds_barrier();
+  int left = 0;                                                 // tiles of the item that are not added up yet
+  // step u: the latents of tile u - 1, and tile u + 2 is asked for; the last step has no scores beside it
+  for (int u = 0;; ++u) {
+    const bool newer = ask_next();
+    bool stored = false;
+    if (u > 0) {
+      if (left == 0) {
+        at.next(a);
+        left = at.n;
+      }
+      const char* blk = lds + ((u - 1) & 3) * S::BUF + g * S::GRP;
+      h8 p[MT][2];
+#pragma unroll
+      for (int r = 0; r < MT; ++r)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          p[r][i] = ld_h8(pt + ((u - 1) & 1) * S::PT + (16 * r + c) * 128 + 16 * ((2 * g + i) ^ tile_key<8>(c)));
+      // (past the sequence's end s and z are zeros: whatever is there takes no part)
+      const int tile0 = at.it.tok0 + (at.first + at.n - left) * kStep4, most = at.it.last - tile0;
+      h8 s[2], z[2];
+#pragma unroll
+      for (int k = 0; k < S::CT; ++k) {
+        const int col = wo * S::CT + k;
+        if (k == 0 || col % 4 == 0) {
+          const char* sz = blk + S::LAT + S::KEY + (col / 4) * 32;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            s[i] = in_code_order(ld_h8(sz + 16 * i));
+            z[i] = in_code_order(ld_h8(sz + 32 * S::G + 16 * i));
+            if (most < kStep4 - 1) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (16 * g + 8 * i + code_order(j) > most) s[i][j] = z[i][j] = (_Float16)0.f;
+            }
+          }
+        }
+        typedef int i2 __attribute__((ext_vector_type(2)));
+        const char* from = blk + c * (DC / 2) + 16 * ((col >> 1) ^ code_key<S::PC>(c)) + 8 * (col & 1);
+        const i2 w = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
+            (__attribute__((address_space(3))) i2*)(__attribute__((address_space(3))) char*)from);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const h8 v = values8((uint32_t)w[i], s[i], z[i]);
+#pragma unroll
+          for (int r = 0; r < MT; ++r) o[k][r] = mfma16(v, p[r][i], o[k][r]);
+        }
+      }
+      if (--left == 0) {
+        const size_t seg = (size_t)wg + at.it.index;
+#pragma unroll
+        for (int r = 0; r < MT; ++r)
+#pragma unroll
+          for (int k = 0; k < S::CT; ++k) {
+            *reinterpret_cast<f4*>(a.part_o + (seg * S::M + 16 * r + c) * DC + 16 * (wo * S::CT + k) + 4 * g) = o[k][r];
+            o[k][r] = f4{};
+          }
+        stored = true;
+      }
+    }
+    if (u >= asked) break;
+    // tile u + 1 is there: all but this step's copies and, behind them, the stores (16 bytes
+    // a lane each: no fewer than these)
+    constexpr int ST = S::CT * MT;
+    if (!newer)
+      vm_wait<0>();
+    else if (stored)
+      vm_wait<S::CN + ST>();
+    else
+      vm_wait<S::CN>();
+    lds_barrier();
+    if (__builtin_amdgcn_readfirstlane(passed[u & 1]) == u) {
+      lds_barrier();
+      lds_barrier();
+#pragma unroll
+      for (int r = 0; r < MT; ++r) {
+        const float keep = skeep[16 * r + c];
+#pragma unroll
+        for (int k = 0; k < S::CT; ++k) o[k][r] *= keep;
+      }
+    }
+  }
+}
+
+// ---- the tokens' weights -----------------------------------------------------------
+// sums[b][j] += sum_h softmax_h(j), once the rows' references and sums are known: the scores
+// again, 32 heads a wave (RB such blocks beside each other), 16 tokens a product. A token's
+// weights are added up in one order: heads by rows, lanes, then blocks.
+constexpr int kSumTokens = 512;   // of a workgroup
+
+template <int DC, int DR, int RB>
+__global__ void __launch_bounds__(256) latent4_sums_kernel(Decode4Args b) {
+  constexpr int G = DC / 64 + 1, KS = (DC + DR) / 32, TG = 4 / RB;
+  __shared__ float part[2][4][16];
+  const DecodeArgs& a = b.d;
+  const LatentArgs& l = a.l;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const int rb = wave % RB, tw = wave / RB, seq = blockIdx.x % a.B;
+  const int len = clamp_len(a, a.kv_len[seq]), tok0 = blockIdx.x / a.B * kSumTokens, end = min(len, tok0 + kSumTokens);
+  if (tok0 >= end) return;
+  h8 q[2][KS];
+  float ref[2][4], inv[2][4];
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const __half* from = a.ql + ((size_t)seq * l.H + min(32 * rb + 16 * r + c, l.H - 1)) * (DC + DR);
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+      q[r][k] = in_code_order(ld_h8(from + (DR == 32 && k == KS - 1 ? DC + 8 * g : 64 * (k / 2) + 16 * g + 8 * (k % 2))));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int h = 32 * rb + 16 * r + 4 * g + e;
+      const float2 ml = *reinterpret_cast<const float2*>(a.row_ml + 2 * ((size_t)seq * l.H + min(h, l.H - 1)));
+      ref[r][e] = h < l.H ? ml.x : INFINITY;             // (a head that is not there: weight 0)
+      inv[r][e] = h < l.H ? ml.y : 0.f;
+    }
+  }
+  const float unit = l.scale * kLog2e;
+  const Page4 p4 = page4(DC, DR, l.page);
+  int it = 0;
+  for (int t0 = tok0; t0 < end; t0 += 16 * TG, ++it) {
+    const int t = t0 + 16 * tw;
+    int32_t page = -1;
+    if (t < end) page = l.table[seq * l.table_stride + t / l.page];
+    const bool there = page >= 0 && page < l.n_pages;
+    float w = 0.f;
+    if (there) {
+      const char* from = reinterpret_cast<const char*>(l.pages) + (size_t)page * p4.bytes;
+      const int in = (t & (l.page - 1)) + c;
+      const char* lat = from + in * (DC / 2);
+      const char* key = from + p4.keys + in * (DR / 2);
+      const _Float16* sz = reinterpret_cast<const _Float16*>(from + p4.steps) + in;
+      f4 x[2] = {};
+#pragma unroll
+      for (int n = 0; n < G; ++n) {
+        const h8 s = splat8(sz[n * l.page]), z = splat8(sz[(G + n) * l.page]);
+        if (n < G - 1 || DR == 64) {
+          const u2 v = *reinterpret_cast<const u2*>((n < G - 1 ? lat + 32 * n : key) + 8 * g);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const h8 kk = values8(v[i], s, z);
+#pragma unroll
+            for (int r = 0; r < 2; ++r) x[r] = mfma16(q[r][2 * n + i], kk, x[r]);
+          }
+        } else {
+          const h8 kk = values8(*reinterpret_cast<const uint32_t*>(key + 4 * g), s, z);
+#pragma unroll
+          for (int r = 0; r < 2; ++r) x[r] = mfma16(q[r][KS - 1], kk, x[r]);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w += exp2_fast(fmaf(x[r][e], unit, -ref[r][e])) * inv[r][e];
+      w = col_sum(w);
+    }
+    if constexpr (RB > 1) {
+      if (g == 0) part[it & 1][wave][c] = w;
+      __syncthreads();
+      w = 0.f;
+#pragma unroll
+      for (int k = 0; k < RB; ++k) w += part[it & 1][tw * RB + k][c];
+    }
+    if (there && rb == 0 && g == 0 && t + c < end) b.sums[seq * b.sums_stride + t + c] += w;
+  }
+}
+
+template <int DC, int DR, int MT>
+hipError_t launch_attention(const DecodeArgs& a, hipStream_t st) {
+  constexpr int lds = Decode4Shape<DC, DR, MT>::LDS;
+  static_assert(lds <= 160 * 1024, "LDS of a CU");
+  auto kernel = latent4_decode_kernel<DC, DR, MT>;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3(a.p.wgs), dim3(64 * Decode4Shape<DC, DR, MT>::NW), lds, st, a);
+  return hipGetLastError();
+}
+template <int DC, int DR>
+hipError_t launch_sums(const Decode4Args& b, hipStream_t st) {
+  const DecodeArgs& a = b.d;
+  const dim3 grid((unsigned)((a.max_len + kSumTokens - 1) / kSumTokens) * a.B), block(256);
+  if (a.l.H <= 32)
+    hipLaunchKernelGGL((latent4_sums_kernel<DC, DR, 1>), grid, block, 0, st, b);
+  else if (a.l.H <= 64)
+    hipLaunchKernelGGL((latent4_sums_kernel<DC, DR, 2>), grid, block, 0, st, b);
+  else
+    hipLaunchKernelGGL((latent4_sums_kernel<DC, DR, 4>), grid, block, 0, st, b);
+  return hipGetLastError();
+}
+template <int DC, int DR>
+hipError_t launch_decode4(const Decode4Args& b, hipStream_t st) {
+  const DecodeArgs& a = b.d;
+  hipError_t e = a.p.rows == 16   ? launch_attention<DC, DR, 1>(a, st)
+                 : a.p.rows == 32 ? launch_attention<DC, DR, 2>(a, st)
+                                  : launch_attention<DC, DR, 4>(a, st);
+  if (e == hipSuccess) e = launch_up<DC, kStep4>(a, st);
+  if (e == hipSuccess && b.sums && a.max_len > 0) e = launch_sums<DC, DR>(b, st);
+  return e;
+}
+
+int tiles_host(int len) { return (len + kStep4 - 1) / kStep4; }
+
+// As moe_latent.hip's, without a shared prefix.
+DecodePlan decode4_plan(int H, int Dc, int Dr, int B, int max_len, bool sums, size_t* row_ml) {
+  DecodePlan p{};
+  p.rows = H <= 16 ? 16 : H <= 32 ? 32 : 64;
+  p.head_blocks = (H + p.rows - 1) / p.rows;
+  const int wgs = kCus * (Dc <= 128 ? 2 : 1);
+  p.least = std::max(1, (int)(0.18 * std::sqrt((double)tiles_host(max_len)) + 0.5));
+  const long long tiles = (long long)B * p.head_blocks * tiles_host(max_len);
+  p.wgs = (int)std::min<long long>(wgs, (std::max<long long>(tiles, 1) + 7) / 8 * 8);
+  const size_t rows = (size_t)B * H, parts = (size_t)p.wgs + (size_t)B * p.head_blocks;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off += round256(bytes);
+    return o;
+  };
+  p.ql = take(rows * (Dc + Dr) * 2);
+  p.lat = take(rows * Dc * 2);
+  p.starts = take(((size_t)B + 1) * 4);
+  p.part_o = take(parts * p.rows * Dc * 4);
+  p.part_ml = take(parts * p.rows * 32);
+  *row_ml = off;
+  if (sums) take(rows * 8);
+  p.total = off;
+  return p;
+}
+
+hipError_t launch_latent4_decode(const Decode4Args& b, hipStream_t st) {
+  const DecodeArgs& a = b.d;
+  const LatentArgs& l = a.l;
+  const dim3 ga(l.Dc / 64 + 1, l.H, (a.B + 63) / 64);
+  if (l.Dn == 128)
+    hipLaunchKernelGGL((latent_absorb_kernel<128, kStep4>), ga, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((latent_absorb_kernel<64, kStep4>), ga, dim3(256), 0, st, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (l.Dr == 64)
+    return l.Dc == 512 ? launch_decode4<512, 64>(b, st) : l.Dc == 256 ? launch_decode4<256, 64>(b, st) : launch_decode4<128, 64>(b, st);
+  return l.Dc == 512 ? launch_decode4<512, 32>(b, st) : l.Dc == 256 ? launch_decode4<256, 32>(b, st) : launch_decode4<128, 32>(b, st);
+}
+
+}  // namespace
+}  // namespace moe
+
+// ---- C ABI (contracts in include/moe_api.h) ---------------------------------------
+
+namespace {
+
+bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+
+constexpr int kMaxLen = 1 << 26, kMaxBatch = 1 << 16;
+
+bool decode4_shape_ok(const moe_latent_spec* s, int B, int max_len) {
+  if (moe_latent_spec_check(s) != MOE_OK || B < 0 || B > kMaxBatch || max_len < 0 || max_len > kMaxLen) return false;
+  // places on the plan's line
+  const int64_t rows = ((int64_t)B * s->heads + 15) / 16 + B;
+  return rows * (((int64_t)max_len + 63) / 64 + 32) < (int64_t(1) << 30);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t moe_latent4_page_bytes(const moe_latent_spec* s) {
+  if (moe_latent_spec_check(s) != MOE_OK) return 0;
+  return moe::page4(s->d_latent, s->d_rope, s->page_tokens).bytes;
+}
+
+int moe_latent4_append(const moe_latent_spec* spec, const moe_latent_cache* cache, const float* kv, const void* gamma_f16,
+                       const float* rope, int max_pos, const int32_t* seq, const int32_t* slot, const int32_t* pos, int T,
+                       const void* q_f16, void* q_out_f16, uint32_t* status, void* stream) {
+  const int rc = moe::latent_cache_check(spec, cache);
+  if (rc != MOE_OK) return rc;
+  if (T < 0 || T > (1 << 22) || max_pos < 1 || (!q_f16) != (!q_out_f16)) return MOE_EINVAL;
+  if (T == 0) return MOE_OK;
+  if (!kv || !gamma_f16 || !rope || !seq || !slot || !pos) return MOE_EINVAL;
+  if (misaligned(kv, 16) || misaligned(gamma_f16, 16) || misaligned(rope, 16) || misaligned(seq, 4) ||
+      misaligned(slot, 4) || misaligned(pos, 4) || misaligned(q_f16, 16) || misaligned(q_out_f16, 16) || misaligned(status, 4))
+    return MOE_EALIGN;
+  moe::Append4Args b{};
+  moe::AppendArgs& a = b.a;
+  a.l = moe::latent_args(spec, cache);
+  a.l.q = static_cast<const __half*>(q_f16);
+  a.l.status = status;
+  a.kv = kv;
+  a.gamma = static_cast<const __half*>(gamma_f16);
+  a.rope = rope;
+  a.max_pos = max_pos;
+  a.T = T;
+  a.seq = seq;
+  a.pos = pos;
+  a.q_out = static_cast<__half*>(q_out_f16);
+  b.slot = slot;
+  b.pages = static_cast<char*>(cache->pages);
+  const int n = q_f16 ? a.l.H * (a.l.Dn + a.l.Dr) : 0;
+  hipLaunchKernelGGL(moe::latent4_append_kernel, dim3(T, 1 + (n + 2047) / 2048), dim3(256), 0,
+                     static_cast<hipStream_t>(stream), b);
+  return hipGetLastError() == hipSuccess ? MOE_OK : MOE_EHIP;
+}
+
+int moe_latent4_read(const moe_latent_spec* spec, const moe_latent_cache* cache, const int32_t* seq, const int32_t* slot,
+                     int T, void* rows_f16, uint32_t* status, void* stream) {
+  const int rc = moe::latent_cache_check(spec, cache);
+  if (rc != MOE_OK) return rc;
+  if (T < 0 || T > (1 << 24)) return MOE_EINVAL;
+  if (T == 0) return MOE_OK;
+  if (!seq || !slot || !rows_f16) return MOE_EINVAL;
+  if (misaligned(seq, 4) || misaligned(slot, 4) || misaligned(rows_f16, 16) || misaligned(status, 4)) return MOE_EALIGN;
+  moe::LatentArgs l = moe::latent_args(spec, cache);
+  l.status = status;
+  const int64_t n = (int64_t)T * ((l.Dc + l.Dr) / 8);
+  hipLaunchKernelGGL(moe::latent4_read_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0,
+                     static_cast<hipStream_t>(stream), l, seq, slot, T, static_cast<__half*>(rows_f16));
+  return hipGetLastError() == hipSuccess ? MOE_OK : MOE_EHIP;
+}
+
+size_t moe_latent4_decode_workspace_bytes(const moe_latent_spec* s, int B, int max_len, int sums) {
+  if (!decode4_shape_ok(s, B, max_len)) return 0;
+  size_t at;
+  return moe::decode4_plan(s->heads, s->d_latent, s->d_rope, B < 1 ? 1 : B, max_len, sums != 0, &at).total;
+}
+
+int moe_latent4_decode(const moe_latent_spec* spec, const moe_latent_cache* cache, const void* w_kvb_f16,
+                       const void* q_f16, int B, const int32_t* kv_len, int max_len, void* out_f16, float* sums,
+                       int64_t sums_stride, uint32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = moe::latent_cache_check(spec, cache);
+  if (rc != MOE_OK) return rc;
+  if (!decode4_shape_ok(spec, B, max_len) || B > cache->n_seqs || (sums && sums_stride < max_len)) return MOE_EINVAL;
+  if (sums && (int64_t)B * ((max_len + moe::kSumTokens - 1) / moe::kSumTokens) * 256 > (int64_t)UINT32_MAX)
+    return MOE_EINVAL;  // (a grid's threads)
+  if (B == 0) return MOE_OK;
+  if (!w_kvb_f16 || !q_f16 || !kv_len || !out_f16 || !workspace) return MOE_EINVAL;
+  if (misaligned(w_kvb_f16, 16) || misaligned(q_f16, 16) || misaligned(kv_len, 4) || misaligned(out_f16, 16) ||
+      misaligned(sums, 4) || misaligned(status, 4) || misaligned(workspace, 16))
+    return MOE_EALIGN;
+  moe::Decode4Args b{};
+  moe::DecodeArgs& a = b.d;
+  a.l = moe::latent_args(spec, cache);
+  a.l.w = static_cast<const __half*>(w_kvb_f16);
+  a.l.q = static_cast<const __half*>(q_f16);
+  a.l.out = static_cast<__half*>(out_f16);
+  a.l.status = status;
+  a.B = B;
+  a.max_len = max_len;
+  a.kv_len = kv_len;
+  size_t row_ml;
+  a.p = moe::decode4_plan(a.l.H, a.l.Dc, a.l.Dr, B, max_len, sums != nullptr, &row_ml);
+  if (workspace_bytes < a.p.total) return MOE_ENOMEM;
+  char* ws = static_cast<char*>(workspace);
+  a.ql = reinterpret_cast<__half*>(ws + a.p.ql);
+  a.lat = reinterpret_cast<__half*>(ws + a.p.lat);
+  a.starts = reinterpret_cast<int32_t*>(ws + a.p.starts);
+  a.part_o = reinterpret_cast<float*>(ws + a.p.part_o);
+  a.part_ml = reinterpret_cast<float*>(ws + a.p.part_ml);
+  a.row_ml = sums ? reinterpret_cast<float*>(ws + row_ml) : nullptr;
+  b.sums = sums;
+  b.sums_stride = sums_stride;
+  return moe::launch_latent4_decode(b, static_cast<hipStream_t>(stream)) == hipSuccess ? MOE_OK : MOE_EHIP;
+}
+
+}  // extern "C"

@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "moe_latent.h"
+#include "moe_latent4.h"
 #include "moe_tile.h"
 
 namespace moe {
@@ -72,12 +73,16 @@ constexpr int kExpandProducts = DC == 512 ? 2 : 4;
 template <int DC>
 constexpr int kExpandWaves = 16 / kExpandProducts<DC>;
 
-template <int DC>
+// A 4-bit cache's rows (FOUR) come by way of registers, where their values are formed: a tile's
+// codes are asked for two tiles ahead and put into one of two slots behind the products of
+// the tile before it.
+template <int DC, bool FOUR>
 __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
     latent_expand_kernel(PrefillArgs a, int side, int col_groups, int splits) {
   constexpr int NM = kExpandProducts<DC>, NW = kExpandWaves<DC>, PR = DC / 8, CW = PR / 2 / NW, SLOT = kExpandTokens * DC * 2, KS = DC / 32;
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  int64_t* where = reinterpret_cast<int64_t*>(lds + kExpandSlots * SLOT);
+  constexpr int SLOTS = FOUR ? 2 : kExpandSlots;
+  int64_t* where = reinterpret_cast<int64_t*>(lds + SLOTS * SLOT);
   __shared__ uint32_t lost[4];
   const LatentArgs& l = a.l;
   const int row_halves = DC + l.Dr;
@@ -115,7 +120,18 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
     int32_t page = -1;
     if (wave < 4 && tok < s.len) page = l.table[b * l.table_stride + tok / l.page];
     const bool there = page >= 0 && page < l.n_pages;
-    if (there) {
+    if (FOUR && there) {
+      const Page4 p4 = page4(DC, l.Dr, l.page);
+      const char* from = reinterpret_cast<const char*>(l.pages) + (size_t)page * p4.bytes;
+      const int pieces = l.Dr / 8, rows = min(16, s.len - tok), in = tok % l.page;
+      const _Float16* sz = reinterpret_cast<const _Float16*>(from + p4.steps) + (DC / 64) * l.page + in;
+      for (int e = lane; e < rows * pieces; e += 64) {
+        const int r = e / pieces, k = e % pieces;
+        const h8 v = values8(*reinterpret_cast<const uint32_t*>(from + p4.keys + (in + r) * (l.Dr / 2) + 4 * k), splat8(sz[r]),
+                             splat8(sz[(DC / 64 + 1) * l.page + r]));
+        *reinterpret_cast<h8*>(a.kr + (size_t)(s.first + tok + r) * l.Dr + 8 * k) = in_value_order(v);
+      }
+    } else if (there) {
       const __half* rope = l.pages + ((size_t)page * l.page + tok % l.page) * row_halves + DC;
       const int pieces = l.Dr / 8, rows = min(16, s.len - tok);
       for (int e = lane; e < rows * pieces; e += 64)
@@ -132,7 +148,8 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
     }
   }
   if (n < 1) return;
-  // Where the tokens' rows are, as byte offsets (one without a page: -1; zeros are stored).
+  // Where the tokens' rows are, as byte offsets, or as numbers in 4 bits (one without a page: -1;
+  // zeros are stored).
   // Behind the last token its own values are stored again.
   for (int i = threadIdx.x; i < n * kExpandTokens; i += 64 * NW) {
     const int at = min(first + i, a.kv_total - 1);
@@ -141,7 +158,7 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
     const int tok = at - s.first;
     int page = -1;
     if (tok >= 0 && tok < s.len) page = l.table[b * l.table_stride + tok / l.page];
-    where[i] = page >= 0 && page < l.n_pages ? ((int64_t)page * l.page + tok % l.page) * (2 * row_halves) : -1;
+    where[i] = page >= 0 && page < l.n_pages ? ((int64_t)page * l.page + tok % l.page) * (FOUR ? 1 : 2 * row_halves) : -1;
   }
   vm_drain();                                            // (the weights: asked for before the page ids)
   __syncthreads();
@@ -158,7 +175,38 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
 #pragma unroll
     for (int j = 0; j < CW; ++j) dma16(src[j], at0 + slot * SLOT + 1024 * (CW * wave + j));
   };
-  for (int u = 0; u < 3; ++u) copy(u);
+  // the same of a 4-bit row: to registers, and from there as values
+  uint32_t code[FOUR ? CW : 1];
+  _Float16 step[FOUR ? CW : 1], mid[FOUR ? CW : 1];
+  const Page4 p4 = page4(DC, l.Dr, l.page);
+  const int shift = 31 - __clz(l.page);
+  auto ask = [&](int u) {
+    const int t = min(u, n - 1);
+#pragma unroll
+    for (int j = 0; j < CW; ++j) {
+      const int p = 64 * (CW * wave + j) + lane, r = p / PR, k = (p % PR) ^ tile_key<PR>(r);
+      const int64_t row = max(where[t * kExpandTokens + r], (int64_t)0);
+      const int in = (int)row & (l.page - 1);
+      const char* from = reinterpret_cast<const char*>(l.pages) + (row >> shift) * p4.bytes;
+      code[j] = *reinterpret_cast<const uint32_t*>(from + in * (DC / 2) + 4 * k);
+      const _Float16* s = reinterpret_cast<const _Float16*>(from + p4.steps) + (k >> 3) * l.page + in;
+      step[j] = s[0];
+      mid[j] = s[(DC / 64 + 1) * l.page];
+    }
+  };
+  auto put = [&](int u) {
+#pragma unroll
+    for (int j = 0; j < CW; ++j)
+      *reinterpret_cast<h8*>(lds + (u & 1) * SLOT + 1024 * (CW * wave + j) + 16 * lane) =
+          in_value_order(values8(code[j], splat8(step[j]), splat8(mid[j])));
+  };
+  if constexpr (FOUR) {
+    ask(0);
+    put(0);
+    ask(1);
+  } else {
+    for (int u = 0; u < 3; ++u) copy(u);
+  }
   const int h = min(col0, N - 1) / hd, in = min(col0, N - 1) % hd;
   // Values are stored finite: a row's weight 0 of a token that it does not see then gives 0,
   // whatever the token holds. (Its keys stay as they are, and make NaN of the rows that see it.)
@@ -181,16 +229,23 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
   const int to_row = in < l.Dn ? l.Dn : l.Dv;
   for (int u = 0; u < n; ++u) {
     // what was asked for after tile u: the copies of two tiles, and NM stores a tile
-    if (idle || u == 0)
+    if (FOUR) {
+    } else if (idle || u == 0)
       vm_wait<2 * CW>();
     else if (u == 1)
       vm_wait<2 * CW + NM>();
     else
       vm_wait<2 * CW + 2 * NM>();
     lds_barrier();
-    copy(u + 3);
-    if (idle) continue;
-    const char* x = lds + (u % kExpandSlots) * SLOT;
+    if constexpr (!FOUR) copy(u + 3);
+    if (idle) {
+      if constexpr (FOUR) {
+        put(u + 1);
+        ask(u + 2);
+      }
+      continue;
+    }
+    const char* x = lds + (u % SLOTS) * SLOT;
     // (the reads of KR steps are asked for before the products of the KR before them)
     f4 y[2][NM] = {};
     constexpr int KR = 4;
@@ -214,6 +269,10 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int m = 0; m < NM; ++m) y[t][m] = mfma16(w[k + i][m], v[k / KR & 1][i][t], y[t][m]);
+    }
+    if constexpr (FOUR) {
+      put(u + 1);
+      ask(u + 2);
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -425,6 +484,9 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
       continue;
     }
     const float inv = total > 0.f ? 1.f / total : total != total ? total : 0.f;  // (no token: zeros)
+    if (a.row_ml && g == 0)
+      *reinterpret_cast<float2*>(a.row_ml + 2 * ((size_t)(qs.first + row) * l.H + h)) =
+          float2{m[r] == -INFINITY ? INFINITY : ref[r], inv};
     __half* to = l.out + ((size_t)(qs.first + row) * l.H + h) * DV + 4 * g;
 #pragma unroll
     for (int k = 0; k < CT; ++k) {
@@ -465,8 +527,93 @@ __global__ void __launch_bounds__(256) latent_parts_kernel(PrefillArgs a) {
     o += v * w;
   }
   const float inv = sum > 0.f ? 1.f / sum : sum != sum ? sum : 0.f;
+  if (a.row_ml && col == 0)
+    *reinterpret_cast<float2*>(a.row_ml + 2 * ((size_t)(qs.first + row) * l.H + h)) = float2{top == -INFINITY ? INFINITY : top, inv};
   const h4 v = {(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
   *reinterpret_cast<h4*>(l.out + ((size_t)(qs.first + row) * l.H + h) * l.Dv + col) = v;
+}
+
+// ---- the tokens' weights ------------------------------------------------------------
+// sums[b][j] += sum over rows and heads of softmax(j), once the rows' references and sums are
+// known: the scores again. A workgroup takes one head's 128 tokens (a wave 32 of them, their
+// keys in registers) by all query rows that see them, 16 at a time; a second launch adds up
+// the heads, in order.
+constexpr int kSumTile = 128;
+
+template <int DN, int DR>
+__global__ void __launch_bounds__(256) latent_prefill_sums_kernel(PrefillArgs a) {
+  constexpr int KS = (DN + DR) / 32;
+  const LatentArgs& l = a.l;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const int h = blockIdx.x % l.H, t = blockIdx.x / l.H;
+  // (tiles of all sequences one behind the other, with gaps, as the 64-token tiles are)
+  auto base = [&](int k) { return min(max(a.kv_start[k], 0), a.kv_total) / kSumTile + k; };
+  const int b = last_at_most(a.B, t, base);
+  const Span qs = span_of(a.q_start, b, a.T), ks = context_of(a, b);
+  const int tile0 = (t - base(b)) * kSumTile, tok0 = tile0 + 32 * wave;
+  if (tile0 < 0 || tok0 >= ks.len) return;
+  h8 k[2][KS];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const size_t at = ks.first + min(tok0 + 16 * i + c, ks.len - 1);
+#pragma unroll
+    for (int n = 0; n < KS; ++n)
+      k[i][n] = n < DN / 32 ? ld_h8(a.k + ((size_t)h * a.kv_total + at) * DN + 32 * n + 8 * g)
+                            : ld_h8(a.kr + at * DR + 32 * (n - DN / 32) + 8 * g);
+  }
+  const uint32_t lost = a.lost[tile_base(a, b) + tok0 / kTile] >> (tok0 / 16 % 4);
+  const float unit = l.scale * kLog2e;
+  const int shift = ks.len - qs.len;                     // position of query row 0
+  f4 w[2] = {};
+  for (int row0 = max(0, tok0 - shift) & ~15; row0 < qs.len; row0 += 16) {
+    const int row = min(row0 + c, qs.len - 1);
+    const size_t at = (size_t)(qs.first + row) * l.H + h;
+    const float2 ml = *reinterpret_cast<const float2*>(a.row_ml + 2 * at);
+    const float ref = row0 + c < qs.len ? ml.x : INFINITY, inv = row0 + c < qs.len ? ml.y : 0.f;
+    f4 s[2] = {};
+#pragma unroll
+    for (int n = 0; n < KS; ++n) {
+      const h8 q = ld_h8(l.q + at * (DN + DR) + 32 * n + 8 * g);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) s[i] = mfma16(k[i][n], q, s[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool sees = tok0 + 16 * i + 4 * g + e <= shift + row0 + c && row0 + c < qs.len;
+        w[i][e] += sees ? __builtin_amdgcn_exp2f(fmaf(s[i][e], unit, -ref)) * inv : 0.f;
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float v = row16_sum(w[i][e]);
+      const int tok = tok0 + 16 * i + 4 * g + e;
+      if (c == 0 && tok < ks.len) a.part_sums[(size_t)h * a.kv_total + ks.first + tok] = lost >> i & 1 ? 0.f : v;
+    }
+}
+
+__global__ void __launch_bounds__(256) latent_sums_join_kernel(PrefillArgs a) {
+  const int at = blockIdx.x * 256 + threadIdx.x;
+  if (at >= a.kv_total) return;
+  const int b = last_at_most(a.B, at, [&](int k) { return a.kv_start[k]; });
+  const Span s = context_of(a, b);
+  const int tok = at - s.first;
+  if (tok < 0 || tok >= s.len || tok >= a.sums_len) return;
+  float w = 0.f;
+  for (int h = 0; h < a.l.H; ++h) w += a.part_sums[(size_t)h * a.kv_total + at];
+  a.sums[b * a.sums_stride + tok] += w;
+}
+
+template <int DN, int DR>
+hipError_t launch_sums(const PrefillArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((latent_prefill_sums_kernel<DN, DR>), dim3((unsigned)(a.kv_total / kSumTile + a.B) * a.l.H), dim3(256), 0, st, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(latent_sums_join_kernel, dim3((a.kv_total + 255) / 256), dim3(256), 0, st, a);
+  return hipGetLastError();
 }
 
 template <int DN, int DR, int DV, bool PARTS>
@@ -498,17 +645,24 @@ hipError_t launch_attention(const PrefillArgs& a, hipStream_t st) {
 
 // As many splits of the tokens as fill the CUs (the weights of 512 latent columns leave room
 // for one workgroup there, else two), and at least one per kExpandMost tokens.
-template <int DC>
+template <int DC, bool FOUR>
 hipError_t launch_expand(const PrefillArgs& a, hipStream_t st) {
-  constexpr int lds = kExpandSlots * kExpandTokens * DC * 2 + kExpandMost * 8, slots = 256 * (DC == 512 ? 1 : 2);
+  constexpr int lds = (FOUR ? 2 : kExpandSlots) * kExpandTokens * DC * 2 + kExpandMost * 8, slots = 256 * (DC == 512 ? 1 : 2);
   const int groups = (a.l.H * (a.l.Dn + a.l.Dv) + kExpandCols - 1) / kExpandCols;
   const int tiles = (a.kv_total + kExpandTokens - 1) / kExpandTokens, most = kExpandMost / kExpandTokens;
   const int splits = std::max({1, std::min((slots + groups - 1) / groups, tiles), (tiles + most - 1) / most});
-  auto kernel = latent_expand_kernel<DC>;
+  auto kernel = latent_expand_kernel<DC, FOUR>;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(kernel, dim3((unsigned)groups * splits), dim3(64 * kExpandWaves<DC>), lds, st, a, a.kv_total / kTile + a.B, groups, splits);
   return hipGetLastError();
+}
+
+template <bool FOUR>
+hipError_t launch_expand(const PrefillArgs& a, hipStream_t st) {
+  return a.l.Dc == 512   ? launch_expand<512, FOUR>(a, st)
+         : a.l.Dc == 256 ? launch_expand<256, FOUR>(a, st)
+                         : launch_expand<128, FOUR>(a, st);
 }
 
 }  // namespace
@@ -525,9 +679,12 @@ int prefill_parts(int max_q, int H, int B, int kv_total) {
 
 hipError_t launch_latent_prefill(const PrefillArgs& a, hipStream_t st) {
   const LatentArgs& l = a.l;
-  const hipError_t e = l.Dc == 512 ? launch_expand<512>(a, st) : l.Dc == 256 ? launch_expand<256>(a, st) : launch_expand<128>(a, st);
+  hipError_t e = a.four ? launch_expand<true>(a, st) : launch_expand<false>(a, st);
   if (e != hipSuccess) return e;
-  return l.Dn == 128 ? launch_attention<128>(a, st) : launch_attention<64>(a, st);
+  e = l.Dn == 128 ? launch_attention<128>(a, st) : launch_attention<64>(a, st);
+  if (e != hipSuccess || !a.row_ml || a.kv_total < 1) return e;
+  if (l.Dn == 128) return l.Dr == 64 ? launch_sums<128, 64>(a, st) : launch_sums<128, 32>(a, st);
+  return l.Dr == 64 ? launch_sums<64, 64>(a, st) : launch_sums<64, 32>(a, st);
 }
 
 }  // namespace moe
@@ -540,7 +697,7 @@ bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p
 size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
 struct PrefillLayout {
-  size_t k, v, kr, lost, part_o, part_ml, total;
+  size_t k, v, kr, lost, part_o, part_ml, row_ml, part_sums, total;
 };
 constexpr int kMaxTotal = 1 << 24, kMaxBatch = 1 << 16;
 
@@ -548,7 +705,7 @@ bool prefill_shape_ok(const moe_latent_spec* s, int T, int B, int kv_total) {
   return moe_latent_spec_check(s) == MOE_OK && T >= 0 && T <= kMaxTotal && B >= 0 && B <= kMaxBatch && kv_total >= 0 &&
          kv_total <= kMaxTotal;
 }
-PrefillLayout prefill_layout(const moe_latent_spec* s, int B, int kv_total) {
+PrefillLayout prefill_layout(const moe_latent_spec* s, int T, int B, int kv_total, bool sums) {
   PrefillLayout p{};
   const size_t n = kv_total;
   p.k = 0;
@@ -557,35 +714,32 @@ PrefillLayout prefill_layout(const moe_latent_spec* s, int B, int kv_total) {
   p.lost = p.kr + round256(n * s->d_rope * 2);
   p.part_o = p.lost + round256((n / moe::kTile + B) * 4);
   p.part_ml = p.part_o + (size_t)moe::kPartGroups * moe::kPartRows * s->d_v * 4;
-  p.total = p.part_ml + (size_t)moe::kPartGroups * moe::kPartRows * 8;
+  p.row_ml = p.part_ml + (size_t)moe::kPartGroups * moe::kPartRows * 8;
+  p.part_sums = p.row_ml + (sums ? round256((size_t)T * s->heads * 8) : 0);
+  p.total = p.part_sums + (sums ? round256((size_t)s->heads * n * 4) : 0);
   return p;
 }
-
-}  // namespace
-
-extern "C" {
-
-size_t moe_latent_prefill_workspace_bytes(const moe_latent_spec* s, int B, int kv_total) {
-  if (!prefill_shape_ok(s, 0, B, kv_total)) return 0;
-  return prefill_layout(s, B < 1 ? 1 : B, kv_total < 1 ? 1 : kv_total).total;
+size_t prefill_bytes(const moe_latent_spec* s, int T, int B, int kv_total, bool sums) {
+  if (!prefill_shape_ok(s, T, B, kv_total)) return 0;
+  return prefill_layout(s, T, B < 1 ? 1 : B, kv_total < 1 ? 1 : kv_total, sums).total;
 }
 
-int moe_latent_prefill(const moe_latent_spec* spec, const moe_latent_cache* cache, const void* w_kvb_f16,
-                       const void* q_f16, int T, const int32_t* q_start, const int32_t* kv_start, int B, int kv_total,
-                       int max_q, void* out_f16, uint32_t* status, void* workspace, size_t workspace_bytes,
-                       void* stream) {
+int prefill(bool four, const moe_latent_spec* spec, const moe_latent_cache* cache, const void* w_kvb_f16, const void* q_f16,
+            int T, const int32_t* q_start, const int32_t* kv_start, int B, int kv_total, int max_q, void* out_f16,
+            float* sums, int64_t sums_stride, int sums_len, uint32_t* status, void* workspace, size_t workspace_bytes,
+            void* stream) {
   const int rc = moe::latent_cache_check(spec, cache);
   if (rc != MOE_OK) return rc;
-  if (!prefill_shape_ok(spec, T, B, kv_total) || B > cache->n_seqs || max_q < 0 || max_q > T)
+  if (!prefill_shape_ok(spec, T, B, kv_total) || B > cache->n_seqs || max_q < 0 || max_q > T || (sums && (sums_len < 1 || sums_stride < sums_len)))
     return MOE_EINVAL;
   if (T == 0 || B == 0) return T == 0 ? MOE_OK : MOE_EINVAL;
   if (max_q < 1 || (int64_t)((max_q + moe::kPartRows - 1) / moe::kPartRows) * spec->heads * B * 512 > (int64_t)UINT32_MAX)
     return MOE_EINVAL;  // (a grid's threads)
   if (!w_kvb_f16 || !q_f16 || !q_start || !kv_start || !out_f16 || !workspace) return MOE_EINVAL;
   if (misaligned(w_kvb_f16, 16) || misaligned(q_f16, 16) || misaligned(q_start, 4) || misaligned(kv_start, 4) ||
-      misaligned(out_f16, 16) || misaligned(status, 4) || misaligned(workspace, 16))
+      misaligned(out_f16, 16) || misaligned(sums, 4) || misaligned(status, 4) || misaligned(workspace, 16))
     return MOE_EALIGN;
-  const PrefillLayout p = prefill_layout(spec, B, kv_total);
+  const PrefillLayout p = prefill_layout(spec, T, B, kv_total, sums != nullptr);
   if (workspace_bytes < p.total) return MOE_ENOMEM;
   moe::PrefillArgs a{};
   a.l = moe::latent_args(spec, cache);
@@ -607,7 +761,43 @@ int moe_latent_prefill(const moe_latent_spec* spec, const moe_latent_cache* cach
   a.part_o = reinterpret_cast<float*>(ws + p.part_o);
   a.part_ml = reinterpret_cast<float*>(ws + p.part_ml);
   a.parts = moe::prefill_parts(max_q, spec->heads, B, kv_total);
+  a.four = four;
+  if (sums) {
+    a.row_ml = reinterpret_cast<float*>(ws + p.row_ml);
+    a.part_sums = reinterpret_cast<float*>(ws + p.part_sums);
+    a.sums = sums;
+    a.sums_stride = sums_stride;
+    a.sums_len = sums_len;
+  }
   return moe::launch_latent_prefill(a, static_cast<hipStream_t>(stream)) == hipSuccess ? MOE_OK : MOE_EHIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t moe_latent_prefill_workspace_bytes(const moe_latent_spec* s, int B, int kv_total) {
+  return prefill_bytes(s, 0, B, kv_total, false);
+}
+
+int moe_latent_prefill(const moe_latent_spec* spec, const moe_latent_cache* cache, const void* w_kvb_f16,
+                       const void* q_f16, int T, const int32_t* q_start, const int32_t* kv_start, int B, int kv_total,
+                       int max_q, void* out_f16, uint32_t* status, void* workspace, size_t workspace_bytes,
+                       void* stream) {
+  return prefill(false, spec, cache, w_kvb_f16, q_f16, T, q_start, kv_start, B, kv_total, max_q, out_f16, nullptr, 0, 0,
+                 status, workspace, workspace_bytes, stream);
+}
+
+size_t moe_latent4_prefill_workspace_bytes(const moe_latent_spec* s, int T, int B, int kv_total, int sums) {
+  return prefill_bytes(s, T, B, kv_total, sums != 0);
+}
+
+int moe_latent4_prefill(const moe_latent_spec* spec, const moe_latent_cache* cache, const void* w_kvb_f16,
+                        const void* q_f16, int T, const int32_t* q_start, const int32_t* kv_start, int B, int kv_total,
+                        int max_q, void* out_f16, float* sums, int64_t sums_stride, int sums_len, uint32_t* status,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  return prefill(true, spec, cache, w_kvb_f16, q_f16, T, q_start, kv_start, B, kv_total, max_q, out_f16, sums, sums_stride, sums_len,
+                 status, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"
