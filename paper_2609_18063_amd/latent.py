@@ -9,7 +9,9 @@ with adapters on the attention projections (§3.3). A block is, on the residual 
 
 :class:`LatentCache` holds the pages of all layers and one page table for them; pages are counted by the
 library's pool, so that sequences fork (a full page is shared, the last, partly filled one copied), end and move
-together without the device being read back.
+together without the device being read back. With ``bits=4`` the rows are quantized (324 bytes of 576 values instead of
+1152), and with ``weights`` each token's attention weights are added up, by which :meth:`LatentCache.evict` takes
+sequences back to a budget of tokens.
 """
 
 import torch
@@ -19,18 +21,29 @@ from . import binding as B
 
 class LatentCache:
     """Pages of every layer and the page tables of up to ``n_seqs`` sequences (the same page ids in every layer).
-    Tables and pages change on the current stream, which has to be the one that reads them."""
+    Tables and pages change on the current stream, which has to be the one that reads them.
 
-    def __init__(self, spec, n_layers, n_pages, n_seqs, max_tokens):
+    ``bits``: 16 (fp16 rows) or 4. ``weights`` (4 bits): keep the sums of every token's attention weights, ``sums`` fp32
+    ``[layers, sequences, tokens]``. A sequence's places and positions are the same until :meth:`evict` takes tokens out
+    of it: then its next token's position is its place and ``evicted[seq]`` more."""
+
+    def __init__(self, spec, n_layers, n_pages, n_seqs, max_tokens, bits=16, weights=False):
+        if bits not in (4, 16) or (weights and bits != 4):
+            raise ValueError("bits is 16 or 4, and weights are kept with 4")
         P = spec.page_tokens
-        self.spec, self.n_layers, self.max_pages = spec, n_layers, -(-max_tokens // P)
-        self.pages = torch.zeros(n_layers, n_pages, P, spec.d_latent + spec.d_rope, dtype=torch.float16, device="cuda")
+        self.spec, self.n_layers, self.max_pages, self.bits = spec, n_layers, -(-max_tokens // P), bits
+        if bits == 4:
+            self.pages = torch.zeros(n_layers, n_pages, B.latent4_page_bytes(spec), dtype=torch.uint8, device="cuda")
+        else:
+            self.pages = torch.zeros(n_layers, n_pages, P, spec.d_latent + spec.d_rope, dtype=torch.float16, device="cuda")
+        self.sums = torch.zeros(n_layers, n_seqs, self.max_pages * P, device="cuda") if weights else None
         self.table = torch.full((n_seqs, self.max_pages), -1, dtype=torch.int32, device="cuda")
         self.status = torch.zeros(1, dtype=torch.int32, device="cuda")
-        self.layers = [B.latent_cache(self.pages[n], self.table) for n in range(n_layers)]
+        self.layers = [B.latent4_cache(spec, p, self.table) if bits == 4 else B.latent_cache(p, self.table) for p in self.pages]
         self.pool = B.PagePool(n_pages, P)
         self.ids = [None] * n_seqs       # host copy of each sequence's pages; None: no such sequence
         self.tokens = [0] * n_seqs
+        self.evicted = [0] * n_seqs      # tokens that were taken out of each
 
     def _publish(self, seq):
         row = torch.full((self.max_pages,), -1, dtype=torch.int32)
@@ -42,7 +55,9 @@ class LatentCache:
         if None not in self.ids:
             raise ValueError("all %d sequences are in use" % len(self.ids))
         seq = self.ids.index(None)
-        self.ids[seq], self.tokens[seq] = [], 0
+        self.ids[seq], self.tokens[seq], self.evicted[seq] = [], 0, 0
+        if self.sums is not None:
+            self.sums[:, seq].zero_()
         return seq
 
     def _live(self, seq):
@@ -50,7 +65,7 @@ class LatentCache:
             raise ValueError("there is no sequence %d" % seq)
 
     def grow(self, seq, n):
-        """Room for ``n`` more tokens of ``seq``; returns the position of the first."""
+        """Room for ``n`` more tokens of ``seq``; returns the place of the first (its position, if none were evicted)."""
         self._live(seq)
         if n < 0:
             raise ValueError("sequence %d cannot grow by %d tokens" % (seq, n))
@@ -73,7 +88,9 @@ class LatentCache:
         except B.MoeError:
             self.ids[new] = None
             raise
-        self.tokens[new] = self.tokens[seq]
+        self.tokens[new], self.evicted[new] = self.tokens[seq], self.evicted[seq]
+        if self.sums is not None:
+            self.sums[:, new].copy_(self.sums[:, seq])
         if pairs:
             B.page_copy(self.pages, torch.tensor(pairs, dtype=torch.int32).cuda(), self.status)
         self._publish(new)
@@ -86,6 +103,47 @@ class LatentCache:
         self.pool.free(self.ids[seq])
         self.ids[seq], self.tokens[seq] = None, 0
         self.table[seq].fill_(-1)
+
+    def evict(self, budget, sinks=0, recent=0):
+        """Take every sequence of more than ``budget`` tokens back to that many: in each layer the first ``sinks``, the last
+        ``recent`` and those with the largest sums stay, in their order. They move to pages of their own (forks may share
+        the old ones), so as many have to be free; returns the number of tokens taken out of each sequence."""
+        if self.sums is None:
+            raise ValueError("a cache without weights has nothing to evict by")
+        if budget < 1 or sinks < 0 or recent < 0 or sinks + recent > budget:
+            raise ValueError("a budget of %d tokens cannot keep the first %d and the last %d" % (budget, sinks, recent))
+        todo = [s for s, n in enumerate(self.tokens) if self.ids[s] is not None and n > budget]
+        gone = [self.tokens[s] - budget if s in todo else 0 for s in range(len(self.ids))]
+        if not todo:
+            return gone
+        need = -(-budget // self.spec.page_tokens)
+        ids = self.pool.alloc(need * len(todo))
+        at = torch.tensor(todo).cuda()
+        sums, table = self.sums[:, at], self.table[at]
+        to = torch.tensor(ids, dtype=torch.int32).view(len(todo), need).cuda()
+        keep = torch.empty(self.n_layers, len(todo), budget, dtype=torch.int32, device="cuda")
+        B.evict_select(sums, torch.tensor([self.tokens[s] for s in todo], dtype=torch.int32).cuda(), budget, sinks, recent, keep,
+                       sums, self.status)
+        B.latent4_move(self.spec, self.pages, table, keep, to, self.status)
+        self.sums[:, at] = sums
+        for k, s in enumerate(todo):
+            self.pool.free(self.ids[s])
+            self.ids[s], self.tokens[s] = ids[k * need:(k + 1) * need], budget
+            self.evicted[s] += gone[s]
+            self._publish(s)
+        return gone
+
+    def rows(self, n, seq):
+        """The rows of ``seq`` in layer ``n`` as fp16 ``[tokens, d_latent + d_rope]``."""
+        self._live(seq)
+        T, P = self.tokens[seq], self.spec.page_tokens
+        if self.bits == 16:
+            ids = torch.tensor(self.ids[seq], dtype=torch.int64).cuda()
+            return self.pages[n].index_select(0, ids).flatten(0, 1)[:T]
+        out = torch.empty(T, self.spec.d_latent + self.spec.d_rope, dtype=torch.float16, device="cuda")
+        B.latent4_read(self.spec, self.layers[n], torch.full((T,), seq, dtype=torch.int32, device="cuda"),
+                       torch.arange(T, dtype=torch.int32, device="cuda"), out, self.status)
+        return out
 
     def compact(self):
         """Move the live pages to the lowest ids, in the tables too; returns the number of pages moved."""
@@ -133,56 +191,81 @@ class LatentAttention:
         shapes = ((self.n_q, d), (self.n_kv, d), (d, self.n_o))
         self.ws = self._ws(max(B.linear_workspace_bytes(o, i, rank, max_rows) for o, i in shapes))
         rows = min(max_rows, len(cache.ids))
-        self.ws_decode = self._ws(B.latent_decode_workspace_bytes(s, rows, self.max_len))
+        if cache.bits == 4:
+            self.ws_decode = self._ws(B.latent4_decode_workspace_bytes(s, rows, self.max_len, sums=cache.sums is not None))
+        else:
+            self.ws_decode = self._ws(B.latent_decode_workspace_bytes(s, rows, self.max_len))
         self.ws_prefill = None
 
     @staticmethod
     def _ws(n):
         return torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
 
-    def _project(self, n, x, seq, pos):
+    def _project(self, n, x, seq, pos, slot):
         b, T = self.blocks[n], x.shape[0]
         q, kv = self.qb[:T], self.kvb[:T]
         B.linear_int4(b.q, self.n_q, self.d, b.rank, b.lora_scale, x, q.view(T, -1), self.ws)
         B.linear_int4(b.kv, self.n_kv, self.d, b.rank, b.lora_scale, x, kv, self.ws)
-        B.latent_append(self.spec, self.cache.layers[n], kv, b.gamma, self.rope, seq, pos, self.cache.status, q=q, q_out=q)
+        c = self.cache
+        if c.bits == 4:
+            B.latent4_append(self.spec, c.layers[n], kv, b.gamma, self.rope, seq, pos if slot is None else slot, pos, c.status, q=q,
+                             q_out=q)
+        elif slot is None:
+            B.latent_append(self.spec, c.layers[n], kv, b.gamma, self.rope, seq, pos, c.status, q=q, q_out=q)
+        else:
+            raise ValueError("in an fp16 cache a token's place is its position")
         return q
+
+    def _sums(self, n, seqs):
+        return None if self.cache.sums is None else self.cache.sums[n, :seqs]
 
     def _out(self, n, r):
         b, T = self.blocks[n], r.shape[0]
         B.linear_int4(b.o, self.d, self.n_o, b.rank, b.lora_scale, self.ob[:T].view(T, -1), r, self.ws, add=True)
 
-    def decode(self, n, x, r, seq, pos, kv_len, max_len=None):
+    def decode(self, n, x, r, seq, pos, kv_len, max_len=None, slot=None):
         """Layer ``n`` for one token of each of the first ``len(x)`` table rows: ``x`` fp16 ``[B, d]`` (the normed
         residual), ``r`` fp32 ``[B, d]`` in and out; ``seq``, ``pos`` and ``kv_len`` (the token among them) int32
-        ``[B]`` on the GPU. ``max_len``: a bound on kv_len (the table's, if none). Capturable."""
-        q = self._project(n, x, seq, pos)
-        B.latent_decode(self.spec, self.cache.layers[n], self.blocks[n].w_kvb, q, kv_len,
-                        self.max_len if max_len is None else max_len, self.ob[:x.shape[0]], self.cache.status,
-                        self.ws_decode)
+        ``[B]`` on the GPU. ``max_len``: a bound on kv_len (the table's, if none). ``slot`` (4 bits): the tokens' places,
+        where they are not their positions. Capturable."""
+        q = self._project(n, x, seq, pos, slot)
+        c, most, o = self.cache, self.max_len if max_len is None else max_len, self.ob[:x.shape[0]]
+        if c.bits == 4:
+            B.latent4_decode(self.spec, c.layers[n], self.blocks[n].w_kvb, q, kv_len, most, o, c.status, self.ws_decode,
+                             sums=self._sums(n, x.shape[0]))
+        else:
+            B.latent_decode(self.spec, c.layers[n], self.blocks[n].w_kvb, q, kv_len, most, o, c.status, self.ws_decode)
         self._out(n, r)
 
-    def prefill(self, n, x, r, seq, pos, q_start, kv_start, kv_total, max_q):
+    def prefill(self, n, x, r, seq, pos, q_start, kv_start, kv_total, max_q, slot=None):
         """Layer ``n`` for chunks of prompts: the ragged batch of ``moe_latent_prefill``, sequence b in table row b.
         Rows of padding behind the last sequence (``seq`` -1) keep their ``r``. Eager only: its workspace grows with
         ``kv_total``, ``H (d_nope + d_v)`` halves a token, for one layer at a time."""
-        q = self._project(n, x, seq, pos)
-        need = B.latent_prefill_workspace_bytes(self.spec, q_start.numel() - 1, kv_total)
+        q = self._project(n, x, seq, pos, slot)
+        c, seqs = self.cache, q_start.numel() - 1
+        if c.bits == 4:
+            need = B.latent4_prefill_workspace_bytes(self.spec, x.shape[0], seqs, kv_total, sums=c.sums is not None)
+        else:
+            need = B.latent_prefill_workspace_bytes(self.spec, seqs, kv_total)
         if self.ws_prefill is None or self.ws_prefill.nbytes < need:
             self.ws_prefill = self._ws(need)
         o = self.ob[:x.shape[0]].zero_()                 # (rows of padding are not written, and W_o 0 = 0)
-        B.latent_prefill(self.spec, self.cache.layers[n], self.blocks[n].w_kvb, q, q_start, kv_start, kv_total, max_q, o,
-                         self.cache.status, self.ws_prefill)
+        if c.bits == 4:
+            B.latent4_prefill(self.spec, c.layers[n], self.blocks[n].w_kvb, q, q_start, kv_start, kv_total, max_q, o, c.status,
+                              self.ws_prefill, sums=self._sums(n, seqs))
+        else:
+            B.latent_prefill(self.spec, c.layers[n], self.blocks[n].w_kvb, q, q_start, kv_start, kv_total, max_q, o, c.status,
+                             self.ws_prefill)
         self._out(n, r)
 
 
 class ChainAttention:
-    """The blocks as a decode chain's attention: one sequence, one token a step. ``pos`` and ``kv_len`` live on
+    """The blocks as a decode chain's attention: one sequence, one token a step, on a cache of ``bits``. ``pos`` and ``kv_len`` live on
     the GPU, so that captured steps replay at any token; ``at`` sets them before a token. What the calls find wrong
     is in ``cache.status``, not in the chain's."""
 
-    def __init__(self, d, spec, blocks, n_tokens):
-        self.cache = LatentCache(spec, len(blocks), -(-n_tokens // spec.page_tokens), 1, n_tokens)
+    def __init__(self, d, spec, blocks, n_tokens, bits=16):
+        self.cache = LatentCache(spec, len(blocks), -(-n_tokens // spec.page_tokens), 1, n_tokens, bits=bits)
         self.cache.grow(self.cache.start(), n_tokens)
         self.attn = LatentAttention(d, spec, blocks, self.cache, rope_table(n_tokens, spec.d_rope))
         self.n_tokens = n_tokens
