@@ -165,6 +165,48 @@ struct Walk {
   }
 };
 
+// The runs of tiles of every workgroup, written out (the 4-bit cache: its attention walks the line
+// in a short loop then, which the instruction cache and the scalar registers have room for). A
+// workgroup's first run stands at its number, the others behind all of those; the whole
+// workgroup calls, behind the writes of the starts. `lds`: room for some of them.
+__device__ __forceinline__ void list_runs(const DecodeArgs& a, int all, int* lds, int room) {
+  const bool held = a.B <= room;
+  if (held) {
+    for (int b = threadIdx.x; b < a.B; b += 256) lds[b] = a.starts[b];
+    __syncthreads();
+  }
+  const int per = max(a.p.least, (all + a.p.wgs - 1) / a.p.wgs);
+  for (int wg = threadIdx.x; wg < a.p.wgs; wg += 256) {
+    int t = (int)min((int64_t)all, (int64_t)wg * per);
+    const int end = min(all, t + per);
+    DecodeRun run{};
+    DecodeRun* to = a.runs + wg;
+    while (t < end) {
+      int lo = 0, hi = a.B;                              // (of equal starts the last one has the tile)
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if ((held ? lds[mid] : a.starts[mid]) <= t)
+          lo = mid;
+        else
+          hi = mid;
+      }
+      const int s0 = held ? lds[lo] : a.starts[lo], len = clamp_len(a, a.kv_len[lo]);
+      const Item it = own_item<64>(a, lo, (t - s0) / places(tiles_of<64>(len)), s0, len);
+      const int from = it.start + kItemCost, upto = min(end, from + it.tiles), first = max(t - from, 0), n = upto - from - first;
+      t = upto < end ? from + it.tiles : end;
+      if (n <= 0) continue;
+      const int seg = wg + it.index;
+      if (run.n) {
+        run.next = a.p.wgs + seg;
+        *to = run;
+        to = a.runs + a.p.wgs + seg;
+      }
+      run = DecodeRun{it.row0, it.rows, first, n, it.last, lo, seg, -1};
+    }
+    *to = run;
+  }
+}
+
 // ---- q into the latent space ------------------------------------------------------
 // qt_h = W_uk,h^T q_n,h for 64 latent columns of one head and 64 sequences a workgroup;
 // W_uk,h's columns are staged in LDS and read transposed. qt is rounded to fp16, the
@@ -202,6 +244,10 @@ __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
       __syncthreads();
     }
     if (threadIdx.x == 0) a.starts[a.B] = base;
+    if constexpr (STEP == 64) {
+      __syncthreads();
+      list_runs(a, base, reinterpret_cast<int*>(wt), (int)sizeof(wt) / 4);
+    }
     return;
   }
   const int hd = l.Dn + l.Dr, row = l.Dc + l.Dr, c0 = blockIdx.x * 64;
@@ -226,7 +272,8 @@ __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
     for (int e = threadIdx.x; e < (b1 - b0) * pieces; e += 256) {
       const size_t r = (size_t)(b0 + e / pieces) * l.H + h;
       const int p = 8 * (e % pieces);
-      *reinterpret_cast<U4*>(a.ql + r * row + l.Dc + p) = ld16(l.q + r * hd + l.Dn + p);
+      const h8 v = ld_h8(l.q + r * hd + l.Dn + p);
+      *reinterpret_cast<h8*>(a.ql + r * row + l.Dc + p) = STEP == 64 ? in_code_order(v) : v;
     }
   }
 #pragma unroll
@@ -254,7 +301,14 @@ __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
     if (bt + 16 < b1) queries(bt + 16);
     if (bt + c < b1) {
       const h4 v = {(_Float16)d[0], (_Float16)d[1], (_Float16)d[2], (_Float16)d[3]};
-      *reinterpret_cast<h4*>(a.ql + r * row + c0 + 16 * wave + 4 * g) = v;
+      if constexpr (STEP == 64) {
+        // (the 4-bit cache's products take eight elements in code order: 0, 4, 1, 5, 2, 6, 3, 7)
+        _Float16* to = reinterpret_cast<_Float16*>(a.ql + r * row + c0 + 16 * wave + 8 * (g >> 1) + (g & 1));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[2 * e] = v[e];
+      } else {
+        *reinterpret_cast<h4*>(a.ql + r * row + c0 + 16 * wave + 4 * g) = v;
+      }
     }
   }
 }

@@ -57,9 +57,19 @@ struct DecodePlan {
   int chunks, row_blocks;        // prefix: token chunks x row blocks
   int chunk_tiles, prefix_places;
   int wgs, least;                // workgroups, and the least share of the line of one
-  size_t ql, lat, starts, part_o, part_ml, total;  // byte offsets in the workspace
+  size_t ql, lat, starts, part_o, part_ml, runs, total;  // byte offsets in the workspace
 };
 DecodePlan decode_plan(int H, int Dc, int Dr, int B, int max_len, int prefix_len);
+
+// A workgroup's run of tiles of one item (the 4-bit cache; n 0: none).
+struct DecodeRun {
+  int row0, rows;                // the item's query rows
+  int first, n;                  // first tile, tiles
+  int last;                      // last token that may be read
+  int seq;                       // table row
+  int seg;                       // partial result
+  int next;                      // the workgroup's next run, or -1
+};
 
 struct DecodeArgs {
   LatentArgs l;
@@ -73,6 +83,7 @@ struct DecodeArgs {
   float* part_o;                 // [wgs + items][rows][Dc]
   float* part_ml;                // [wgs + items][2][rows][2]
   float* row_ml;                 // [B * H][2]: a row's reference and 1 / sum, or null
+  DecodeRun* runs;               // [2 wgs + items], the 4-bit cache
 };
 hipError_t launch_latent_decode(const DecodeArgs& a, hipStream_t st);
 

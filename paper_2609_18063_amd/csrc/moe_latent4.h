@@ -25,10 +25,8 @@ __host__ __device__ inline Page4 page4(int Dc, int Dr, int P) {
   return Page4{P * Dc / 2, rows, rows + P * 4 * (Dc / 64 + 1)};
 }
 
-// The order in which the eight codes of a word come out: 0, 4, 1, 5, 2, 6, 3, 7.
+// The order in which the eight codes of a word come out: 0, 4, 1, 5, 2, 6, 3, 7 (in_code_order).
 __device__ __forceinline__ constexpr int code_order(int i) { return (i >> 1) + 4 * (i & 1); }
-__device__ __forceinline__ h8 in_code_order(h8 v) { return __builtin_shufflevector(v, v, 0, 4, 1, 5, 2, 6, 3, 7); }
-__device__ __forceinline__ h8 in_value_order(h8 v) { return __builtin_shufflevector(v, v, 0, 2, 4, 6, 1, 3, 5, 7); }
 
 // The eight codes of a word less 8, exact halves in code order: a code in the low bits of the
 // half 1024 is 1024 + q, four bits up in the half 64 it is 64 + q.
@@ -37,9 +35,14 @@ __device__ __forceinline__ h8 codes8(uint32_t w) {
     const _Float16 b = (_Float16)(base + 8.f);
     return __builtin_bit_cast(h2, v) - h2{b, b};
   };
+  const auto pick = [](uint32_t v, uint32_t mask, uint32_t base) {
+    uint32_t r;  // (one instruction; left to itself the compiler takes two, with a literal each)
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(v), "s"(mask), "v"(base));
+    return r;
+  };
   const uint32_t u = w >> 8;
-  const h2 a = at((w & 0x000F000Fu) | 0x64006400u, 1024.f), b = at((w & 0x00F000F0u) | 0x54005400u, 64.f);
-  const h2 c = at((u & 0x000F000Fu) | 0x64006400u, 1024.f), d = at((u & 0x00F000F0u) | 0x54005400u, 64.f);
+  const h2 a = at(pick(w, 0x000F000Fu, 0x64006400u), 1024.f), b = at(pick(w, 0x00F000F0u, 0x54005400u), 64.f);
+  const h2 c = at(pick(u, 0x000F000Fu, 0x64006400u), 1024.f), d = at(pick(u, 0x00F000F0u, 0x54005400u), 64.f);
   return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 // The values, rounded once to fp16.

@@ -127,19 +127,21 @@ __global__ void __launch_bounds__(256) latent4_read_kernel(LatentArgs l, const i
 }
 
 // ---- attention over the cache ---------------------------------------------------
-// The schedule is moe_latent.hip's: of eight waves four form the scores and weights of a tile
-// of 64 tokens, the other four add up the weighted latents of the tile before, each a quarter
-// of the latent columns, and make the copies, two tiles ahead in four buffers. The codes stay
-// codes in LDS: a wave takes those it needs out of it, along a token for the scores and across
-// 16 tokens (the 4-bit transposing read) for the sums, and forms the values in registers, so
-// that LDS and HBM carry 4 bits a value.
+// A workgroup takes its runs of tiles (64 tokens each) one after the other. The schedule is
+// moe_latent.hip's: of eight waves four form the scores, transposed (tokens x query rows), and
+// the weights of a tile, the other four add up the weighted latents of the tile before, each a
+// quarter of the latent columns, and make the copies, two tiles ahead in four buffers. The codes
+// stay codes in LDS: a wave takes those it needs out of it, along a token for the scores and
+// across 16 tokens (the 4-bit transposing read) for the sums, and forms the values in registers,
+// so that LDS and HBM carry 4 bits a value.
 template <int DC, int DR, int MT>
 struct Decode4Shape {
   static constexpr int M = 16 * MT, G = DC / 64 + 1;
   static constexpr int NS = 4, NW = 2 * NS;                    // score waves (as many add up), waves
   static constexpr int WR = MT == 4 ? 2 : 1, TW = NS / WR;     // row blocks by token shares of the score waves
   static constexpr int RT = MT / WR, TT = 4 / TW;              // 16-row and 16-token tiles of one
-  static constexpr int KS = (DC + DR) / 32, CT = DC / 64;      // products of a score, 16-column tiles of an adding wave
+  static constexpr int NJ = DC / 128, KW = DR / 32;            // 16-byte pieces of a token's codes a lane has, words of its key
+  static constexpr int KS = 4 * NJ + KW, CT = DC / 64;         // products of a score, 16-column tiles of an adding wave
   // a group of 16 tokens: latents' codes, keys' codes, s and z
   static constexpr int LAT = 8 * DC, KEY = 8 * DR, TAIL = (KEY + 64 * G + 1023) / 1024 * 1024, GRP = LAT + TAIL;
   static constexpr int BUF = 4 * GRP, LN = LAT / 1024, CN = GRP / 1024;  // copies of a wave
@@ -157,6 +159,13 @@ struct Decode4Args {
   int64_t sums_stride;
 };
 
+// (through the scalar unit, as one load)
+__device__ __forceinline__ DecodeRun ld_run(const DecodeRun* p) {
+  const int32_t* q = reinterpret_cast<const int32_t*>(p);
+  return DecodeRun{ld_scalar(q),     ld_scalar(q + 1), ld_scalar(q + 2), ld_scalar(q + 3),
+                   ld_scalar(q + 4), ld_scalar(q + 5), ld_scalar(q + 6), ld_scalar(q + 7)};
+}
+
 template <int DC, int DR, int MT>
 __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_decode_kernel(DecodeArgs a) {
   using S = Decode4Shape<DC, DR, MT>;
@@ -171,29 +180,31 @@ __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_d
   const int wt = wave % S::TW, wr = wave / S::TW, wo = wave - S::NS;  // token share, row block; share of the columns
   // neighbours on the line share a chiplet and its L2
   const int wg = (blockIdx.x % 8) * (a.p.wgs / 8) + blockIdx.x / 8;
-  Walk<kStep4> at;
-  at.begin(a, wg);
+  DecodeRun at = ld_run(a.runs + wg);
   const float unit = l.scale * kLog2e;
   const int shift = 31 - __clz(l.page);
   // 16-token group `grp` (0 .. 3) of a tile, from its first token (past the end: the last group)
-  auto group = [&](const Item& it, int tile, int grp) { return min(it.tok0 + tile * kStep4 + 16 * grp, it.last & ~15); };
-  auto page_of = [&](const Item& it, int tile, int grp) { return ld_scalar(it.pages + (group(it, tile, grp) >> shift)); };
+  auto group = [&](const DecodeRun& run, int tile, int grp) { return min(tile * kStep4 + 16 * grp, run.last & ~15); };
+  auto page_of = [&](const DecodeRun& run, int tile, int grp) {
+    return ld_scalar(l.table + run.seq * l.table_stride + (group(run, tile, grp) >> shift));
+  };
   auto known = [&](int page) { return page >= 0 && page < l.n_pages; };
   if (threadIdx.x < 2) passed[threadIdx.x] = -1;
 
   if (wave < S::NS) {
     __builtin_amdgcn_s_setprio(2);
-    bool more = at.next(a);
+    bool more = at.n > 0;
     h8 q[S::RT][S::KS];
-    // (a product's k: of a word's eight codes in their order, of 16 (32-value keys: 8) a lane group)
+    // (a product's k: the eight codes of a word, of which a lane has 32 latents' of 128, 128 j + 32 g .. + 31,
+    // all of one group, and of the key 8 KW)
     auto queries = [&]() {
 #pragma unroll
       for (int r = 0; r < S::RT; ++r) {
-        const size_t row = at.it.row0 + min((wr * S::RT + r) * 16 + c, at.it.rows - 1);
+        const size_t row = at.row0 + min((wr * S::RT + r) * 16 + c, at.rows - 1);
 #pragma unroll
         for (int k = 0; k < S::KS; ++k) {
-          const int e = DR == 32 && k == S::KS - 1 ? DC + 8 * g : 64 * (k / 2) + 16 * g + 8 * (k % 2);
-          q[r][k] = in_code_order(ld_h8(a.ql + row * (DC + DR) + e));
+          const int e = k < 4 * S::NJ ? 128 * (k / 4) + 32 * g + 8 * (k % 4) : DC + 8 * S::KW * g + 8 * (k - 4 * S::NJ);
+          q[r][k] = ld_h8(a.ql + row * (DC + DR) + e);
         }
       }
     };
@@ -210,7 +221,7 @@ __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_d
     int page[S::TT] = {};
     auto pages = [&](int tile) {
 #pragma unroll
-      for (int t = 0; t < S::TT; ++t) page[t] = page_of(at.it, tile, wt * S::TT + t);
+      for (int t = 0; t < S::TT; ++t) page[t] = page_of(at, tile, wt * S::TT + t);
     };
     if (more) {
       queries();
@@ -219,35 +230,39 @@ __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_d
     start();
     vm_drain();
     lds_barrier();
-    // row i of a product is token 8 (i / 8) + code_order(i % 8), so that a lane has the weights
-    // of four tokens that follow each other in code order
-    const int tok = 8 * (c >> 3) + code_order(c & 7);
     // step u: the scores of tile u, the k-th of its item
     for (int u = 0, k = 0; more; ++u) {
       const char* buf = lds + (u & 3) * S::BUF + wt * S::TT * S::GRP;
       f4 x[S::TT][S::RT] = {};
 #pragma unroll
       for (int t = 0; t < S::TT; ++t) {
-        const char* lat = buf + t * S::GRP + tok * (DC / 2);
-        const char* key = buf + t * S::GRP + S::LAT + tok * (DR / 2);
-        const _Float16* sz = reinterpret_cast<const _Float16*>(buf + t * S::GRP + S::LAT + S::KEY) + tok;
+        const char* lat = buf + t * S::GRP + c * (DC / 2);
+        const char* key = buf + t * S::GRP + S::LAT + c * (DR / 2) + 4 * S::KW * g;
+        const _Float16* sz = reinterpret_cast<const _Float16*>(buf + t * S::GRP + S::LAT + S::KEY) + c;
+        u4 w[S::NJ];
+        uint32_t kw[S::KW];
+        _Float16 s[S::NJ + 1], z[S::NJ + 1];
 #pragma unroll
-        for (int n = 0; n < S::G; ++n) {
-          const h8 s = splat8(sz[16 * n]), z = splat8(sz[16 * (S::G + n)]);
-          if (n < S::G - 1 || DR == 64) {
-            const char* p = n < S::G - 1 ? lat + 16 * ((2 * n + (g >> 1)) ^ code_key<S::PC>(tok)) + 8 * (g & 1) : key + 8 * g;
-            const u2 w = *reinterpret_cast<const u2*>(p);
+        for (int j = 0; j < S::NJ; ++j) w[j] = *reinterpret_cast<const u4*>(lat + 16 * ((4 * j + g) ^ code_key<S::PC>(c)));
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const h8 kk = values8(w[i], s, z);
+        for (int j = 0; j <= S::NJ; ++j) {
+          const int n = j < S::NJ ? 2 * j + (g >> 1) : S::G - 1;
+          s[j] = sz[16 * n];
+          z[j] = sz[16 * (S::G + n)];
+        }
+        if constexpr (S::KW == 2) {
+          const u2 v = *reinterpret_cast<const u2*>(key);
+          kw[0] = v[0];
+          kw[1] = v[1];
+        } else {
+          kw[0] = *reinterpret_cast<const uint32_t*>(key);
+        }
 #pragma unroll
-              for (int r = 0; r < S::RT; ++r) x[t][r] = mfma16(kk, q[r][2 * n + i], x[t][r]);
-            }
-          } else {
-            const h8 kk = values8(*reinterpret_cast<const uint32_t*>(key + 4 * g), s, z);
+        for (int k = 0; k < S::KS; ++k) {
+          const int j = k < 4 * S::NJ ? k / 4 : S::NJ;
+          const h8 v = values8(k < 4 * S::NJ ? w[k / 4][k % 4] : kw[k - 4 * S::NJ], splat8(s[j]), splat8(z[j]));
 #pragma unroll
-            for (int r = 0; r < S::RT; ++r) x[t][r] = mfma16(kk, q[r][S::KS - 1], x[t][r]);
-          }
+          for (int r = 0; r < S::RT; ++r) x[t][r] = mfma16(v, q[r][k], x[t][r]);
         }
       }
       bool lost[S::TT];
@@ -255,15 +270,18 @@ __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_d
 #pragma unroll
       for (int t = 0; t < S::TT; ++t) {
         lost[t] = !known(page[t]);
-        left[t] = at.it.last - (at.it.tok0 + (at.first + k) * kStep4 + 16 * (wt * S::TT + t));
+        left[t] = at.last - ((at.first + k) * kStep4 + 16 * (wt * S::TT + t));
       }
-      const size_t seg = (size_t)wg + at.it.index;
-      // (the next item's query is asked for while this step's weights are formed)
+      const size_t seg = at.seg;
+      // (the next run's query is asked for while this step's weights are formed)
       const bool ends = ++k == at.n;
       if (ends) {
         k = 0;
-        more = at.next(a);
-        if (more) queries();
+        more = at.next >= 0;
+        if (more) {
+          at = ld_run(a.runs + at.next);
+          queries();
+        }
       }
       if (more) pages(at.first + k);
 #pragma unroll
@@ -274,9 +292,9 @@ __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_d
           for (int r = 0; r < S::RT; ++r)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (8 * (g >> 1) + code_order(4 * (g & 1) + e) > most) x[t][r][e] = -INFINITY;
+              if (4 * g + e > most) x[t][r][e] = -INFINITY;
         }
-      // the weights: of the tile's tokens in code order, eight at a time
+      // the weights, in the tokens' order
       float add[S::TT][S::RT];
       auto weights = [&]() {
 #pragma unroll
@@ -359,7 +377,21 @@ __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_d
   // this wave copies 16-token group wo of a tile
   const uint32_t at0 = lds_at(lds);
   const Page4 p4 = page4(DC, DR, l.page);
-  auto copy = [&](const Item& it, int tile, int buf, int page) {
+  // a lane's offsets: latents' codes in pieces whose places are keyed, then the keys' codes in one
+  // run and 32 bytes of each s and z (past the last: it again)
+  uint32_t lat_off[S::LN], tail_off[S::CN - S::LN], tail_step[S::CN - S::LN];
+#pragma unroll
+  for (int j = 0; j < S::LN; ++j) {
+    const int n = 64 * j + lane, row = n / S::PC;
+    lat_off[j] = row * (DC / 2) + 16 * ((n % S::PC) ^ code_key<S::PC>(row));
+  }
+#pragma unroll
+  for (int j = 0; j < S::CN - S::LN; ++j) {
+    const int n = 64 * j + lane, k = min(n - DR / 2, 4 * S::G - 1);
+    tail_off[j] = n < DR / 2 ? p4.keys + 16 * n : p4.steps + (k >> 1) * 2 * l.page + 16 * (k & 1);
+    tail_step[j] = n < DR / 2 ? DR / 2 : 2;
+  }
+  auto copy = [&](const DecodeRun& run, int tile, int buf, int page) {
     if (!known(page)) {
       // (zeros, whose scores are masked; the waits for copies find fewer than they allow)
       if (lane == 0 && l.status) atomicOr(l.status, MOE_STATUS_BAD_PAGE);
@@ -368,55 +400,44 @@ __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_d
       vm_wait<0>();
       return;
     }
-    const uint32_t to = at0 + buf * S::BUF + wo * S::GRP;
+    const uint32_t to = at0 + buf * S::BUF + wo * S::GRP, in = group(run, tile, wo) & (l.page - 1);
     const char* from = reinterpret_cast<const char*>(l.pages) + (size_t)page * p4.bytes;
-    const uint32_t in = group(it, tile, wo) & (l.page - 1);
-    int ln = lane;                                              // (offsets formed here, not held in registers)
-    asm volatile("" : "+v"(ln));
 #pragma unroll
-    for (int j = 0; j < S::LN; ++j) {
-      const int n = 64 * j + ln, row = n / S::PC;
-      dma16(from, in * (DC / 2) + row * (DC / 2) + 16 * ((n % S::PC) ^ code_key<S::PC>(row)), to + 1024 * j);
-    }
-    // keys' codes in one run, then 32 bytes of each s and z (past the last: it again)
+    for (int j = 0; j < S::LN; ++j) dma16(from + in * (DC / 2), lat_off[j], to + 1024 * j);
 #pragma unroll
-    for (int j = 0; j < S::CN - S::LN; ++j) {
-      const int n = 64 * j + ln, k = min(n - DR / 2, 4 * S::G - 1);
-      dma16(from, n < DR / 2 ? p4.keys + in * (DR / 2) + 16 * n : p4.steps + (k >> 1) * 2 * l.page + 2 * in + 16 * (k & 1),
-            to + S::LAT + 1024 * j);
-    }
+    for (int j = 0; j < S::CN - S::LN; ++j) dma16(from, tail_off[j] + in * tail_step[j], to + S::LAT + 1024 * j);
   };
   // the tiles asked for so far, and the next one
-  Walk<kStep4> ask = at;
+  DecodeRun ask = at;
   int asked = 0, k = 0;
-  bool more = ask.next(a);
-  int page = more ? page_of(ask.it, ask.first, wo) : 0;
+  bool more = ask.n > 0;
+  int page = more ? page_of(ask, ask.first, wo) : 0;
   auto ask_next = [&]() {
     if (!more) return false;
-    copy(ask.it, ask.first + k, asked & 3, page);
+    copy(ask, ask.first + k, asked & 3, page);
     ++asked;
     if (++k == ask.n) {
       k = 0;
-      more = ask.next(a);
+      more = ask.next >= 0;
+      if (more) ask = ld_run(a.runs + ask.next);
     }
-    if (more) page = page_of(ask.it, ask.first + k, wo);
+    if (more) page = page_of(ask, ask.first + k, wo);
     return true;
   };
   ask_next();
   ask_next();
+  // (a lane's address is a token's; the one of lane i is that of the i-th code of a word, so that
+  // the codes, which come out in code order, are in the tokens' order)
+  const int row = 8 * (c >> 3) + 2 * (c & 3) + (c >> 2 & 1);
   f4 o[S::CT][MT] = {};
   vm_drain();
   lds_barrier();
-  int left = 0;                                                 // tiles of the item that are not added up yet
+  int left = at.n;                                              // tiles of the run that are not added up yet
   // step u: the latents of tile u - 1, and tile u + 2 is asked for; the last step has no scores beside it
   for (int u = 0;; ++u) {
     const bool newer = ask_next();
     bool stored = false;
     if (u > 0) {
-      if (left == 0) {
-        at.next(a);
-        left = at.n;
-      }
       const char* blk = lds + ((u - 1) & 3) * S::BUF + g * S::GRP;
       h8 p[MT][2];
 #pragma unroll
@@ -425,37 +446,50 @@ __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_d
         for (int i = 0; i < 2; ++i)
           p[r][i] = ld_h8(pt + ((u - 1) & 1) * S::PT + (16 * r + c) * 128 + 16 * ((2 * g + i) ^ tile_key<8>(c)));
       // (past the sequence's end s and z are zeros: whatever is there takes no part)
-      const int tile0 = at.it.tok0 + (at.first + at.n - left) * kStep4, most = at.it.last - tile0;
-      h8 s[2], z[2];
-#pragma unroll
-      for (int k = 0; k < S::CT; ++k) {
-        const int col = wo * S::CT + k;
-        if (k == 0 || col % 4 == 0) {
-          const char* sz = blk + S::LAT + S::KEY + (col / 4) * 32;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            s[i] = in_code_order(ld_h8(sz + 16 * i));
-            z[i] = in_code_order(ld_h8(sz + 32 * S::G + 16 * i));
-            if (most < kStep4 - 1) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j)
-                if (16 * g + 8 * i + code_order(j) > most) s[i][j] = z[i][j] = (_Float16)0.f;
-            }
-          }
-        }
-        typedef int i2 __attribute__((ext_vector_type(2)));
-        const char* from = blk + c * (DC / 2) + 16 * ((col >> 1) ^ code_key<S::PC>(c)) + 8 * (col & 1);
-        const i2 w = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
-            (__attribute__((address_space(3))) i2*)(__attribute__((address_space(3))) char*)from);
+      const int most = at.last - (at.first + at.n - left) * kStep4;
+      // (the codes of KR column tiles, all of one group, are asked for before the products of the KR before them)
+      typedef int i2 __attribute__((ext_vector_type(2)));
+      constexpr int KR = S::CT < 4 ? S::CT : 4;
+      i2 w[2][KR];
+      h8 s[2][2], z[2][2];
+      auto read = [&](int n) {
+        const char* sz = blk + S::LAT + S::KEY + ((wo * S::CT + n) / 4) * 32;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const h8 v = values8((uint32_t)w[i], s[i], z[i]);
-#pragma unroll
-          for (int r = 0; r < MT; ++r) o[k][r] = mfma16(v, p[r][i], o[k][r]);
+          s[n / KR & 1][i] = ld_h8(sz + 16 * i);
+          z[n / KR & 1][i] = ld_h8(sz + 32 * S::G + 16 * i);
         }
+#pragma unroll
+        for (int k = 0; k < KR; ++k) {
+          const int col = wo * S::CT + n + k;
+          const char* from = blk + row * (DC / 2) + 16 * ((col >> 1) ^ code_key<S::PC>(row)) + 8 * (col & 1);
+          w[n / KR & 1][k] = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
+              (__attribute__((address_space(3))) i2*)(__attribute__((address_space(3))) char*)from);
+        }
+      };
+      read(0);
+#pragma unroll
+      for (int n = 0; n < S::CT; n += KR) {
+        if (n + KR < S::CT) read(n + KR);
+        __builtin_amdgcn_sched_barrier(0);
+        h8(&sn)[2] = s[n / KR & 1], (&zn)[2] = z[n / KR & 1];
+        if (most < kStep4 - 1)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (16 * g + 8 * i + j > most) sn[i][j] = zn[i][j] = (_Float16)0.f;
+#pragma unroll
+        for (int k = 0; k < KR; ++k)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const h8 v = values8((uint32_t)w[n / KR & 1][k][i], sn[i], zn[i]);
+#pragma unroll
+            for (int r = 0; r < MT; ++r) o[n + k][r] = mfma16(v, p[r][i], o[n + k][r]);
+          }
       }
       if (--left == 0) {
-        const size_t seg = (size_t)wg + at.it.index;
+        const size_t seg = at.seg;
 #pragma unroll
         for (int r = 0; r < MT; ++r)
 #pragma unroll
@@ -464,6 +498,10 @@ __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_d
             o[k][r] = f4{};
           }
         stored = true;
+        if (at.next >= 0) {
+          at = ld_run(a.runs + at.next);
+          left = at.n;
+        }
       }
     }
     if (u >= asked) break;
@@ -513,7 +551,7 @@ __global__ void __launch_bounds__(256) latent4_sums_kernel(Decode4Args b) {
     const __half* from = a.ql + ((size_t)seq * l.H + min(32 * rb + 16 * r + c, l.H - 1)) * (DC + DR);
 #pragma unroll
     for (int k = 0; k < KS; ++k)
-      q[r][k] = in_code_order(ld_h8(from + (DR == 32 && k == KS - 1 ? DC + 8 * g : 64 * (k / 2) + 16 * g + 8 * (k % 2))));
+      q[r][k] = ld_h8(from + (DR == 32 && k == KS - 1 ? DC + 8 * g : 64 * (k / 2) + 16 * g + 8 * (k % 2)));
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int h = 32 * rb + 16 * r + 4 * g + e;
@@ -628,6 +666,7 @@ DecodePlan decode4_plan(int H, int Dc, int Dr, int B, int max_len, bool sums, si
   p.starts = take(((size_t)B + 1) * 4);
   p.part_o = take(parts * p.rows * Dc * 4);
   p.part_ml = take(parts * p.rows * 32);
+  p.runs = take((p.wgs + parts) * sizeof(DecodeRun));
   *row_ml = off;
   if (sums) take(rows * 8);
   p.total = off;
@@ -762,6 +801,7 @@ int moe_latent4_decode(const moe_latent_spec* spec, const moe_latent_cache* cach
   a.starts = reinterpret_cast<int32_t*>(ws + a.p.starts);
   a.part_o = reinterpret_cast<float*>(ws + a.p.part_o);
   a.part_ml = reinterpret_cast<float*>(ws + a.p.part_ml);
+  a.runs = reinterpret_cast<moe::DecodeRun*>(ws + a.p.runs);
   a.row_ml = sums ? reinterpret_cast<float*>(ws + row_ml) : nullptr;
   b.sums = sums;
   b.sums_stride = sums_stride;

@@ -37,6 +37,11 @@ __device__ __forceinline__ h8 join(h4 a, h4 b) {
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
+// The order in which the eight 4-bit codes of a word become halves (moe_latent4.h): 0, 4, 1, 5,
+// 2, 6, 3, 7, and back.
+__device__ __forceinline__ h8 in_code_order(h8 v) { return __builtin_shufflevector(v, v, 0, 4, 1, 5, 2, 6, 3, 7); }
+__device__ __forceinline__ h8 in_value_order(h8 v) { return __builtin_shufflevector(v, v, 0, 2, 4, 6, 1, 3, 5, 7); }
+
 // The LDS address of a shared object.
 __device__ __forceinline__ uint32_t lds_at(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
