@@ -28,25 +28,32 @@ __host__ __device__ inline Page4 page4(int Dc, int Dr, int P) {
 // The order in which the eight codes of a word come out: 0, 4, 1, 5, 2, 6, 3, 7 (in_code_order).
 __device__ __forceinline__ constexpr int code_order(int i) { return (i >> 1) + 4 * (i & 1); }
 
+// The constants below, opaque to the compiler: mask and base of one v_and_or_b32 have to lie in
+// registers (as literals they take two instructions).
+struct CodeBits {
+  uint32_t even, odd, even_base, odd_base;
+};
+__device__ __forceinline__ CodeBits code_bits() {
+  CodeBits b{0x000F000Fu, 0x00F000F0u, 0x64006400u, 0x54005400u};
+  asm("" : "+s"(b.even), "+s"(b.odd), "+v"(b.even_base), "+v"(b.odd_base));
+  return b;
+}
 // The eight codes of a word less 8, exact halves in code order: a code in the low bits of the
 // half 1024 is 1024 + q, four bits up in the half 64 it is 64 + q.
-__device__ __forceinline__ h8 codes8(uint32_t w) {
+__device__ __forceinline__ h8 codes8(uint32_t w, const CodeBits& k) {
   const auto at = [](uint32_t v, float base) {
     const _Float16 b = (_Float16)(base + 8.f);
     return __builtin_bit_cast(h2, v) - h2{b, b};
   };
-  const auto pick = [](uint32_t v, uint32_t mask, uint32_t base) {
-    uint32_t r;  // (one instruction; left to itself the compiler takes two, with a literal each)
-    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(v), "s"(mask), "v"(base));
-    return r;
-  };
   const uint32_t u = w >> 8;
-  const h2 a = at(pick(w, 0x000F000Fu, 0x64006400u), 1024.f), b = at(pick(w, 0x00F000F0u, 0x54005400u), 64.f);
-  const h2 c = at(pick(u, 0x000F000Fu, 0x64006400u), 1024.f), d = at(pick(u, 0x00F000F0u, 0x54005400u), 64.f);
+  const h2 a = at((w & k.even) | k.even_base, 1024.f), b = at((w & k.odd) | k.odd_base, 64.f);
+  const h2 c = at((u & k.even) | k.even_base, 1024.f), d = at((u & k.odd) | k.odd_base, 64.f);
   return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 // The values, rounded once to fp16.
-__device__ __forceinline__ h8 values8(uint32_t w, h8 s, h8 z) { return __builtin_elementwise_fma(codes8(w), s, z); }
+__device__ __forceinline__ h8 values8(uint32_t w, h8 s, h8 z, const CodeBits& k) {
+  return __builtin_elementwise_fma(codes8(w, k), s, z);
+}
 __device__ __forceinline__ h8 splat8(_Float16 v) { return h8{v, v, v, v, v, v, v, v}; }
 
 }  // namespace moe

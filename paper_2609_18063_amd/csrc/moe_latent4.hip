@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(256) latent4_read_kernel(LatentArgs l, const i
   const int k = at & (l.page - 1), G = l.Dc / 64 + 1, grp = min(e / 64, G - 1);
   const char* code = e < l.Dc ? from + k * (l.Dc / 2) + e / 2 : from + p4.keys + k * (l.Dr / 2) + (e - l.Dc) / 2;
   const _Float16* s = reinterpret_cast<const _Float16*>(from + p4.steps) + (size_t)grp * l.page + k;
-  const h8 v = values8(*reinterpret_cast<const uint32_t*>(code), splat8(s[0]), splat8(s[(size_t)G * l.page]));
+  const h8 v = values8(*reinterpret_cast<const uint32_t*>(code), splat8(s[0]), splat8(s[(size_t)G * l.page]), code_bits());
   *reinterpret_cast<h8*>(rows + (size_t)t * row + e) = in_value_order(v);
 }
 
@@ -152,6 +152,13 @@ struct Decode4Shape {
 // XOR key of a row's pieces: 16 rows at one piece lie on all banks.
 template <int PC>
 __device__ __forceinline__ int code_key(int row) { return row * PC / 16; }
+
+// For the scheduler: N products behind the 13 instructions that form the next ones' values.
+template <int N>
+__device__ __forceinline__ void pace() {
+  __builtin_amdgcn_sched_group_barrier(0x2, 13, 0);
+  __builtin_amdgcn_sched_group_barrier(0x8, N, 0);
+}
 
 struct Decode4Args {
   DecodeArgs d;
@@ -190,6 +197,7 @@ __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_d
   };
   auto known = [&](int page) { return page >= 0 && page < l.n_pages; };
   if (threadIdx.x < 2) passed[threadIdx.x] = -1;
+  const CodeBits bits = code_bits();
 
   if (wave < S::NS) {
     __builtin_amdgcn_s_setprio(2);
@@ -257,12 +265,19 @@ __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_d
         } else {
           kw[0] = *reinterpret_cast<const uint32_t*>(key);
         }
+        // (a product's values are formed beside the product before it)
+        h8 v[2];
+        auto form = [&](int k) {
+          const int j = k < 4 * S::NJ ? k / 4 : S::NJ;
+          v[k & 1] = values8(k < 4 * S::NJ ? w[k / 4][k % 4] : kw[k - 4 * S::NJ], splat8(s[j]), splat8(z[j]), bits);
+        };
+        form(0);
 #pragma unroll
         for (int k = 0; k < S::KS; ++k) {
-          const int j = k < 4 * S::NJ ? k / 4 : S::NJ;
-          const h8 v = values8(k < 4 * S::NJ ? w[k / 4][k % 4] : kw[k - 4 * S::NJ], splat8(s[j]), splat8(z[j]));
+          if (k + 1 < S::KS) form(k + 1);
 #pragma unroll
-          for (int r = 0; r < S::RT; ++r) x[t][r] = mfma16(v, q[r][k], x[t][r]);
+          for (int r = 0; r < S::RT; ++r) x[t][r] = mfma16(v[k & 1], q[r][k], x[t][r]);
+          pace<S::RT>();
         }
       }
       bool lost[S::TT];
@@ -473,20 +488,24 @@ __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_d
         if (n + KR < S::CT) read(n + KR);
         __builtin_amdgcn_sched_barrier(0);
         h8(&sn)[2] = s[n / KR & 1], (&zn)[2] = z[n / KR & 1];
-        if (most < kStep4 - 1)
+        if (most < kStep4 - 1) {
+          asm volatile("");                                     // (a branch: as selects they would cost every tile)
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
               if (16 * g + 8 * i + j > most) sn[i][j] = zn[i][j] = (_Float16)0.f;
+        }
+        h8 v[2];
+        auto form = [&](int k) { v[k & 1] = values8((uint32_t)w[n / KR & 1][k / 2][k % 2], sn[k % 2], zn[k % 2], bits); };
+        form(0);
 #pragma unroll
-        for (int k = 0; k < KR; ++k)
+        for (int k = 0; k < 2 * KR; ++k) {
+          if (k + 1 < 2 * KR) form(k + 1);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const h8 v = values8((uint32_t)w[n / KR & 1][k][i], sn[i], zn[i]);
-#pragma unroll
-            for (int r = 0; r < MT; ++r) o[n + k][r] = mfma16(v, p[r][i], o[n + k][r]);
-          }
+          for (int r = 0; r < MT; ++r) o[n + k / 2][r] = mfma16(v[k & 1], p[r][k % 2], o[n + k / 2][r]);
+          pace<MT>();
+        }
       }
       if (--left == 0) {
         const size_t seg = at.seg;
@@ -562,6 +581,7 @@ __global__ void __launch_bounds__(256) latent4_sums_kernel(Decode4Args b) {
   }
   const float unit = l.scale * kLog2e;
   const Page4 p4 = page4(DC, DR, l.page);
+  const CodeBits bits = code_bits();
   int it = 0;
   for (int t0 = tok0; t0 < end; t0 += 16 * TG, ++it) {
     const int t = t0 + 16 * tw;
@@ -583,12 +603,12 @@ __global__ void __launch_bounds__(256) latent4_sums_kernel(Decode4Args b) {
           const u2 v = *reinterpret_cast<const u2*>((n < G - 1 ? lat + 32 * n : key) + 8 * g);
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const h8 kk = values8(v[i], s, z);
+            const h8 kk = values8(v[i], s, z, bits);
 #pragma unroll
             for (int r = 0; r < 2; ++r) x[r] = mfma16(q[r][2 * n + i], kk, x[r]);
           }
         } else {
-          const h8 kk = values8(*reinterpret_cast<const uint32_t*>(key + 4 * g), s, z);
+          const h8 kk = values8(*reinterpret_cast<const uint32_t*>(key + 4 * g), s, z, bits);
 #pragma unroll
           for (int r = 0; r < 2; ++r) x[r] = mfma16(q[r][KS - 1], kk, x[r]);
         }

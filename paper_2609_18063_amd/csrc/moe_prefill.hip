@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
       for (int e = lane; e < rows * pieces; e += 64) {
         const int r = e / pieces, k = e % pieces;
         const h8 v = values8(*reinterpret_cast<const uint32_t*>(from + p4.keys + (in + r) * (l.Dr / 2) + 4 * k), splat8(sz[r]),
-                             splat8(sz[(DC / 64 + 1) * l.page + r]));
+                             splat8(sz[(DC / 64 + 1) * l.page + r]), code_bits());
         *reinterpret_cast<h8*>(a.kr + (size_t)(s.first + tok + r) * l.Dr + 8 * k) = in_value_order(v);
       }
     } else if (there) {
@@ -179,6 +179,7 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
   uint32_t code[FOUR ? CW : 1];
   _Float16 step[FOUR ? CW : 1], mid[FOUR ? CW : 1];
   const Page4 p4 = page4(DC, l.Dr, l.page);
+  const CodeBits bits = code_bits();
   const int shift = 31 - __clz(l.page);
   auto ask = [&](int u) {
     const int t = min(u, n - 1);
@@ -198,7 +199,7 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
 #pragma unroll
     for (int j = 0; j < CW; ++j)
       *reinterpret_cast<h8*>(lds + (u & 1) * SLOT + 1024 * (CW * wave + j) + 16 * lane) =
-          in_value_order(values8(code[j], splat8(step[j]), splat8(mid[j])));
+          in_value_order(values8(code[j], splat8(step[j]), splat8(mid[j]), bits));
   };
   if constexpr (FOUR) {
     ask(0);
