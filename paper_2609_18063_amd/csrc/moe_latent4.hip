@@ -549,76 +549,94 @@ __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_d
 
 // ---- the tokens' weights -----------------------------------------------------------
 // sums[b][j] += sum_h softmax_h(j), once the rows' references and sums are known: the scores
-// again, 32 heads a wave (RB such blocks beside each other), 16 tokens a product. A token's
-// weights are added up in one order: heads by rows, lanes, then blocks.
-constexpr int kSumTokens = 512;   // of a workgroup
+// again, 16 RT heads a wave (RB such blocks beside each other), 16 tokens a product. A token's
+// weights are added up in one order: heads by rows, lanes, then blocks. The codes go from memory
+// to registers, 16 bytes a lane, as each is used once, and the next 16 tokens' are asked for
+// before these are used. Bound by latency where a wave has a step or two, by the values'
+// forming after that (512 latents: 40,000 tokens of 16 heads 10 us, 320,000 of 32 heads 35).
+// Workgroups at most, while a sequence has one (what is on the chip at once: with 256 and 1024
+// 320,000 tokens take 42 us; 60,000 of 32 heads 13, 15 and 22 with 256, 512 and 1024).
+constexpr int kSumGroups = 512;
 
-template <int DC, int DR, int RB>
-__global__ void __launch_bounds__(256) latent4_sums_kernel(Decode4Args b) {
-  constexpr int G = DC / 64 + 1, KS = (DC + DR) / 32, TG = 4 / RB;
+template <int DC, int DR, int RT, int RB>
+__global__ void __launch_bounds__(256) latent4_sums_kernel(Decode4Args b, int tokens) {
+  constexpr int G = DC / 64 + 1, NJ = DC / 128, KW = DR / 32, KS = 4 * NJ + KW, TG = 4 / RB;
   __shared__ float part[2][4][16];
   const DecodeArgs& a = b.d;
   const LatentArgs& l = a.l;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int rb = wave % RB, tw = wave / RB, seq = blockIdx.x % a.B;
-  const int len = clamp_len(a, a.kv_len[seq]), tok0 = blockIdx.x / a.B * kSumTokens, end = min(len, tok0 + kSumTokens);
-  if (tok0 >= end) return;
-  h8 q[2][KS];
-  float ref[2][4], inv[2][4];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const int rb = wave % RB, tw = wave / RB, seq = blockIdx.x % a.B, tok0 = blockIdx.x / a.B * tokens;
+  const int shift = 31 - __clz(l.page);
+  const Page4 p4 = page4(DC, DR, l.page);
+  struct Raw {                                               // what a lane has of 16 tokens' codes
+    u4 w[NJ];
+    uint32_t kw[KW];
+    _Float16 s[NJ + 1], z[NJ + 1];
+    int page;
+  };
+  auto page_of = [&](int t) { return ld_scalar(l.table + seq * l.table_stride + min(t >> shift, l.max_pages - 1)); };
+  auto known = [&](int page) { return page >= 0 && page < l.n_pages; };
+  auto load = [&](Raw& raw, int t, int page) {
+    raw.page = page;
+    if (!known(page)) return;
+    const char* from = reinterpret_cast<const char*>(l.pages) + (size_t)page * p4.bytes;
+    const int in = (t & (l.page - 1)) + c;
+    const char* lat = from + in * (DC / 2) + 16 * g;
+    const char* key = from + p4.keys + in * (DR / 2) + 4 * KW * g;
+    const _Float16* sz = reinterpret_cast<const _Float16*>(from + p4.steps) + in;
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    const __half* from = a.ql + ((size_t)seq * l.H + min(32 * rb + 16 * r + c, l.H - 1)) * (DC + DR);
+    for (int j = 0; j < NJ; ++j) raw.w[j] = *reinterpret_cast<const u4*>(lat + 64 * j);
+#pragma unroll
+    for (int i = 0; i < KW; ++i) raw.kw[i] = *reinterpret_cast<const uint32_t*>(key + 4 * i);
+#pragma unroll
+    for (int j = 0; j <= NJ; ++j) {
+      const int n = j < NJ ? 2 * j + (g >> 1) : G - 1;
+      raw.s[j] = sz[n * l.page];
+      raw.z[j] = sz[(G + n) * l.page];
+    }
+  };
+  Raw now;
+  load(now, tok0 + 16 * tw, page_of(tok0 + 16 * tw));
+  h8 q[RT][KS];
+  float ref[RT][4], inv[RT][4];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const int h0 = 16 * (RT * rb + r);
+    const __half* from = a.ql + ((size_t)seq * l.H + min(h0 + c, l.H - 1)) * (DC + DR);
 #pragma unroll
     for (int k = 0; k < KS; ++k)
-      q[r][k] = ld_h8(from + (DR == 32 && k == KS - 1 ? DC + 8 * g : 64 * (k / 2) + 16 * g + 8 * (k % 2)));
+      q[r][k] = ld_h8(from + (k < 4 * NJ ? 128 * (k / 4) + 32 * g + 8 * (k % 4) : DC + 8 * (KW * g + k - 4 * NJ)));
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int h = 32 * rb + 16 * r + 4 * g + e;
+      const int h = h0 + 4 * g + e;
       const float2 ml = *reinterpret_cast<const float2*>(a.row_ml + 2 * ((size_t)seq * l.H + min(h, l.H - 1)));
-      ref[r][e] = h < l.H ? ml.x : INFINITY;             // (a head that is not there: weight 0)
+      ref[r][e] = h < l.H ? ml.x : INFINITY;                 // (a head that is not there: weight 0)
       inv[r][e] = h < l.H ? ml.y : 0.f;
     }
   }
+  const int end = min(clamp_len(a, a.kv_len[seq]), tok0 + tokens);
   const float unit = l.scale * kLog2e;
-  const Page4 p4 = page4(DC, DR, l.page);
   const CodeBits bits = code_bits();
   int it = 0;
   for (int t0 = tok0; t0 < end; t0 += 16 * TG, ++it) {
     const int t = t0 + 16 * tw;
-    int32_t page = -1;
-    if (t < end) page = l.table[seq * l.table_stride + t / l.page];
-    const bool there = page >= 0 && page < l.n_pages;
-    float w = 0.f;
-    if (there) {
-      const char* from = reinterpret_cast<const char*>(l.pages) + (size_t)page * p4.bytes;
-      const int in = (t & (l.page - 1)) + c;
-      const char* lat = from + in * (DC / 2);
-      const char* key = from + p4.keys + in * (DR / 2);
-      const _Float16* sz = reinterpret_cast<const _Float16*>(from + p4.steps) + in;
-      f4 x[2] = {};
+    const bool there = t < end && known(now.page);
+    const Raw raw = now;
+    if (t0 + 16 * TG < end) load(now, t + 16 * TG, page_of(t + 16 * TG));
+    f4 x[RT] = {};
 #pragma unroll
-      for (int n = 0; n < G; ++n) {
-        const h8 s = splat8(sz[n * l.page]), z = splat8(sz[(G + n) * l.page]);
-        if (n < G - 1 || DR == 64) {
-          const u2 v = *reinterpret_cast<const u2*>((n < G - 1 ? lat + 32 * n : key) + 8 * g);
+    for (int k = 0; k < KS; ++k) {
+      const int j = k < 4 * NJ ? k / 4 : NJ;
+      const h8 v = values8(k < 4 * NJ ? raw.w[k / 4][k % 4] : raw.kw[k - 4 * NJ], splat8(raw.s[j]), splat8(raw.z[j]), bits);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const h8 kk = values8(v[i], s, z, bits);
-#pragma unroll
-            for (int r = 0; r < 2; ++r) x[r] = mfma16(q[r][2 * n + i], kk, x[r]);
-          }
-        } else {
-          const h8 kk = values8(*reinterpret_cast<const uint32_t*>(key + 4 * g), s, z, bits);
-#pragma unroll
-          for (int r = 0; r < 2; ++r) x[r] = mfma16(q[r][KS - 1], kk, x[r]);
-        }
-      }
-#pragma unroll
-      for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w += exp2_fast(fmaf(x[r][e], unit, -ref[r][e])) * inv[r][e];
-      w = col_sum(w);
+      for (int r = 0; r < RT; ++r) x[r] = mfma16(q[r][k], v, x[r]);
     }
+    float w = 0.f;
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w += exp2_fast(fmaf(x[r][e], unit, -ref[r][e])) * inv[r][e];
+    w = there ? col_sum(w) : 0.f;
     if constexpr (RB > 1) {
       if (g == 0) part[it & 1][wave][c] = w;
       __syncthreads();
@@ -640,17 +658,23 @@ hipError_t launch_attention(const DecodeArgs& a, hipStream_t st) {
   hipLaunchKernelGGL(kernel, dim3(a.p.wgs), dim3(64 * Decode4Shape<DC, DR, MT>::NW), lds, st, a);
   return hipGetLastError();
 }
-template <int DC, int DR>
+template <int DC, int DR, int RT, int RB>
 hipError_t launch_sums(const Decode4Args& b, hipStream_t st) {
   const DecodeArgs& a = b.d;
-  const dim3 grid((unsigned)((a.max_len + kSumTokens - 1) / kSumTokens) * a.B), block(256);
-  if (a.l.H <= 32)
-    hipLaunchKernelGGL((latent4_sums_kernel<DC, DR, 1>), grid, block, 0, st, b);
-  else if (a.l.H <= 64)
-    hipLaunchKernelGGL((latent4_sums_kernel<DC, DR, 2>), grid, block, 0, st, b);
-  else
-    hipLaunchKernelGGL((latent4_sums_kernel<DC, DR, 4>), grid, block, 0, st, b);
+  constexpr int step = 64 / RB;                              // tokens of a workgroup's step
+  const int64_t steps = (a.max_len + step - 1) / step, most = (kSumGroups + a.B - 1) / a.B;
+  const int each = (int)((steps + most - 1) / most);
+  hipLaunchKernelGGL((latent4_sums_kernel<DC, DR, RT, RB>), dim3((unsigned)((steps + each - 1) / each) * a.B), dim3(256), 0,
+                     st, b, each * step);
   return hipGetLastError();
+}
+template <int DC, int DR>
+hipError_t launch_sums(const Decode4Args& b, hipStream_t st) {
+  const int H = b.d.l.H;
+  return H <= 16   ? launch_sums<DC, DR, 1, 1>(b, st)
+         : H <= 32 ? launch_sums<DC, DR, 2, 1>(b, st)
+         : H <= 64 ? launch_sums<DC, DR, 2, 2>(b, st)
+                   : launch_sums<DC, DR, 2, 4>(b, st);
 }
 template <int DC, int DR>
 hipError_t launch_decode4(const Decode4Args& b, hipStream_t st) {
@@ -659,7 +683,7 @@ hipError_t launch_decode4(const Decode4Args& b, hipStream_t st) {
                  : a.p.rows == 32 ? launch_attention<DC, DR, 2>(a, st)
                                   : launch_attention<DC, DR, 4>(a, st);
   if (e == hipSuccess) e = launch_up<DC, kStep4>(a, st);
-  if (e == hipSuccess && b.sums && a.max_len > 0) e = launch_sums<DC, DR>(b, st);
+  if (e == hipSuccess && b.sums && a.max_len > 0 && a.l.max_pages > 0) e = launch_sums<DC, DR>(b, st);
   return e;
 }
 
@@ -668,9 +692,12 @@ int tiles_host(int len) { return (len + kStep4 - 1) / kStep4; }
 // As moe_latent.hip's, without a shared prefix.
 DecodePlan decode4_plan(int H, int Dc, int Dr, int B, int max_len, bool sums, size_t* row_ml) {
   DecodePlan p{};
-  p.rows = H <= 16 ? 16 : H <= 32 ? 32 : 64;
-  p.head_blocks = (H + p.rows - 1) / p.rows;
   const int wgs = kCus * (Dc <= 128 ? 2 : 1);
+  // 64 rows to a tile form its values once for all of them, but cost a longer start and twice the
+  // partial results (512 latents, 128 heads, 8 sequences, the call: 500 tokens 38 us with 64 rows, 34 with
+  // 32; 6,000 61, 57; 12,000, which is 12 tiles a workgroup, 79, 79.5; 24,000 110, 121)
+  p.rows = H <= 16 ? 16 : H <= 32 || (long long)B * ((H + 63) / 64) * tiles_host(max_len) < 12 * wgs ? 32 : 64;
+  p.head_blocks = (H + p.rows - 1) / p.rows;
   p.least = std::max(1, (int)(0.18 * std::sqrt((double)tiles_host(max_len)) + 0.5));
   const long long tiles = (long long)B * p.head_blocks * tiles_host(max_len);
   p.wgs = (int)std::min<long long>(wgs, (std::max<long long>(tiles, 1) + 7) / 8 * 8);
@@ -795,8 +822,6 @@ int moe_latent4_decode(const moe_latent_spec* spec, const moe_latent_cache* cach
   const int rc = moe::latent_cache_check(spec, cache);
   if (rc != MOE_OK) return rc;
   if (!decode4_shape_ok(spec, B, max_len) || B > cache->n_seqs || (sums && sums_stride < max_len)) return MOE_EINVAL;
-  if (sums && (int64_t)B * ((max_len + moe::kSumTokens - 1) / moe::kSumTokens) * 256 > (int64_t)UINT32_MAX)
-    return MOE_EINVAL;  // (a grid's threads)
   if (B == 0) return MOE_OK;
   if (!w_kvb_f16 || !q_f16 || !kv_len || !out_f16 || !workspace) return MOE_EINVAL;
   if (misaligned(w_kvb_f16, 16) || misaligned(q_f16, 16) || misaligned(kv_len, 4) || misaligned(out_f16, 16) ||
