@@ -51,6 +51,52 @@ __device__ __forceinline__ int tile_base(const PrefillArgs& a, int b) {
   return min(max(a.kv_start[b], 0), a.kv_total) / kTile + b;
 }
 
+// ---- a 4-bit cache's rows ---------------------------------------------------------------
+// The context's tokens as fp16 rows in the workspace, in the lists' order; what follows reads
+// these. Each value is formed once here, where the expansion would form it for every 256 of its columns
+// (3,100 tokens of 512 latents by 32 heads: expanded from the codes 77 us, from the rows 44 and
+// this 5, which is its latency). 16 tokens a workgroup, four a wave; rows without a page are left.
+template <int DC>
+__global__ void __launch_bounds__(256) latent4_rows_kernel(PrefillArgs a) {
+  constexpr int L = DC / 8, N = 4 * L / 64;                // lanes of a token, tokens of a lane
+  const LatentArgs& l = a.l;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, t = blockIdx.x / 4;
+  const int b = last_at_most(a.B, t, [&](int k) { return tile_base(a, k); });
+  const Span s = context_of(a, b);
+  const int tok = (t - tile_base(a, b)) * kTile + 16 * (blockIdx.x % 4);
+  if (tok < 0 || tok >= s.len) return;
+  const int page = l.table[b * l.table_stride + tok / l.page];
+  if (page < 0 || page >= l.n_pages) return;
+  const Page4 p4 = page4(DC, l.Dr, l.page);
+  const char* from = reinterpret_cast<const char*>(l.pages) + (size_t)page * p4.bytes;
+  const _Float16* sz = reinterpret_cast<const _Float16*>(from + p4.steps);
+  const int in = tok % l.page, row_halves = DC + l.Dr, mids = (DC / 64 + 1) * l.page;
+  const CodeBits bits = code_bits();
+  auto put = [&](int r, int at, uint32_t codes, _Float16 step, _Float16 mid) {  // (s.len: the page's later tokens are not its)
+    if (tok + r < s.len)
+      *reinterpret_cast<h8*>(a.rows + (size_t)(s.first + tok + r) * row_halves + at) =
+          in_value_order(values8(codes, splat8(step), splat8(mid), bits));
+  };
+  uint32_t codes[N];
+  _Float16 step[N], mid[N];
+  const int k = lane % L, r0 = 4 * wave + lane / L * N;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    codes[i] = *reinterpret_cast<const uint32_t*>(from + (in + r0 + i) * (DC / 2) + 4 * k);
+    const _Float16* at = sz + (k >> 3) * l.page + in + r0 + i;
+    step[i] = at[0];
+    mid[i] = at[mids];
+  }
+  const int words = l.Dr / 8, r1 = 4 * wave + lane / words;
+  if (lane < 4 * words) {
+    const _Float16* at = sz + (DC / 64) * l.page + in + r1;
+    put(r1, DC + 8 * (lane % words), *reinterpret_cast<const uint32_t*>(from + p4.keys + (in + r1) * (l.Dr / 2) + 4 * (lane % words)),
+        at[0], at[mids]);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) put(r0 + i, 8 * k, codes[i], step[i], mid[i]);
+}
+
 // ---- expanding the context ----------------------------------------------------------
 // 256 of the H (Dn + Dv) columns by up to 512 context tokens a workgroup. A wave keeps its
 // columns' weights of all Dc latents in registers and reads whole tokens, 32 a step, through
@@ -73,19 +119,16 @@ constexpr int kExpandProducts = DC == 512 ? 2 : 4;
 template <int DC>
 constexpr int kExpandWaves = 16 / kExpandProducts<DC>;
 
-// A 4-bit cache's rows (FOUR) come by way of registers, where their values are formed: a tile's
-// codes are asked for two tiles ahead and put into one of two slots behind the products of
-// the tile before it.
-template <int DC, bool FOUR>
+template <int DC>
 __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
     latent_expand_kernel(PrefillArgs a, int side, int col_groups, int splits) {
   constexpr int NM = kExpandProducts<DC>, NW = kExpandWaves<DC>, PR = DC / 8, CW = PR / 2 / NW, SLOT = kExpandTokens * DC * 2, KS = DC / 32;
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  constexpr int SLOTS = FOUR ? 2 : kExpandSlots;
-  int64_t* where = reinterpret_cast<int64_t*>(lds + SLOTS * SLOT);
+  int64_t* where = reinterpret_cast<int64_t*>(lds + kExpandSlots * SLOT);
   __shared__ uint32_t lost[4];
   const LatentArgs& l = a.l;
   const int row_halves = DC + l.Dr;
+  const __half* base = a.rows ? a.rows : l.pages;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int c = lane & 15, g = lane >> 4, hd = l.Dn + l.Dv, N = l.H * hd;
   const int split = blockIdx.x / col_groups, col0 = (blockIdx.x % col_groups) * kExpandCols + 16 * NM * wave;
@@ -120,19 +163,8 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
     int32_t page = -1;
     if (wave < 4 && tok < s.len) page = l.table[b * l.table_stride + tok / l.page];
     const bool there = page >= 0 && page < l.n_pages;
-    if (FOUR && there) {
-      const Page4 p4 = page4(DC, l.Dr, l.page);
-      const char* from = reinterpret_cast<const char*>(l.pages) + (size_t)page * p4.bytes;
-      const int pieces = l.Dr / 8, rows = min(16, s.len - tok), in = tok % l.page;
-      const _Float16* sz = reinterpret_cast<const _Float16*>(from + p4.steps) + (DC / 64) * l.page + in;
-      for (int e = lane; e < rows * pieces; e += 64) {
-        const int r = e / pieces, k = e % pieces;
-        const h8 v = values8(*reinterpret_cast<const uint32_t*>(from + p4.keys + (in + r) * (l.Dr / 2) + 4 * k), splat8(sz[r]),
-                             splat8(sz[(DC / 64 + 1) * l.page + r]), code_bits());
-        *reinterpret_cast<h8*>(a.kr + (size_t)(s.first + tok + r) * l.Dr + 8 * k) = in_value_order(v);
-      }
-    } else if (there) {
-      const __half* rope = l.pages + ((size_t)page * l.page + tok % l.page) * row_halves + DC;
+    if (there) {
+      const __half* rope = base + (a.rows ? (size_t)(s.first + tok) : (size_t)page * l.page + tok % l.page) * row_halves + DC;
       const int pieces = l.Dr / 8, rows = min(16, s.len - tok);
       for (int e = lane; e < rows * pieces; e += 64)
         *reinterpret_cast<U4*>(a.kr + (size_t)(s.first + tok + e / pieces) * l.Dr + 8 * (e % pieces)) =
@@ -148,8 +180,7 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
     }
   }
   if (n < 1) return;
-  // Where the tokens' rows are, as byte offsets, or as numbers in 4 bits (one without a page: -1;
-  // zeros are stored).
+  // Where the tokens' rows are, as byte offsets (one without a page: -1; zeros are stored).
   // Behind the last token its own values are stored again.
   for (int i = threadIdx.x; i < n * kExpandTokens; i += 64 * NW) {
     const int at = min(first + i, a.kv_total - 1);
@@ -158,7 +189,8 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
     const int tok = at - s.first;
     int page = -1;
     if (tok >= 0 && tok < s.len) page = l.table[b * l.table_stride + tok / l.page];
-    where[i] = page >= 0 && page < l.n_pages ? ((int64_t)page * l.page + tok % l.page) * (FOUR ? 1 : 2 * row_halves) : -1;
+    where[i] = page >= 0 && page < l.n_pages
+                   ? (a.rows ? at : (int64_t)page * l.page + tok % l.page) * 2 * row_halves : -1;
   }
   vm_drain();                                            // (the weights: asked for before the page ids)
   __syncthreads();
@@ -169,45 +201,13 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
 #pragma unroll
     for (int j = 0; j < CW; ++j) {
       const int p = 64 * (CW * wave + j) + lane, r = p / PR;
-      src[j] = reinterpret_cast<const char*>(l.pages) + max(where[t * kExpandTokens + r], (int64_t)0) +
+      src[j] = reinterpret_cast<const char*>(base) + max(where[t * kExpandTokens + r], (int64_t)0) +
                16 * ((p % PR) ^ tile_key<PR>(r));
     }
 #pragma unroll
     for (int j = 0; j < CW; ++j) dma16(src[j], at0 + slot * SLOT + 1024 * (CW * wave + j));
   };
-  // the same of a 4-bit row: to registers, and from there as values
-  uint32_t code[FOUR ? CW : 1];
-  _Float16 step[FOUR ? CW : 1], mid[FOUR ? CW : 1];
-  const Page4 p4 = page4(DC, l.Dr, l.page);
-  const CodeBits bits = code_bits();
-  const int shift = 31 - __clz(l.page);
-  auto ask = [&](int u) {
-    const int t = min(u, n - 1);
-#pragma unroll
-    for (int j = 0; j < CW; ++j) {
-      const int p = 64 * (CW * wave + j) + lane, r = p / PR, k = (p % PR) ^ tile_key<PR>(r);
-      const int64_t row = max(where[t * kExpandTokens + r], (int64_t)0);
-      const int in = (int)row & (l.page - 1);
-      const char* from = reinterpret_cast<const char*>(l.pages) + (row >> shift) * p4.bytes;
-      code[j] = *reinterpret_cast<const uint32_t*>(from + in * (DC / 2) + 4 * k);
-      const _Float16* s = reinterpret_cast<const _Float16*>(from + p4.steps) + (k >> 3) * l.page + in;
-      step[j] = s[0];
-      mid[j] = s[(DC / 64 + 1) * l.page];
-    }
-  };
-  auto put = [&](int u) {
-#pragma unroll
-    for (int j = 0; j < CW; ++j)
-      *reinterpret_cast<h8*>(lds + (u & 1) * SLOT + 1024 * (CW * wave + j) + 16 * lane) =
-          in_value_order(values8(code[j], splat8(step[j]), splat8(mid[j]), bits));
-  };
-  if constexpr (FOUR) {
-    ask(0);
-    put(0);
-    ask(1);
-  } else {
-    for (int u = 0; u < 3; ++u) copy(u);
-  }
+  for (int u = 0; u < 3; ++u) copy(u);
   const int h = min(col0, N - 1) / hd, in = min(col0, N - 1) % hd;
   // Values are stored finite: a row's weight 0 of a token that it does not see then gives 0,
   // whatever the token holds. (Its keys stay as they are, and make NaN of the rows that see it.)
@@ -230,23 +230,16 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
   const int to_row = in < l.Dn ? l.Dn : l.Dv;
   for (int u = 0; u < n; ++u) {
     // what was asked for after tile u: the copies of two tiles, and NM stores a tile
-    if (FOUR) {
-    } else if (idle || u == 0)
+    if (idle || u == 0)
       vm_wait<2 * CW>();
     else if (u == 1)
       vm_wait<2 * CW + NM>();
     else
       vm_wait<2 * CW + 2 * NM>();
     lds_barrier();
-    if constexpr (!FOUR) copy(u + 3);
-    if (idle) {
-      if constexpr (FOUR) {
-        put(u + 1);
-        ask(u + 2);
-      }
-      continue;
-    }
-    const char* x = lds + (u % SLOTS) * SLOT;
+    copy(u + 3);
+    if (idle) continue;
+    const char* x = lds + (u % kExpandSlots) * SLOT;
     // (the reads of KR steps are asked for before the products of the KR before them)
     f4 y[2][NM] = {};
     constexpr int KR = 4;
@@ -270,10 +263,6 @@ __global__ void __launch_bounds__(64 * kExpandWaves<DC>, 2)
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int m = 0; m < NM; ++m) y[t][m] = mfma16(w[k + i][m], v[k / KR & 1][i][t], y[t][m]);
-    }
-    if constexpr (FOUR) {
-      put(u + 1);
-      ask(u + 2);
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -646,24 +635,18 @@ hipError_t launch_attention(const PrefillArgs& a, hipStream_t st) {
 
 // As many splits of the tokens as fill the CUs (the weights of 512 latent columns leave room
 // for one workgroup there, else two), and at least one per kExpandMost tokens.
-template <int DC, bool FOUR>
+template <int DC>
 hipError_t launch_expand(const PrefillArgs& a, hipStream_t st) {
-  constexpr int lds = (FOUR ? 2 : kExpandSlots) * kExpandTokens * DC * 2 + kExpandMost * 8, slots = 256 * (DC == 512 ? 1 : 2);
+  constexpr int lds = kExpandSlots * kExpandTokens * DC * 2 + kExpandMost * 8, slots = 256 * (DC == 512 ? 1 : 2);
   const int groups = (a.l.H * (a.l.Dn + a.l.Dv) + kExpandCols - 1) / kExpandCols;
   const int tiles = (a.kv_total + kExpandTokens - 1) / kExpandTokens, most = kExpandMost / kExpandTokens;
   const int splits = std::max({1, std::min((slots + groups - 1) / groups, tiles), (tiles + most - 1) / most});
-  auto kernel = latent_expand_kernel<DC, FOUR>;
+  if (a.rows) hipLaunchKernelGGL((latent4_rows_kernel<DC>), dim3((unsigned)(a.kv_total / kTile + a.B) * 4), dim3(256), 0, st, a);
+  auto kernel = latent_expand_kernel<DC>;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(kernel, dim3((unsigned)groups * splits), dim3(64 * kExpandWaves<DC>), lds, st, a, a.kv_total / kTile + a.B, groups, splits);
   return hipGetLastError();
-}
-
-template <bool FOUR>
-hipError_t launch_expand(const PrefillArgs& a, hipStream_t st) {
-  return a.l.Dc == 512   ? launch_expand<512, FOUR>(a, st)
-         : a.l.Dc == 256 ? launch_expand<256, FOUR>(a, st)
-                         : launch_expand<128, FOUR>(a, st);
 }
 
 }  // namespace
@@ -680,7 +663,9 @@ int prefill_parts(int max_q, int H, int B, int kv_total) {
 
 hipError_t launch_latent_prefill(const PrefillArgs& a, hipStream_t st) {
   const LatentArgs& l = a.l;
-  hipError_t e = a.four ? launch_expand<true>(a, st) : launch_expand<false>(a, st);
+  hipError_t e = l.Dc == 512   ? launch_expand<512>(a, st)
+                 : l.Dc == 256 ? launch_expand<256>(a, st)
+                               : launch_expand<128>(a, st);
   if (e != hipSuccess) return e;
   e = l.Dn == 128 ? launch_attention<128>(a, st) : launch_attention<64>(a, st);
   if (e != hipSuccess || !a.row_ml || a.kv_total < 1) return e;
@@ -698,7 +683,7 @@ bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p
 size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
 struct PrefillLayout {
-  size_t k, v, kr, lost, part_o, part_ml, row_ml, part_sums, total;
+  size_t k, v, kr, lost, part_o, part_ml, row_ml, part_sums, rows, total;
 };
 constexpr int kMaxTotal = 1 << 24, kMaxBatch = 1 << 16;
 
@@ -706,7 +691,7 @@ bool prefill_shape_ok(const moe_latent_spec* s, int T, int B, int kv_total) {
   return moe_latent_spec_check(s) == MOE_OK && T >= 0 && T <= kMaxTotal && B >= 0 && B <= kMaxBatch && kv_total >= 0 &&
          kv_total <= kMaxTotal;
 }
-PrefillLayout prefill_layout(const moe_latent_spec* s, int T, int B, int kv_total, bool sums) {
+PrefillLayout prefill_layout(const moe_latent_spec* s, int T, int B, int kv_total, bool four, bool sums) {
   PrefillLayout p{};
   const size_t n = kv_total;
   p.k = 0;
@@ -717,12 +702,13 @@ PrefillLayout prefill_layout(const moe_latent_spec* s, int T, int B, int kv_tota
   p.part_ml = p.part_o + (size_t)moe::kPartGroups * moe::kPartRows * s->d_v * 4;
   p.row_ml = p.part_ml + (size_t)moe::kPartGroups * moe::kPartRows * 8;
   p.part_sums = p.row_ml + (sums ? round256((size_t)T * s->heads * 8) : 0);
-  p.total = p.part_sums + (sums ? round256((size_t)s->heads * n * 4) : 0);
+  p.rows = p.part_sums + (sums ? round256((size_t)s->heads * n * 4) : 0);
+  p.total = p.rows + (four ? round256(n * (s->d_latent + s->d_rope) * 2) : 0);
   return p;
 }
-size_t prefill_bytes(const moe_latent_spec* s, int T, int B, int kv_total, bool sums) {
+size_t prefill_bytes(const moe_latent_spec* s, int T, int B, int kv_total, bool four, bool sums) {
   if (!prefill_shape_ok(s, T, B, kv_total)) return 0;
-  return prefill_layout(s, T, B < 1 ? 1 : B, kv_total < 1 ? 1 : kv_total, sums).total;
+  return prefill_layout(s, T, B < 1 ? 1 : B, kv_total < 1 ? 1 : kv_total, four, sums).total;
 }
 
 int prefill(bool four, const moe_latent_spec* spec, const moe_latent_cache* cache, const void* w_kvb_f16, const void* q_f16,
@@ -740,7 +726,7 @@ int prefill(bool four, const moe_latent_spec* spec, const moe_latent_cache* cach
   if (misaligned(w_kvb_f16, 16) || misaligned(q_f16, 16) || misaligned(q_start, 4) || misaligned(kv_start, 4) ||
       misaligned(out_f16, 16) || misaligned(sums, 4) || misaligned(status, 4) || misaligned(workspace, 16))
     return MOE_EALIGN;
-  const PrefillLayout p = prefill_layout(spec, T, B, kv_total, sums != nullptr);
+  const PrefillLayout p = prefill_layout(spec, T, B, kv_total, four, sums != nullptr);
   if (workspace_bytes < p.total) return MOE_ENOMEM;
   moe::PrefillArgs a{};
   a.l = moe::latent_args(spec, cache);
@@ -762,7 +748,7 @@ int prefill(bool four, const moe_latent_spec* spec, const moe_latent_cache* cach
   a.part_o = reinterpret_cast<float*>(ws + p.part_o);
   a.part_ml = reinterpret_cast<float*>(ws + p.part_ml);
   a.parts = moe::prefill_parts(max_q, spec->heads, B, kv_total);
-  a.four = four;
+  a.rows = four ? reinterpret_cast<__half*>(ws + p.rows) : nullptr;
   if (sums) {
     a.row_ml = reinterpret_cast<float*>(ws + p.row_ml);
     a.part_sums = reinterpret_cast<float*>(ws + p.part_sums);
@@ -778,7 +764,7 @@ int prefill(bool four, const moe_latent_spec* spec, const moe_latent_cache* cach
 extern "C" {
 
 size_t moe_latent_prefill_workspace_bytes(const moe_latent_spec* s, int B, int kv_total) {
-  return prefill_bytes(s, 0, B, kv_total, false);
+  return prefill_bytes(s, 0, B, kv_total, false, false);
 }
 
 int moe_latent_prefill(const moe_latent_spec* spec, const moe_latent_cache* cache, const void* w_kvb_f16,
@@ -790,7 +776,7 @@ int moe_latent_prefill(const moe_latent_spec* spec, const moe_latent_cache* cach
 }
 
 size_t moe_latent4_prefill_workspace_bytes(const moe_latent_spec* s, int T, int B, int kv_total, int sums) {
-  return prefill_bytes(s, T, B, kv_total, sums != 0);
+  return prefill_bytes(s, T, B, kv_total, true, sums != 0);
 }
 
 int moe_latent4_prefill(const moe_latent_spec* spec, const moe_latent_cache* cache, const void* w_kvb_f16,
