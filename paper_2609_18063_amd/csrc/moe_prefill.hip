@@ -525,64 +525,95 @@ __global__ void __launch_bounds__(256) latent_parts_kernel(PrefillArgs a) {
 
 // ---- the tokens' weights ------------------------------------------------------------
 // sums[b][j] += sum over rows and heads of softmax(j), once the rows' references and sums are
-// known: the scores again. A workgroup takes one head's 128 tokens (a wave 32 of them, their
-// keys in registers) by all query rows that see them, 16 at a time; a second launch adds up
-// the heads, in order.
+// known: the scores again. A workgroup takes one head's 128 tokens by all query rows that see them:
+// a wave 64 tokens, whose keys it has in registers, by every other 16 rows, the next ones asked
+// for before these are used (with 32 tokens a wave and no row ahead it waited for its rows:
+// MEASURED). The two waves' sums are added up in order; a second launch adds up the heads, in order.
 constexpr int kSumTile = 128;
 
 template <int DN, int DR>
 __global__ void __launch_bounds__(256) latent_prefill_sums_kernel(PrefillArgs a) {
   constexpr int KS = (DN + DR) / 32;
+  __shared__ float other[kSumTile];
   const LatentArgs& l = a.l;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int h = blockIdx.x % l.H, t = blockIdx.x / l.H;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const int h = blockIdx.x % l.H, t = blockIdx.x / l.H, half = wave / 2;
   // (tiles of all sequences one behind the other, with gaps, as the 64-token tiles are)
   auto base = [&](int k) { return min(max(a.kv_start[k], 0), a.kv_total) / kSumTile + k; };
   const int b = last_at_most(a.B, t, base);
   const Span qs = span_of(a.q_start, b, a.T), ks = context_of(a, b);
-  const int tile0 = (t - base(b)) * kSumTile, tok0 = tile0 + 32 * wave;
-  if (tile0 < 0 || tok0 >= ks.len) return;
-  h8 k[2][KS];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const size_t at = ks.first + min(tok0 + 16 * i + c, ks.len - 1);
-#pragma unroll
-    for (int n = 0; n < KS; ++n)
-      k[i][n] = n < DN / 32 ? ld_h8(a.k + ((size_t)h * a.kv_total + at) * DN + 32 * n + 8 * g)
-                            : ld_h8(a.kr + at * DR + 32 * (n - DN / 32) + 8 * g);
-  }
-  const uint32_t lost = a.lost[tile_base(a, b) + tok0 / kTile] >> (tok0 / 16 % 4);
-  const float unit = l.scale * kLog2e;
+  const int tile0 = (t - base(b)) * kSumTile, tok0 = tile0 + kTile * (wave & 1);
+  if (tile0 < 0 || tile0 >= ks.len) return;
   const int shift = ks.len - qs.len;                     // position of query row 0
-  f4 w[2] = {};
-  for (int row0 = max(0, tok0 - shift) & ~15; row0 < qs.len; row0 += 16) {
-    const int row = min(row0 + c, qs.len - 1);
-    const size_t at = (size_t)(qs.first + row) * l.H + h;
-    const float2 ml = *reinterpret_cast<const float2*>(a.row_ml + 2 * at);
-    const float ref = row0 + c < qs.len ? ml.x : INFINITY, inv = row0 + c < qs.len ? ml.y : 0.f;
-    f4 s[2] = {};
+  const float unit = l.scale * kLog2e;
+  f4 w[4] = {};
+  int row0 = (max(0, tok0 - shift) & ~15) + 16 * half;
+  if (tok0 < ks.len && row0 < qs.len) {
+    h8 next[KS];
+    float2 next_ml;
+    auto ask = [&](int row0) {
+      const size_t at = (size_t)(qs.first + min(row0 + c, qs.len - 1)) * l.H + h;
 #pragma unroll
-    for (int n = 0; n < KS; ++n) {
-      const h8 q = ld_h8(l.q + at * (DN + DR) + 32 * n + 8 * g);
+      for (int n = 0; n < KS; ++n) next[n] = ld_h8(l.q + at * (DN + DR) + 32 * n + 8 * g);
+      next_ml = *reinterpret_cast<const float2*>(a.row_ml + 2 * at);
+    };
+    ask(row0);
+    h8 k[4][KS];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) s[i] = mfma16(k[i][n], q, s[i]);
+    for (int i = 0; i < 4; ++i) {
+      const size_t at = ks.first + min(tok0 + 16 * i + c, ks.len - 1);
+#pragma unroll
+      for (int n = 0; n < KS; ++n)
+        k[i][n] = n < DN / 32 ? ld_h8(a.k + ((size_t)h * a.kv_total + at) * DN + 32 * n + 8 * g)
+                              : ld_h8(a.kr + at * DR + 32 * (n - DN / 32) + 8 * g);
     }
+    for (; row0 < qs.len; row0 += 32) {
+      const bool in = row0 + c < qs.len;
+      const float ref = in ? next_ml.x : INFINITY, inv = in ? next_ml.y : 0.f;  // (rows past the last: it again, weight 0)
+      h8 q[KS];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+      for (int n = 0; n < KS; ++n) q[n] = next[n];
+      if (row0 + 32 < qs.len) ask(row0 + 32);
+      f4 s[4] = {};
+#pragma unroll
+      for (int n = 0; n < KS; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = mfma16(k[i][n], q[n], s[i]);
+      // (a token behind a row takes nothing of it, NaN neither)
+      auto add = [&](auto edge) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float v = __builtin_amdgcn_exp2f(fmaf(s[i][e], unit, -ref)) * inv;
+            w[i][e] += edge && tok0 + 16 * i + 4 * g + e > shift + row0 + c ? 0.f : v;
+          }
+      };
+      if (tok0 + kTile - 1 > shift + row0)
+        add(std::true_type{});
+      else
+        add(std::false_type{});
+    }
+  }
+  const uint32_t lost = tok0 < ks.len ? a.lost[tile_base(a, b) + tok0 / kTile] : 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[i][e] = row16_sum(w[i][e]);
+  if (half == 1 && c == 0)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<f4*>(other + kTile * (wave & 1) + 16 * i + 4 * g) = w[i];
+  __syncthreads();
+  if (half == 0 && c == 0)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const bool sees = tok0 + 16 * i + 4 * g + e <= shift + row0 + c && row0 + c < qs.len;
-        w[i][e] += sees ? __builtin_amdgcn_exp2f(fmaf(s[i][e], unit, -ref)) * inv : 0.f;
+        const int tok = tok0 + 16 * i + 4 * g + e;
+        if (tok < ks.len)
+          a.part_sums[(size_t)h * a.kv_total + ks.first + tok] =
+              lost >> i & 1 ? 0.f : w[i][e] + other[kTile * (wave & 1) + 16 * i + 4 * g + e];
       }
-  }
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float v = row16_sum(w[i][e]);
-      const int tok = tok0 + 16 * i + 4 * g + e;
-      if (c == 0 && tok < ks.len) a.part_sums[(size_t)h * a.kv_total + ks.first + tok] = lost >> i & 1 ? 0.f : v;
-    }
 }
 
 __global__ void __launch_bounds__(256) latent_sums_join_kernel(PrefillArgs a) {
