@@ -525,15 +525,19 @@ __global__ void __launch_bounds__(256) latent_parts_kernel(PrefillArgs a) {
 
 // ---- the tokens' weights ------------------------------------------------------------
 // sums[b][j] += sum over rows and heads of softmax(j), once the rows' references and sums are
-// known: the scores again. A workgroup takes one head's 128 tokens by all query rows that see them:
-// a wave 64 tokens, whose keys it has in registers, by every other 16 rows, the next ones asked
-// for before these are used (with 32 tokens a wave and no row ahead it waited for its rows:
-// MEASURED). The two waves' sums are added up in order; a second launch adds up the heads, in order.
-constexpr int kSumTile = 128;
+// known: the scores again. A workgroup takes one head's 128 tokens by all query rows that see them,
+// 32 a step: a wave 64 tokens, whose keys it has in registers, by 16 of the rows, which come
+// through LDS in three slots, copied two steps ahead (read by each wave for itself, 16
+// rows of 64 bytes an instruction, the rows bound it: 1,555 query rows on 4,200 tokens by 16 heads
+// 50 us, now 37, of which the keys' reads, of that kind too, take 5 a workgroup). The two waves' sums
+// are added up in order; a second launch adds up the heads, in order.
+constexpr int kSumTile = 128, kSumRows = 32;
 
 template <int DN, int DR>
-__global__ void __launch_bounds__(256) latent_prefill_sums_kernel(PrefillArgs a) {
-  constexpr int KS = (DN + DR) / 32;
+__global__ void __launch_bounds__(256, 2) latent_prefill_sums_kernel(PrefillArgs a) {
+  constexpr int KS = (DN + DR) / 32, PR = (DN + DR) / 8, SLOT = kSumRows * PR * 16, CN = SLOT / 1024, CW = (CN + 3) / 4;
+  __shared__ __attribute__((aligned(16))) char rows[3 * SLOT];
+  __shared__ __attribute__((aligned(16))) char mls[3][kSumRows * 8];
   __shared__ float other[kSumTile];
   const LatentArgs& l = a.l;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
@@ -545,19 +549,25 @@ __global__ void __launch_bounds__(256) latent_prefill_sums_kernel(PrefillArgs a)
   const int tile0 = (t - base(b)) * kSumTile, tok0 = tile0 + kTile * (wave & 1);
   if (tile0 < 0 || tile0 >= ks.len) return;
   const int shift = ks.len - qs.len;                     // position of query row 0
+  const int first = max(0, tile0 - shift) & ~15;         // the first row that may see a token
   const float unit = l.scale * kLog2e;
-  f4 w[4] = {};
-  int row0 = (max(0, tok0 - shift) & ~15) + 16 * half;
-  if (tok0 < ks.len && row0 < qs.len) {
-    h8 next[KS];
-    float2 next_ml;
-    auto ask = [&](int row0) {
-      const size_t at = (size_t)(qs.first + min(row0 + c, qs.len - 1)) * l.H + h;
+  const uint32_t at0 = lds_at(rows);
+  // piece k of row r of a step is at (k ^ key) of its own part, nope or rope
+  auto place = [](int r, int k) {
+    return k < DN / 8 ? k ^ tile_key<DN / 8>(r) : DN / 8 + ((k - DN / 8) ^ tile_key<DR / 8>(r));
+  };
+  auto copy = [&](int u) {                               // (past the last row: it again)
 #pragma unroll
-      for (int n = 0; n < KS; ++n) next[n] = ld_h8(l.q + at * (DN + DR) + 32 * n + 8 * g);
-      next_ml = *reinterpret_cast<const float2*>(a.row_ml + 2 * at);
-    };
-    ask(row0);
+    for (int j = 0; j < CW; ++j) {
+      const int piece = min(CW * wave + j, CN - 1), p = 64 * piece + lane, r = p / PR;
+      const size_t at = (size_t)(qs.first + min(first + kSumRows * u + r, qs.len - 1)) * l.H + h;
+      dma16(reinterpret_cast<const char*>(l.q + at * (DN + DR)) + 16 * place(r, p % PR), at0 + u % 3 * SLOT + 1024 * piece);
+    }
+    const size_t at = (size_t)(qs.first + min(first + kSumRows * u + lane / 2, qs.len - 1)) * l.H + h;
+    dma4(a.row_ml + 2 * at + lane % 2, lds_at(mls[u % 3]));  // (every wave the same)
+  };
+  f4 w[4] = {};
+  if (first < qs.len) {
     h8 k[4][KS];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -567,18 +577,25 @@ __global__ void __launch_bounds__(256) latent_prefill_sums_kernel(PrefillArgs a)
         k[i][n] = n < DN / 32 ? ld_h8(a.k + ((size_t)h * a.kv_total + at) * DN + 32 * n + 8 * g)
                               : ld_h8(a.kr + at * DR + 32 * (n - DN / 32) + 8 * g);
     }
-    for (; row0 < qs.len; row0 += 32) {
-      const bool in = row0 + c < qs.len;
-      const float ref = in ? next_ml.x : INFINITY, inv = in ? next_ml.y : 0.f;  // (rows past the last: it again, weight 0)
-      h8 q[KS];
-#pragma unroll
-      for (int n = 0; n < KS; ++n) q[n] = next[n];
-      if (row0 + 32 < qs.len) ask(row0 + 32);
+    copy(0);
+    copy(1);
+    const int n = (qs.len - first + kSumRows - 1) / kSumRows;
+    for (int u = 0; u < n; ++u) {
+      vm_wait<CW + 1>();                                 // (all but the copies of step u + 1)
+      lds_barrier();
+      copy(u + 2);
+      const int row0 = first + kSumRows * u + 16 * half;
+      if (row0 >= qs.len || row0 + 15 + shift < tok0) continue;
       f4 s[4] = {};
 #pragma unroll
-      for (int n = 0; n < KS; ++n)
+      for (int n = 0; n < KS; ++n) {
+        const h8 q = ld_h8(rows + u % 3 * SLOT + ((16 * half + c) * PR + place(16 * half + c, 4 * n + g)) * 16);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = mfma16(k[i][n], q[n], s[i]);
+        for (int i = 0; i < 4; ++i) s[i] = mfma16(k[i][n], q, s[i]);
+      }
+      const float2 ml = *reinterpret_cast<const float2*>(mls[u % 3] + 8 * (16 * half + c));
+      const bool in = row0 + c < qs.len;
+      const float ref = in ? ml.x : INFINITY, inv = in ? ml.y : 0.f;
       // (a token behind a row takes nothing of it, NaN neither)
       auto add = [&](auto edge) {
 #pragma unroll
@@ -594,6 +611,7 @@ __global__ void __launch_bounds__(256) latent_prefill_sums_kernel(PrefillArgs a)
       else
         add(std::false_type{});
     }
+    vm_wait<0>();                                        // (copies may be in flight into this workgroup's LDS)
   }
   const uint32_t lost = tok0 < ks.len ? a.lost[tile_base(a, b) + tok0 / kTile] : 0;
 #pragma unroll
