@@ -23,25 +23,48 @@ struct Append4Args {
   char* pages;
 };
 
-__device__ __forceinline__ double pair_min(double v, double o) { return o < v ? o : v; }
-__device__ __forceinline__ double pair_max(double v, double o) { return o > v ? o : v; }
+// op over 16, 32 or 64 lanes, by lane moves (a trip through LDS for each of a double's halves
+// costs more than the sums); every lane has the result.
+template <int CTRL>
+__device__ __forceinline__ double dpp_d(double v) {
+  return __hiloint2double(dpp_i<CTRL>(0, __double2hiint(v)), dpp_i<CTRL>(0, __double2loint(v)));
+}
+template <typename Op>
+__device__ __forceinline__ double over_lanes(double v, int lanes, Op op) {
+  v = op(v, dpp_d<0xB1>(v));
+  v = op(v, dpp_d<0x4E>(v));
+  v = op(v, dpp_d<0x141>(v));
+  v = op(v, dpp_d<0x140>(v));
+  auto both = [&](auto lo, auto hi) { return op(__hiloint2double(hi[0], lo[0]), __hiloint2double(hi[1], lo[1])); };
+  if (lanes > 16) {
+    const uint32_t lo = __double2loint(v), hi = __double2hiint(v);
+    v = both(__builtin_amdgcn_permlane16_swap(lo, lo, false, false), __builtin_amdgcn_permlane16_swap(hi, hi, false, false));
+  }
+  if (lanes > 32) {
+    const uint32_t lo = __double2loint(v), hi = __double2hiint(v);
+    v = both(__builtin_amdgcn_permlane32_swap(lo, lo, false, false), __builtin_amdgcn_permlane32_swap(hi, hi, false, false));
+  }
+  return v;
+}
 
 // Two neighbouring values of a group a thread, `lanes` (16 or 32) threads a group.
 __device__ __forceinline__ void store_group(double x, double y, int lanes, char* code, __half* s_at, __half* z_at) {
-  double lo = pair_min(x, y), hi = pair_max(x, y);
-  int odd = !isfinite(x) || !isfinite(y);
-  for (int o = 1; o < lanes; o <<= 1) {
-    lo = pair_min(lo, __shfl_xor(lo, o, kWave));
-    hi = pair_max(hi, __shfl_xor(hi, o, kWave));
-    odd |= __shfl_xor(odd, o, kWave);
-  }
+  auto lower = [](double v, double o) { return o < v ? o : v; };
+  auto upper = [](double v, double o) { return o > v ? o : v; };
+  const double lo = over_lanes(lower(x, y), lanes, lower), hi = over_lanes(upper(x, y), lanes, upper);
+  const int first = threadIdx.x & 63 & -lanes;
+  const bool odd = __ballot(!isfinite(x) || !isfinite(y)) >> first & ((1ull << lanes) - 1);
   __half s = __float2half_rn((float)((hi - lo) / 15.0));
   const double step = (double)__half2float(s);
   __half z = __float2half_rn((float)(lo + 8.0 * step));
   // (a value that is not finite, or beyond fp16, makes NaN of its group)
   if (odd || !isfinite(__half2float(s)) || !isfinite(__half2float(z))) s = z = __ushort_as_half(0x7E00);
-  const double base = (double)__half2float(z), div = step == 0.0 ? 1.0 : step;
-  auto q = [&](double v) { return (int)fmin(fmax(rint((v - base) / div) + 8.0, 0.0), 15.0); };
+  const double base = (double)__half2float(z), div = step == 0.0 ? 1.0 : step, inv = 1.0 / div;
+  auto q = [&](double v) {
+    double n = (v - base) * inv;
+    if (fabs(fabs(n - rint(n)) - 0.5) < 1e-9) n = (v - base) / div;  // (beside a border: as defined)
+    return (int)fmin(fmax(rint(n) + 8.0, 0.0), 15.0);
+  };
   *code = (char)(q(x) | q(y) << 4);
   if ((threadIdx.x & (lanes - 1)) == 0) {
     *s_at = s;
@@ -54,7 +77,14 @@ __device__ __forceinline__ void store_group(double x, double y, int lanes, char*
 __global__ void __launch_bounds__(256) latent4_append_kernel(Append4Args b) {
   const AppendArgs& a = b.a;
   const LatentArgs& l = a.l;
-  const int t = blockIdx.x, seq = a.seq[t], pos = a.pos[t], slot = b.slot[t];
+  const int t = blockIdx.x, seq = a.seq[t], pos = a.pos[t], slot = b.slot[t], e = 2 * threadIdx.x;
+  const float* kv = a.kv + (size_t)t * (l.Dc + l.Dr);
+  float2 v = {0.f, 0.f}, x = {0.f, 0.f}, gm = {0.f, 0.f}; // two of Dc <= 512 a thread
+  if (blockIdx.y == 0 && e < l.Dc) {
+    v = *reinterpret_cast<const float2*>(kv + e);
+    gm = __half22float2(*reinterpret_cast<const __half2*>(a.gamma + e));
+  }
+  if (blockIdx.y == 0 && e < l.Dr) x = *reinterpret_cast<const float2*>(kv + l.Dc + e);
   if (seq < 0) return;                                   // a padding row
   int32_t page = -1;
   const bool in = seq < l.n_seqs && pos >= 0 && pos < a.max_pos && slot >= 0 && slot / l.page < l.max_pages;
@@ -70,30 +100,20 @@ __global__ void __launch_bounds__(256) latent4_append_kernel(Append4Args b) {
     return;
   }
   __shared__ double red[4];
-  const float* kv = a.kv + (size_t)t * (l.Dc + l.Dr);
   const Page4 p4 = page4(l.Dc, l.Dr, l.page);
   char* to = b.pages + (size_t)page * p4.bytes;
-  const int at = slot & (l.page - 1), G = l.Dc / 64 + 1, e = 2 * threadIdx.x;
+  const int at = slot & (l.page - 1), G = l.Dc / 64 + 1;
   __half* s_to = reinterpret_cast<__half*>(to + p4.steps) + at;
   __half* z_to = s_to + (size_t)G * l.page;
-  float2 v = {0.f, 0.f}, x = {0.f, 0.f}, r = {0.f, 0.f}; // two of Dc <= 512 a thread
-  float2 gm = {0.f, 0.f};
-  if (e < l.Dc) {
-    v = *reinterpret_cast<const float2*>(kv + e);
-    gm = __half22float2(*reinterpret_cast<const __half2*>(a.gamma + e));
-  }
-  if (e < l.Dr) {
-    x = *reinterpret_cast<const float2*>(kv + l.Dc + e);
-    r = cs[threadIdx.x];
-  }
-  double s = (double)v.x * v.x + (double)v.y * v.y;
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, kWave);
+  float2 r = {0.f, 0.f};
+  if (e < l.Dr) r = cs[threadIdx.x];
+  const double s = over_lanes((double)v.x * v.x + (double)v.y * v.y, 64, [](double p, double q) { return p + q; });
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
-  const double root = sqrt((red[0] + red[1] + red[2] + red[3]) / (double)l.Dc + 1e-6);
+  const double inv = 1.0 / sqrt((red[0] + red[1] + red[2] + red[3]) / (double)l.Dc + 1e-6);
   if (e < l.Dc) {
     const int grp = threadIdx.x >> 5;
-    store_group(v.x / root * gm.x, v.y / root * gm.y, 32, to + at * (l.Dc / 2) + threadIdx.x, s_to + grp * l.page,
+    store_group(v.x * inv * gm.x, v.y * inv * gm.y, 32, to + at * (l.Dc / 2) + threadIdx.x, s_to + grp * l.page,
                 z_to + grp * l.page);
   }
   if (e < l.Dr)
@@ -683,7 +703,7 @@ hipError_t launch_decode4(const Decode4Args& b, hipStream_t st) {
                  : a.p.rows == 32 ? launch_attention<DC, DR, 2>(a, st)
                                   : launch_attention<DC, DR, 4>(a, st);
   if (e == hipSuccess) e = launch_up<DC, kStep4>(a, st);
-  if (e == hipSuccess && b.sums && a.max_len > 0 && a.l.max_pages > 0) e = launch_sums<DC, DR>(b, st);
+  if (e == hipSuccess && b.sums && a.max_len > 0) e = launch_sums<DC, DR>(b, st);
   return e;
 }
 
