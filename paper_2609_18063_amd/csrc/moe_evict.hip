@@ -16,6 +16,8 @@ namespace {
 // narrowed to the m-th largest, 256 bins at a time between the smallest and the largest key
 // (sums spread over few octaves: bins over all 32 bits would be hit by all at once); then
 // one pass in order writes what stays.
+// Rows of up to 8,192 sums are HELD in registers over these passes. Bound by the passes' barriers
+// (192 rows of 6,000 sums: 15 us, read anew in each pass 19; one row of 1,100: 8.7, 8.4).
 struct SelectArgs {
   const float* sums;             // [rows][width], row = layer * B + sequence
   float* sums_out;               // the same shape; may be the same array
@@ -25,10 +27,11 @@ struct SelectArgs {
   uint32_t* status;
 };
 
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave, kBins = 256, kEach = 4;
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave, kBins = 256, kEach = 4, kHeldRounds = 2;
 
 __device__ __forceinline__ uint32_t wave_min_u32(uint32_t v) { return ~wave_max_u32(~v); }
 
+template <bool HELD>
 __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(SelectArgs a) {
   __shared__ uint32_t hist[kSelectWaves][kBins];
   __shared__ uint32_t low[kSelectWaves], high[kSelectWaves], found[2];
@@ -44,15 +47,38 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(SelectArgs
     last = first;
     m = 0;
   }
+  // four tokens in a row a thread, a round behind the other
+  constexpr int kRound = kSelectThreads * kEach;
+  float held[HELD ? kHeldRounds : 1][kEach];
+  auto load = [&](int i, float (&v)[kEach]) {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) v[j] = i + j < n ? sums[i + j] : 0.f;
+  };
+  if constexpr (HELD)
+#pragma unroll
+    for (int r = 0; r < kHeldRounds; ++r) load(r * kRound + kEach * tid, held[r]);
+  // all of the ranked tokens' keys that are this thread's
+  auto each = [&](auto f) {
+    if constexpr (HELD) {
+#pragma unroll
+      for (int r = 0; r < kHeldRounds; ++r)
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+          const int i = r * kRound + kEach * tid + j;
+          if (i >= first && i < last) f(topk_key(held[r][j]));
+        }
+    } else {
+      for (int i = first + tid; i < last; i += kSelectThreads) f(topk_key(sums[i]));
+    }
+  };
   uint32_t least = 0xFFFFFFFFu;                                  // keys above it stay (none is above this), and `ties` at it
   int ties = 0;
   if (m > 0) {
     uint32_t lo = 0xFFFFFFFFu, hi = 0;
-    for (int i = first + tid; i < last; i += kSelectThreads) {
-      const uint32_t k = topk_key(sums[i]);
+    each([&](uint32_t k) {
       lo = min(lo, k);
       hi = max(hi, k);
-    }
+    });
     lo = wave_min_u32(lo);
     hi = wave_max_u32(hi);
     if (lane == 0) {
@@ -72,10 +98,10 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(SelectArgs
     while (true) {
       for (int i = tid; i < kSelectWaves * kBins; i += kSelectThreads) (&hist[0][0])[i] = 0;
       __syncthreads();
-      for (int i = first + tid; i < last; i += kSelectThreads) {
-        const uint32_t k = topk_key(sums[i]) - lo;               // (below lo: wraps past the span)
+      each([&](uint32_t key) {
+        const uint32_t k = key - lo;                             // (below lo: wraps past the span)
         if (k <= span) atomicAdd(&hist[wave][k >> shift], 1u);
-      }
+      });
       __syncthreads();
       if (wave == 0) {
         // lane's four bins, from the largest keys down
@@ -117,17 +143,14 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(SelectArgs
   // (never past its own place, so that the sums may move within one array: a round's are
   // all read before the first is written).
   int above = 0, equal = 0;                                      // tokens that stay for sure, and ties, before this round
-  for (int i0 = 0; i0 < n; i0 += kSelectThreads * kEach) {
+  auto round = [&](int i0, const float (&v)[kEach]) {
     const int i = i0 + kEach * tid;
-    float v[kEach];
     uint32_t mine = 0;                                           // of this thread: ties << 16 | sure ones
     int what[kEach];                                             // 1: stays, 2: a tie
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
       what[j] = 0;
-      v[j] = 0.f;
       if (i + j >= n) continue;
-      v[j] = sums[i + j];
       const uint32_t k = topk_key(v[j]);
       what[j] = i + j < first || i + j >= last || k > least ? 1 : k == least ? 2 : 0;
       mine += what[j] == 1 ? 1u : what[j] == 2 ? 1u << 16 : 0u;
@@ -160,6 +183,17 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(SelectArgs
     above += all & 0xFFFF;
     equal += all >> 16;
     __syncthreads();
+  };
+  if constexpr (HELD) {
+#pragma unroll
+    for (int r = 0; r < kHeldRounds; ++r)
+      if (r * kRound < n) round(r * kRound, held[r]);
+  } else {
+    for (int i0 = 0; i0 < n; i0 += kRound) {
+      float v[kEach];
+      load(i0 + kEach * tid, v);
+      round(i0, v);
+    }
   }
   for (int i = stay + tid; i < a.budget; i += kSelectThreads) keep[i] = -1;
   for (int i = stay + tid; i < a.width; i += kSelectThreads) out[i] = 0.f;
@@ -250,8 +284,9 @@ int moe_evict_select(const float* sums, float* sums_out, int n_layers, int B, in
   if (misaligned(sums, 4) || misaligned(sums_out, 4) || misaligned(kv_len, 4) || misaligned(keep, 4) || misaligned(status, 4))
     return MOE_EALIGN;
   const moe::SelectArgs a{sums, sums_out, kv_len, B, width, budget, sinks, recent, keep, status};
-  hipLaunchKernelGGL(moe::evict_select_kernel, dim3((unsigned)(n_layers * B)), dim3(moe::kSelectThreads), 0,
-                     static_cast<hipStream_t>(stream), a);
+  const bool held = width <= moe::kHeldRounds * moe::kEach * moe::kSelectThreads;
+  hipLaunchKernelGGL(held ? moe::evict_select_kernel<true> : moe::evict_select_kernel<false>, dim3((unsigned)(n_layers * B)),
+                     dim3(moe::kSelectThreads), 0, static_cast<hipStream_t>(stream), a);
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_EHIP;
 }
 
