@@ -479,11 +479,12 @@ size_t moe_latent4_page_bytes(const moe_latent_spec* spec);
  * As moe_latent_append, into a 4-bit cache: the row (c / sqrt(mean(c^2) + 1e-6) *
  * gamma, rot(k_r)) is quantized by groups,
  *   s = fp16((hi - lo) / 15), z = fp16(lo + 8 s), q = clamp(rint((v - z) / s) + 8, 0, 15)
- * with lo and hi the group's smallest and largest value (s = 0: q = 8), all of it
- * formed in 64 bits from the fp32 inputs. A group with a value that is not finite, or whose s or z is
+ * with lo and hi the group's smallest and largest value (s = 0: the quotient is that by
+ * 1, and the value z whatever q is), all of it formed in 64 bits from the fp32 inputs. A group with a value that is not finite, or whose s or z is
  * beyond fp16, is NaN throughout.
  * slot: device int32 [T], the token's place in its sequence; pos its position, which gives the
- * angles. They are the same until tokens of the sequence are evicted.
+ * angles. They are the same until tokens of the sequence are evicted. No two tokens of a call
+ * may have one place: what is there then is of neither.
  */
 int moe_latent4_append(const moe_latent_spec* spec, const moe_latent_cache* cache, const float* kv,
                        const void* gamma_f16, const float* rope, int max_pos, const int32_t* seq,

@@ -432,3 +432,141 @@ def test_graphs_of_both_forms(torch_cuda):
         assert int(c.status) == 0
         total = [16.0 if k else 0.0 for k in n]
         assert np.allclose(sums.sum(1).cpu().numpy(), total, rtol=1e-5)
+
+
+@pytest.mark.parametrize("H,dims,lens", [
+    (33, S, [300, 0, 64]), (64, S, [1000]), (128, S, [70, 500]), (65, M, [129, 5]), (64, (256, 64, 128, 64), [65, 700]), (40, W, [130, 1]),
+    (128, W, [300])])
+def test_decode_many_heads_and_a_far_bound(torch_cuda, H, dims, lens):
+    """A bound on the lengths that is far above them: 64 query rows to a tile."""
+    torch, g = torch_cuda, np.random.default_rng(H + sum(lens))
+    c = Cache4(torch, g, H, *dims, 32, lens)
+    q = _queries(g, len(lens), c)
+    wide, sums = _sums(torch, g, len(lens), 1 << 20)
+    was = wide[:, :2000].cpu().numpy()
+    got = c.decode(q, most=1 << 20, sums=sums)
+    assert int(c.status) == 0
+    now = wide[:, :2000].cpu().numpy()
+    for b, rows in enumerate(c.rows):
+        c.check(got[b:b + 1], q[b:b + 1], b, rows)
+        c.check_sums(now[b], was[b], q[b:b + 1], rows)
+
+
+@pytest.mark.parametrize("H,dims,page,lens", [(2, S, 16, [40000, 33000]), (128, S, 64, [9000]), (16, W, 64, [33500])])
+def test_long_contexts(torch_cuda, H, dims, page, lens):
+    """Sums of several steps a workgroup. (Of the outputs' heads the oracle forms a few.)"""
+    torch, g = torch_cuda, np.random.default_rng(sum(lens))
+    c = Cache4(torch, g, H, *dims, page, lens)
+    q = _queries(g, len(lens), c)
+    wide, sums = _sums(torch, g, len(lens), max(lens))
+    was = wide.cpu().numpy()
+    got, now = c.decode(q, sums=sums), wide.cpu().numpy()
+    assert int(c.status) == 0
+    for b, rows in enumerate(c.rows):
+        for h in {0, H // 2, H - 1}:
+            want, bound = A.attend(q[b:b + 1, h], rows, c.w[h, :c.Dn], c.w[h, c.Dn:], c.scale, cached=A.HALF)
+            assert (np.abs(got[b:b + 1, h].astype(np.float64) - want) <= bound).all(), (b, h)
+        c.check_sums(now[b], was[b], q[b:b + 1], rows)
+
+
+@pytest.mark.parametrize("B,dims", [(2500, S), (4300, (128, 64, 128, 64))])
+def test_decode_of_many_sequences(torch_cuda, B, dims):
+    """More sequences than a workgroup holds the lengths of; many of them empty."""
+    torch, g = torch_cuda, np.random.default_rng(B)
+    lens = [int(n) for n in g.integers(0, 4, B)]
+    lens[3], lens[B // 2], lens[-1] = 200, 65, 17
+    c = Cache4(torch, g, 1, *dims, 16, lens)
+    q = _queries(g, B, c)
+    wide, sums = _sums(torch, g, B, 200)
+    was = wide.cpu().numpy()
+    got, now = c.decode(q, sums=sums), wide.cpu().numpy()
+    assert int(c.status) == 0
+    assert not got[np.array(lens) == 0].any()
+    for b in [0, 1, 2, 3, 4, B // 2 - 1, B // 2, B // 2 + 1, B - 2, B - 1] + list(range(7, B, 41)):
+        if lens[b]:
+            c.check(got[b:b + 1], q[b:b + 1], b, c.rows[b])
+        c.check_sums(now[b], was[b], q[b:b + 1], c.rows[b])
+
+
+def test_prefill_sums_of_a_nan_row(torch_cuda):
+    """A NaN in one query row: NaN of that row, and of the sums of the tokens that it sees; those behind it stay."""
+    torch, g = torch_cuda, np.random.default_rng(31)
+    c = Cache4(torch, g, 2, *S, 16, [300, 20])
+    q = _queries(g, 170, c)
+    q[40, 1, 5] = np.nan                                  # sees tokens 0 .. 190
+    _, sums = _sums(torch, g, 2, 300)
+    was = sums.cpu().numpy()
+    got, now = c.prefill(q, [150, 20], sums=sums), sums.cpu().numpy()
+    assert int(c.status) == 0
+    assert np.isnan(got[40, 1]).all() and np.isfinite(np.delete(got, 40, 0)).all()
+    assert np.isnan(now[0, :191]).all()
+    seen = np.arange(150, 300) + 1
+    want, bound = A.token_weights(np.delete(q[:150], 40, 0), c.rows[0], c.w[:, :64], c.scale, np.delete(seen, 40))
+    off = np.abs(now[0, 191:] - was[0, 191:].astype(np.float64) - want[191:])
+    assert (off <= bound[191:] + 4 * A.SINGLE + A.SINGLE * want[191:]).all()
+    c.check_sums(now[1], was[1], q[150:], c.rows[1], np.arange(20) + 1)
+
+
+def test_cache_past_32_bits(torch_cuda):
+    """Pages at byte offsets beyond 2^32: written, read back, moved and attended to by both forms."""
+    torch, g = torch_cuda, np.random.default_rng(18)
+    from paper_2609_18063_amd import binding as B
+    H, n = 3, 90
+    c = Cache4(torch, g, H, *S, 1024, [n])
+    size = B.latent4_page_bytes(c.spec)
+    n_pages = (1 << 32) // size + 60
+    big = torch.empty(n_pages, size, dtype=torch.uint8, device="cuda")
+    far = n_pages - 3
+    table = torch.tensor([[far], [far + 1], [5]], dtype=torch.int32, device="cuda")
+    cache = B.latent4_cache(c.spec, big, table)
+    raw = g.standard_normal((n, S[0] + S[1])).astype(np.float32)
+    rope = torch.zeros(n, S[1] // 2, 2, device="cuda")
+    rope[..., 0] = 1
+    place = c.i32(range(n))
+    B.latent4_append(c.spec, cache, torch.from_numpy(raw).cuda(), torch.ones(S[0], dtype=torch.float16, device="cuda"), rope,
+                     c.i32([0] * n), place, place, c.status)
+    B.latent4_move(c.spec, big[None], table[:1].repeat(2, 1), place.view(1, 1, n).repeat(1, 2, 1), table[1:].contiguous(), c.status)
+    x = raw.astype(np.float64)
+    x[:, :S[0]] /= np.sqrt((x[:, :S[0]] ** 2).mean(-1, keepdims=True) + 1e-6)
+    codes, s, z = A.quantize_row(x, S[0])
+    rows = A.row_values(codes, s, z, S[0])
+    for b in range(3):
+        back = torch.empty(n, S[0] + S[1], dtype=torch.float16, device="cuda")
+        B.latent4_read(c.spec, cache, c.i32([b] * n), place, back, c.status)
+        assert (np.abs(back.cpu().numpy() - rows) <= np.abs(rows) * A.HALF + 2.0**-25).all()  # one rounding to fp16
+    c.cache, c.lens, c.rows = cache, [n] * 3, [rows] * 3
+    q = _queries(g, 3, c)
+    was = np.zeros((3, n), np.float32)
+    for call in (c.decode, lambda q, sums: c.prefill(q, [1, 1, 1], sums=sums)):
+        sums = torch.zeros(3, n, device="cuda")
+        got = call(q, sums=sums)
+        for b in range(3):
+            c.check(got[b:b + 1], q[b:b + 1], b, rows)
+            c.check_sums(sums[b].cpu().numpy(), was[b], q[b:b + 1], rows)
+    assert int(c.status) == 0
+
+
+def test_calls_on_another_stream(torch_cuda):
+    """The stream that a call names: what is ordered before it there is seen, what is ordered behind it sees it."""
+    torch, g = torch_cuda, np.random.default_rng(4)
+    c = Cache4(torch, g, 4, *M, 16, [150, 40])
+    B, q = c.B, _queries(g, 2, c)
+    qt = torch.from_numpy(q).cuda()
+    late, out = torch.zeros_like(qt), torch.zeros(2, 4, M[3], dtype=torch.float16, device="cuda")
+    sums = torch.zeros(2, 150, device="cuda")
+    lens, ws = c.i32([150, 40]), c.workspace(B.latent4_decode_workspace_bytes(c.spec, 2, 150, True))
+    keep, kept = torch.zeros(1, 2, 30, dtype=torch.int32, device="cuda"), torch.zeros(1, 2, 150, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(2000000)
+        late.copy_(qt)
+    B.latent4_decode(c.spec, c.cache, c.wt, late, lens, 150, out, c.status, ws, sums=sums, stream=side)
+    B.evict_select(sums[None], lens, 30, 2, 5, keep, kept, c.status, stream=side)
+    side.synchronize()
+    for b in range(2):
+        c.check(out[b:b + 1].cpu().numpy(), q[b:b + 1], b, c.rows[b])
+        want = A.evict(sums[b].cpu().numpy(), c.lens[b], 30, 2, 5)
+        assert keep[0, b].tolist() == want
+        assert torch.equal(kept[0, b, :30], sums[b][torch.tensor(want, device="cuda")])
+    assert int(c.status) == 0
