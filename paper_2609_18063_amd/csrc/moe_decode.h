@@ -168,13 +168,9 @@ struct Walk {
 // The runs of tiles of every workgroup, written out (the 4-bit cache: its attention walks the line
 // in a short loop then, which the instruction cache and the scalar registers have room for). A
 // workgroup's first run stands at its number, the others behind all of those; the whole
-// workgroup calls, behind the writes of the starts. `lds`: room for some of them.
-__device__ __forceinline__ void list_runs(const DecodeArgs& a, int all, int* lds, int room) {
-  const bool held = a.B <= room;
-  if (held) {
-    for (int b = threadIdx.x; b < a.B; b += 256) lds[b] = a.starts[b];
-    __syncthreads();
-  }
+// workgroup calls, behind the writes of the starts. held: the first `room` of lds are the starts, the
+// next ones the lengths.
+__device__ __forceinline__ void list_runs(const DecodeArgs& a, int all, const int* lds, int room, bool held) {
   const int per = max(a.p.least, (all + a.p.wgs - 1) / a.p.wgs);
   for (int wg = threadIdx.x; wg < a.p.wgs; wg += 256) {
     int t = (int)min((int64_t)all, (int64_t)wg * per);
@@ -190,7 +186,7 @@ __device__ __forceinline__ void list_runs(const DecodeArgs& a, int all, int* lds
         else
           hi = mid;
       }
-      const int s0 = held ? lds[lo] : a.starts[lo], len = clamp_len(a, a.kv_len[lo]);
+      const int s0 = held ? lds[lo] : a.starts[lo], len = held ? lds[room + lo] : clamp_len(a, a.kv_len[lo]);
       const Item it = own_item<64>(a, lo, (t - s0) / places(tiles_of<64>(len)), s0, len);
       const int from = it.start + kItemCost, upto = min(end, from + it.tiles), first = max(t - from, 0), n = upto - from - first;
       t = upto < end ? from + it.tiles : end;
@@ -217,36 +213,51 @@ __device__ __forceinline__ void list_runs(const DecodeArgs& a, int all, int* lds
 template <int DN, int STEP>
 __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
   __shared__ __attribute__((aligned(16))) char wt[DN * 128];
-  __shared__ int scan[256];
+  __shared__ int scan[4];
   const LatentArgs& l = a.l;
   const int h = blockIdx.y, b0 = blockIdx.z * 64, b1 = min(b0 + 64, a.B);
   if ((int)blockIdx.x == l.Dc / 64) {
     if (blockIdx.y || blockIdx.z) return;
+    constexpr int kRoom = STEP == 64 ? DN * 16 : 0;       // (as many starts, and lengths, does wt hold)
+    int* held = reinterpret_cast<int*>(wt);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int base = a.p.prefix_places;
     for (int c0 = 0; c0 < a.B; c0 += 256) {
       const int b = c0 + threadIdx.x;
-      int n = 0;
+      int n = 0, len = 0;
       if (b < a.B) {
-        const int len = clamp_len(a, a.kv_len[b]);
-        if (len != a.kv_len[b] && l.status) atomicOr(l.status, MOE_STATUS_BAD_LENGTH);
+        const int given = a.kv_len[b];
+        len = clamp_len(a, given);
+        if (len != given && l.status) atomicOr(l.status, MOE_STATUS_BAD_LENGTH);
         n = places(tiles_of<STEP>(len)) * a.p.head_blocks;
       }
-      scan[threadIdx.x] = n;
-      __syncthreads();
-      for (int o = 1; o < 256; o <<= 1) {
-        const int v = (int)threadIdx.x >= o ? scan[threadIdx.x - o] : 0;
-        __syncthreads();
-        scan[threadIdx.x] += v;
-        __syncthreads();
+      int up = n;
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) {
+        const int v = __shfl_up(up, o, kWave);
+        if (lane >= o) up += v;
       }
-      if (b < a.B) a.starts[b] = base + scan[threadIdx.x] - n;
-      base += scan[255];
+      if (lane == kWave - 1) scan[wave] = up;
+      __syncthreads();
+      int all = 0;
+      for (int w = 0; w < 4; ++w) {
+        if (w < wave) up += scan[w];
+        all += scan[w];
+      }
+      if (b < a.B) {
+        a.starts[b] = base + up - n;
+        if (b < kRoom) {
+          held[b] = base + up - n;
+          held[kRoom + b] = len;
+        }
+      }
+      base += all;
       __syncthreads();
     }
     if (threadIdx.x == 0) a.starts[a.B] = base;
     if constexpr (STEP == 64) {
       __syncthreads();
-      list_runs(a, base, reinterpret_cast<int*>(wt), (int)sizeof(wt) / 4);
+      list_runs(a, base, held, kRoom, a.B <= kRoom);
     }
     return;
   }
@@ -299,17 +310,17 @@ __global__ void __launch_bounds__(256) latent_absorb_kernel(DecodeArgs a) {
 #pragma unroll
     for (int k = 0; k < DN / 32; ++k) d = mfma16(wa[k], x[k], d);
     if (bt + 16 < b1) queries(bt + 16);
-    if (bt + c < b1) {
-      const h4 v = {(_Float16)d[0], (_Float16)d[1], (_Float16)d[2], (_Float16)d[3]};
-      if constexpr (STEP == 64) {
-        // (the 4-bit cache's products take eight elements in code order: 0, 4, 1, 5, 2, 6, 3, 7)
-        _Float16* to = reinterpret_cast<_Float16*>(a.ql + r * row + c0 + 16 * wave + 8 * (g >> 1) + (g & 1));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) to[2 * e] = v[e];
-      } else {
-        *reinterpret_cast<h4*>(a.ql + r * row + c0 + 16 * wave + 4 * g) = v;
-      }
+    h4 v = {(_Float16)d[0], (_Float16)d[1], (_Float16)d[2], (_Float16)d[3]};
+    if constexpr (STEP == 64) {
+      // (the 4-bit cache's products take eight elements in code order, 0, 4, 1, 5, 2, 6, 3, 7: of the two
+      // lanes that have them one takes the first four, the other the last)
+      typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+      const u2 w = __builtin_bit_cast(u2, v);
+      const auto both = __builtin_amdgcn_permlane16_swap(w[0], w[1], false, false);
+      const uint32_t x = both[0], y = both[1];
+      v = __builtin_bit_cast(h4, u2{(x & 0xFFFFu) | y << 16, x >> 16 | (y & 0xFFFF0000u)});
     }
+    if (bt + c < b1) *reinterpret_cast<h4*>(a.ql + r * row + c0 + 16 * wave + 4 * g) = v;
   }
 }
 
