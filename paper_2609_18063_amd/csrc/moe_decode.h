@@ -446,21 +446,20 @@ __global__ void __launch_bounds__(NT) latent_join_kernel(DecodeArgs a) {
 constexpr int kFusedTokens = 768;
 
 template <int DC, bool JOIN, int STEP>
-__global__ void __launch_bounds__(256) latent_up_kernel(DecodeArgs a) {
+__device__ __forceinline__ void latent_up(const DecodeArgs& a, int tile, int h, int block) {
   constexpr int NT = 256, KS = DC / 128;
   __shared__ f4 red[4][kWave];
   __shared__ JoinShared<JOIN ? NT : 1> sh;
   __shared__ __attribute__((aligned(16))) _Float16 joined[JOIN ? DC : 8];
   const LatentArgs& l = a.l;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int v0 = blockIdx.x * 16, h = blockIdx.y;
-  const int b0 = blockIdx.z * 128, b1 = min(b0 + 128, a.B);
+  const int v0 = tile * 16, b0 = block * 128, b1 = min(b0 + 128, a.B);
   h8 w[KS];
   const __half* wv = l.w + ((size_t)h * (l.Dn + l.Dv) + l.Dn + v0 + c) * DC + wave * (DC / 4) + 8 * g;
 #pragma unroll
   for (int k = 0; k < KS; ++k) w[k] = ld_h8(wv + 32 * k);
   if constexpr (JOIN) {
-    const h4 v = join_row<NT, STEP>(a, h, 0, 1, a.row_ml && blockIdx.x == 0, sh);
+    const h4 v = join_row<NT, STEP>(a, h, 0, 1, a.row_ml && tile == 0, sh);
     if (threadIdx.x < DC / 4) *reinterpret_cast<h4*>(&joined[4 * threadIdx.x]) = v;
     __syncthreads();
   }
@@ -489,22 +488,36 @@ __global__ void __launch_bounds__(256) latent_up_kernel(DecodeArgs a) {
   }
 }
 
-template <int DC, int STEP>
-hipError_t launch_up(const DecodeArgs& a, hipStream_t st) {
-  const LatentArgs& l = a.l;
-  const dim3 grid(l.Dv / 16, l.H, (a.B + 127) / 128), block(256);
-  if (a.B == 1 && a.prefix_len == 0 && a.max_len <= kFusedTokens) {
-    hipLaunchKernelGGL((latent_up_kernel<DC, true, STEP>), grid, block, 0, st, a);
-    return hipGetLastError();
-  }
-  const int rows = a.B * l.H;
+template <int DC, bool JOIN, int STEP>
+__global__ void __launch_bounds__(256) latent_up_kernel(DecodeArgs a) {
+  latent_up<DC, JOIN, STEP>(a, blockIdx.x, blockIdx.y, blockIdx.z);
+}
+
+inline bool joins_itself(const DecodeArgs& a) { return a.B == 1 && a.prefix_len == 0 && a.max_len <= kFusedTokens; }
+inline dim3 up_grid(const DecodeArgs& a) { return dim3(a.l.Dv / 16, a.l.H, (a.B + 127) / 128); }
+
+template <int STEP>
+hipError_t launch_join(const DecodeArgs& a, hipStream_t st) {
+  const int rows = a.B * a.l.H;
   if (rows > 2 * kCus)
     hipLaunchKernelGGL((latent_join_kernel<128, STEP>), dim3(rows), dim3(128), 0, st, a);
-  else
-    hipLaunchKernelGGL((latent_join_kernel<512, STEP>), dim3(rows, rows <= kCus / 2 ? 4 : rows <= kCus ? 2 : 1), dim3(512), 0, st, a);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((latent_up_kernel<DC, false, STEP>), grid, block, 0, st, a);
+  else {
+    // (the 4-bit cache's attention takes half the time, so the join's share counts: 16 rows of 250
+    // partial results 9.8 us with eight slices, 11.3 with four; 32 rows of 47 6.4 with either)
+    const int slices = STEP == 64 && rows <= kCus / 8 && a.l.Dc >= 256 ? 8 : rows <= kCus / 2 ? 4 : rows <= kCus ? 2 : 1;
+    hipLaunchKernelGGL((latent_join_kernel<512, STEP>), dim3(rows, slices), dim3(512), 0, st, a);
+  }
+  return hipGetLastError();
+}
+template <int DC, int STEP>
+hipError_t launch_up(const DecodeArgs& a, hipStream_t st) {
+  const bool joins = joins_itself(a);
+  if (!joins) {
+    const hipError_t e = launch_join<STEP>(a, st);
+    if (e != hipSuccess) return e;
+  }
+  auto kernel = joins ? latent_up_kernel<DC, true, STEP> : latent_up_kernel<DC, false, STEP>;
+  hipLaunchKernelGGL(kernel, up_grid(a), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
