@@ -25,9 +25,6 @@ __host__ __device__ inline Page4 page4(int Dc, int Dr, int P) {
   return Page4{P * Dc / 2, rows, rows + P * 4 * (Dc / 64 + 1)};
 }
 
-// The order in which the eight codes of a word come out: 0, 4, 1, 5, 2, 6, 3, 7 (in_code_order).
-__device__ __forceinline__ constexpr int code_order(int i) { return (i >> 1) + 4 * (i & 1); }
-
 // The constants below, opaque to the compiler: mask and base of one v_and_or_b32 have to lie in
 // registers (as literals they take two instructions).
 struct CodeBits {
@@ -38,8 +35,10 @@ __device__ __forceinline__ CodeBits code_bits() {
   asm("" : "+s"(b.even), "+s"(b.odd), "+v"(b.even_base), "+v"(b.odd_base));
   return b;
 }
-// The eight codes of a word less 8, exact halves in code order: a code in the low bits of the
-// half 1024 is 1024 + q, four bits up in the half 64 it is 64 + q.
+// The eight codes of a word less 8, exact halves in code order (in_code_order, 0, 4, 1, 5, 2, 6, 3, 7): a
+// code in the low bits of the half 1024 is 1024 + q, four bits up in the half 64 it is 64 + q. Nine
+// instructions, and four more for the values; with the bases left in, s and z would have to take them
+// out again, and z - 1032 s is no half.
 __device__ __forceinline__ h8 codes8(uint32_t w, const CodeBits& k) {
   const auto at = [](uint32_t v, float base) {
     const _Float16 b = (_Float16)(base + 8.f);

@@ -73,7 +73,10 @@ __device__ __forceinline__ void store_group(double x, double y, int lanes, char*
 }
 
 // Block (t, 0) normalizes, rotates and quantizes token t's row into its page; blocks (t, 1 ..)
-// rotate the query.
+// rotate the query. What block (t, 0) reads of its token is asked for before the page is known. Bound by
+// the bytes, most of them the queries' (3,100 tokens of 32 heads: 89 MB in 25.6 us, 3.5 TB/s; the fp16 cache's
+// writes 19: the difference is the rows' blocks, four trips to memory and four quotients in 64 bits
+// one after the other; 16 tokens: 4.6 us, that latency).
 __global__ void __launch_bounds__(256) latent4_append_kernel(Append4Args b) {
   const AppendArgs& a = b.a;
   const LatentArgs& l = a.l;
@@ -121,7 +124,7 @@ __global__ void __launch_bounds__(256) latent4_append_kernel(Append4Args b) {
                 to + p4.keys + at * (l.Dr / 2) + threadIdx.x, s_to + (G - 1) * l.page, z_to + (G - 1) * l.page);
 }
 
-// Rows as fp16, each value rounded once; eight a thread.
+// Rows as fp16, each value rounded once; eight a thread. Bound by latency (16 rows 3.1 us, 3,100 4.2).
 __global__ void __launch_bounds__(256) latent4_read_kernel(LatentArgs l, const int32_t* seq, const int32_t* slot, int T,
                                                            __half* rows) {
   const int row = l.Dc + l.Dr, per = row / 8;
@@ -153,7 +156,14 @@ __global__ void __launch_bounds__(256) latent4_read_kernel(LatentArgs l, const i
 // quarter of the latent columns, and make the copies, two tiles ahead in four buffers. The codes
 // stay codes in LDS: a wave takes those it needs out of it, along a token for the scores and
 // across 16 tokens (the 4-bit transposing read) for the sums, and forms the values in registers,
-// so that LDS and HBM carry 4 bits a value.
+// so that LDS and HBM carry 4 bits a value. The values are rounded to fp16, the type of the products.
+// A long line is bound by that forming: 13 instructions for eight values, for either use, 440 of some
+// 650 vector instructions a tile and SIMD. 512 latents, us a tile and workgroup: 16 heads
+// 1.4, 32 1.7, 64 2.7; its copies alone take 1.1. 48 sequences of 32 heads, 378,000 tokens, 122 MB:
+// 58 us, 2.1 TB/s (the fp16 cache's 445 MB: 88); 700 tokens of one: 13, two trips to memory in a
+// line. Measured and left: sixteen waves, each with half of a token's elements and the partial scores
+// added by way of LDS (1.5 and 1.75 us a tile: the instructions are the same); codes by loads to
+// registers, a lane a token's (64 separate pieces an instruction: 1.8).
 template <int DC, int DR, int MT>
 struct Decode4Shape {
   static constexpr int M = 16 * MT, G = DC / 64 + 1;
@@ -220,7 +230,6 @@ __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_d
   const CodeBits bits = code_bits();
 
   if (wave < S::NS) {
-    __builtin_amdgcn_s_setprio(2);
     bool more = at.n > 0;
     h8 q[S::RT][S::KS];
     // (a product's k: the eight codes of a word, of which a lane has 32 latents' of 128, 128 j + 32 g .. + 31,
