@@ -91,7 +91,8 @@ def test_prefill_refusals(B):
     for sums in (False, True):
         need = B.latent4_prefill_workspace_bytes(_spec(B), 20, 2, 50, sums)
         assert need > 0 and call(wb=need - 1, sums=P[9] if sums else None) == B.MOE_ENOMEM
-    assert B.latent4_prefill_workspace_bytes(_spec(B), 20, 2, 50) == B.latent_prefill_workspace_bytes(_spec(B), 2, 50)
+    rows = -(-50 * (_spec(B).d_latent + _spec(B).d_rope) * 2 // 256) * 256  # the context's rows as fp16
+    assert B.latent4_prefill_workspace_bytes(_spec(B), 20, 2, 50) == B.latent_prefill_workspace_bytes(_spec(B), 2, 50) + rows
 
 
 def test_evict_refusals(B):
