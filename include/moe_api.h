@@ -480,7 +480,8 @@ size_t moe_latent4_page_bytes(const moe_latent_spec* spec);
  * gamma, rot(k_r)) is quantized by groups,
  *   s = fp16((hi - lo) / 15), z = fp16(lo + 8 s), q = clamp(rint((v - z) / s) + 8, 0, 15)
  * with lo and hi the group's smallest and largest value (s = 0: the quotient is that by
- * 1, and the value z whatever q is), all of it formed in 64 bits from the fp32 inputs. A group with a value that is not finite, or whose s or z is
+ * 1, and the value z whatever q is), all of it formed in 64 bits from the fp32 inputs, s and
+ * z rounded to fp16 by way of fp32. A group with a value that is not finite, or whose s or z is
  * beyond fp16, is NaN throughout.
  * slot: device int32 [T], the token's place in its sequence; pos its position, which gives the
  * angles. They are the same until tokens of the sequence are evicted. No two tokens of a call

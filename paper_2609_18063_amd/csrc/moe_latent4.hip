@@ -54,9 +54,15 @@ __device__ __forceinline__ void store_group(double x, double y, int lanes, char*
   const double lo = over_lanes(lower(x, y), lanes, lower), hi = over_lanes(upper(x, y), lanes, upper);
   const int first = threadIdx.x & 63 & -lanes;
   const bool odd = __ballot(!isfinite(x) || !isfinite(y)) >> first & ((1ull << lanes) - 1);
-  __half s = __float2half_rn((float)((hi - lo) / 15.0));
+  // (rounded by way of fp32, as defined: the compiler would make one rounding of the two)
+  auto half = [](double v) {
+    float f = (float)v;
+    asm("" : "+v"(f));
+    return __float2half_rn(f);
+  };
+  __half s = half((hi - lo) / 15.0);
   const double step = (double)__half2float(s);
-  __half z = __float2half_rn((float)(lo + 8.0 * step));
+  __half z = half(lo + 8.0 * step);
   // (a value that is not finite, or beyond fp16, makes NaN of its group)
   if (odd || !isfinite(__half2float(s)) || !isfinite(__half2float(z))) s = z = __ushort_as_half(0x7E00);
   const double base = (double)__half2float(z), div = step == 0.0 ? 1.0 : step, inv = 1.0 / div;

@@ -183,6 +183,30 @@ def test_append_and_read(torch_cuda, H, dims, page, T):
         assert np.array_equal(qt.cpu().numpy()[keep], got[keep])
 
 
+def test_append_of_many_rows(torch_cuda):
+    """To the bit also where s or z, rounded to fp16 by way of fp32, is not what one rounding makes of it."""
+    torch, g = torch_cuda, np.random.default_rng(77)
+    Dc, Dr, Dn, Dv = S
+    T, page = 30000, 64
+    c = Cache4(torch, g, 1, *S, page, [1], spare=0)
+    raw = torch.zeros(-(-T // page), c.pages.shape[1], dtype=torch.uint8, device="cuda")
+    mem = A.Pages4(raw.shape[0], page, Dc, Dr)
+    table = c.i32(range(raw.shape[0]))[None]
+    kv = g.standard_normal((T, Dc + Dr)).astype(np.float32)
+    gamma, rope = np.ones(Dc, np.float16), np.zeros((T, Dr // 2, 2), np.float32)
+    rope[..., 0] = 1
+    place = np.arange(T)
+    c.B.latent4_append(c.spec, c.B.latent4_cache(c.spec, raw, table), torch.from_numpy(kv).cuda(), torch.from_numpy(gamma).cuda(),
+                       torch.from_numpy(rope).cuda(), c.i32([0] * T), c.i32(place), c.i32(place), c.status)
+    want = A.cache_row(kv, gamma, rope[..., 0].astype(np.float64), rope[..., 1].astype(np.float64))
+    codes, s, z = A.quantize_row(want, Dc)
+    lo, hi = want[:, :64].min(-1), want[:, :64].max(-1)
+    assert (((hi - lo) / 15).astype(np.float16) != s[:, 0]).any()
+    mem.raw[:] = 0
+    mem.put(place // page, place % page, codes, s, z)
+    assert np.array_equal(raw.cpu().numpy(), mem.raw) and int(c.status) == 0
+
+
 def test_append_values_that_are_not_finite(torch_cuda):
     """A NaN, an infinity, or a step or middle beyond fp16 makes NaN of its group (of all latents, where the norm sees
     it), and of no other row."""
