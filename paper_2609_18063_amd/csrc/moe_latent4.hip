@@ -163,8 +163,8 @@ __global__ void __launch_bounds__(256) latent4_read_kernel(LatentArgs l, const i
 // stay codes in LDS: a wave takes those it needs out of it, along a token for the scores and
 // across 16 tokens (the 4-bit transposing read) for the sums, and forms the values in registers,
 // so that LDS and HBM carry 4 bits a value. The values are rounded to fp16, the type of the products.
-// A long line is bound by that forming: 13 instructions for eight values, for either use, 440 of some
-// 650 vector instructions a tile and SIMD. 512 latents, us a tile and workgroup: 16 heads
+// A long line is bound by that forming: 13 instructions for eight values, for either use, 440 of the
+// 550 vector instructions a tile and SIMD, beside 68 products. 512 latents, us a tile and workgroup: 16 heads
 // 1.4, 32 1.7, 64 2.7; its copies alone take 1.1. 48 sequences of 32 heads, 378,000 tokens, 122 MB:
 // 58 us, 2.1 TB/s (the fp16 cache's 445 MB: 88); 700 tokens of one: 13, two trips to memory in a
 // line. Measured and left: sixteen waves, each with half of a token's elements and the partial scores
