@@ -97,7 +97,7 @@ struct PrefillArgs {
   float *part_o, *part_ml;       // [kPartGroups][kPartRows][Dv] and [..][2], with parts > 1
   uint32_t* lost;                // per 64-token tile: its 16-token groups without a page
   __half* rows;                  // [kv_total][Dc + Dr], of a 4-bit cache (moe_latent4.h), or null
-  float* row_ml;                 // [T][H][2]: a row's reference and 1 / sum, or null
+  float* row_ml;                 // [H][T][2]: a row's reference and 1 / sum, or null
   float* part_sums;              // [H][kv_total]: a head's weights of each token over the rows, with row_ml
   float* sums;                   // [B][sums_stride], the first sums_len used; with row_ml
   int64_t sums_stride;

@@ -475,7 +475,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) latent_prefill_kernel(PrefillA
     }
     const float inv = total > 0.f ? 1.f / total : total != total ? total : 0.f;  // (no token: zeros)
     if (a.row_ml && g == 0)
-      *reinterpret_cast<float2*>(a.row_ml + 2 * ((size_t)(qs.first + row) * l.H + h)) =
+      *reinterpret_cast<float2*>(a.row_ml + 2 * ((size_t)h * a.T + qs.first + row)) =
           float2{m[r] == -INFINITY ? INFINITY : ref[r], inv};
     __half* to = l.out + ((size_t)(qs.first + row) * l.H + h) * DV + 4 * g;
 #pragma unroll
@@ -518,7 +518,7 @@ __global__ void __launch_bounds__(256) latent_parts_kernel(PrefillArgs a) {
   }
   const float inv = sum > 0.f ? 1.f / sum : sum != sum ? sum : 0.f;
   if (a.row_ml && col == 0)
-    *reinterpret_cast<float2*>(a.row_ml + 2 * ((size_t)(qs.first + row) * l.H + h)) = float2{top == -INFINITY ? INFINITY : top, inv};
+    *reinterpret_cast<float2*>(a.row_ml + 2 * ((size_t)h * a.T + qs.first + row)) = float2{top == -INFINITY ? INFINITY : top, inv};
   const h4 v = {(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
   *reinterpret_cast<h4*>(l.out + ((size_t)(qs.first + row) * l.H + h) * l.Dv + col) = v;
 }
@@ -526,27 +526,27 @@ __global__ void __launch_bounds__(256) latent_parts_kernel(PrefillArgs a) {
 // ---- the tokens' weights ------------------------------------------------------------
 // sums[b][j] += sum over rows and heads of softmax(j), once the rows' references and sums are
 // known: the scores again. A workgroup takes one head's 128 tokens by all query rows that see them,
-// 32 a step: a wave 64 tokens, whose keys it has in registers, by 16 of the rows, which come
-// through LDS in three slots, copied two steps ahead (read by each wave for itself, 16
-// rows of 64 bytes an instruction, the rows bound it: 1,555 query rows on 4,200 tokens by 16 heads
-// 50 us, now 37, of which the keys' reads, of that kind too, take 5 a workgroup). The two waves' sums
-// are added up in order; a second launch adds up the heads, in order.
+// 32 a step: a wave 32 tokens, whose keys it has in registers, by 16 of the rows, which come
+// through LDS in three slots, copied two steps ahead. 1,555 query rows on 4,190 tokens by 16 heads: 36 us
+// (rows read by each wave for itself, 16 pieces of 64 bytes an instruction: 50; without the copies 30,
+// without the barriers too 28, which the exponentials and sums bound, and the longest context). The two
+// waves' sums are added up in order; a second launch adds up the heads, in order.
 constexpr int kSumTile = 128, kSumRows = 32;
 
 template <int DN, int DR>
-__global__ void __launch_bounds__(256, 2) latent_prefill_sums_kernel(PrefillArgs a) {
-  constexpr int KS = (DN + DR) / 32, PR = (DN + DR) / 8, SLOT = kSumRows * PR * 16, CN = SLOT / 1024, CW = (CN + 3) / 4;
+__global__ void __launch_bounds__(512, 4) latent_prefill_sums_kernel(PrefillArgs a) {
+  constexpr int KS = (DN + DR) / 32, PR = (DN + DR) / 8, SLOT = kSumRows * PR * 16, CN = SLOT / 1024, CW = (CN + 7) / 8;
   __shared__ __attribute__((aligned(16))) char rows[3 * SLOT];
   __shared__ __attribute__((aligned(16))) char mls[3][kSumRows * 8];
   __shared__ float other[kSumTile];
   const LatentArgs& l = a.l;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int h = blockIdx.x % l.H, t = blockIdx.x / l.H, half = wave / 2;
+  const int h = blockIdx.x % l.H, t = blockIdx.x / l.H, half = wave / 4;
   // (tiles of all sequences one behind the other, with gaps, as the 64-token tiles are)
   auto base = [&](int k) { return min(max(a.kv_start[k], 0), a.kv_total) / kSumTile + k; };
   const int b = last_at_most(a.B, t, base);
   const Span qs = span_of(a.q_start, b, a.T), ks = context_of(a, b);
-  const int tile0 = (t - base(b)) * kSumTile, tok0 = tile0 + kTile * (wave & 1);
+  const int tile0 = (t - base(b)) * kSumTile, tok0 = tile0 + 32 * (wave & 3);
   if (tile0 < 0 || tile0 >= ks.len) return;
   const int shift = ks.len - qs.len;                     // position of query row 0
   const int first = max(0, tile0 - shift) & ~15;         // the first row that may see a token
@@ -563,22 +563,23 @@ __global__ void __launch_bounds__(256, 2) latent_prefill_sums_kernel(PrefillArgs
       const size_t at = (size_t)(qs.first + min(first + kSumRows * u + r, qs.len - 1)) * l.H + h;
       dma16(reinterpret_cast<const char*>(l.q + at * (DN + DR)) + 16 * place(r, p % PR), at0 + u % 3 * SLOT + 1024 * piece);
     }
-    const size_t at = (size_t)(qs.first + min(first + kSumRows * u + lane / 2, qs.len - 1)) * l.H + h;
+    const size_t at = (size_t)h * a.T + qs.first + min(first + kSumRows * u + lane / 2, qs.len - 1);
     dma4(a.row_ml + 2 * at + lane % 2, lds_at(mls[u % 3]));  // (every wave the same)
   };
-  f4 w[4] = {};
+  f4 w[2] = {};
   if (first < qs.len) {
-    h8 k[4][KS];
+    copy(0);
+    copy(1);
+    h8 k[2][KS];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
       const size_t at = ks.first + min(tok0 + 16 * i + c, ks.len - 1);
 #pragma unroll
       for (int n = 0; n < KS; ++n)
         k[i][n] = n < DN / 32 ? ld_h8(a.k + ((size_t)h * a.kv_total + at) * DN + 32 * n + 8 * g)
                               : ld_h8(a.kr + at * DR + 32 * (n - DN / 32) + 8 * g);
     }
-    copy(0);
-    copy(1);
+    vm_drain();
     const int n = (qs.len - first + kSumRows - 1) / kSumRows;
     for (int u = 0; u < n; ++u) {
       vm_wait<CW + 1>();                                 // (all but the copies of step u + 1)
@@ -586,12 +587,12 @@ __global__ void __launch_bounds__(256, 2) latent_prefill_sums_kernel(PrefillArgs
       copy(u + 2);
       const int row0 = first + kSumRows * u + 16 * half;
       if (row0 >= qs.len || row0 + 15 + shift < tok0) continue;
-      f4 s[4] = {};
+      f4 s[2] = {};
 #pragma unroll
       for (int n = 0; n < KS; ++n) {
         const h8 q = ld_h8(rows + u % 3 * SLOT + ((16 * half + c) * PR + place(16 * half + c, 4 * n + g)) * 16);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = mfma16(k[i][n], q, s[i]);
+        for (int i = 0; i < 2; ++i) s[i] = mfma16(k[i][n], q, s[i]);
       }
       const float2 ml = *reinterpret_cast<const float2*>(mls[u % 3] + 8 * (16 * half + c));
       const bool in = row0 + c < qs.len;
@@ -599,38 +600,38 @@ __global__ void __launch_bounds__(256, 2) latent_prefill_sums_kernel(PrefillArgs
       // (a token behind a row takes nothing of it, NaN neither)
       auto add = [&](auto edge) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float v = __builtin_amdgcn_exp2f(fmaf(s[i][e], unit, -ref)) * inv;
             w[i][e] += edge && tok0 + 16 * i + 4 * g + e > shift + row0 + c ? 0.f : v;
           }
       };
-      if (tok0 + kTile - 1 > shift + row0)
+      if (tok0 + 31 > shift + row0)
         add(std::true_type{});
       else
         add(std::false_type{});
     }
     vm_wait<0>();                                        // (copies may be in flight into this workgroup's LDS)
   }
-  const uint32_t lost = tok0 < ks.len ? a.lost[tile_base(a, b) + tok0 / kTile] : 0;
+  const uint32_t lost = tok0 < ks.len ? a.lost[tile_base(a, b) + tok0 / kTile] >> (tok0 / 16 % 4) : 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[i][e] = row16_sum(w[i][e]);
   if (half == 1 && c == 0)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<f4*>(other + kTile * (wave & 1) + 16 * i + 4 * g) = w[i];
+    for (int i = 0; i < 2; ++i) *reinterpret_cast<f4*>(other + 32 * (wave & 3) + 16 * i + 4 * g) = w[i];
   __syncthreads();
   if (half == 0 && c == 0)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int tok = tok0 + 16 * i + 4 * g + e;
         if (tok < ks.len)
           a.part_sums[(size_t)h * a.kv_total + ks.first + tok] =
-              lost >> i & 1 ? 0.f : w[i][e] + other[kTile * (wave & 1) + 16 * i + 4 * g + e];
+              lost >> i & 1 ? 0.f : w[i][e] + other[32 * (wave & 3) + 16 * i + 4 * g + e];
       }
 }
 
@@ -648,7 +649,7 @@ __global__ void __launch_bounds__(256) latent_sums_join_kernel(PrefillArgs a) {
 
 template <int DN, int DR>
 hipError_t launch_sums(const PrefillArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((latent_prefill_sums_kernel<DN, DR>), dim3((unsigned)(a.kv_total / kSumTile + a.B) * a.l.H), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((latent_prefill_sums_kernel<DN, DR>), dim3((unsigned)(a.kv_total / kSumTile + a.B) * a.l.H), dim3(512), 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(latent_sums_join_kernel, dim3((a.kv_total + 255) / 256), dim3(256), 0, st, a);
