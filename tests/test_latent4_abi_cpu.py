@@ -139,3 +139,14 @@ def test_oracle_rows():
 def test_oracle_evicts():
     assert A.evict(np.array([5, 1, 1, 9, 1, 2.0]), 6, 4, 1, 1) == [0, 1, 3, 5]
     assert A.evict(np.array([0, np.nan, 1.0]), 3, 1, 0, 0) == [2] and A.evict(np.array([1.0, 2]), 2, 3, 1, 1) == [0, 1]
+
+
+@pytest.mark.parametrize("H", [1, 17, 33, 64, 65, 128])
+@pytest.mark.parametrize("dims", [(128, 32), (256, 64), (512, 64)])
+def test_a_larger_calls_workspace_does_for_a_smaller_one(B, H, dims):
+    """A serving loop keeps one for its largest batch and longest context."""
+    spec = B.make_latent_spec(H, *dims, 64, 64, 64, 0.1)
+    for sums in (False, True):
+        v = [(b, n, B.latent4_decode_workspace_bytes(spec, b, n, sums))
+             for b in (1, 2, 9, 64, 300, 5000) for n in (0, 1, 65, 769, 5000, 12000, 16384, 50000, 400000, 1 << 20)]
+        assert all(y <= x for b, n, x in v for b2, n2, y in v if b2 <= b and n2 <= n)
