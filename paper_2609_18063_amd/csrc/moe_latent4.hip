@@ -749,7 +749,9 @@ DecodePlan decode4_plan(int H, int Dc, int Dr, int B, int max_len, bool sums, si
   p.rows = H <= 16 ? 16 : H <= 32 || (long long)B * ((H + 63) / 64) * tiles_host(max_len) < 12 * wgs ? 32 : 64;
   p.head_blocks = (H + p.rows - 1) / p.rows;
   p.least = std::max(1, (int)(0.18 * std::sqrt((double)tiles_host(max_len)) + 0.5));
-  const long long tiles = (long long)B * p.head_blocks * tiles_host(max_len);
+  // (so many workgroups, up to one a CU, that a short line's tiles have one each: 2 sequences of 700 tokens, the
+  // call 24.8 us, with a workgroup a tile, of which the items' places leave some empty, 26.2)
+  const long long tiles = (long long)B * p.head_blocks * (tiles_host(max_len) + kItemCost);
   p.wgs = (int)std::min<long long>(wgs, (std::max<long long>(tiles, 1) + 7) / 8 * 8);
   const size_t rows = (size_t)B * H, parts = (size_t)p.wgs + (size_t)B * p.head_blocks;
   size_t off = 0;
