@@ -140,9 +140,9 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(SelectArgs
   }
   __syncthreads();
   // In order, four tokens a thread: a token that stays goes behind those that do before it
-  // (never past its own place, so that the sums may move within one array: a round's are
+  // (never past its own place, so that the sums may move within one array: a step's are
   // all read before the first is written).
-  int above = 0, equal = 0;                                      // tokens that stay for sure, and ties, before this round
+  int above = 0, equal = 0;                                      // tokens that stay for sure, and ties, before these
   auto round = [&](int i0, const float (&v)[kEach]) {
     const int i = i0 + kEach * tid;
     uint32_t mine = 0;                                           // of this thread: ties << 16 | sure ones

@@ -23,84 +23,102 @@ struct Append4Args {
   char* pages;
 };
 
-// op over 16, 32 or 64 lanes, by lane moves (a trip through LDS for each of a double's halves
-// costs more than the sums); every lane has the result.
+// op over 8 or 64 lanes, by lane moves (a trip through LDS for each of a double's halves costs
+// more than the sums); every lane has the result.
 template <int CTRL>
 __device__ __forceinline__ double dpp_d(double v) {
   return __hiloint2double(dpp_i<CTRL>(0, __double2hiint(v)), dpp_i<CTRL>(0, __double2loint(v)));
 }
-template <typename Op>
-__device__ __forceinline__ double over_lanes(double v, int lanes, Op op) {
+template <int LANES, typename Op>
+__device__ __forceinline__ double over_lanes(double v, Op op) {
   v = op(v, dpp_d<0xB1>(v));
   v = op(v, dpp_d<0x4E>(v));
   v = op(v, dpp_d<0x141>(v));
-  v = op(v, dpp_d<0x140>(v));
-  auto both = [&](auto lo, auto hi) { return op(__hiloint2double(hi[0], lo[0]), __hiloint2double(hi[1], lo[1])); };
-  if (lanes > 16) {
-    const uint32_t lo = __double2loint(v), hi = __double2hiint(v);
+  if constexpr (LANES == 64) {
+    auto both = [&](auto lo, auto hi) { return op(__hiloint2double(hi[0], lo[0]), __hiloint2double(hi[1], lo[1])); };
+    v = op(v, dpp_d<0x140>(v));
+    uint32_t lo = __double2loint(v), hi = __double2hiint(v);
     v = both(__builtin_amdgcn_permlane16_swap(lo, lo, false, false), __builtin_amdgcn_permlane16_swap(hi, hi, false, false));
-  }
-  if (lanes > 32) {
-    const uint32_t lo = __double2loint(v), hi = __double2hiint(v);
+    lo = __double2loint(v), hi = __double2hiint(v);
     v = both(__builtin_amdgcn_permlane32_swap(lo, lo, false, false), __builtin_amdgcn_permlane32_swap(hi, hi, false, false));
   }
   return v;
 }
 
-// Two neighbouring values of a group a thread, `lanes` (16 or 32) threads a group.
-__device__ __forceinline__ void store_group(double x, double y, int lanes, char* code, __half* s_at, __half* z_at) {
+// Eight neighbouring values of a group a lane, eight lanes a group; the codes of the lane's.
+__device__ __forceinline__ uint32_t group_codes(const double (&v)[8], __half& s, __half& z) {
   auto lower = [](double v, double o) { return o < v ? o : v; };
   auto upper = [](double v, double o) { return o > v ? o : v; };
-  const double lo = over_lanes(lower(x, y), lanes, lower), hi = over_lanes(upper(x, y), lanes, upper);
-  const int first = threadIdx.x & 63 & -lanes;
-  const bool odd = __ballot(!isfinite(x) || !isfinite(y)) >> first & ((1ull << lanes) - 1);
+  double lo = v[0], hi = v[0];
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    lo = lower(lo, v[i]);
+    hi = upper(hi, v[i]);
+    odd = odd || !isfinite(v[i]);
+  }
+  lo = over_lanes<8>(lo, lower);
+  hi = over_lanes<8>(hi, upper);
+  odd = __ballot(odd) >> (threadIdx.x & 56) & 0xFF;
   // (rounded by way of fp32, as defined: the compiler would make one rounding of the two)
   auto half = [](double v) {
     float f = (float)v;
     asm("" : "+v"(f));
     return __float2half_rn(f);
   };
-  __half s = half((hi - lo) / 15.0);
+  s = half((hi - lo) / 15.0);
   const double step = (double)__half2float(s);
-  __half z = half(lo + 8.0 * step);
+  z = half(lo + 8.0 * step);
   // (a value that is not finite, or beyond fp16, makes NaN of its group)
   if (odd || !isfinite(__half2float(s)) || !isfinite(__half2float(z))) s = z = __ushort_as_half(0x7E00);
   const double base = (double)__half2float(z), div = step == 0.0 ? 1.0 : step, inv = 1.0 / div;
-  auto q = [&](double v) {
-    double n = (v - base) * inv;
-    if (fabs(fabs(n - rint(n)) - 0.5) < 1e-9) n = (v - base) / div;  // (beside a border: as defined)
-    return (int)fmin(fmax(rint(n) + 8.0, 0.0), 15.0);
-  };
-  *code = (char)(q(x) | q(y) << 4);
-  if ((threadIdx.x & (lanes - 1)) == 0) {
-    *s_at = s;
-    *z_at = z;
+  uint32_t codes = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    double n = (v[i] - base) * inv, r = rint(n);
+    if (fabs(fabs(n - r) - 0.5) < 1e-9) r = rint((v[i] - base) / div);  // (beside a border: as defined)
+    codes |= (uint32_t)(int)fmin(fmax(r + 8.0, 0.0), 15.0) << 4 * i;
   }
+  return codes;
 }
 
-// Block (t, 0) normalizes, rotates and quantizes token t's row into its page; blocks (t, 1 ..)
-// rotate the query. What block (t, 0) reads of its token is asked for before the page is known. Bound by
-// the bytes, most of them the queries' (3,100 tokens of 32 heads: 89 MB in 25.6 us, 3.5 TB/s; the fp16 cache's
-// writes 19: the difference is the rows' blocks, four trips to memory and four quotients in 64 bits
-// one after the other; 16 tokens: 4.6 us, that latency).
+// Blocks (., 0) normalize, rotate and quantize rows into their pages, a wave a token's: of its groups
+// eight lanes one, eight values a lane (with two a thread, 256 threads a token, the reductions and
+// quotients were four times as many: 3,100 tokens in 24.0 us). Blocks (t, 1 ..) rotate token t's query. What
+// a row's wave reads is asked for before the page is known. Bound by the bytes, most of them the queries'
+// (3,100 tokens of 32 heads: 89 MB in 21.5 us, 4.1 TB/s; 16 tokens: 4.8 us, latency and the 64-bit quotients).
 __global__ void __launch_bounds__(256) latent4_append_kernel(Append4Args b) {
   const AppendArgs& a = b.a;
   const LatentArgs& l = a.l;
-  const int t = blockIdx.x, seq = a.seq[t], pos = a.pos[t], slot = b.slot[t], e = 2 * threadIdx.x;
+  const int lane = threadIdx.x & 63, t = blockIdx.y ? blockIdx.x : blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (t >= a.T) return;
+  const int seq = a.seq[t], pos = a.pos[t], slot = b.slot[t];
+  const int G = l.Dc / 64 + 1, grp = lane >> 3, e = 8 * lane;
   const float* kv = a.kv + (size_t)t * (l.Dc + l.Dr);
-  float2 v = {0.f, 0.f}, x = {0.f, 0.f}, gm = {0.f, 0.f}; // two of Dc <= 512 a thread
-  if (blockIdx.y == 0 && e < l.Dc) {
-    v = *reinterpret_cast<const float2*>(kv + e);
-    gm = __half22float2(*reinterpret_cast<const __half2*>(a.gamma + e));
+  float x[8] = {}, y[8] = {};                            // of a latent group, or the key's
+  h8 gm = {};
+  const int key = 8 * (lane & 7) & (l.Dr - 1);           // (32 values: lanes 4 .. 7 have them again)
+  if (blockIdx.y == 0) {
+    auto read = [](float (&to)[8], const float* from) {
+      const f4 p = *reinterpret_cast<const f4*>(from), q = *reinterpret_cast<const f4*>(from + 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        to[i] = p[i];
+        to[4 + i] = q[i];
+      }
+    };
+    if (e < l.Dc) {
+      read(x, kv + e);
+      gm = ld_h8(a.gamma + e);
+    }
+    read(y, kv + l.Dc + key);
   }
-  if (blockIdx.y == 0 && e < l.Dr) x = *reinterpret_cast<const float2*>(kv + l.Dc + e);
   if (seq < 0) return;                                   // a padding row
   int32_t page = -1;
   const bool in = seq < l.n_seqs && pos >= 0 && pos < a.max_pos && slot >= 0 && slot / l.page < l.max_pages;
   if (in) page = l.table[seq * l.table_stride + slot / l.page];
   if (page < 0 || page >= l.n_pages) {
-    if (blockIdx.y == 0 && threadIdx.x == 0 && l.status)
-      atomicOr(l.status, in ? MOE_STATUS_BAD_PAGE : MOE_STATUS_BAD_INDEX);
+    if (blockIdx.y == 0 && lane == 0 && l.status) atomicOr(l.status, in ? MOE_STATUS_BAD_PAGE : MOE_STATUS_BAD_INDEX);
     return;
   }
   const float2* cs = reinterpret_cast<const float2*>(a.rope) + (size_t)pos * (l.Dr / 2);
@@ -108,26 +126,46 @@ __global__ void __launch_bounds__(256) latent4_append_kernel(Append4Args b) {
     rotate_query(a, t, blockIdx.y - 1, cs);
     return;
   }
-  __shared__ double red[4];
   const Page4 p4 = page4(l.Dc, l.Dr, l.page);
   char* to = b.pages + (size_t)page * p4.bytes;
-  const int at = slot & (l.page - 1), G = l.Dc / 64 + 1;
+  const int at = slot & (l.page - 1);
   __half* s_to = reinterpret_cast<__half*>(to + p4.steps) + at;
-  __half* z_to = s_to + (size_t)G * l.page;
-  float2 r = {0.f, 0.f};
-  if (e < l.Dr) r = cs[threadIdx.x];
-  const double s = over_lanes((double)v.x * v.x + (double)v.y * v.y, 64, [](double p, double q) { return p + q; });
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
-  __syncthreads();
-  const double inv = 1.0 / sqrt((red[0] + red[1] + red[2] + red[3]) / (double)l.Dc + 1e-6);
-  if (e < l.Dc) {
-    const int grp = threadIdx.x >> 5;
-    store_group(v.x * inv * gm.x, v.y * inv * gm.y, 32, to + at * (l.Dc / 2) + threadIdx.x, s_to + grp * l.page,
-                z_to + grp * l.page);
+  float2 r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = cs[key / 2 + i];
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sum += (double)x[i] * x[i];
+  sum = over_lanes<64>(sum, [](double p, double q) { return p + q; });
+  const double inv = 1.0 / sqrt(sum / (double)l.Dc + 1e-6);
+  double v[8];
+  auto store = [&](int group, bool holds) {
+    __half s, z;
+    const uint32_t codes = group_codes(v, s, z);
+    if (!holds) return;
+    *reinterpret_cast<uint32_t*>(group < G - 1 ? to + at * (l.Dc / 2) + e / 2 : to + p4.keys + at * (l.Dr / 2) + key / 2) = codes;
+    if ((lane & 7) == 0) {
+      s_to[group * l.page] = s;
+      s_to[(G + group) * l.page] = z;
+    }
+  };
+  auto turned = [&]() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = (double)y[2 * i] * r[i].x - (double)y[2 * i + 1] * r[i].y;
+      v[2 * i + 1] = (double)y[2 * i] * r[i].y + (double)y[2 * i + 1] * r[i].x;
+    }
+  };
+  // (up to 256 latents the key's lanes are the ones behind the latents', else the first ones again)
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = x[i] * inv * (double)gm[i];
+  const bool keyed = 8 * (lane & 7) < l.Dr;
+  if (grp == G - 1) turned();
+  store(min(grp, G - 1), grp < G - 1 || (grp == G - 1 && keyed));
+  if (G - 1 >= 8) {
+    turned();
+    store(G - 1, grp == 0 && keyed);
   }
-  if (e < l.Dr)
-    store_group((double)x.x * r.x - (double)x.y * r.y, (double)x.x * r.y + (double)x.y * r.x, l.Dr / 2,
-                to + p4.keys + at * (l.Dr / 2) + threadIdx.x, s_to + (G - 1) * l.page, z_to + (G - 1) * l.page);
 }
 
 // Rows as fp16, each value rounded once; eight a thread. Bound by latency (16 rows 3.1 us, 3,100 4.2).
@@ -166,7 +204,7 @@ __global__ void __launch_bounds__(256) latent4_read_kernel(LatentArgs l, const i
 // A long line is bound by that forming: 13 instructions for eight values, for either use, 440 of the
 // 550 vector instructions a tile and SIMD, beside 68 products. 512 latents, us a tile and workgroup: 16 heads
 // 1.4, 32 1.7, 64 2.7; its copies alone take 1.1. 48 sequences of 32 heads, 378,000 tokens, 122 MB:
-// 58 us, 2.1 TB/s (the fp16 cache's 445 MB: 88); 700 tokens of one: 13, two trips to memory in a
+// 58 us, 2.1 TB/s (the fp16 cache's 445 MB: 88); 700 tokens of one: 12, three trips to memory in a
 // line. Measured and left: sixteen waves, each with half of a token's elements and the partial scores
 // added by way of LDS (1.5 and 1.75 us a tile: the instructions are the same); codes by loads to
 // registers, a lane a token's (64 separate pieces an instruction: 1.8).
