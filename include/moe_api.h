@@ -520,7 +520,8 @@ int moe_latent4_decode(const moe_latent_spec* spec, const moe_latent_cache* cach
 /*
  * As moe_latent_prefill, over a 4-bit cache. sums: as of moe_latent4_decode, over all rows of a
  * sequence's chunk and all heads; a row has room for sums_len tokens (1 .. sums_stride),
- * and those beyond get none. `sums` of the workspace size: whether the call has them; it grows
+ * and those beyond get none. (Rows of a chunk longer than max_q that no output is formed of add
+ * nothing.) `sums` of the workspace size: whether the call has them; it grows
  * with T too then.
  */
 size_t moe_latent4_prefill_workspace_bytes(const moe_latent_spec* spec, int T, int B, int kv_total, int sums);

@@ -550,6 +550,8 @@ __global__ void __launch_bounds__(512, 4) latent_prefill_sums_kernel(PrefillArgs
   if (tile0 < 0 || tile0 >= ks.len) return;
   const int shift = ks.len - qs.len;                     // position of query row 0
   const int first = max(0, tile0 - shift) & ~15;         // the first row that may see a token
+  // (of a chunk longer than max_q the attention forms no more rows, and notes no reference, than these)
+  const int end = min(qs.len, (a.max_q + kRows - 1) / kRows * kRows);
   const float unit = l.scale * kLog2e;
   const uint32_t at0 = lds_at(rows);
   // piece k of row r of a step is at (k ^ key) of its own part, nope or rope
@@ -560,14 +562,14 @@ __global__ void __launch_bounds__(512, 4) latent_prefill_sums_kernel(PrefillArgs
 #pragma unroll
     for (int j = 0; j < CW; ++j) {
       const int piece = min(CW * wave + j, CN - 1), p = 64 * piece + lane, r = p / PR;
-      const size_t at = (size_t)(qs.first + min(first + kSumRows * u + r, qs.len - 1)) * l.H + h;
+      const size_t at = (size_t)(qs.first + min(first + kSumRows * u + r, end - 1)) * l.H + h;
       dma16(reinterpret_cast<const char*>(l.q + at * (DN + DR)) + 16 * place(r, p % PR), at0 + u % 3 * SLOT + 1024 * piece);
     }
-    const size_t at = (size_t)h * a.T + qs.first + min(first + kSumRows * u + lane / 2, qs.len - 1);
+    const size_t at = (size_t)h * a.T + qs.first + min(first + kSumRows * u + lane / 2, end - 1);
     dma4(a.row_ml + 2 * at + lane % 2, lds_at(mls[u % 3]));  // (every wave the same)
   };
   f4 w[2] = {};
-  if (first < qs.len) {
+  if (first < end) {
     copy(0);
     copy(1);
     h8 k[2][KS];
@@ -580,13 +582,13 @@ __global__ void __launch_bounds__(512, 4) latent_prefill_sums_kernel(PrefillArgs
                               : ld_h8(a.kr + at * DR + 32 * (n - DN / 32) + 8 * g);
     }
     vm_drain();
-    const int n = (qs.len - first + kSumRows - 1) / kSumRows;
+    const int n = (end - first + kSumRows - 1) / kSumRows;
     for (int u = 0; u < n; ++u) {
       vm_wait<CW + 1>();                                 // (all but the copies of step u + 1)
       lds_barrier();
       copy(u + 2);
       const int row0 = first + kSumRows * u + 16 * half;
-      if (row0 >= qs.len || row0 + 15 + shift < tok0) continue;
+      if (row0 >= end || row0 + 15 + shift < tok0) continue;
       f4 s[2] = {};
 #pragma unroll
       for (int n = 0; n < KS; ++n) {
@@ -595,7 +597,7 @@ __global__ void __launch_bounds__(512, 4) latent_prefill_sums_kernel(PrefillArgs
         for (int i = 0; i < 2; ++i) s[i] = mfma16(k[i][n], q, s[i]);
       }
       const float2 ml = *reinterpret_cast<const float2*>(mls[u % 3] + 8 * (16 * half + c));
-      const bool in = row0 + c < qs.len;
+      const bool in = row0 + c < end;
       const float ref = in ? ml.x : INFINITY, inv = in ? ml.y : 0.f;
       // (a token behind a row takes nothing of it, NaN neither)
       auto add = [&](auto edge) {

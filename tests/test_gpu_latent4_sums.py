@@ -1,5 +1,5 @@
 """The 4-bit cache's sums of attention weights: what a call adds, token by token, in the norm and in total, over the forms
-that heads, rows and lengths select."""
+that heads, rows and lengths select; and rows that no output is formed of."""
 
 import numpy as np
 import pytest
@@ -89,4 +89,27 @@ def test_prefill_adds(torch_cuda, H, dims, page, lens, counts):
             _check(c, now, b, q[at:at + n], np.arange(lens[b] - n, lens[b]) + 1)
         else:
             assert not now[b].any()
+        at += n
+
+
+@pytest.mark.parametrize("counts,context,max_q,rows", [
+    ([300, 30], 200, 100, 256), ([700, 30], 0, 257, 512), ([30, 300], 90, 1, 256), ([300, 30], 3000, 100, 256)])
+def test_prefill_rows_beyond_the_longest_chunk(torch_cuda, counts, context, max_q, rows):
+    """A chunk longer than max_q, which the status tells: the rows that no output is formed of add nothing. (The workspace
+    is NaN before the call.)"""
+    torch, g = torch_cuda, np.random.default_rng(max_q)
+    lens = [n + context for n in counts]
+    c = Cache4(torch, g, 5, *S, 16, lens)
+    q = _queries(g, sum(counts), c)
+    sums = torch.zeros(2, max(lens), device="cuda")
+    got = c.prefill(q, counts, max_q=max_q, sums=sums)
+    assert int(c.status) == c.B.MOE_STATUS_BAD_LENGTH
+    now, at = sums.cpu().numpy(), 0
+    assert np.isfinite(now).all()
+    for b, n in enumerate(counts):
+        k = min(n, rows)
+        seen = np.arange(lens[b] - n, lens[b])[:k] + 1
+        c.check(got[at:at + k], q[at:at + k], b, c.rows[b], seen)
+        assert (got[at + k:at + n] == 7).all()
+        _check(c, now, b, q[at:at + k], seen)
         at += n
