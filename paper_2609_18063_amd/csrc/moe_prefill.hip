@@ -777,6 +777,8 @@ int prefill(bool four, const moe_latent_spec* spec, const moe_latent_cache* cach
   if (T == 0 || B == 0) return T == 0 ? MOE_OK : MOE_EINVAL;
   if (max_q < 1 || (int64_t)((max_q + moe::kPartRows - 1) / moe::kPartRows) * spec->heads * B * 512 > (int64_t)UINT32_MAX)
     return MOE_EINVAL;  // (a grid's threads)
+  if (sums && ((int64_t)kv_total / moe::kSumTile + B) * spec->heads * 512 > (int64_t)UINT32_MAX)
+    return MOE_EINVAL;  // (the sums' launch, before anything of the call is written)
   if (!w_kvb_f16 || !q_f16 || !q_start || !kv_start || !out_f16 || !workspace) return MOE_EINVAL;
   if (misaligned(w_kvb_f16, 16) || misaligned(q_f16, 16) || misaligned(q_start, 4) || misaligned(kv_start, 4) ||
       misaligned(out_f16, 16) || misaligned(sums, 4) || misaligned(status, 4) || misaligned(workspace, 16))
