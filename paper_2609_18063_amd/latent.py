@@ -201,12 +201,14 @@ class LatentAttention:
     def _ws(n):
         return torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
 
-    def _project(self, n, x, seq, pos, slot):
+    def _project(self, n, x, seq, pos, slot, seqs):
+        c = self.cache
+        if slot is None and any(gone and c.ids[s] is not None for s, gone in enumerate(c.evicted[:seqs])):
+            raise ValueError("behind an eviction a token's place is not its position: slot has to be given")
         b, T = self.blocks[n], x.shape[0]
         q, kv = self.qb[:T], self.kvb[:T]
         B.linear_int4(b.q, self.n_q, self.d, b.rank, b.lora_scale, x, q.view(T, -1), self.ws)
         B.linear_int4(b.kv, self.n_kv, self.d, b.rank, b.lora_scale, x, kv, self.ws)
-        c = self.cache
         if c.bits == 4:
             B.latent4_append(self.spec, c.layers[n], kv, b.gamma, self.rope, seq, pos if slot is None else slot, pos, c.status, q=q,
                              q_out=q)
@@ -227,8 +229,9 @@ class LatentAttention:
         """Layer ``n`` for one token of each of the first ``len(x)`` table rows: ``x`` fp16 ``[B, d]`` (the normed
         residual), ``r`` fp32 ``[B, d]`` in and out; ``seq``, ``pos`` and ``kv_len`` (the token among them) int32
         ``[B]`` on the GPU. ``max_len``: a bound on kv_len (the table's, if none). ``slot`` (4 bits): the tokens' places,
-        where they are not their positions. Capturable."""
-        q = self._project(n, x, seq, pos, slot)
+        needed where tokens of one of these rows were evicted, as positions are no places then. Capturable (a step captured
+        without ``slot`` is not for replays behind an eviction, which it cannot see)."""
+        q = self._project(n, x, seq, pos, slot, x.shape[0])
         c, most, o = self.cache, self.max_len if max_len is None else max_len, self.ob[:x.shape[0]]
         if c.bits == 4:
             B.latent4_decode(self.spec, c.layers[n], self.blocks[n].w_kvb, q, kv_len, most, o, c.status, self.ws_decode,
@@ -240,9 +243,9 @@ class LatentAttention:
     def prefill(self, n, x, r, seq, pos, q_start, kv_start, kv_total, max_q, slot=None):
         """Layer ``n`` for chunks of prompts: the ragged batch of ``moe_latent_prefill``, sequence b in table row b.
         Rows of padding behind the last sequence (``seq`` -1) keep their ``r``. Eager only: its workspace grows with
-        ``kv_total``, ``H (d_nope + d_v)`` halves a token, for one layer at a time."""
-        q = self._project(n, x, seq, pos, slot)
+        ``kv_total``, ``H (d_nope + d_v)`` halves a token, for one layer at a time. ``slot``: as of :meth:`decode`."""
         c, seqs = self.cache, q_start.numel() - 1
+        q = self._project(n, x, seq, pos, slot, seqs)
         if c.bits == 4:
             need = B.latent4_prefill_workspace_bytes(self.spec, x.shape[0], seqs, kv_total, sums=c.sums is not None)
         else:
