@@ -118,14 +118,18 @@ class LatentCache:
             return gone
         need = -(-budget // self.spec.page_tokens)
         ids = self.pool.alloc(need * len(todo))
-        at = torch.tensor(todo).cuda()
-        sums, table = self.sums[:, at], self.table[at]
-        to = torch.tensor(ids, dtype=torch.int32).view(len(todo), need).cuda()
-        keep = torch.empty(self.n_layers, len(todo), budget, dtype=torch.int32, device="cuda")
-        B.evict_select(sums, torch.tensor([self.tokens[s] for s in todo], dtype=torch.int32).cuda(), budget, sinks, recent, keep,
-                       sums, self.status)
-        B.latent4_move(self.spec, self.pages, table, keep, to, self.status)
-        self.sums[:, at] = sums
+        try:
+            at = torch.tensor(todo).cuda()
+            sums, table = self.sums[:, at], self.table[at]
+            to = torch.tensor(ids, dtype=torch.int32).view(len(todo), need).cuda()
+            keep = torch.empty(self.n_layers, len(todo), budget, dtype=torch.int32, device="cuda")
+            B.evict_select(sums, torch.tensor([self.tokens[s] for s in todo], dtype=torch.int32).cuda(), budget, sinks, recent, keep,
+                           sums, self.status)
+            B.latent4_move(self.spec, self.pages, table, keep, to, self.status)
+            self.sums[:, at] = sums
+        except BaseException:                              # (out of memory, a refused call: no sequence has these pages yet)
+            self.pool.free(ids)
+            raise
         for k, s in enumerate(todo):
             self.pool.free(self.ids[s])
             self.ids[s], self.tokens[s] = ids[k * need:(k + 1) * need], budget

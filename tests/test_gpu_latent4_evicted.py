@@ -1,4 +1,5 @@
-"""A 4-bit cache behind an eviction: calls that would take a token's position for its place."""
+"""A 4-bit cache behind an eviction: calls that would take a token's position for its place, and evictions that fail on
+their way."""
 
 import numpy as np
 import pytest
@@ -64,4 +65,34 @@ def test_positions_are_no_places_behind_an_eviction(torch_cuda):
     cache.grow(1, 31)
     both(2, False)
     assert int(cache.status) == 0
+    cache.close()
+
+
+@pytest.mark.parametrize("call", ["evict_select", "latent4_move"])
+def test_an_eviction_that_fails_gives_its_pages_back(torch_cuda, monkeypatch, call):
+    """Whatever ends it behind the allocation of the new pages: the pool, the sequences, their rows and sums are as before, and
+    the same eviction then runs."""
+    torch = torch_cuda
+    from paper_2609_18063_amd import binding as B, latent
+    cache = latent.LatentCache(_spec(16), 2, 20, 2, 128, bits=4, weights=True)
+    for n in (100, 50):
+        cache.grow(cache.start(), n)
+    cache.pages.random_(0, 256)
+    cache.sums.uniform_()
+    free, state = cache.pool.available(), [list(cache.ids), list(cache.tokens), list(cache.evicted)]
+    was = [cache.sums.clone(), cache.table.clone()]
+
+    def fail(*a, **kw):
+        raise torch.cuda.OutOfMemoryError("as if")
+
+    with monkeypatch.context() as m:
+        m.setattr(B, call, fail)
+        with pytest.raises(torch.cuda.OutOfMemoryError):
+            cache.evict(40)
+    assert cache.pool.available() == free and [cache.ids, cache.tokens, cache.evicted] == state
+    assert torch.equal(cache.sums, was[0]) and torch.equal(cache.table, was[1])
+    assert cache.evict(40) == [60, 10] and int(cache.status) == 0
+    for s in (0, 1):
+        cache.end(s)
+    assert cache.pool.available() == 20
     cache.close()
