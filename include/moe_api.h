@@ -503,7 +503,10 @@ int moe_latent4_read(const moe_latent_spec* spec, const moe_latent_cache* cache,
 
 /*
  * As moe_latent_decode, over a 4-bit cache and without a shared prefix (forks share pages
- * through their tables). The values are rounded to fp16, the type of the products.
+ * through their tables). The values are rounded to fp16, the type of the products: with the
+ * fp16 form's roundings outputs are off by 3.8 to 5.7e-4 of a row's norm over the same codes
+ * (the output's own rounding is 2.1e-4) and the weights added to sums by 2.1 to 2.9e-4 of
+ * theirs (unit rows, queries of 1.5). The work is cut by max_len: a close one is faster, with sums above all.
  * sums: device fp32 or NULL, sequence b's row at sums + b sums_stride (sums_stride >=
  * max_len): the weights of its tokens over all heads are added to it,
  *   sums[b][j] += sum over h of softmax_h(j),  j < kv_len[b],

@@ -49,7 +49,8 @@ __device__ __forceinline__ h8 codes8(uint32_t w, const CodeBits& k) {
   const h2 c = at((u & k.even) | k.even_base, 1024.f), d = at((u & k.odd) | k.odd_base, 64.f);
   return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-// The values, rounded once to fp16.
+// The values, rounded once to fp16, the type of the products (2^-11 of a value, beside a code's half step
+// of 1/30 of its group's range; exact, s and z would have to be taken out of the products, group by group).
 __device__ __forceinline__ h8 values8(uint32_t w, h8 s, h8 z, const CodeBits& k) {
   return __builtin_elementwise_fma(codes8(w, k), s, z);
 }

@@ -84,9 +84,10 @@ __device__ __forceinline__ uint32_t group_codes(const double (&v)[8], __half& s,
 
 // Blocks (., 0) normalize, rotate and quantize rows into their pages, a wave a token's: of its groups
 // eight lanes one, eight values a lane (with two a thread, 256 threads a token, the reductions and
-// quotients were four times as many: 3,100 tokens in 24.0 us). Blocks (t, 1 ..) rotate token t's query. What
-// a row's wave reads is asked for before the page is known. Bound by the bytes, most of them the queries'
-// (3,100 tokens of 32 heads: 89 MB in 21.5 us, 4.1 TB/s; 16 tokens: 4.8 us, latency and the 64-bit quotients).
+// quotients were four times as many: 3,100 tokens in 24.0 us). Blocks (t, 1 ..) rotate token t's query; the
+// grid is theirs, so that of the blocks (., 0) three in four find no token. What a row's wave reads is asked
+// for before the page is known. Most of the bytes are the queries' (3,100 tokens of 32 heads: 84 MB in 21.5 us, 3.9
+// of a copy's 5.15 TB/s; 16 tokens: 4.8 us, latency and the 64-bit quotients).
 __global__ void __launch_bounds__(256) latent4_append_kernel(Append4Args b) {
   const AppendArgs& a = b.a;
   const LatentArgs& l = a.l;
@@ -200,12 +201,15 @@ __global__ void __launch_bounds__(256) latent4_read_kernel(LatentArgs l, const i
 // quarter of the latent columns, and make the copies, two tiles ahead in four buffers. The codes
 // stay codes in LDS: a wave takes those it needs out of it, along a token for the scores and
 // across 16 tokens (the 4-bit transposing read) for the sums, and forms the values in registers,
-// so that LDS and HBM carry 4 bits a value. The values are rounded to fp16, the type of the products.
-// A long line is bound by that forming: 13 instructions for eight values, for either use, 440 of the
-// 550 vector instructions a tile and SIMD, beside 68 products. 512 latents, us a tile and workgroup: 16 heads
+// so that LDS and HBM carry 4 bits a value. The values are rounded to fp16, the type of the products (held as
+// two halves each they would double the products and the forming); a weight too, as in moe_latent.h.
+// Of a tile's 550 vector instructions a SIMD 440 are that forming, 13 for eight values and either use,
+// beside 68 products. On a long line no unit is full: of about 4,100 clocks a tile (32 heads) vector
+// instructions take 2,200 and products 1,100, with two waves a SIMD in step by a barrier a tile, and what the
+// others go to has not been told apart. 512 latents, us a tile and workgroup: 16 heads
 // 1.4, 32 1.7, 64 2.7; its copies alone take 1.1. 48 sequences of 32 heads, 378,000 tokens, 122 MB:
-// 58 us, 2.1 TB/s (the fp16 cache's 445 MB: 88); 700 tokens of one: 12, three trips to memory in a
-// line. Measured and left: sixteen waves, each with half of a token's elements and the partial scores
+// 58 us, 2.1 TB/s (the fp16 cache's 445 MB: 88); 700 tokens of one: 12, of which a tile is 1.7 and the trips to memory
+// before it (run, page, codes) are part. Measured and left: sixteen waves, each with half of a token's elements and the partial scores
 // added by way of LDS (1.5 and 1.75 us a tile: the instructions are the same); codes by loads to
 // registers, a lane a token's (64 separate pieces an instruction: 1.8).
 template <int DC, int DR, int MT>
@@ -625,10 +629,13 @@ __global__ void __launch_bounds__((64 * Decode4Shape<DC, DR, MT>::NW)) latent4_d
 // again, 16 RT heads a wave (RB such blocks beside each other), 16 tokens a product. A token's
 // weights are added up in one order: heads by rows, lanes, then blocks. The codes go from memory
 // to registers, 16 bytes a lane, as each is used once, and the next 16 tokens' are asked for
-// before these are used. Bound by latency where a wave has a step or two, by the values'
-// forming after that (512 latents: 40,000 tokens of 16 heads 10 us, 320,000 of 32 heads 35).
+// before these are used. Bound by latency where a wave has a step or two, then mostly by the values'
+// forming (512 latents: 40,000 tokens of 16 heads 10 us, 320,000 of 32 heads 35).
 // Workgroups at most, while a sequence has one (what is on the chip at once: with 256 and 1024
-// 320,000 tokens take 42 us; 60,000 of 32 heads 13, 15 and 22 with 256, 512 and 1024).
+// 320,000 tokens take 42 us; 60,000 of 32 heads 13, 15 and 22 with 256, 512 and 1024). A workgroup's
+// tokens are cut by the bound max_len, and all of these are with the longest length for it: 20 sequences of up to
+// 3,001 tokens, the call 28 us, take 42 under a bound of 32,768 and 73 under 131,072, where
+// a sequence's tokens are one workgroup's; 48 of up to 16,384 tokens 126 us, and 352 under 131,072.
 constexpr int kSumGroups = 512;
 
 template <int DC, int DR, int RT, int RB>
@@ -786,6 +793,8 @@ DecodePlan decode4_plan(int H, int Dc, int Dr, int B, int max_len, bool sums, si
   // 32; 6,000 61, 57; 12,000, which is 12 tiles a workgroup, 79, 79.5; 24,000 110, 121)
   p.rows = H <= 16 ? 16 : H <= 32 || (long long)B * ((H + 63) / 64) * tiles_host(max_len) < 12 * wgs ? 32 : 64;
   p.head_blocks = (H + p.rows - 1) / p.rows;
+  // (by the bound, as the lengths are on the device: under one far above them a share is long and the workgroups
+  // are few: 20 sequences of up to 3,001 tokens, the call 24 us, 27 under a bound of 131,072 and 42 under 2^20)
   p.least = std::max(1, (int)(0.18 * std::sqrt((double)tiles_host(max_len)) + 0.5));
   // (so many workgroups, up to one a CU, that a short line's tiles have one each: 2 sequences of 700 tokens, the
   // call 24.8 us, with a workgroup a tile, of which the items' places leave some empty, 26.2)

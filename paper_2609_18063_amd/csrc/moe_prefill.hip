@@ -56,6 +56,8 @@ __device__ __forceinline__ int tile_base(const PrefillArgs& a, int b) {
 // these. Each value is formed once here, where the expansion would form it for every 256 of its columns
 // (3,100 tokens of 512 latents by 32 heads: expanded from the codes 77 us, from the rows 44 and
 // this 5, which is its latency). 16 tokens a workgroup, four a wave; rows without a page are left.
+// A value is rounded to fp16, as an operand of the expansion's products, whose results are rounded
+// again: a rounding more than with fp16 pages, of 2^-11 where a code's half step is 1/30 of its group's range.
 template <int DC>
 __global__ void __launch_bounds__(256) latent4_rows_kernel(PrefillArgs a) {
   constexpr int L = DC / 8, N = 4 * L / 64;                // lanes of a token, tokens of a lane
